@@ -314,6 +314,147 @@ tactic_status tactic_build_clusters(const uint16_t* K, const uint16_t* V,
                                     int32_t* perm, uint16_t* K_sorted, uint16_t* V_sorted,
                                     void* workspace, size_t workspace_bytes, hipStream_t stream);
 
+/* ---- Attention beside the decode: prompts, other scores, shared prefixes, and
+ * caches that keep the rows of the largest attention weights.  The scores of
+ * these calls are
+ *     s = q . k / sqrt(128),   capped: cap * tanh(s / cap),
+ *     minus slope_h * |position of q - position of k|,
+ * and a pair that a mask leaves out has no weight, whatever its key and value
+ * hold (infinities and NaN too).  A query that sees no key gets zeros and a
+ * logarithm of -inf.  bf16 in, sums in 32 bits, one order of every sum. */
+typedef struct {
+  float cap;                   /* 0: none; otherwise positive and finite */
+  const float* slopes;         /* device fp32 [Hq] or NULL: none */
+  const int32_t* documents;    /* device [total_tokens] or NULL: document of each row; a query sees
+                                  the rows of its own document only */
+  const int32_t* prefix_len;   /* device [B] or NULL, prompts only: every query of sequence b sees
+                                  its first prefix_len[b] tokens, later ones included */
+} tactic_score_mod;
+
+/* The queries of a prompt (or of a chunk of one): sequence b has queries
+ * [q_indptr[b], q_indptr[b+1]), which are its last tokens: query i of m is at
+ * position n_b - m + i and sees the positions up to its own (and its prefix).
+ * Queries ahead of a sequence's first token (m > n_b) see nothing. */
+typedef struct {
+  int64_t total_queries;       /* host: q_indptr[B] */
+  int64_t max_queries;         /* host: largest q_indptr[b+1] - q_indptr[b] */
+  const int64_t* q_indptr;     /* device [B+1], q_indptr[0] = 0, non-decreasing */
+} tactic_query_shape;
+
+/* Attention of a prompt's queries over the cache that holds their keys already.
+ *   q     bf16 [total_queries][Hq][128]
+ *   K, V  as in tactic_dense_decode, rows in token order
+ *   mod   or NULL: plain causal attention
+ *   out   bf16 [total_queries][Hq][128]
+ *   lse   fp32 [Hq][total_queries] or NULL: log of the sum of exp(score)
+ * The weights of the values are rounded to bf16 (2^-8 relative), the output
+ * once.  Workspace: the size below, for any mod; contents are irrelevant. */
+size_t tactic_prompt_attention_workspace_size(const tactic_kv_shape* shape, const tactic_query_shape* queries);
+tactic_status tactic_prompt_attention(const uint16_t* q, const uint16_t* K, const uint16_t* V,
+                                      const tactic_kv_shape* shape, const tactic_query_shape* queries,
+                                      const tactic_score_mod* mod, uint16_t* out, float* lse,
+                                      void* workspace, size_t workspace_bytes, hipStream_t stream);
+/* The same over a paged cache (perm is ignored: prompts are in token order). */
+tactic_status tactic_prompt_attention_paged(const uint16_t* q, const tactic_paged_kv* kv,
+                                            const tactic_kv_shape* shape, const tactic_query_shape* queries,
+                                            const tactic_score_mod* mod, uint16_t* out, float* lse,
+                                            void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* The attention weights that queries give to each cached row, added to running
+ * sums: weights[g][j] += sum over the last `window` queries of the sequence (0:
+ * all) and the heads of g of exp(score - lse), with the lse of
+ * tactic_prompt_attention for the same arguments (a query of lse -inf gives
+ * none).  weights: fp32 [Hkv][total_tokens]; rows past a sequence's tokens keep
+ * their values.  Workspace as above. */
+tactic_status tactic_prompt_weights(const uint16_t* q, const uint16_t* K, const tactic_kv_shape* shape,
+                                    const tactic_query_shape* queries, const tactic_score_mod* mod,
+                                    const float* lse, int64_t window, float* weights, void* workspace,
+                                    size_t workspace_bytes, hipStream_t stream);
+
+/* Single tokens with the same scores: like tactic_dense_decode, for caches that
+ * may hold any positions. */
+typedef struct {
+  const int32_t* positions;    /* device [Hkv][total_tokens] or NULL (the row): position of each row */
+  const int32_t* q_pos;        /* device [B] or NULL (n_b - 1): position of each query; with positions
+                                  and slopes it must be given */
+  const int32_t* q_documents;  /* device [B]: document of each query, with mod->documents only */
+} tactic_token_rows;
+
+/*   rows     or NULL: positions are rows
+ *   out      fp32 [B][Hq][128];  lse  fp32 [B][Hq] or NULL
+ *   weights  fp32 [Hkv][total_tokens] or NULL: the weights of this step, summed over a group's
+ *            heads, are added to it
+ * mod->prefix_len must be NULL.  The workspace is larger with weights (4 bytes per row and query head). */
+size_t tactic_scored_decode_workspace_size(const tactic_kv_shape* shape, int32_t with_weights);
+tactic_status tactic_scored_decode(const uint16_t* q, const uint16_t* K, const uint16_t* V,
+                                   const tactic_kv_shape* shape, const tactic_score_mod* mod,
+                                   const tactic_token_rows* rows, float* out, float* lse, float* weights,
+                                   void* workspace, size_t workspace_bytes, hipStream_t stream);
+tactic_status tactic_scored_decode_paged(const uint16_t* q, const tactic_paged_kv* kv,
+                                         const tactic_kv_shape* shape, const tactic_score_mod* mod,
+                                         const tactic_token_rows* rows, float* out, float* lse, float* weights,
+                                         void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Sequences that share long prefixes: sequence b attends the tokens of prefix
+ * prefix_of[b] (positions 0 .. P-1), then its own (positions P ..).  A prefix's
+ * keys are read once for all its sequences. */
+typedef struct {
+  int32_t n_prefixes;          /* host, >= 1 */
+  int32_t max_members;         /* host: most sequences of one prefix */
+  int64_t total_tokens;        /* host: prefix_indptr[n_prefixes] */
+  int64_t max_len;             /* host: longest prefix */
+  const int64_t* prefix_indptr;  /* device [n_prefixes + 1] rows of each prefix */
+  const int32_t* prefix_of;    /* device [B]: prefix of each sequence, negative: none */
+  const int32_t* members;      /* device: the sequences of prefix 0, of prefix 1, ... */
+  const int32_t* member_indptr;  /* device [n_prefixes + 1] into members */
+  int32_t total_members;       /* host: member_indptr[n_prefixes] */
+} tactic_prefixes;
+
+/*   K_prefix, V_prefix  bf16 [Hkv][prefixes->total_tokens][128]
+ *   K, V, shape         the sequences' own tokens, as in tactic_dense_decode (NULL without any)
+ *   out fp32 [B][Hq][128], lse fp32 [B][Hq] or NULL
+ * mod (or NULL) may hold a cap and slopes.  prefix_of and members must agree. */
+size_t tactic_shared_decode_workspace_size(const tactic_kv_shape* shape, const tactic_prefixes* prefixes);
+tactic_status tactic_shared_decode(const uint16_t* q, const uint16_t* K_prefix, const uint16_t* V_prefix,
+                                   const uint16_t* K, const uint16_t* V, const tactic_kv_shape* shape,
+                                   const tactic_prefixes* prefixes, const tactic_score_mod* mod, float* out,
+                                   float* lse, void* workspace, size_t workspace_bytes, hipStream_t stream);
+/* The same over paged caches; the prefixes' page table is [n_prefixes][max_pages].  Both may use the
+ * same page arrays. */
+tactic_status tactic_shared_decode_paged(const uint16_t* q, const tactic_paged_kv* kv_prefix,
+                                         const tactic_paged_kv* kv, const tactic_kv_shape* shape,
+                                         const tactic_prefixes* prefixes, const tactic_score_mod* mod,
+                                         float* out, float* lse, void* workspace, size_t workspace_bytes,
+                                         hipStream_t stream);
+
+/* Eviction by accumulated weight: sequence b keeps min(n_b, keep[b], its span in
+ * the other cache) rows of every KV head - the `recent` newest by position
+ * (positions above newest[b] - recent, latest first where they are too many),
+ * then those of the largest weights, the lower row among equal ones (NaN ranks
+ * below every number) - and they are written in ascending row order.
+ *   weights fp32, positions int32 (or NULL: the row) [Hkv][total_tokens]
+ *   keep device int32 [B];  newest device int32 [B] or NULL (n_b - 1): no position is above it
+ *   out_indptr device [B+1], out_total, out_max host: spans of the other cache, as in tactic_kv_shape
+ *   K_out, V_out, weights_out, positions_out [Hkv][out_total]...: must not overlap the inputs; rows
+ *   behind the kept ones are left as they were
+ *   out_len device int64 [B]: rows kept.  recent in [0, 2^22]. */
+size_t tactic_evict_workspace_size(const tactic_kv_shape* shape, int64_t out_total);
+tactic_status tactic_evict(const uint16_t* K, const uint16_t* V, const tactic_kv_shape* shape,
+                           const float* weights, const int32_t* positions, const int32_t* keep,
+                           const int32_t* newest, int32_t recent, const int64_t* out_indptr, int64_t out_total,
+                           int64_t out_max, uint16_t* K_out, uint16_t* V_out, float* weights_out,
+                           int32_t* positions_out, int64_t* out_len, void* workspace, size_t workspace_bytes,
+                           hipStream_t stream);
+
+/* A new token for every sequence (k, v bf16 [B][Hkv][128], at position newest[b]): behind the last
+ * row while the span has room, else in place of the row of each KV head that tactic_evict would drop
+ * first (recent as there, counted from the new token).  The new row's weight is 0, and seq_len[b]
+ * (device, shape->seq_len's array) grows up to the span.  rows int32 [B][Hkv]: where it went (-1: an
+ * empty span). */
+tactic_status tactic_insert_token(const uint16_t* k, const uint16_t* v, const int32_t* newest, int32_t recent,
+                                  const tactic_kv_shape* shape, int64_t* seq_len, uint16_t* K, uint16_t* V,
+                                  float* weights, int32_t* positions, int32_t* rows, hipStream_t stream);
+
 /* Measurement helper, not part of the method: reads every 16-byte word of
  * `buf` (bytes, a multiple of 16) once with streaming loads from `workgroups`
  * workgroups of 256 threads (0: as many as fit on the device at once) and

@@ -6,4 +6,6 @@ include/tactic.h); this package only marshals torch tensors into those calls.
 from ._capi import TacticError, lib, LIB_PATH, EXPORTS  # noqa: F401
 from .tactic import (ClusterBuild, ClusterBuilder, ClusterSet, DenseDecoder, PagedCache, RaggedBatch,  # noqa: F401
                      SparseDecoder, decode_params, sparse_decode_workspace_bytes, stream_read_gbps)
-from .cache import RecentTailCache  # noqa: F401
+from .attention import (CacheEvictor, PromptAttention, ScoredDecoder, ScoreMod, SharedPrefixDecoder,  # noqa: F401
+                        TokenInserter)
+from .cache import EvictingCache, RecentTailCache  # noqa: F401

@@ -25,6 +25,10 @@ EXPORTS = (
     "tactic_probe_stream_read",
     "tactic_build_clusters_workspace_size", "tactic_build_clusters", "tactic_status_string",
     "tactic_last_error",
+    "tactic_prompt_attention_workspace_size", "tactic_prompt_attention", "tactic_prompt_attention_paged",
+    "tactic_prompt_weights", "tactic_scored_decode_workspace_size", "tactic_scored_decode",
+    "tactic_scored_decode_paged", "tactic_shared_decode_workspace_size", "tactic_shared_decode",
+    "tactic_shared_decode_paged", "tactic_evict_workspace_size", "tactic_evict", "tactic_insert_token",
 )
 
 
@@ -62,6 +66,24 @@ class PagedKV(ctypes.Structure):
 class KMeansParams(ctypes.Structure):
     _fields_ = [("max_iters", c_int32), ("reserved", c_int32), ("prev_centroids", c_void_p),
                 ("prev_cl_indptr", c_void_p)]
+
+
+class ScoreMod(ctypes.Structure):
+    _fields_ = [("cap", c_float), ("slopes", c_void_p), ("documents", c_void_p), ("prefix_len", c_void_p)]
+
+
+class QueryShape(ctypes.Structure):
+    _fields_ = [("total_queries", c_int64), ("max_queries", c_int64), ("q_indptr", c_void_p)]
+
+
+class TokenRows(ctypes.Structure):
+    _fields_ = [("positions", c_void_p), ("q_pos", c_void_p), ("q_documents", c_void_p)]
+
+
+class Prefixes(ctypes.Structure):
+    _fields_ = [("n_prefixes", c_int32), ("max_members", c_int32), ("total_tokens", c_int64), ("max_len", c_int64),
+                ("prefix_indptr", c_void_p), ("prefix_of", c_void_p), ("members", c_void_p),
+                ("member_indptr", c_void_p), ("total_members", c_int32)]
 
 
 class TacticError(RuntimeError):
@@ -117,6 +139,30 @@ def lib() -> ctypes.CDLL:
     L.tactic_build_clusters.restype = c_int
     L.tactic_probe_stream_read.argtypes = [c_void_p, c_size_t, c_int32, c_void_p, c_void_p]
     L.tactic_probe_stream_read.restype = c_int
+    shape, mod, ws = POINTER(KVShape), POINTER(ScoreMod), [c_void_p, c_size_t, c_void_p]
+    queries, rows, pre, paged = POINTER(QueryShape), POINTER(TokenRows), POINTER(Prefixes), POINTER(PagedKV)
+    for name, args in {
+            "tactic_prompt_attention": [c_void_p] * 3 + [shape, queries, mod, c_void_p, c_void_p] + ws,
+            "tactic_prompt_attention_paged": [c_void_p, paged, shape, queries, mod, c_void_p, c_void_p] + ws,
+            "tactic_prompt_weights": [c_void_p, c_void_p, shape, queries, mod, c_void_p, c_int64, c_void_p] + ws,
+            "tactic_scored_decode": [c_void_p] * 3 + [shape, mod, rows] + [c_void_p] * 3 + ws,
+            "tactic_scored_decode_paged": [c_void_p, paged, shape, mod, rows] + [c_void_p] * 3 + ws,
+            "tactic_shared_decode": [c_void_p] * 5 + [shape, pre, mod, c_void_p, c_void_p] + ws,
+            "tactic_shared_decode_paged": [c_void_p, paged, paged, shape, pre, mod, c_void_p, c_void_p] + ws,
+            "tactic_evict": [c_void_p, c_void_p, shape] + [c_void_p] * 4 + [c_int32, c_void_p, c_int64, c_int64] +
+                            [c_void_p] * 5 + ws,
+            "tactic_insert_token": [c_void_p] * 3 + [c_int32, shape] + [c_void_p] * 7,
+    }.items():
+        getattr(L, name).argtypes = args
+        getattr(L, name).restype = c_int
+    for name, args in {
+            "tactic_prompt_attention_workspace_size": [shape, queries],
+            "tactic_scored_decode_workspace_size": [shape, c_int32],
+            "tactic_shared_decode_workspace_size": [shape, pre],
+            "tactic_evict_workspace_size": [shape, c_int64],
+    }.items():
+        getattr(L, name).argtypes = args
+        getattr(L, name).restype = c_size_t
     L.tactic_status_string.argtypes = [c_int]
     L.tactic_status_string.restype = c_char_p
     L.tactic_last_error.argtypes = []
@@ -132,6 +178,6 @@ def check(status: int, what: str) -> None:
                           f"{L.tactic_last_error().decode()} (status {status})")
 
 
-__all__ = ["KVShape", "ClusterMeta", "DecodeParams", "DecodePlan", "DecodeView", "KMeansParams", "PagedKV",
+__all__ = ["KVShape", "ScoreMod", "QueryShape", "TokenRows", "Prefixes", "ClusterMeta", "DecodeParams", "DecodePlan", "DecodeView", "KMeansParams", "PagedKV",
            "TacticError", "lib", "check", "EXPORTS", "LIB_PATH", "FIT_FIELDS", "FIT_NAMES", "NOALLOC_SCRATCH_BYTES",
            "c_double"]

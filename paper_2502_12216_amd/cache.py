@@ -16,6 +16,7 @@ from typing import List, Optional, Sequence
 import numpy as np
 import torch
 
+from .attention import CacheEvictor, PromptAttention, ScoredDecoder, ScoreMod, TokenInserter
 from .tactic import (ClusterBuilder, ClusterSet, DenseDecoder, RaggedBatch, SparseDecoder, decode_params,
                      sparse_decode_workspace_bytes)
 
@@ -151,3 +152,66 @@ class RecentTailCache:
     @property
     def recent(self) -> List[int]:
         return [n - c for n, c in zip(self.lens, self.clustered)]
+
+
+class EvictingCache:
+    """One layer's KV cache of a fixed number of rows per sequence, for a batch decoded in lockstep.
+
+    prefill() attends the prompts in full, sums the attention weights that their last `window` queries
+    give to every token, and keeps each sequence's `budget` rows of the largest sums, the `recent` newest
+    among them.  append() writes a new token over the row of the least sum once a sequence is full;
+    decode() attends the rows held and adds this step's weights to their sums.  Positions are the
+    tokens' own, so a bias by distance is that of the whole sequence."""
+
+    def __init__(self, n_q_heads: int, n_kv_heads: int, batch: int, budget: int, recent: int = 256, window: int = 0,
+                 cap: float = 0.0, slopes: Optional[torch.Tensor] = None, device="cuda"):
+        if not 0 <= int(recent) < int(budget):
+            raise ValueError("recent must be in [0, budget)")
+        self.Hq, self.Hkv, self.budget, self.recent = int(n_q_heads), int(n_kv_heads), int(budget), int(recent)
+        self.window = int(window)
+        self.mod = ScoreMod(cap=cap, slopes=slopes)
+        self.device = device
+        self.batch = RaggedBatch([0] * int(batch), self.Hq, self.Hkv, device=device, capacities=[self.budget] * int(batch))
+        self.K = torch.zeros(self.Hkv, self.batch.total, 128, dtype=torch.bfloat16, device=device)
+        self.V = torch.zeros_like(self.K)
+        self.weights = torch.zeros(self.Hkv, self.batch.total, dtype=torch.float32, device=device)
+        self.positions = torch.zeros(self.Hkv, self.batch.total, dtype=torch.int32, device=device)
+        self.newest = torch.full((int(batch),), -1, dtype=torch.int32, device=device)  # the last token's position
+        self.inserter = TokenInserter(self.batch, self.recent)
+        self.decoder = ScoredDecoder(self.batch)
+
+    def _set_lens(self, lens: Sequence[int]) -> None:
+        self.batch.seq_lens = [min(int(n), self.budget) for n in lens]
+
+    def prefill(self, q: Sequence[torch.Tensor], K: Sequence[torch.Tensor], V: Sequence[torch.Tensor]) -> torch.Tensor:
+        """q[b] bf16 [n_b][Hq][128], K[b], V[b] bf16 [Hkv][n_b][128] in token order.  Returns the prompts'
+        attention, bf16 [sum n_b][Hq][128]."""
+        lens = [int(k.shape[1]) for k in K]
+        if len(lens) != self.batch.batch:
+            raise ValueError("prefill needs a prompt for every sequence")
+        full = RaggedBatch(lens, self.Hq, self.Hkv, device=self.device)
+        Kc, Vc, qc = torch.cat(list(K), 1).contiguous(), torch.cat(list(V), 1).contiguous(), torch.cat(list(q)).contiguous()
+        prompt = PromptAttention(full, lens)
+        out, lse = prompt(qc, Kc, Vc, self.mod)
+        sums = torch.zeros(self.Hkv, full.total, dtype=torch.float32, device=self.K.device)
+        prompt.add_weights(qc, Kc, lse, sums, self.mod, window=self.window)
+        keep = torch.full_like(self.newest, self.budget)
+        CacheEvictor(full, self.batch, self.recent)(Kc, Vc, sums, keep, self.K, self.V, self.weights, self.positions)
+        self.newest.copy_(torch.as_tensor(np.asarray(lens, dtype=np.int32) - 1))
+        self._set_lens(lens)
+        return out
+
+    def append(self, k: torch.Tensor, v: torch.Tensor) -> torch.Tensor:
+        """k, v bf16 [B][Hkv][128], the new token of every sequence.  Only device work is enqueued.  Returns
+        the rows int32 [B][Hkv] that they went to."""
+        self.newest += 1
+        rows = self.inserter(k, v, self.K, self.V, self.weights, self.positions, self.newest)
+        self._set_lens([n + 1 for n in self.batch.seq_lens])
+        return rows
+
+    def decode(self, q: torch.Tensor) -> torch.Tensor:
+        """Attention of q (bf16 [B][Hq][128], the last token's queries) over the rows held, fp32 [B][Hq][128];
+        their weights are added to the sums."""
+        out, _ = self.decoder(q, self.K, self.V, self.mod, positions=self.positions, q_pos=self.newest,
+                              weights=self.weights)
+        return out

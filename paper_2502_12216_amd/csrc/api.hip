@@ -11,15 +11,17 @@
 
 #include "../../include/tactic.h"
 #include "common.hpp"
+#include "host.hpp"
 #include "kernels.hpp"
 #include "kmeans.hpp"
 #include "plan.hpp"
 
 namespace {
-
 thread_local std::string g_last_error;
+}
 
-tactic_status fail(tactic_status s, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+namespace tactic_host {
+
 tactic_status fail(tactic_status s, const char* fmt, ...) {
   char buf[512];
   va_list ap;
@@ -32,28 +34,6 @@ tactic_status fail(tactic_status s, const char* fmt, ...) {
 
 tactic_status hip_fail(hipError_t e, const char* what) {
   return fail(TACTIC_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-}
-
-int64_t align_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
-
-struct Layout {
-  int64_t cur = 0;
-  int64_t take(int64_t bytes) {
-    const int64_t o = cur;
-    cur = align_up(cur + bytes, 256);
-    return o;
-  }
-};
-
-tactic::SelParams sel_params(const tactic_decode_params* p) {
-  tactic::SelParams s;
-  s.target_frac = p->target_frac;
-  s.exact_bp = p->exact_bp;
-  s.win_bp = p->win_bp;
-  s.win_min = p->win_min;
-  s.p1_bp = p->p1_bp;
-  s.p2_bp = p->p2_bp;
-  return s;
 }
 
 tactic_status check_shape(const tactic_kv_shape* s) {
@@ -79,6 +59,23 @@ tactic_status check_shape(const tactic_kv_shape* s) {
   return TACTIC_OK;
 }
 
+}  // namespace tactic_host
+
+using namespace tactic_host;
+
+namespace {
+
+tactic::SelParams sel_params(const tactic_decode_params* p) {
+  tactic::SelParams s;
+  s.target_frac = p->target_frac;
+  s.exact_bp = p->exact_bp;
+  s.win_bp = p->win_bp;
+  s.win_min = p->win_min;
+  s.p1_bp = p->p1_bp;
+  s.p2_bp = p->p2_bp;
+  return s;
+}
+
 tactic_status check_params(const tactic_decode_params* p) {
   if (!p) return fail(TACTIC_ERR_INVALID_ARG, "params is null");
   if (!(p->target_frac > 0.f && p->target_frac <= 1.f))
@@ -91,7 +88,9 @@ tactic_status check_params(const tactic_decode_params* p) {
   return TACTIC_OK;
 }
 
-tactic_status paged_args(const tactic_paged_kv* kv, const tactic_kv_shape* s, tactic::PagedKV* pk) {
+}  // namespace
+
+tactic_status tactic_host::paged_args(const tactic_paged_kv* kv, const tactic_kv_shape* s, tactic::PagedKV* pk) {
   if (!kv || !kv->K_pages || !kv->V_pages || !kv->page_table) return fail(TACTIC_ERR_INVALID_ARG, "null paged-KV pointer");
   if (kv->page_size < 1 || kv->max_pages < 1 || kv->num_pages < 1)
     return fail(TACTIC_ERR_INVALID_ARG, "page_size, max_pages and num_pages must be >= 1");
@@ -109,13 +108,17 @@ tactic_status paged_args(const tactic_paged_kv* kv, const tactic_kv_shape* s, ta
   return TACTIC_OK;
 }
 
+namespace {
+
 const tactic::DecodePlan* as_plan(const tactic_decode_plan* p) {
   return reinterpret_cast<const tactic::DecodePlan*>(p);
 }
 
+}  // namespace
+
 // Workspace of a dense launch on `grid` attention workgroups: a partial slot
 // per (KV group, workgroup) pair that can meet, and the split's offsets.
-size_t dense_workspace_bytes(const tactic_kv_shape* s, int64_t grid) {
+size_t tactic_host::dense_workspace_bytes(const tactic_kv_shape* s, int64_t grid) {
   const int64_t BG = (int64_t)s->batch * s->n_kv_heads;
   const int64_t G = s->n_q_heads / s->n_kv_heads;
   Layout L;
@@ -123,8 +126,6 @@ size_t dense_workspace_bytes(const tactic_kv_shape* s, int64_t grid) {
   L.take((BG + 2) * 8);
   return (size_t)L.cur;
 }
-
-}  // namespace
 
 extern "C" {
 

@@ -1,0 +1,372 @@
+// Accumulated attention weights of a prompt, and what a cache keeps by them:
+// eviction into another cache and the insertion of single tokens into full ones.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "common.hpp"
+#include "kernels.hpp"
+#include "scores.hpp"
+
+namespace tactic {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// ---------------------------------------------------------------------------
+// weights[g][j] += sum over the last `window` queries and the group's heads of
+// 2^(s_ij - lse_i).  A workgroup holds 256 keys of a (sequence, KV head), 64 per
+// wave, as the B operands of S = Q K^T and streams the query rows through LDS, 64
+// at a time: a lane's accumulators are the rows of one key, so the sum over rows
+// needs no exchange but one between the halves at the end.  Bound by the matrix
+// unit and by one exponential per score; with few queries by reading K.
+// grid (key tiles + sequences, Hkv, splits of the rows)
+// ---------------------------------------------------------------------------
+constexpr int kWKeys = 256, kWRows = 64;
+
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void prompt_weights_kernel(WeightArgs a) {
+  __shared__ __align__(16) unsigned char s_q[2][kWRows * 256];
+  __shared__ __align__(16) float s_lse[2][kWRows], s_slope[2][kWRows];
+  __shared__ __align__(16) int s_lim[2][kWRows], s_pos[2][kWRows], s_doc[2][kWRows];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, col = lane & 31;
+  const int g = blockIdx.y, split = blockIdx.z;
+  int lo = 0, hi = a.B - 1;  // key tiles of sequence b start at floor(rows before it / 256) + b
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (a.kv_indptr[mid] / kWKeys + mid <= (int64_t)blockIdx.x) lo = mid;
+    else hi = mid - 1;
+  }
+  const int b = lo;
+  const int64_t kvb = a.kv_indptr[b];
+  const int n = (int)seq_tokens(a.kv_indptr, a.seq_len, b);
+  const int64_t k0l = ((int64_t)blockIdx.x - kvb / kWKeys - b) * kWKeys;
+  if (k0l < 0 || k0l >= n) return;
+  const int k0 = (int)k0l;
+  const int64_t q0 = a.q_indptr[b], m = a.q_indptr[b + 1] - q0;
+  const int pre = a.prefix_len ? a.prefix_len[b] : 0;
+  // tokens [i0, m) of the sequence's queries: within the window, and able to see the tile
+  int64_t i0 = a.window > 0 ? max(m - a.window, (int64_t)0) : 0;
+  if (pre <= k0) i0 = max(i0, (int64_t)k0 - (n - m));
+  i0 = max(i0, m - n);  // queries ahead of the first token see nothing
+  const int64_t r0 = i0 * a.G, rows = (m - i0) * a.G;
+  const int tiles = rows > 0 ? (int)((rows + kWRows - 1) / kWRows) : 0;
+  const int t_lo = (int)((int64_t)tiles * split / a.splits), t_hi = (int)((int64_t)tiles * (split + 1) / a.splits);
+
+  // keys of this wave: blocks of 32, a key per column (rows past the end repeat the last)
+  bf16x8 kf[2][8];
+  int key[2], kdoc[2];
+#pragma unroll
+  for (int bb = 0; bb < 2; ++bb) {
+    key[bb] = k0 + wave * 64 + bb * 32 + col;
+    const int64_t at = ((int64_t)g * a.total + kvb + min(key[bb], n - 1)) * kHeadDim + 8 * half;
+    kdoc[bb] = a.documents ? a.documents[kvb + min(key[bb], n - 1)] : 0;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) kf[bb][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(a.K + at + 16 * s));
+  }
+  const float to_cap = a.cap > 0.f ? kInvSqrtDim / a.cap : 0.f, cap2 = a.cap * kLog2e;
+  float sum[2] = {0.f, 0.f};
+
+  uint4 qreg[4];
+  float lse_r = 0.f, slope_r = 0.f;
+  int lim_r = 0, pos_r = 0, doc_r = 0;
+  auto fetch = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = (wave * 4 + i) * 64 + lane, r = c >> 4;
+      const int64_t row = r0 + min((int64_t)t * kWRows + r, rows - 1);
+      const int64_t at = ((q0 + row / a.G) * a.Hq + g * a.G + row % a.G) * kHeadDim;
+      qreg[i] = *reinterpret_cast<const uint4*>(a.q + at + ((c & 15) ^ (4 * (r & 3) + ((r >> 2) & 3))) * 8);
+    }
+    if (tid < kWRows) {
+      const int64_t x = (int64_t)t * kWRows + tid, row = r0 + min(x, rows - 1), i = row / a.G, h = g * a.G + row % a.G;
+      const int pos = (int)(n - m + i);
+      lse_r = a.lse[h * a.n_queries + q0 + i] * kLog2e;
+      slope_r = a.slopes ? a.slopes[h] * kLog2e : 0.f;
+      pos_r = pos;
+      // a row past the end, and one whose sum says that it saw nothing, gives no weight
+      lim_r = x < rows && lse_r != -INFINITY ? min(max(pos + 1, pre), n) : 0;
+      doc_r = a.documents && pos >= 0 ? a.documents[kvb + pos] : 0;
+    }
+  };
+  auto store = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(s_q[buf] + ((wave * 4 + i) * 64 + lane) * 16) = qreg[i];
+    if (tid < kWRows) {
+      s_lse[buf][tid] = lse_r;
+      s_slope[buf][tid] = slope_r;
+      s_lim[buf][tid] = lim_r;
+      s_pos[buf][tid] = pos_r;
+      s_doc[buf][tid] = doc_r;
+    }
+  };
+  if (t_lo < t_hi) {
+    fetch(t_lo);
+    store(0);
+  }
+  __syncthreads();
+  int buf = 0;
+  for (int t = t_lo; t < t_hi; ++t) {
+    if (t + 1 < t_hi) fetch(t + 1);
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb) {
+      f32x16 acc[2];
+#pragma unroll
+      for (int bb = 0; bb < 2; ++bb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[bb][r] = 0.f;
+      const unsigned char* qrow = s_q[buf] + (rb * 32 + col) * 256;
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        const bf16x8 qv = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(qrow + ((2 * s + half) ^ (4 * (col & 3) + ((col >> 2) & 3))) * 16));
+        acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qv, kf[0][s], acc[0], 0, 0, 0);
+        acc[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qv, kf[1][s], acc[1], 0, 0, 0);
+      }
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        const int at = rb * 32 + 8 * q4 + 4 * half;  // accumulator 4 q4 + j is row at + j
+        const float4 ls = *reinterpret_cast<const float4*>(s_lse[buf] + at);
+        const int4 lm = *reinterpret_cast<const int4*>(s_lim[buf] + at);
+        const float lsa[4] = {ls.x, ls.y, ls.z, ls.w};
+        const int lma[4] = {lm.x, lm.y, lm.z, lm.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int bb = 0; bb < 2; ++bb) {
+            float v = acc[bb][4 * q4 + j];
+            v = a.cap > 0.f ? cap2 * tanh_any(v * to_cap) : v * (kInvSqrtDim * kLog2e);
+            if (a.slopes) v = fmaf(-s_slope[buf][at + j], fabsf((float)(s_pos[buf][at + j] - key[bb])), v);
+            bool seen = key[bb] < lma[j];
+            if (a.documents) seen = seen && s_doc[buf][at + j] == kdoc[bb];
+            sum[bb] += seen ? fast_exp2(v - lsa[j]) : 0.f;
+          }
+      }
+    }
+    if (t + 1 < t_hi) store(buf ^ 1);
+    __syncthreads();
+    buf ^= 1;
+  }
+#pragma unroll
+  for (int bb = 0; bb < 2; ++bb) {
+    const float s = sum[bb] + __shfl_xor(sum[bb], 32, 64);
+    if (half == 0 && key[bb] < n) {
+      const int64_t at = (int64_t)g * a.total + kvb + key[bb];
+      if (a.splits == 1) a.weights[at] += s;
+      else a.part[(int64_t)split * a.Hkv * a.total + at] = s;
+    }
+  }
+}
+
+// Adds the splits' sums in order.  grid (rows / 256, Hkv, B)
+__global__ __launch_bounds__(256) void sum_weights_kernel(WeightArgs a) {
+  const int g = blockIdx.y, b = blockIdx.z;
+  const int64_t n = seq_tokens(a.kv_indptr, a.seq_len, b), r = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (r >= n) return;
+  const int64_t at = (int64_t)g * a.total + a.kv_indptr[b] + r;
+  float x = 0.f;
+  for (int s = 0; s < a.splits; ++s) x += a.part[(int64_t)s * a.Hkv * a.total + at];
+  a.weights[at] += x;
+}
+
+hipError_t launch_prompt_weights(const WeightArgs& a, int64_t max_len, hipStream_t st) {
+  if (max_len == 0) return hipSuccess;
+  hipLaunchKernelGGL(prompt_weights_kernel, dim3((unsigned)(a.total / kWKeys + a.B), a.Hkv, a.splits), dim3(256), 0, st, a);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && a.splits > 1) {
+    hipLaunchKernelGGL(sum_weights_kernel, dim3((unsigned)((max_len + 255) / 256), a.Hkv, a.B), dim3(256), 0, st, a);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+// ---------------------------------------------------------------------------
+// Which rows stay.  Rows are ranked by a 32-bit key: weights ascending (-0 as 0,
+// NaN below every number), above them the recent rows by position.  Among equal
+// keys the lower row ranks first.
+// ---------------------------------------------------------------------------
+constexpr uint32_t kRecentKey = 0xff800001u;  // above the key of +inf
+
+__device__ __forceinline__ uint32_t rank_key(float w, int64_t pos, int64_t newest, int recent) {
+  const int64_t age = newest - pos;  // 0: the newest
+  if (age < recent) return kRecentKey + (uint32_t)max((int64_t)recent - 1 - max(age, (int64_t)0), (int64_t)0);
+  if (w != w) return 0u;
+  const uint32_t u = __float_as_uint(w + 0.f);
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+
+// One workgroup per (KV head, sequence) finds the kept rows: the key of the last
+// kept one digit by digit (256 counts of 8 bits each), then the kept rows in
+// ascending order by a running count.
+__global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
+  __shared__ uint32_t s_hist[256];
+  __shared__ uint32_t s_sum[16], s_eq[16];
+  __shared__ uint32_t s_prefix, s_need;
+  const int g = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t kvb = a.kv_indptr[b], outb = a.out_indptr[b];
+  const int n = (int)seq_tokens(a.kv_indptr, a.seq_len, b);
+  const int64_t room = a.out_indptr[b + 1] - outb;
+  const int keep = (int)min((int64_t)n, min(max((int64_t)a.keep[b], (int64_t)0), room));
+  if (g == 0 && tid == 0) a.out_len[b] = keep;
+  if (keep == 0) return;
+  const int64_t newest = a.newest ? a.newest[b] : n - 1;
+  const float* w = a.weights + (int64_t)g * a.total + kvb;
+  const int32_t* pos = a.positions ? a.positions + (int64_t)g * a.total + kvb : nullptr;
+  auto key_at = [&](int r) { return rank_key(w[r], pos ? pos[r] : r, newest, a.recent); };
+  uint32_t prefix = 0, need = (uint32_t)keep;
+  if (keep < n) {
+    for (int shift = 24; shift >= 0; shift -= 8) {
+      if (tid < 256) s_hist[tid] = 0;
+      __syncthreads();
+      for (int r = tid; r < n; r += 1024) {
+        const uint32_t k = key_at(r);
+        if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&s_hist[(k >> shift) & 255], 1u);
+      }
+      __syncthreads();
+      if (wave == 0) {  // the digit that holds the need-th largest, four counts per lane from the top
+        uint32_t c[4], mine = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          c[j] = s_hist[255 - (lane * 4 + j)];
+          mine += c[j];
+        }
+        const uint32_t incl = wave_incl_scan((int)mine), before = incl - mine;
+        if (before < need && need <= incl) {
+          uint32_t run = before;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if (run < need && need <= run + c[j]) {
+              s_prefix = prefix | ((uint32_t)(255 - (lane * 4 + j)) << shift);
+              s_need = need - run;
+            }
+            run += c[j];
+          }
+        }
+      }
+      __syncthreads();
+      prefix = s_prefix;
+      need = s_need;
+      __syncthreads();
+    }
+  }
+  // rows above the key, and the first `need` rows of exactly that key (all kept: key 0, every row)
+  int32_t* rows = a.rows + (int64_t)g * a.out_total + outb;
+  uint32_t base = 0, eq_base = 0;
+  for (int r0 = 0; r0 < n; r0 += 1024) {
+    const int r = r0 + tid;
+    const uint32_t k = r < n ? key_at(r) : 0;
+    const bool above = r < n && k > prefix, equal = r < n && k == prefix;
+    const uint64_t em = __ballot(equal), below = (1ull << lane) - 1;
+    if (lane == 0) s_eq[wave] = __popcll(em);
+    __syncthreads();
+    uint32_t e = eq_base + __popcll(em & below), e_all = eq_base;
+    for (int i = 0; i < 16; ++i) {
+      e += i < wave ? s_eq[i] : 0;
+      e_all += s_eq[i];
+    }
+    const bool kept = above || (equal && e < need);
+    const uint64_t km = __ballot(kept);
+    if (lane == 0) s_sum[wave] = __popcll(km);
+    __syncthreads();
+    uint32_t at = base + __popcll(km & below), all = base;
+    for (int i = 0; i < 16; ++i) {
+      at += i < wave ? s_sum[i] : 0;
+      all += s_sum[i];
+    }
+    if (kept && at < (uint32_t)keep) rows[at] = r;
+    base = all;
+    eq_base = e_all;
+    __syncthreads();
+  }
+}
+
+// Copies the kept rows: 16 lanes per row, K and V.  grid (rows / 64, Hkv, B)
+__global__ __launch_bounds__(256) void evict_gather_kernel(EvictArgs a) {
+  const int g = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, part = tid & 15;
+  const int64_t kvb = a.kv_indptr[b], outb = a.out_indptr[b], keep = a.out_len[b];
+  const int64_t base = (int64_t)blockIdx.x * 64;
+  if (base >= keep) return;
+  const int32_t* rows = a.rows + (int64_t)g * a.out_total + outb;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t at = base + i * 16 + (tid >> 4);
+    if (at >= keep) continue;
+    const int64_t r = rows[at];
+    const int64_t from = (int64_t)g * a.total + kvb + r, to = (int64_t)g * a.out_total + outb + at;
+    const uint4 k = *reinterpret_cast<const uint4*>(a.K + from * kHeadDim + part * 8);
+    const uint4 v = *reinterpret_cast<const uint4*>(a.V + from * kHeadDim + part * 8);
+    *reinterpret_cast<uint4*>(a.K_out + to * kHeadDim + part * 8) = k;
+    *reinterpret_cast<uint4*>(a.V_out + to * kHeadDim + part * 8) = v;
+    if (part == 0) {
+      a.weights_out[to] = a.weights[from];
+      a.positions_out[to] = a.positions ? a.positions[from] : (int32_t)r;
+    }
+  }
+}
+
+hipError_t launch_evict(const EvictArgs& a, int64_t max_out, hipStream_t st) {
+  hipLaunchKernelGGL(evict_select_kernel, dim3(a.Hkv, a.B), dim3(1024), 0, st, a);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && max_out > 0) {
+    hipLaunchKernelGGL(evict_gather_kernel, dim3((unsigned)((max_out + 63) / 64), a.Hkv, a.B), dim3(256), 0, st, a);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+// ---------------------------------------------------------------------------
+// One token per sequence: behind the last row while there is room, else in the
+// place of the row that ranks last.  One workgroup per (KV head, sequence).
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void insert_token_kernel(InsertArgs a) {
+  __shared__ uint64_t s_min[4];
+  const int g = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t kvb = a.kv_indptr[b], span = a.kv_indptr[b + 1] - kvb;
+  const int n = (int)seq_tokens(a.kv_indptr, a.seq_len, b);
+  const int64_t base = (int64_t)g * a.total + kvb;
+  int64_t row = n;
+  if (span == 0) {
+    if (tid == 0) a.rows[(int64_t)b * a.Hkv + g] = -1;
+    return;
+  }
+  if (n >= span) {
+    const int64_t newest = a.newest[b];
+    uint64_t best = ~0ull;  // lowest key, among equal ones the highest row
+    for (int r = tid; r < n; r += 256) {
+      const uint64_t k = rank_key(a.weights[base + r], a.positions[base + r], newest, a.recent);
+      best = min(best, (k << 32) | (uint32_t)~r);
+    }
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) best = min(best, (uint64_t)__shfl_xor((unsigned long long)best, s, 64));
+    if (lane == 0) s_min[wave] = best;
+    __syncthreads();
+    best = min(min(s_min[0], s_min[1]), min(s_min[2], s_min[3]));
+    row = (int64_t)(uint32_t)~(uint32_t)best;
+  }
+  const int64_t from = ((int64_t)b * a.Hkv + g) * kHeadDim, to = (base + row) * kHeadDim;
+  if (tid < 16) *reinterpret_cast<uint4*>(a.K + to + tid * 8) = *reinterpret_cast<const uint4*>(a.k + from + tid * 8);
+  else if (tid < 32) *reinterpret_cast<uint4*>(a.V + to + (tid - 16) * 8) = *reinterpret_cast<const uint4*>(a.v + from + (tid - 16) * 8);
+  else if (tid == 32) {
+    a.weights[base + row] = 0.f;
+    a.positions[base + row] = a.newest[b];
+    a.rows[(int64_t)b * a.Hkv + g] = (int32_t)row;
+  }
+}
+
+__global__ __launch_bounds__(256) void advance_lengths_kernel(InsertArgs a) {
+  const int b = blockIdx.x * 256 + threadIdx.x;
+  if (b < a.B) {
+    const int64_t span = a.kv_indptr[b + 1] - a.kv_indptr[b];
+    a.seq_len[b] = min(max(a.seq_len[b], (int64_t)0) + 1, span);
+  }
+}
+
+hipError_t launch_insert(const InsertArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL(insert_token_kernel, dim3(a.Hkv, a.B), dim3(256), 0, st, a);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess) {
+    hipLaunchKernelGGL(advance_lengths_kernel, dim3((a.B + 255) / 256), dim3(256), 0, st, a);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+}  // namespace tactic

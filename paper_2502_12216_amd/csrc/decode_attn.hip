@@ -16,9 +16,12 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "common.hpp"
 #include "kernels.hpp"
 #include "plan.hpp"
+#include "scores.hpp"
 
 namespace tactic {
 
@@ -232,9 +235,14 @@ constexpr int attn_tok(int G) { return G == 8 ? 4 : 2; }
 // error against 64 bits unchanged (2.7e-7 to 6.8e-7 over seeds).  For G = 4
 // (64% busy at three waves) the same form gains 2% on a large selection and
 // loses 1% on small ones and paged dense decode.
-template <int G, int TOK, bool kPaged>
+//
+// kMod (dense only): 1 caps the scores and adds a bias by distance, 2 also reads a
+// position or a document per row, beside the row's keys; both can write the
+// scores out (32 bits, a row's heads side by side: 4 G bytes beside its 512).  A
+// row of another document has no weight, whatever its values hold.
+template <int G, int TOK, bool kPaged, int kMod = 0>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(G >= 8 ? 2 : 3)))
-void attn_splitk_kernel(AttnArgs a) {
+void attn_splitk_kernel(AttnArgs a, std::conditional_t<kMod != 0, TokenMod, NoMod> mod) {
   constexpr int LPR = 16;                 // lanes per 256-byte row
   constexpr int kPart = G * (kHeadDim + 2);
   constexpr int EPL = kHeadDim / LPR;     // bf16 elements per lane
@@ -349,6 +357,25 @@ void attn_splitk_kernel(AttnArgs a) {
         for (int h = 0; h < G; ++h) acc[h][e] = 0.f;
       }
     }
+    // kMod: this lane's head's slope, the query's position and document, the rows' metadata
+    float slope2 = 0.f, to_cap = 0.f;
+    int qpos = 0, base = 0, qdoc = 0;
+    const int32_t *posp = nullptr, *docp = nullptr;
+    float* scp = nullptr;
+    if constexpr (kMod != 0) {
+      const int64_t row0 = (int64_t)kvh * a.total + kvb;
+      slope2 = mod.slopes ? mod.slopes[jg * G + hl] * kLog2e : 0.f;
+      to_cap = mod.cap > 0.f ? kInvSqrtDim / mod.cap : 0.f;
+      if (mod.pos_base && mod.base_of[b] >= 0)
+        base = (int)(mod.pos_base[mod.base_of[b] + 1] - mod.pos_base[mod.base_of[b]]);
+      qpos = mod.q_pos ? mod.q_pos[b] : base + nseq - 1;
+      if constexpr (kMod == 2) {  // (an array that is not there is read at one place that is, and not used)
+        posp = mod.positions ? mod.positions + row0 : reinterpret_cast<const int32_t*>(a.kv_indptr);
+        docp = mod.documents ? mod.documents + kvb : reinterpret_cast<const int32_t*>(a.kv_indptr);
+        qdoc = mod.documents ? mod.q_documents[b] : 0;
+      }
+      if (mod.scores && sl == (kMatrix ? hl : hl * (16 / G))) scp = mod.scores + row0 * G + hl;
+    }
     auto sum_of = [&](int h, int e) __attribute__((always_inline)) {
       if constexpr (kMatrix) return accv[h / 4][e][h % 4];
       else return acc[h][e];
@@ -368,6 +395,7 @@ void attn_splitk_kernel(AttnArgs a) {
     int64_t p0 = 0;   // its first position in the group's token list
     struct Tile {
       uint4 k[TOK], v[TOK];
+      int pos[kMod == 2 ? TOK : 1], doc[kMod == 2 ? TOK : 1];
     };
     auto word = [](const uint4& x, int w) __attribute__((always_inline)) {
       return w == 0 ? x.x : (w == 1 ? x.y : (w == 2 ? x.z : x.w));
@@ -377,6 +405,14 @@ void attn_splitk_kernel(AttnArgs a) {
     auto load_tile = [&](int tile) __attribute__((always_inline)) -> Tile {
       Tile r;
       const int tb = tile * kTileTok + gid * TOK;
+      if constexpr (kMod == 2) {
+#pragma unroll
+        for (int i = 0; i < TOK; ++i) {  // (a row past the sub-range reads the last one's)
+          const int64_t row = p0 + min(tb + i, cnt - 1);
+          r.pos[i] = posp[mod.positions ? row : 0];
+          r.doc[i] = docp[mod.documents ? row : 0];
+        }
+      }
       if (kMatrix && (tile + 1) * kTileTok <= cnt) {
         int64_t row[TOK];
 #pragma unroll
@@ -406,9 +442,11 @@ void attn_splitk_kernel(AttnArgs a) {
     // max grows), p * v with each head's weight broadcast from its lanes
     auto consume = [&](const Tile& x, int tile) __attribute__((always_inline)) {
       float s[TOK];
+      bool other[TOK];  // kMod 2: of another document
 #pragma unroll
       for (int i = 0; i < TOK; ++i) {
-        const bool valid = tile * kTileTok + gid * TOK + i < cnt;
+        const int t = tile * kTileTok + gid * TOK + i;
+        const bool valid = t < cnt;
         float d[G];
 #pragma unroll
         for (int h = 0; h < G; ++h) {
@@ -419,11 +457,27 @@ void attn_splitk_kernel(AttnArgs a) {
         float r;
         if constexpr (kMatrix) r = reduce_heads_mod8(d, sl);
         else r = reduce_heads<G>(d, sl);
-        s[i] = valid ? r * kScaleLog2 : -INFINITY;
+        if constexpr (kMod == 0) {
+          s[i] = valid ? r * kScaleLog2 : -INFINITY;
+        } else {
+          float v = mod.cap > 0.f ? mod.cap * kLog2e * tanh_any(r * to_cap) : r * kScaleLog2;
+          if (mod.slopes) {
+            int kpos = base + (int)(p0 + t);
+            if constexpr (kMod == 2) kpos = mod.positions ? x.pos[i] : kpos;
+            v = fmaf(-slope2, fabsf((float)(qpos - kpos)), v);
+          }
+          if constexpr (kMod == 2) {
+            other[i] = mod.documents && x.doc[i] != qdoc;
+            v = other[i] ? -INFINITY : v;
+          }
+          s[i] = valid ? v : -INFINITY;
+          if (scp && valid) scp[(p0 + t) * G] = v;
+        }
       }
       float mn = m;
 #pragma unroll
       for (int i = 0; i < TOK; ++i) mn = fmaxf(mn, s[i]);
+      if constexpr (kMod != 0) mn = fminf(mn, 3.402823466e38f);  // a score of +inf: the sum is inf, the output NaN
       if (__any(mn > m)) {
         const float corr = mn > m ? fast_exp2(m - mn) : 1.f;
         m = mn;
@@ -466,7 +520,13 @@ void attn_splitk_kernel(AttnArgs a) {
         short4_t vt[EPL];  // the four tokens' values of each dimension
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-          const uint32_t v0 = word(x.v[0], w), v1 = word(x.v[1], w), v2 = word(x.v[2], w), v3 = word(x.v[3], w);
+          uint32_t v0 = word(x.v[0], w), v1 = word(x.v[1], w), v2 = word(x.v[2], w), v3 = word(x.v[3], w);
+          if constexpr (kMod == 2) {  // no weight, also where the value is not finite
+            v0 = other[0] ? 0u : v0;
+            v1 = other[1] ? 0u : v1;
+            v2 = other[2] ? 0u : v2;
+            v3 = other[3] ? 0u : v3;
+          }
           vt[2 * w] = pair4(pack_lo(v0, v1), pack_lo(v2, v3));
           vt[2 * w + 1] = pair4(pack_hi(v0, v1), pack_hi(v2, v3));
         }
@@ -485,8 +545,10 @@ void attn_splitk_kernel(AttnArgs a) {
           float vf[EPL];
 #pragma unroll
           for (int w = 0; w < W; ++w) {
-            vf[2 * w] = bf16lo(word(x.v[i], w));
-            vf[2 * w + 1] = bf16hi(word(x.v[i], w));
+            uint32_t vw = word(x.v[i], w);
+            if constexpr (kMod == 2) vw = other[i] ? 0u : vw;  // no weight, also where the value is not finite
+            vf[2 * w] = bf16lo(vw);
+            vf[2 * w + 1] = bf16hi(vw);
           }
 #pragma unroll
           for (int h = 0; h < G; ++h) {
@@ -709,11 +771,16 @@ void attn_splitk_kernel(AttnArgs a) {
 // reductions, all loads independent of one another) and the slices add in
 // order.  Every sum has a fixed order, so results do not depend on
 // scheduling.  Groups without tokens get zeros.
-template <int G>
-__global__ __launch_bounds__(512) void combine_kernel(AttnArgs a) {
+//
+// kMore: the splits of a shared prefix join behind the group's own partials, and
+// the logarithm of the sum and the row's (maximum, 1 / sum) are written too; a row
+// that sees nothing gets zeros and -inf.
+template <int G, bool kMore>
+__global__ __launch_bounds__(512) void combine_kernel(AttnArgs a, std::conditional_t<kMore, JoinArgs, NoMod> more) {
   constexpr int kPart = G * (kHeadDim + 2);
-  __shared__ float s_w[kMaxAttnGrid];     // running maximum, then weight, of each partial
-  __shared__ float s_l[kMaxAttnGrid];     // running sum of each partial
+  constexpr int kCap = kMaxAttnGrid + (kMore ? kMaxSplits : 0);
+  __shared__ float s_w[kCap];             // running maximum, then weight, of each partial
+  __shared__ float s_l[kCap];             // running sum of each partial
   __shared__ float s_num[4][kHeadDim];
   __shared__ float s_red[8];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
@@ -723,12 +790,20 @@ __global__ __launch_bounds__(512) void combine_kernel(AttnArgs a) {
   float* out = a.out + ((int64_t)b * a.Hq + jg * G + h) * kHeadDim;
   // workgroups w0..w1 covered this group's tokens; their partials sit in slots bg + w
   const int64_t share = a.ameta[0], P0 = a.ameta[1 + bg], P1 = a.ameta[2 + bg];
-  if (P1 <= P0 || share <= 0) {
-    if (slice == 0) out[d] = 0.f;
-    return;
+  const bool none = P1 <= P0 || share <= 0;
+  if constexpr (!kMore) {
+    if (none) {
+      if (slice == 0) out[d] = 0.f;
+      return;
+    }
   }
-  const int64_t w0 = (P0 + kSegmentCost) / share, w1 = (P1 - 1) / share;
+  const int64_t w0 = none ? 0 : (P0 + kSegmentCost) / share, w1 = none ? -1 : (P1 - 1) / share;
   const int np = (int)min(w1 - w0 + 1, (int64_t)kMaxAttnGrid);
+  int npre = 0;  // splits of the sequence's prefix
+  const int64_t row = (int64_t)b * a.Hq + jg * G + h;
+  if constexpr (kMore) {
+    if (more.prefix_of && more.prefix_of[b] >= 0) npre = more.pre_splits;
+  }
   const float* pb = a.partials + (bg + w0) * kPart;
   const float* pd = pb + h * kHeadDim + d;  // this thread's output dimension of partial 0
   constexpr int kPre = 8;                   // numerator loads issued before the reductions
@@ -746,6 +821,15 @@ __global__ __launch_bounds__(512) void combine_kernel(AttnArgs a) {
     s_l[c] = pb[(int64_t)c * kPart + G * kHeadDim + G + h];
     mx = fmaxf(mx, mc);
   }
+  if constexpr (kMore) {
+    for (int c = tid; c < npre; c += 512) {
+      const float* ml = more.pre_ml + 2 * ((int64_t)c * more.rows + row);
+      s_w[np + c] = ml[0];
+      s_l[np + c] = ml[1];
+      mx = fmaxf(mx, ml[0]);
+    }
+    __syncthreads();  // (the weights below are not this thread's own entries)
+  }
   mx = wave_allmax_f(mx);
   if (lane == 0) s_red[wave] = mx;
   __syncthreads();
@@ -755,7 +839,7 @@ __global__ __launch_bounds__(512) void combine_kernel(AttnArgs a) {
   __syncthreads();  // s_red is reused below
   // 2. weights and denominator
   float den = 0.f;
-  for (int c = tid; c < np; c += 512) {  // the entries this thread wrote
+  for (int c = tid; c < np + npre; c += 512) {  // (not kMore: the entries this thread wrote)
     const float mc = s_w[c];
     const float wc = mc == -INFINITY ? 0.f : fast_exp2(mc - M);
     s_w[c] = wc;
@@ -773,68 +857,136 @@ __global__ __launch_bounds__(512) void combine_kernel(AttnArgs a) {
   }
 #pragma unroll 8
   for (int c = slice + 4 * kPre; c < np; c += 4) num = fmaf(s_w[c], pd[(int64_t)c * kPart], num);
+  if constexpr (kMore) {
+    const float* pre_o = more.pre_o + row * kHeadDim + d;
+#pragma unroll 4
+    for (int c = slice; c < npre; c += 4)  // (a split without keys wrote no sums)
+      if (s_w[np + c] != 0.f) num = fmaf(s_w[np + c], pre_o[(int64_t)c * more.rows * kHeadDim], num);
+  }
   s_num[slice][d] = num;
   __syncthreads();
   if (slice == 0) {
     float dd = 0.f;
 #pragma unroll
     for (int w = 0; w < 8; ++w) dd += s_red[w];
-    out[d] = (((s_num[0][d] + s_num[1][d]) + s_num[2][d]) + s_num[3][d]) / dd;
+    const float sum = ((s_num[0][d] + s_num[1][d]) + s_num[2][d]) + s_num[3][d];
+    if constexpr (kMore) {
+      const bool empty = M == -INFINITY;
+      out[d] = empty ? 0.f : sum / dd;
+      if (d == 0) {
+        if (more.lse) more.lse[row] = empty ? -INFINITY : (M + __builtin_amdgcn_logf(dd)) * kLn2;
+        if (more.norm) {
+          more.norm[2 * row] = M;
+          more.norm[2 * row + 1] = empty ? 0.f : 1.f / dd;
+        }
+      }
+    } else {
+      out[d] = sum / dd;
+    }
   }
 }
 
 static size_t attn_dyn_lds(const AttnArgs& a) { return ((size_t)a.B * a.NV + 1) * sizeof(int64_t); }
 
-template <bool kPaged>
-static hipError_t launch_attn_t(const AttnArgs& a, int G, int grid, hipStream_t st) {
+template <bool kPaged, int kMod, typename Mod>
+static hipError_t launch_attn_t(const AttnArgs& a, const Mod& m, int G, int grid, hipStream_t st) {
   const size_t lds = attn_dyn_lds(a);
   switch (G) {
-    case 1: hipLaunchKernelGGL((attn_splitk_kernel<1, attn_tok(1), kPaged>), dim3(grid), dim3(256), lds, st, a); break;
-    case 2: hipLaunchKernelGGL((attn_splitk_kernel<2, attn_tok(2), kPaged>), dim3(grid), dim3(256), lds, st, a); break;
-    case 4: hipLaunchKernelGGL((attn_splitk_kernel<4, attn_tok(4), kPaged>), dim3(grid), dim3(256), lds, st, a); break;
-    case 8: hipLaunchKernelGGL((attn_splitk_kernel<8, attn_tok(8), kPaged>), dim3(grid), dim3(256), lds, st, a); break;
+    case 1: hipLaunchKernelGGL((attn_splitk_kernel<1, attn_tok(1), kPaged, kMod>), dim3(grid), dim3(256), lds, st, a, m); break;
+    case 2: hipLaunchKernelGGL((attn_splitk_kernel<2, attn_tok(2), kPaged, kMod>), dim3(grid), dim3(256), lds, st, a, m); break;
+    case 4: hipLaunchKernelGGL((attn_splitk_kernel<4, attn_tok(4), kPaged, kMod>), dim3(grid), dim3(256), lds, st, a, m); break;
+    case 8: hipLaunchKernelGGL((attn_splitk_kernel<8, attn_tok(8), kPaged, kMod>), dim3(grid), dim3(256), lds, st, a, m); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();
 }
 
 hipError_t launch_attn(const AttnArgs& a, int G, int grid, bool paged, hipStream_t st) {
-  return paged ? launch_attn_t<true>(a, G, grid, st) : launch_attn_t<false>(a, G, grid, st);
+  return paged ? launch_attn_t<true, 0>(a, NoMod{}, G, grid, st) : launch_attn_t<false, 0>(a, NoMod{}, G, grid, st);
+}
+
+hipError_t launch_attn_mod(const AttnArgs& a, const TokenMod& m, int G, int grid, bool paged, hipStream_t st) {
+  const bool rows = m.positions || m.documents;
+  if (paged) return rows ? launch_attn_t<true, 2>(a, m, G, grid, st) : launch_attn_t<true, 1>(a, m, G, grid, st);
+  return rows ? launch_attn_t<false, 2>(a, m, G, grid, st) : launch_attn_t<false, 1>(a, m, G, grid, st);
 }
 
 // Workgroups of the attention kernel that fit on the device at once: the
 // persistent grid is sized to exactly this, so every workgroup streams its
 // share of the tokens from the start.
-template <bool kPaged>
+template <bool kPaged, int kMod>
 static hipError_t resident_t(int G, size_t lds, int* per) {
   switch (G) {
-    case 1: return hipOccupancyMaxActiveBlocksPerMultiprocessor(per, attn_splitk_kernel<1, attn_tok(1), kPaged>, 256, lds);
-    case 2: return hipOccupancyMaxActiveBlocksPerMultiprocessor(per, attn_splitk_kernel<2, attn_tok(2), kPaged>, 256, lds);
-    case 4: return hipOccupancyMaxActiveBlocksPerMultiprocessor(per, attn_splitk_kernel<4, attn_tok(4), kPaged>, 256, lds);
-    case 8: return hipOccupancyMaxActiveBlocksPerMultiprocessor(per, attn_splitk_kernel<8, attn_tok(8), kPaged>, 256, lds);
+    case 1: return hipOccupancyMaxActiveBlocksPerMultiprocessor(per, attn_splitk_kernel<1, attn_tok(1), kPaged, kMod>, 256, lds);
+    case 2: return hipOccupancyMaxActiveBlocksPerMultiprocessor(per, attn_splitk_kernel<2, attn_tok(2), kPaged, kMod>, 256, lds);
+    case 4: return hipOccupancyMaxActiveBlocksPerMultiprocessor(per, attn_splitk_kernel<4, attn_tok(4), kPaged, kMod>, 256, lds);
+    case 8: return hipOccupancyMaxActiveBlocksPerMultiprocessor(per, attn_splitk_kernel<8, attn_tok(8), kPaged, kMod>, 256, lds);
     default: return hipErrorInvalidValue;
   }
 }
 
-hipError_t attn_resident_grid(int G, int n_groups, bool paged, int* grid, int* compute_units) {
+hipError_t attn_resident_grid(int G, int n_groups, bool paged, int* grid, int* compute_units, int mod) {
   int dev = 0, cus = 0, per = 0;
   const size_t lds = ((size_t)n_groups + 1) * sizeof(int64_t);
   hipError_t e = hipGetDevice(&dev);
   if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
   if (e != hipSuccess) return e;
-  e = paged ? resident_t<true>(G, lds, &per) : resident_t<false>(G, lds, &per);
+  switch (mod) {
+    case 0: e = paged ? resident_t<true, 0>(G, lds, &per) : resident_t<false, 0>(G, lds, &per); break;
+    case 1: e = paged ? resident_t<true, 1>(G, lds, &per) : resident_t<false, 1>(G, lds, &per); break;
+    default: e = paged ? resident_t<true, 2>(G, lds, &per) : resident_t<false, 2>(G, lds, &per); break;
+  }
   *grid = (per > 0 ? per : 1) * (cus > 0 ? cus : 1);
   if (compute_units) *compute_units = cus > 0 ? cus : 1;
   return e;
 }
 
-hipError_t launch_combine(const AttnArgs& a, int G, hipStream_t st) {
+template <bool kMore, typename More>
+static hipError_t launch_combine_t(const AttnArgs& a, const More& m, int G, hipStream_t st) {
   const dim3 grid(a.B * a.NV, G);
   switch (G) {
-    case 1: hipLaunchKernelGGL(combine_kernel<1>, grid, dim3(512), 0, st, a); break;
-    case 2: hipLaunchKernelGGL(combine_kernel<2>, grid, dim3(512), 0, st, a); break;
-    case 4: hipLaunchKernelGGL(combine_kernel<4>, grid, dim3(512), 0, st, a); break;
-    case 8: hipLaunchKernelGGL(combine_kernel<8>, grid, dim3(512), 0, st, a); break;
+    case 1: hipLaunchKernelGGL((combine_kernel<1, kMore>), grid, dim3(512), 0, st, a, m); break;
+    case 2: hipLaunchKernelGGL((combine_kernel<2, kMore>), grid, dim3(512), 0, st, a, m); break;
+    case 4: hipLaunchKernelGGL((combine_kernel<4, kMore>), grid, dim3(512), 0, st, a, m); break;
+    case 8: hipLaunchKernelGGL((combine_kernel<8, kMore>), grid, dim3(512), 0, st, a, m); break;
+    default: return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_combine(const AttnArgs& a, int G, hipStream_t st) { return launch_combine_t<false>(a, NoMod{}, G, st); }
+hipError_t launch_join(const AttnArgs& a, const JoinArgs& j, int G, hipStream_t st) { return launch_combine_t<true>(a, j, G, st); }
+
+// The running sums of attention weights: one thread per cached row and KV head
+// adds its group's 2^(s - M) / L (s from the decode, M and 1 / L from the
+// combine).  grid (rows / 256, Hkv, B).  Reads 4 G bytes and writes 4 of each row.
+template <int G>
+__global__ __launch_bounds__(256) void add_weights_kernel(const float* scores, const float* norm, const int64_t* kv_indptr,
+                                                          const int64_t* seq_len, int64_t total, float* weights) {
+  const int g = blockIdx.y, b = blockIdx.z, Hkv = gridDim.y;
+  const int64_t n = seq_tokens(kv_indptr, seq_len, b), r = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (r >= n) return;
+  const int64_t at = (int64_t)g * total + kv_indptr[b] + r;
+  const float* nm = norm + 2 * (((int64_t)b * Hkv + g) * G);
+  float w = weights[at];
+  float x = 0.f;
+#pragma unroll
+  for (int h = 0; h < G; ++h) {
+    const float s = scores[at * G + h];
+    if (s != -INFINITY) x = fmaf(fast_exp2(s - nm[2 * h]), nm[2 * h + 1], x);
+  }
+  weights[at] = w + x;
+}
+
+hipError_t launch_add_weights(const AttnArgs& a, const float* scores, const float* norm, int64_t max_len, float* weights,
+                              int G, hipStream_t st) {
+  if (max_len == 0) return hipSuccess;
+  const dim3 grid((unsigned)((max_len + 255) / 256), a.Hkv, a.B);
+  switch (G) {
+    case 1: hipLaunchKernelGGL(add_weights_kernel<1>, grid, dim3(256), 0, st, scores, norm, a.kv_indptr, a.seq_len, a.total, weights); break;
+    case 2: hipLaunchKernelGGL(add_weights_kernel<2>, grid, dim3(256), 0, st, scores, norm, a.kv_indptr, a.seq_len, a.total, weights); break;
+    case 4: hipLaunchKernelGGL(add_weights_kernel<4>, grid, dim3(256), 0, st, scores, norm, a.kv_indptr, a.seq_len, a.total, weights); break;
+    case 8: hipLaunchKernelGGL(add_weights_kernel<8>, grid, dim3(256), 0, st, scores, norm, a.kv_indptr, a.seq_len, a.total, weights); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();

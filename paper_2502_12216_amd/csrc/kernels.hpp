@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include "common.hpp"
+#include "scores.hpp"
 
 namespace tactic {
 
@@ -145,13 +146,120 @@ struct AttnArgs {
   float* out;                 // [B][Hq][128]
 };
 
+// Attention of many query rows (rows_attn.hip).  mode 0: the prompt form, source b is
+// sequence b with queries [q_indptr[b], q_indptr[b+1]), the last of its tokens; mode 1:
+// a shared prefix, source p is prefix p with the sequences members[member_indptr[p] ..].
+struct RowsArgs {
+  const uint16_t* q;
+  const uint16_t* K;
+  const uint16_t* V;
+  const int64_t* kv_indptr;     // [n_src + 1] of the sources
+  const int64_t* seq_len;       // [n_src] or null
+  int mode, n_src, Hq, Hkv, G, splits, direct, paged;
+  int64_t total, n_queries;     // rows per KV head of K and V; queries in q
+  const int64_t* q_indptr;      // mode 0
+  const int32_t* members;       // mode 1
+  const int32_t* member_indptr;
+  const int64_t* own_indptr;    // mode 1: the sequences' own tokens, for the queries' positions
+  const int64_t* own_len;
+  float cap;                    // 0: none
+  const float* slopes;          // [Hq] or null
+  const int32_t* documents;     // [total] or null (mode 0)
+  const int32_t* prefix_len;    // [n_src] or null (mode 0)
+  const int2* doc_range;        // [n_src][range_stride]: documents of each 64-row tile
+  int64_t range_stride;
+  PagedKV pk;
+  float* part_o;                // [splits][n_queries * Hq][128]
+  float* part_ml;               // [splits][n_queries * Hq][2]: reference maximum (base 2), sum
+  uint16_t* out;                // bf16 [n_queries][Hq][128]
+  float* lse;                   // [Hq][n_queries] or null
+};
+
+// Accumulated attention weights of a prompt's queries (cache_rows.hip).
+struct WeightArgs {
+  const uint16_t* q;
+  const uint16_t* K;
+  const int64_t* kv_indptr;
+  const int64_t* seq_len;
+  const int64_t* q_indptr;
+  const float* lse;             // [Hq][n_queries]
+  int B, Hq, Hkv, G, splits;
+  int64_t total, n_queries, window;  // window 0: every query
+  float cap;
+  const float* slopes;
+  const int32_t* documents;
+  const int32_t* prefix_len;
+  float* part;                  // [splits][Hkv][total], splits > 1
+  float* weights;               // [Hkv][total]
+};
+
+// Eviction into another cache, and insertion of single tokens (cache_rows.hip).
+struct EvictArgs {
+  const uint16_t* K;
+  const uint16_t* V;
+  const float* weights;         // [Hkv][total]
+  const int32_t* positions;     // [Hkv][total] or null: the row
+  const int64_t* kv_indptr;
+  const int64_t* seq_len;
+  const int32_t* keep;          // [B]
+  const int32_t* newest;        // [B] or null: tokens - 1
+  const int64_t* out_indptr;
+  int B, Hkv, recent;
+  int64_t total, out_total;
+  uint16_t* K_out;
+  uint16_t* V_out;
+  float* weights_out;           // [Hkv][out_total]
+  int32_t* positions_out;
+  int64_t* out_len;             // [B]
+  int32_t* rows;                // [Hkv][out_total] workspace: the kept rows
+};
+struct InsertArgs {
+  const uint16_t* k;            // [B][Hkv][128]
+  const uint16_t* v;
+  uint16_t* K;
+  uint16_t* V;
+  float* weights;
+  int32_t* positions;
+  const int32_t* newest;        // [B] position of the new token
+  const int64_t* kv_indptr;
+  int64_t* seq_len;
+  int B, Hkv, recent;
+  int64_t total;
+  int32_t* rows;                // [B][Hkv]
+};
+hipError_t launch_prompt_weights(const WeightArgs& a, int64_t max_len, hipStream_t st);
+hipError_t launch_evict(const EvictArgs& a, int64_t max_out, hipStream_t st);
+hipError_t launch_insert(const InsertArgs& a, hipStream_t st);
+
+// What the combine of the single-token forms joins and writes beside the outputs.
+constexpr int kMaxSplits = 64;  // splits of a row tile's keys
+struct JoinArgs {
+  float* lse;                   // [B][Hq] or null
+  float* norm;                  // [B][Hq][2] or null: maximum (base 2), 1 / sum
+  const float* pre_o;           // [pre_splits][rows][128]
+  const float* pre_ml;          // [pre_splits][rows][2]
+  const int32_t* prefix_of;     // [B] or null: negative for a sequence without a prefix
+  int pre_splits;
+  int64_t rows;                 // B * Hq
+};
+
+// variants 0 to 3: 32, 64, 128 or 256 rows per item
+int rows_per_item(int variant);
+hipError_t launch_doc_range(const RowsArgs& a, int64_t max_tiles, hipStream_t st);
+hipError_t launch_rows_attn(const RowsArgs& a, int variant, bool exact_weights, int64_t items, hipStream_t st);
+hipError_t launch_rows_combine(const RowsArgs& a, hipStream_t st);
+
 hipError_t launch_score(const ScoreArgs& a, int G, int grid_x, int grid_y, hipStream_t st);
 hipError_t launch_sort(const SortArgs& a, bool lds, int n_heads, hipStream_t st);
 hipError_t launch_sample(const FitArgs& a, int split, int n_heads, bool paged, hipStream_t st);
 hipError_t launch_fit_union(const FitArgs& a, int G, int n_groups, hipStream_t st);
 hipError_t launch_attn(const AttnArgs& a, int G, int grid, bool paged, hipStream_t st);
 hipError_t launch_combine(const AttnArgs& a, int G, hipStream_t st);
-hipError_t attn_resident_grid(int G, int n_groups, bool paged, int* grid, int* compute_units = nullptr);
+hipError_t attn_resident_grid(int G, int n_groups, bool paged, int* grid, int* compute_units = nullptr, int mod = 0);
+hipError_t launch_attn_mod(const AttnArgs& a, const TokenMod& m, int G, int grid, bool paged, hipStream_t st);
+hipError_t launch_join(const AttnArgs& a, const JoinArgs& j, int G, hipStream_t st);
+hipError_t launch_add_weights(const AttnArgs& a, const float* scores, const float* norm, int64_t max_len, float* weights,
+                              int G, hipStream_t st);
 hipError_t launch_stream_read(const void* buf, int64_t n16, int workgroups, uint32_t* sink, hipStream_t st);
 
 }  // namespace tactic

@@ -1,0 +1,607 @@
+// Attention of many query rows over one key sequence on the matrix unit: the
+// prompt form (the rows are the G heads of consecutive tokens) and the shared
+// prefix of a decode batch (the rows are the G heads of the sequences that
+// share it).
+//
+// A work item is a row tile (32 rows for each of RW waves) of one KV head and a
+// range of its keys, in tiles of TK.  A wave computes S^T = K Q^T with
+// v_mfma_f32_32x32x16_bf16, so that a lane's accumulators belong to one query
+// row (column lane % 32) and the running maximum and sum of the softmax need one
+// exchange, with lane ^ 32.  The weights of 16 keys in a lane are then the B
+// operand of O^T += V^T P^T as they stand: the matrix unit sums over keys, so
+// their order is free as long as V^T has the same, and the transposing LDS read
+// (ds_read_b64_tr_b16) gives four consecutive keys of one dimension, which is the
+// order the accumulators of S^T have.  KW groups of waves take every KW-th tile
+// and are merged at the end; with more items than keys the ranges are split and
+// joined by rows_combine_kernel, in a fixed order.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "common.hpp"
+#include "kernels.hpp"
+#include "scores.hpp"
+
+namespace tactic {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// LDS rows are 16 chunks of 16 bytes; logical chunk c of row r is stored at chunk
+// c ^ row_swizzle(r): 16 consecutive rows at one chunk (the K operand) and 4 rows
+// of 4 chunks (the transposing V read) both fall in distinct banks.
+__device__ __forceinline__ int row_swizzle(int r) { return 4 * (r & 3) + ((r >> 2) & 3); }
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const f32x2 x = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+}
+
+// Eight weights as the bf16 operands of PARTS products.  1: rounded to nearest
+// (outputs in bf16: off by at most 2^-8 of a weight, as the output's own
+// rounding).  3: an exact split of the fp32 weight for outputs in fp32; the lower
+// parts of a weight that is not zero are at least 2^-126, so that its product with
+// an infinite value stays that infinity.
+template <int PARTS>
+__device__ __forceinline__ void weight_operands(const float* p, bf16x8 (&out)[PARTS]) {
+  if constexpr (PARTS == 1) {
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = pack_bf16(p[2 * i], p[2 * i + 1]);
+    out[0] = __builtin_bit_cast(bf16x8, w);
+  } else {
+    u32x4 w[3];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t h[2], m[2], l[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float x = p[2 * i + j], least = fminf(x, 0x1p-126f);
+        h[j] = __float_as_uint(x);
+        const float r = x - __uint_as_float(h[j] & 0xffff0000u);
+        m[j] = __float_as_uint(fmaxf(r, least));
+        l[j] = __float_as_uint(fmaxf(r - __uint_as_float(__float_as_uint(r) & 0xffff0000u), least));
+      }
+      w[0][i] = __builtin_amdgcn_perm(h[1], h[0], 0x07060302u);
+      w[1][i] = __builtin_amdgcn_perm(m[1], m[0], 0x07060302u);
+      w[2][i] = __builtin_amdgcn_perm(l[1], l[0], 0x07060302u);
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) out[k] = __builtin_bit_cast(bf16x8, w[k]);
+  }
+}
+
+__device__ __forceinline__ float swap_half(float x) { return __shfl_xor(x, 32, 64); }
+
+// Page-table lookup of token `tok` of sequence b (in bounds whatever the table holds).
+__device__ __forceinline__ int64_t page_row(const PagedKV& pk, int Hkv, int b, int kvh, int tok) {
+  const uint32_t pg = (uint32_t)tok / (uint32_t)pk.page_size;
+  int64_t page = pk.page_table[(int64_t)b * pk.max_pages + pg];
+  page = min(max(page, (int64_t)0), pk.num_pages - 1);
+  return (page * Hkv + kvh) * pk.page_size + (tok - (int)(pg * (uint32_t)pk.page_size));
+}
+
+constexpr float kMaxFinite = 3.402823466e38f;  // a score of +inf: the sum becomes inf (its logarithm too), the output NaN
+constexpr float kRescaleSlack = 8.f;  // base-2: a weight may exceed 1 by 2^8 before the sums are rescaled
+
+template <int RW, int KW, int TK, int PARTS>
+__global__ __launch_bounds__(RW * KW * 64) __attribute__((amdgpu_waves_per_eu(2)))
+void rows_attn_kernel(RowsArgs a) {
+  constexpr int ROWS = RW * 32, NW = RW * KW, NB = TK / 32;
+  constexpr int kBufs = RW > 1 ? 2 : 1;                  // one wave alone reads and writes its tile in turn
+  constexpr int kTileBytes = TK * 256 * 2;               // K rows, then V rows
+  constexpr int kLoads = TK * 16 / (RW * 64);            // 16-byte chunks of K (and of V) per thread and tile
+  constexpr int kStage = KW * kBufs * kTileBytes, kMerge = KW > 1 ? NW * 16384 : 0;
+  __shared__ __align__(1024) unsigned char smem[kStage > kMerge ? kStage : kMerge];
+  __shared__ float s_ml[2][NW][32];
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int wr = wave % RW, kg = wave / RW, half = lane >> 5, col = lane & 31;
+
+  // ---- the work item: KV head (fastest, so that a head's items share an XCD's L2
+  // where 8 divides the heads), split, row tile of a source
+  const int g = blockIdx.x % a.Hkv;
+  int rest = blockIdx.x / a.Hkv;
+  const int split = rest % a.splits;
+  rest /= a.splits;
+  int src = 0;
+  {
+    // tiles of source b start at floor(rows before it / ROWS) + b at the latest
+    int lo = 0, hi = a.n_src - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      const int64_t before = a.mode == 0 ? a.q_indptr[mid] : (int64_t)a.member_indptr[mid];
+      if (before * a.G / ROWS + mid <= rest) lo = mid;
+      else hi = mid - 1;
+    }
+    src = lo;
+  }
+  const int64_t q0 = a.mode == 0 ? a.q_indptr[src] : (int64_t)a.member_indptr[src];
+  const int64_t q1 = a.mode == 0 ? a.q_indptr[src + 1] : (int64_t)a.member_indptr[src + 1];
+  const int nrows = (int)((q1 - q0) * a.G);
+  const int ntile = (nrows + ROWS - 1) / ROWS;
+  int tile = rest - (int)(q0 * a.G / ROWS) - src;
+  if (tile < 0 || tile >= ntile) return;
+  tile = ntile - 1 - tile;  // the last rows of a prompt see the most keys: first
+  const int row0 = tile * ROWS;
+  const int64_t kvb = a.kv_indptr[src];
+  const int n = (int)seq_tokens(a.kv_indptr, a.seq_len, src);
+
+  // ---- this lane's row (rows past the end repeat the last one and are not stored)
+  const int row = min(row0 + wr * 32 + col, nrows - 1);
+  const bool own_row = row0 + wr * 32 + col < nrows;
+  const int h = row % a.G;
+  int64_t qrow;         // row of q, out and lse: query * Hq + head
+  int qpos, klim = n;   // keys [0, klim) are seen
+  int qdoc = 0;
+  if (a.mode == 0) {
+    const int i = row / a.G;
+    const int64_t m = q1 - q0;
+    qrow = (q0 + i) * a.Hq + g * a.G + h;
+    qpos = (int)(n - m + i);
+    const int pre = a.prefix_len ? a.prefix_len[src] : 0;
+    klim = min(max(max(qpos + 1, pre), 0), n);
+    if (a.documents) qdoc = qpos >= 0 ? a.documents[kvb + qpos] : 0;
+    if (qpos < 0) klim = 0;  // more queries than tokens: those ahead of the first see nothing
+  } else {
+    const int b = a.members[q0 + row / a.G];
+    qrow = (int64_t)b * a.Hq + g * a.G + h;
+    qpos = n + (int)seq_tokens(a.own_indptr, a.own_len, b) - 1;
+  }
+  // the item's keys: those that its last row sees (prompt rows see ever more)
+  int kend = n;
+  if (a.mode == 0) {
+    const int last = min(row0 + ROWS, nrows) - 1;
+    const int lp = (int)(n - (q1 - q0) + last / a.G);
+    const int pre = a.prefix_len ? a.prefix_len[src] : 0;
+    kend = lp < 0 ? 0 : min(max(lp + 1, pre), n);
+  }
+  const int ktiles = (kend + TK - 1) / TK;
+  const int t_lo = (int)((int64_t)ktiles * split / a.splits), t_hi = (int)((int64_t)ktiles * (split + 1) / a.splits);
+
+  // uniform limits of the wave's rows
+  int w_lo = klim, w_hi = klim, d_lo = qdoc, d_hi = qdoc;
+#pragma unroll
+  for (int s = 1; s < 32; s <<= 1) {
+    w_lo = min(w_lo, __shfl_xor(w_lo, s, 64));
+    w_hi = max(w_hi, __shfl_xor(w_hi, s, 64));
+    d_lo = min(d_lo, __shfl_xor(d_lo, s, 64));
+    d_hi = max(d_hi, __shfl_xor(d_hi, s, 64));
+  }
+  w_lo = __builtin_amdgcn_readfirstlane(w_lo);
+  w_hi = __builtin_amdgcn_readfirstlane(w_hi);
+  d_lo = __builtin_amdgcn_readfirstlane(d_lo);
+  d_hi = __builtin_amdgcn_readfirstlane(d_hi);
+
+  const float slope = a.slopes ? a.slopes[g * a.G + h] * kLog2e : 0.f;
+  const float to_cap = a.cap > 0.f ? kInvSqrtDim / a.cap : 0.f, cap2 = a.cap * kLog2e;
+
+  bf16x8 qf[8];
+  {
+    const uint16_t* qp = a.q + qrow * kHeadDim + 8 * half;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) qf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(qp + 16 * s));
+  }
+
+  // documents: the range of each 64-key tile (from doc_range_kernel) and, for the
+  // item's queries, that of the tiles they lie in
+  const int2* dr = a.documents ? a.doc_range + (int64_t)src * a.range_stride : nullptr;
+  int i_lo = 0, i_hi = 0;
+  if (dr) {
+    const int64_t m = q1 - q0;
+    const int p0 = max((int)(n - m + row0 / a.G), 0), p1 = (int)(n - m + (min(row0 + ROWS, nrows) - 1) / a.G);
+    i_lo = INT32_MAX;
+    i_hi = INT32_MIN;
+    if (p1 >= 0) {
+      for (int t = p0 / 64; t <= p1 / 64; ++t) {
+        i_lo = min(i_lo, dr[t].x);
+        i_hi = max(i_hi, dr[t].y);
+      }
+    }
+  }
+  // first tile from t on, in steps of KW, that may hold a seen key (t_hi or more: none)
+  auto next_tile = [&](int t) __attribute__((always_inline)) -> int {
+    if (!dr) return t;
+    while (t < t_hi) {
+      const int mine = t + lane * KW;
+      bool some = false;
+      if (mine < t_hi) {
+        const int2 r = dr[mine * TK / 64];
+        some = r.x <= i_hi && r.y >= i_lo;
+      }
+      const uint64_t any = __ballot(some);
+      if (any) return t + (__ffsll((unsigned long long)any) - 1) * KW;
+      t += 64 * KW;
+    }
+    return t;
+  };
+  // with several waves to a tile and several tiles at a time all of them step together
+  constexpr bool kSkip = RW == 1 || KW == 1;
+
+  const uint16_t* Kb = a.K + (a.paged ? 0 : ((int64_t)g * a.total + kvb) * kHeadDim);
+  const uint16_t* Vb = a.V + (a.paged ? 0 : ((int64_t)g * a.total + kvb) * kHeadDim);
+  uint4 kreg[kLoads], vreg[kLoads];
+  // chunk i of this thread: stored chunk (wr * kLoads + i) * 64 + lane of the group's tile
+  auto fetch = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int c = (wr * kLoads + i) * 64 + lane, r = c >> 4;
+      const int tok = min(t * TK + r, n - 1);
+      const int64_t at = (a.paged ? page_row(a.pk, a.Hkv, src, g, tok) : (int64_t)tok) * kHeadDim + (((c & 15) ^ row_swizzle(r)) * 8);
+      kreg[i] = *reinterpret_cast<const uint4*>(Kb + at);
+      vreg[i] = *reinterpret_cast<const uint4*>(Vb + at);
+    }
+  };
+  auto store = [&](int buf) __attribute__((always_inline)) {
+    unsigned char* base = smem + (kg * kBufs + buf) * kTileBytes + (wr * kLoads * 64 + lane) * 16;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      *reinterpret_cast<uint4*>(base + i * 1024) = kreg[i];
+      *reinterpret_cast<uint4*>(base + i * 1024 + TK * 256) = vreg[i];
+    }
+  };
+
+  float m_run = -INFINITY, l_run = 0.f;
+  f32x16 o[4];
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+
+  auto compute = [&](int t, int buf) __attribute__((always_inline)) {
+    const unsigned char* kt = smem + (kg * kBufs + buf) * kTileBytes;
+    const unsigned char* vt = kt + TK * 256;
+    const int k0 = t * TK;
+    if (k0 >= w_hi) return;  // none of the wave's rows sees the tile
+    bool masked = k0 + TK > w_lo, docs = false;
+    if (dr) {
+      const int2 r = dr[k0 / 64];
+      if (r.x > d_hi || r.y < d_lo) return;
+      docs = !(r.x == r.y && d_lo == d_hi);
+      masked |= docs;
+    }
+    f32x16 s[NB];
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+      const unsigned char* krow = kt + (kb * 32 + col) * 256;
+#pragma unroll
+      for (int st = 0; st < 8; ++st) {
+        const bf16x8 kf = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(krow + (((2 * st + half) ^ row_swizzle(col)) * 16)));
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[st], s[kb], 0, 0, 0);
+      }
+    }
+    // base-2 scores; accumulator r of block kb is key k0 + 32 kb + 8 (r / 4) + 4 half + r % 4
+    if (a.cap > 0.f) {
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[kb][r] = cap2 * tanh_any(s[kb][r] * to_cap);
+    } else {
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[kb][r] *= kInvSqrtDim * kLog2e;
+    }
+    if (a.slopes) {
+      const float dist = (float)(qpos - k0 - 4 * half);
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          s[kb][r] = fmaf(-slope, fabsf(dist - (float)(kb * 32 + 8 * (r / 4) + r % 4)), s[kb][r]);
+    }
+    if (masked) {
+      const int lim = klim - k0 - 4 * half;
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (kb * 32 + 8 * (r / 4) + r % 4 >= lim) s[kb][r] = -INFINITY;
+      if (docs) {
+        const int32_t* dk = a.documents + kvb;
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (dk[min(k0 + 4 * half + kb * 32 + 8 * (r / 4) + r % 4, n - 1)] != qdoc) s[kb][r] = -INFINITY;
+      }
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
+    mx = fmaxf(mx, swap_half(mx));
+    // the sums keep an old maximum as their reference while no weight exceeds 2^8
+    if (__any(mx > m_run + kRescaleSlack)) {
+      const float mn = fminf(fmaxf(mx, m_run), kMaxFinite);
+      const float c = mn > m_run ? fast_exp2(m_run - mn) : 1.f;
+      m_run = mn;
+      l_run *= c;
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] *= c;
+    }
+    const float ref = m_run == -INFINITY ? 0.f : m_run;
+    float p[NB * 16];
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float x = fast_exp2(s[kb][r] - ref);
+        p[kb * 16 + r] = x;
+        l_run += x;
+      }
+    // a masked key's weight is 0, but 0 times its value is NaN where that is not
+    // finite: such tiles (looked for where something is masked) go another way
+    bool odd = false;
+    if (masked) {
+      uint32_t bad = 0;
+#pragma unroll
+      for (int i = 0; i < TK * 16 / 64; ++i) {
+        const uint4 w = *reinterpret_cast<const uint4*>(vt + (i * 64 + lane) * 16);
+        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          bad |= ((x[j] & 0x7f80u) == 0x7f80u) | ((x[j] & 0x7f800000u) == 0x7f800000u);
+      }
+      odd = __any(bad != 0);
+    }
+    // V^T operand of key chunk c (16 keys) and dimensions 32 d ..: two transposing
+    // reads of 4 keys; lane l of a group of 16 gives the address of row l / 4, 8-byte piece l % 4
+    auto v_operand = [&](int c, int d) __attribute__((always_inline)) -> u32x4 {
+      const int vr = 16 * c + 4 * half + ((lane & 15) >> 2), chunk = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+      const unsigned char* p0 = vt + vr * 256 + ((chunk ^ row_swizzle(vr)) * 16) + (lane & 1) * 8;
+      const unsigned char* p1 = vt + (vr + 8) * 256 + ((chunk ^ row_swizzle(vr + 8)) * 16) + (lane & 1) * 8;
+      typedef __attribute__((address_space(3))) s16x4* lds4;
+      const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)p0));
+      const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)p1));
+      return u32x4{x.x, x.y, y.x, y.y};
+    };
+    if (!odd) {
+#pragma unroll
+      for (int c = 0; c < TK / 16; ++c) {
+        bf16x8 pf[PARTS];
+        weight_operands<PARTS>(p + 8 * c, pf);
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          const bf16x8 vf = __builtin_bit_cast(bf16x8, v_operand(c, d));
+#pragma unroll
+          for (int k = PARTS - 1; k >= 0; --k) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[k], o[d], 0, 0, 0);
+        }
+      }
+    } else {
+      // finite values as above; then, for each kind of value that is not finite,
+      // whether a key with a weight has it in this dimension
+#pragma unroll 1
+      for (int kind = 0; kind < 4; ++kind) {  // finite, +inf, -inf, NaN
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          f32x16 seen;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) seen[r] = 0.f;
+#pragma unroll
+          for (int c = 0; c < TK / 16; ++c) {
+            u32x4 w = v_operand(c, d);
+            float q[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) q[j] = kind == 0 ? p[8 * c + j] : (p[8 * c + j] != 0.f ? 1.f : 0.f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const uint32_t sh = 16 * (j & 1), v = (w[j >> 1] >> sh) & 0xffffu;
+              const bool inf = (v & 0x7fffu) == 0x7f80u, nan = (v & 0x7fffu) > 0x7f80u;
+              uint32_t use;
+              if (kind == 0) use = inf || nan ? 0u : v;
+              else use = (kind == 3 ? nan : (inf && (v >> 15) == (uint32_t)(kind == 2))) ? 0x3f80u : 0u;
+              w[j >> 1] = (w[j >> 1] & ~(0xffffu << sh)) | (use << sh);
+            }
+            bf16x8 pf[PARTS];
+            weight_operands<PARTS>(q, pf);
+#pragma unroll
+            for (int k = PARTS - 1; k >= 0; --k)
+              seen = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pf[k], seen, 0, 0, 0);
+          }
+          const float val = kind == 1 ? INFINITY : (kind == 2 ? -INFINITY : NAN);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[d][r] += kind == 0 ? seen[r] : (seen[r] >= 0.5f ? val : 0.f);
+        }
+      }
+    }
+  };
+
+  // ---- the keys: the next tile's rows are in flight while this one is contracted
+  if constexpr (kSkip) {
+    int t = next_tile(t_lo + kg);
+    int buf = 0;
+    if (t < t_hi) {
+      fetch(t);
+      store(0);
+    }
+    if constexpr (RW > 1) __syncthreads();
+    while (t < t_hi) {
+      const int tn = next_tile(t + KW);
+      if (tn < t_hi) fetch(tn);
+      compute(t, buf);
+      if constexpr (RW > 1) buf ^= 1;
+      if (tn < t_hi) store(buf);
+      if constexpr (RW > 1) __syncthreads();
+      t = tn;
+    }
+  } else {
+    const int steps = (t_hi - t_lo + KW - 1) / KW;
+    int buf = 0;
+    if (t_lo + kg < t_hi) {
+      fetch(t_lo + kg);
+      store(0);
+    }
+    __syncthreads();
+    for (int i = 0; i < steps; ++i) {
+      const int t = t_lo + i * KW + kg;
+      if (t + KW < t_hi) fetch(t + KW);
+      if (t < t_hi) compute(t, buf);
+      buf ^= 1;
+      if (t + KW < t_hi) store(buf);
+      __syncthreads();
+    }
+  }
+
+  // ---- the sums of both halves, then of the KW groups
+  l_run += swap_half(l_run);
+  int d_from = 0, d_to = 4;
+  if constexpr (KW > 1) {
+    __syncthreads();  // the tiles are dead: their storage takes the groups' sums
+    if (half == 0) {
+      s_ml[0][wave][col] = m_run;
+      s_ml[1][wave][col] = l_run;
+    }
+    __syncthreads();
+    float mm = -INFINITY, ll = 0.f;
+#pragma unroll
+    for (int j = 0; j < KW; ++j) mm = fmaxf(mm, s_ml[0][j * RW + wr][col]);
+#pragma unroll
+    for (int j = 0; j < KW; ++j) {
+      const float mj = s_ml[0][j * RW + wr][col];
+      if (mj != -INFINITY) ll = fmaf(s_ml[1][j * RW + wr][col], fast_exp2(mj - mm), ll);
+    }
+    const float c = m_run == -INFINITY ? 0.f : fast_exp2(m_run - mm);
+    float* red = reinterpret_cast<float*>(smem);
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) red[(wave * 64 + d * 16 + r) * 64 + lane] = m_run == -INFINITY ? 0.f : o[d][r] * c;
+    __syncthreads();
+    m_run = mm;
+    l_run = ll;
+    d_from = kg * (4 / KW);
+    d_to = d_from + 4 / KW;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      if (d < d_from || d >= d_to) continue;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float x = 0.f;
+#pragma unroll
+        for (int j = 0; j < KW; ++j) x += red[((j * RW + wr) * 64 + d * 16 + r) * 64 + lane];
+        o[d][r] = x;
+      }
+    }
+  }
+  if (!own_row) return;
+  if (a.direct) {
+    const float inv = l_run != 0.f ? 1.f / l_run : 0.f;  // (NaN stays NaN)
+    uint16_t* op = a.out + qrow * kHeadDim + 4 * half;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      if (d < d_from || d >= d_to) continue;
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        u32x2 w = {pack_bf16(o[d][r] * inv, o[d][r + 1] * inv), pack_bf16(o[d][r + 2] * inv, o[d][r + 3] * inv)};
+        *reinterpret_cast<u32x2*>(op + d * 32 + 2 * r) = w;
+      }
+    }
+    if (a.lse && kg == 0 && half == 0) {
+      const int64_t hq = qrow % a.Hq, qi = qrow / a.Hq;
+      a.lse[hq * a.n_queries + qi] = m_run == -INFINITY ? -INFINITY : (m_run + __builtin_amdgcn_logf(l_run)) * kLn2;
+    }
+  } else {
+    const int64_t slot = (int64_t)split * a.n_queries * a.Hq + qrow;
+    float* op = a.part_o + slot * kHeadDim + 4 * half;
+    if (m_run != -INFINITY) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        if (d < d_from || d >= d_to) continue;
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+          *reinterpret_cast<float4*>(op + d * 32 + 2 * r) = make_float4(o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]);
+      }
+    }
+    if (kg == 0 && half == 0) {
+      a.part_ml[2 * slot] = m_run;
+      a.part_ml[2 * slot + 1] = l_run;
+    }
+  }
+}
+
+// Range of the documents of every 64-row tile: grid (tiles, sequences), one wave each.
+__global__ __launch_bounds__(64) void doc_range_kernel(const int32_t* documents, const int64_t* kv_indptr,
+                                                       const int64_t* seq_len, int64_t stride, int2* out) {
+  const int b = blockIdx.y, t = blockIdx.x;
+  const int n = (int)seq_tokens(kv_indptr, seq_len, b);
+  if (t * 64 >= n) return;
+  const int32_t d = documents[kv_indptr[b] + min(t * 64 + (int)threadIdx.x, n - 1)];
+  int lo = d, hi = d;
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    lo = min(lo, __shfl_xor(lo, s, 64));
+    hi = max(hi, __shfl_xor(hi, s, 64));
+  }
+  if (threadIdx.x == 0) out[b * stride + t] = make_int2(lo, hi);
+}
+
+// Joins the splits of a row: out = sum_s O_s 2^(m_s - M) / sum_s l_s 2^(m_s - M),
+// in the order of the splits.  One wave per row, two dimensions per lane.
+__global__ __launch_bounds__(256) void rows_combine_kernel(RowsArgs a) {
+  const int64_t rows = a.n_queries * a.Hq;
+  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (r >= rows) return;
+  float mx = -INFINITY;
+  for (int s = 0; s < a.splits; ++s) mx = fmaxf(mx, a.part_ml[2 * ((int64_t)s * rows + r)]);
+  float x = 0.f, y = 0.f, l = 0.f;
+  for (int s = 0; s < a.splits; ++s) {
+    const int64_t slot = (int64_t)s * rows + r;
+    const float m = a.part_ml[2 * slot];
+    if (m == -INFINITY) continue;
+    const float c = fast_exp2(m - mx);
+    const float2 v = *reinterpret_cast<const float2*>(a.part_o + slot * kHeadDim + 2 * lane);
+    l = fmaf(a.part_ml[2 * slot + 1], c, l);
+    x = fmaf(v.x, c, x);
+    y = fmaf(v.y, c, y);
+  }
+  const float inv = l != 0.f ? 1.f / l : 0.f;
+  *reinterpret_cast<uint32_t*>(a.out + r * kHeadDim + 2 * lane) = pack_bf16(x * inv, y * inv);
+  if (a.lse && lane == 0)
+    a.lse[(r % a.Hq) * a.n_queries + r / a.Hq] = mx == -INFINITY ? -INFINITY : (mx + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+int rows_per_item(int variant) { return 32 << variant; }
+
+hipError_t launch_doc_range(const RowsArgs& a, int64_t max_tiles, hipStream_t st) {
+  hipLaunchKernelGGL(doc_range_kernel, dim3((unsigned)max_tiles, a.n_src), dim3(64), 0, st, a.documents, a.kv_indptr,
+                     a.seq_len, a.range_stride, const_cast<int2*>(a.doc_range));
+  return hipGetLastError();
+}
+
+hipError_t launch_rows_attn(const RowsArgs& a, int variant, bool exact_weights, int64_t items, hipStream_t st) {
+  const dim3 grid((unsigned)items);
+  if (exact_weights) {
+    switch (variant) {
+      case 0: hipLaunchKernelGGL((rows_attn_kernel<1, 4, 32, 3>), grid, dim3(256), 0, st, a); break;
+      case 1: hipLaunchKernelGGL((rows_attn_kernel<2, 4, 32, 3>), grid, dim3(512), 0, st, a); break;
+      case 2: hipLaunchKernelGGL((rows_attn_kernel<4, 2, 64, 3>), grid, dim3(512), 0, st, a); break;
+      default: hipLaunchKernelGGL((rows_attn_kernel<8, 1, 64, 3>), grid, dim3(512), 0, st, a); break;
+    }
+  } else {
+    switch (variant) {
+      case 0: hipLaunchKernelGGL((rows_attn_kernel<1, 4, 32, 1>), grid, dim3(256), 0, st, a); break;
+      case 1: hipLaunchKernelGGL((rows_attn_kernel<2, 4, 32, 1>), grid, dim3(512), 0, st, a); break;
+      case 2: hipLaunchKernelGGL((rows_attn_kernel<4, 2, 64, 1>), grid, dim3(512), 0, st, a); break;
+      default: hipLaunchKernelGGL((rows_attn_kernel<8, 1, 64, 1>), grid, dim3(512), 0, st, a); break;
+    }
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_rows_combine(const RowsArgs& a, hipStream_t st) {
+  const int64_t rows = a.n_queries * a.Hq;
+  hipLaunchKernelGGL(rows_combine_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace tactic

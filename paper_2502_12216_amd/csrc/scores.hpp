@@ -1,0 +1,46 @@
+// How attention scores are formed beside the plain dot product: a cap, a bias
+// by distance, documents (internal to the library).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+namespace tactic {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kInvSqrtDim = 0.08838834764831845f;  // 1 / sqrt(128)
+
+// tanh(x) with a relative error near the fp32 rounding everywhere: a cap of 50
+// multiplies it, and a weight's relative error is the capped score's absolute one.
+// Up to |x| = 1: the continued fraction x / (1 + z / (3 + z / (5 + ... z / 11))),
+// z = x^2, as one quotient (cut off there it is off by less than 1e-9).  Beyond:
+// 1 - 2 / (1 + e^{2|x|}), which loses nothing to cancellation above 1/2.  NaN stays NaN.
+__device__ __forceinline__ float tanh_small(float x) {
+  const float z = x * x;
+  const float num = fmaf(z, fmaf(z, 21.f, 1260.f), 10395.f);
+  const float den = fmaf(z, fmaf(z, z + 210.f, 4725.f), 10395.f);
+  return x * num * __builtin_amdgcn_rcpf(den);
+}
+__device__ __forceinline__ float tanh_large(float x) {
+  const float e = __builtin_amdgcn_exp2f(fabsf(x) * (2.f * kLog2e));
+  return copysignf(1.f - 2.f * __builtin_amdgcn_rcpf(1.f + e), x);
+}
+__device__ __forceinline__ float tanh_any(float x) { return fabsf(x) <= 1.f ? tanh_small(x) : tanh_large(x); }
+
+// Score rules of the single-token form (attn_splitk_kernel); every pointer may be null.
+struct TokenMod {
+  float cap;                    // 0: none
+  const float* slopes;          // [Hq]
+  const int32_t* positions;     // [Hkv][total] position of each row; null: pos_base[b] + row
+  const int32_t* q_pos;         // [B]; null: pos_base[b] + tokens - 1
+  const int64_t* pos_base;      // [B] pairs (start, end) of the keys ahead of row 0, their difference is the base; null: 0
+  const int32_t* base_of;       // [B] index into pos_base (negative: base 0)
+  const int32_t* documents;     // [total] document of each row
+  const int32_t* q_documents;   // [B]
+  float* scores;                // [Hkv][total][G] base-2 scores out, or null
+};
+struct NoMod {};
+
+}  // namespace tactic
