@@ -46,14 +46,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 // parts of a weight that is not zero are at least 2^-126, so that its product with
 // an infinite value stays that infinity.
 template <int PARTS>
-__device__ __forceinline__ void weight_operands(const float* p, bf16x8 (&out)[PARTS]) {
+__device__ __forceinline__ void weight_operands(const float (&p)[8], u32x4 (&out)[PARTS]) {
   if constexpr (PARTS == 1) {
-    u32x4 w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = pack_bf16(p[2 * i], p[2 * i + 1]);
-    out[0] = __builtin_bit_cast(bf16x8, w);
+    for (int i = 0; i < 4; ++i) out[0][i] = pack_bf16(p[2 * i], p[2 * i + 1]);
   } else {
-    u32x4 w[3];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       uint32_t h[2], m[2], l[2];
@@ -65,13 +62,28 @@ __device__ __forceinline__ void weight_operands(const float* p, bf16x8 (&out)[PA
         m[j] = __float_as_uint(fmaxf(r, least));
         l[j] = __float_as_uint(fmaxf(r - __uint_as_float(__float_as_uint(r) & 0xffff0000u), least));
       }
-      w[0][i] = __builtin_amdgcn_perm(h[1], h[0], 0x07060302u);
-      w[1][i] = __builtin_amdgcn_perm(m[1], m[0], 0x07060302u);
-      w[2][i] = __builtin_amdgcn_perm(l[1], l[0], 0x07060302u);
+      out[0][i] = __builtin_amdgcn_perm(h[1], h[0], 0x07060302u);
+      out[1][i] = __builtin_amdgcn_perm(m[1], m[0], 0x07060302u);
+      out[2][i] = __builtin_amdgcn_perm(l[1], l[0], 0x07060302u);
     }
-#pragma unroll
-    for (int k = 0; k < 3; ++k) out[k] = __builtin_bit_cast(bf16x8, w[k]);
   }
+}
+
+// Which halves of the words are infinite or NaN: 0x3f80 (1.0) there, 0 elsewhere.
+// kind 1: +inf, 2: -inf, 3: NaN
+__device__ __forceinline__ uint32_t odd_halves(uint32_t w, int kind) {
+  uint32_t r = 0;
+#pragma unroll
+  for (int sh = 0; sh < 32; sh += 16) {
+    const uint32_t v = (w >> sh) & 0xffffu;
+    const bool hit = kind == 1 ? v == 0x7f80u : (kind == 2 ? v == 0xff80u : (v & 0x7fffu) > 0x7f80u);
+    r |= hit ? 0x3f80u << sh : 0u;
+  }
+  return r;
+}
+__device__ __forceinline__ uint32_t finite_halves(uint32_t w) {
+  const uint32_t lo = (w & 0x7f80u) == 0x7f80u ? 0u : 0xffffu, hi = (w & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u;
+  return w & (lo | hi);
 }
 
 __device__ __forceinline__ float swap_half(float x) { return __shfl_xor(x, 32, 64); }
@@ -87,7 +99,7 @@ __device__ __forceinline__ int64_t page_row(const PagedKV& pk, int Hkv, int b, i
 constexpr float kMaxFinite = 3.402823466e38f;  // a score of +inf: the sum becomes inf (its logarithm too), the output NaN
 constexpr float kRescaleSlack = 8.f;  // base-2: a weight may exceed 1 by 2^8 before the sums are rescaled
 
-template <int RW, int KW, int TK, int PARTS>
+template <int RW, int KW, int TK, int PARTS, bool kPaged, bool kDocs>
 __global__ __launch_bounds__(RW * KW * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void rows_attn_kernel(RowsArgs a) {
   constexpr int ROWS = RW * 32, NW = RW * KW, NB = TK / 32;
@@ -97,6 +109,7 @@ void rows_attn_kernel(RowsArgs a) {
   constexpr int kStage = KW * kBufs * kTileBytes, kMerge = KW > 1 ? NW * 16384 : 0;
   __shared__ __align__(1024) unsigned char smem[kStage > kMerge ? kStage : kMerge];
   __shared__ float s_ml[2][NW][32];
+  __shared__ __align__(16) int s_doc[kDocs ? KW * kBufs * TK : 4];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wr = wave % RW, kg = wave / RW, half = lane >> 5, col = lane & 31;
@@ -144,7 +157,7 @@ void rows_attn_kernel(RowsArgs a) {
     qpos = (int)(n - m + i);
     const int pre = a.prefix_len ? a.prefix_len[src] : 0;
     klim = min(max(max(qpos + 1, pre), 0), n);
-    if (a.documents) qdoc = qpos >= 0 ? a.documents[kvb + qpos] : 0;
+    if (kDocs) qdoc = qpos >= 0 ? a.documents[kvb + qpos] : 0;
     if (qpos < 0) klim = 0;  // more queries than tokens: those ahead of the first see nothing
   } else {
     const int b = a.members[q0 + row / a.G];
@@ -176,8 +189,12 @@ void rows_attn_kernel(RowsArgs a) {
   d_lo = __builtin_amdgcn_readfirstlane(d_lo);
   d_hi = __builtin_amdgcn_readfirstlane(d_hi);
 
-  const float slope = a.slopes ? a.slopes[g * a.G + h] * kLog2e : 0.f;
-  const float to_cap = a.cap > 0.f ? kInvSqrtDim / a.cap : 0.f, cap2 = a.cap * kLog2e;
+  // Scores stay a factor `scale` below their base-2 value until the exponential,
+  // which takes it along with the maximum in one multiply-add.
+  const bool capped = a.cap > 0.f, biased = a.slopes != nullptr;
+  const float scale = capped ? a.cap * kLog2e : kInvSqrtDim * kLog2e;
+  const float slope = biased ? a.slopes[g * a.G + h] * kLog2e / scale : 0.f;
+  const float to_cap = capped ? kInvSqrtDim / a.cap : 0.f;
 
   bf16x8 qf[8];
   {
@@ -188,9 +205,9 @@ void rows_attn_kernel(RowsArgs a) {
 
   // documents: the range of each 64-key tile (from doc_range_kernel) and, for the
   // item's queries, that of the tiles they lie in
-  const int2* dr = a.documents ? a.doc_range + (int64_t)src * a.range_stride : nullptr;
+  const int2* dr = kDocs ? a.doc_range + (int64_t)src * a.range_stride : nullptr;
   int i_lo = 0, i_hi = 0;
-  if (dr) {
+  if constexpr (kDocs) {
     const int64_t m = q1 - q0;
     const int p0 = max((int)(n - m + row0 / a.G), 0), p1 = (int)(n - m + (min(row0 + ROWS, nrows) - 1) / a.G);
     i_lo = INT32_MAX;
@@ -204,7 +221,7 @@ void rows_attn_kernel(RowsArgs a) {
   }
   // first tile from t on, in steps of KW, that may hold a seen key (t_hi or more: none)
   auto next_tile = [&](int t) __attribute__((always_inline)) -> int {
-    if (!dr) return t;
+    if constexpr (!kDocs) return t;
     while (t < t_hi) {
       const int mine = t + lane * KW;
       bool some = false;
@@ -221,18 +238,22 @@ void rows_attn_kernel(RowsArgs a) {
   // with several waves to a tile and several tiles at a time all of them step together
   constexpr bool kSkip = RW == 1 || KW == 1;
 
-  const uint16_t* Kb = a.K + (a.paged ? 0 : ((int64_t)g * a.total + kvb) * kHeadDim);
-  const uint16_t* Vb = a.V + (a.paged ? 0 : ((int64_t)g * a.total + kvb) * kHeadDim);
+  const uint16_t* Kb = a.K + (kPaged ? 0 : ((int64_t)g * a.total + kvb) * kHeadDim);
+  const uint16_t* Vb = a.V + (kPaged ? 0 : ((int64_t)g * a.total + kvb) * kHeadDim);
   uint4 kreg[kLoads], vreg[kLoads];
+  int doc_r = 0;
   // chunk i of this thread: stored chunk (wr * kLoads + i) * 64 + lane of the group's tile
+  const int f_row = wr * kLoads * 4 + (lane >> 4), f_swz = row_swizzle(f_row), f_col = lane & 15;
   auto fetch = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int c = (wr * kLoads + i) * 64 + lane, r = c >> 4;
-      const int tok = min(t * TK + r, n - 1);
-      const int64_t at = (a.paged ? page_row(a.pk, a.Hkv, src, g, tok) : (int64_t)tok) * kHeadDim + (((c & 15) ^ row_swizzle(r)) * 8);
+      const int tok = min(t * TK + f_row + 4 * i, n - 1);
+      const int64_t at = (kPaged ? page_row(a.pk, a.Hkv, src, g, tok) : (int64_t)tok) * kHeadDim + ((f_col ^ f_swz ^ (i & 3)) * 8);
       kreg[i] = *reinterpret_cast<const uint4*>(Kb + at);
       vreg[i] = *reinterpret_cast<const uint4*>(Vb + at);
+    }
+    if constexpr (kDocs) {
+      if (wr == 0 && lane < TK) doc_r = a.documents[kvb + min(t * TK + lane, n - 1)];
     }
   };
   auto store = [&](int buf) __attribute__((always_inline)) {
@@ -242,22 +263,35 @@ void rows_attn_kernel(RowsArgs a) {
       *reinterpret_cast<uint4*>(base + i * 1024) = kreg[i];
       *reinterpret_cast<uint4*>(base + i * 1024 + TK * 256) = vreg[i];
     }
+    if constexpr (kDocs) {
+      if (wr == 0 && lane < TK) s_doc[(kg * kBufs + buf) * TK + lane] = doc_r;
+    }
+    if constexpr (RW == 1) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // one wave writes and reads the tile
   };
 
-  float m_run = -INFINITY, l_run = 0.f;
+  float m_run = -INFINITY, l4[4] = {0.f, 0.f, 0.f, 0.f};
   f32x16 o[4];
 #pragma unroll
   for (int d = 0; d < 4; ++d)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
 
+  // LDS offsets of the operands.  K: row col (+ 32 kb), chunk 2 st + half.  V: two
+  // transposing reads of 4 keys per operand of 16 keys and 32 dimensions; lane l of a
+  // group of 16 gives the address of row l / 4, 8-byte piece l % 4.  The constant parts
+  // of a chunk enter the swizzled place by exclusive or.
+  const uint32_t k_off = col * 256 + ((half ^ row_swizzle(col)) * 16);
+  const int v_row = 4 * half + ((lane & 15) >> 2);
+  const uint32_t v_off = v_row * 256 + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ row_swizzle(v_row)) * 16) + (lane & 1) * 8;
+  typedef __attribute__((address_space(3))) unsigned char* lds_ptr;
+  typedef __attribute__((address_space(3))) s16x4* lds4_ptr;
+
   auto compute = [&](int t, int buf) __attribute__((always_inline)) {
-    const unsigned char* kt = smem + (kg * kBufs + buf) * kTileBytes;
-    const unsigned char* vt = kt + TK * 256;
+    const lds_ptr kt = (lds_ptr)(smem + (kg * kBufs + buf) * kTileBytes), vt = kt + TK * 256;
     const int k0 = t * TK;
     if (k0 >= w_hi) return;  // none of the wave's rows sees the tile
     bool masked = k0 + TK > w_lo, docs = false;
-    if (dr) {
+    if constexpr (kDocs) {
       const int2 r = dr[k0 / 64];
       if (r.x > d_hi || r.y < d_lo) return;
       docs = !(r.x == r.y && d_lo == d_hi);
@@ -268,26 +302,33 @@ void rows_attn_kernel(RowsArgs a) {
     for (int kb = 0; kb < NB; ++kb) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
-      const unsigned char* krow = kt + (kb * 32 + col) * 256;
 #pragma unroll
       for (int st = 0; st < 8; ++st) {
-        const bf16x8 kf = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(krow + (((2 * st + half) ^ row_swizzle(col)) * 16)));
+        const bf16x8 kf = __builtin_bit_cast(bf16x8, *(__attribute__((address_space(3))) u32x4*)(kt + kb * 8192 + (k_off ^ (st * 32))));
         s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[st], s[kb], 0, 0, 0);
       }
     }
-    // base-2 scores; accumulator r of block kb is key k0 + 32 kb + 8 (r / 4) + 4 half + r % 4
-    if (a.cap > 0.f) {
+    // accumulator r of block kb is key k0 + 32 kb + 8 (r / 4) + 4 half + r % 4
+    if (capped) {
+      float big = 0.f;
 #pragma unroll
       for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[kb][r] = cap2 * tanh_any(s[kb][r] * to_cap);
-    } else {
+        for (int r = 0; r < 16; ++r) big = fmaxf(big, fabsf(s[kb][r]));
+      // (NaN counts as inside: the polynomial keeps it)
+      if (__any(big * to_cap > kTanhPoly)) {
 #pragma unroll
-      for (int kb = 0; kb < NB; ++kb)
+        for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[kb][r] *= kInvSqrtDim * kLog2e;
+          for (int r = 0; r < 16; ++r) s[kb][r] = tanh_any(s[kb][r] * to_cap);
+      } else {
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[kb][r] = tanh_poly(s[kb][r] * to_cap);
+      }
     }
-    if (a.slopes) {
+    if (biased) {
       const float dist = (float)(qpos - k0 - 4 * half);
 #pragma unroll
       for (int kb = 0; kb < NB; ++kb)
@@ -302,114 +343,115 @@ void rows_attn_kernel(RowsArgs a) {
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           if (kb * 32 + 8 * (r / 4) + r % 4 >= lim) s[kb][r] = -INFINITY;
-      if (docs) {
-        const int32_t* dk = a.documents + kvb;
+      if constexpr (kDocs) {
+        const int* dk = s_doc + (kg * kBufs + buf) * TK + 4 * half;
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (dk[min(k0 + 4 * half + kb * 32 + 8 * (r / 4) + r % 4, n - 1)] != qdoc) s[kb][r] = -INFINITY;
+          for (int r = 0; r < 16; r += 4) {
+            const int4 d = *reinterpret_cast<const int4*>(dk + kb * 32 + 2 * r);
+            s[kb][r] = d.x != qdoc ? -INFINITY : s[kb][r];
+            s[kb][r + 1] = d.y != qdoc ? -INFINITY : s[kb][r + 1];
+            s[kb][r + 2] = d.z != qdoc ? -INFINITY : s[kb][r + 2];
+            s[kb][r + 3] = d.w != qdoc ? -INFINITY : s[kb][r + 3];
+          }
       }
     }
-    float mx = s[0][0];
+    float m4[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m4[j] = s[0][j];
 #pragma unroll
     for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
-    mx = fmaxf(mx, swap_half(mx));
+      for (int r = kb == 0 ? 4 : 0; r < 16; ++r) m4[r & 3] = fmaxf(m4[r & 3], s[kb][r]);
+    float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+    mx = fmaxf(mx, swap_half(mx)) * scale;
     // the sums keep an old maximum as their reference while no weight exceeds 2^8
     if (__any(mx > m_run + kRescaleSlack)) {
       const float mn = fminf(fmaxf(mx, m_run), kMaxFinite);
       const float c = mn > m_run ? fast_exp2(m_run - mn) : 1.f;
       m_run = mn;
-      l_run *= c;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) l4[j] *= c;
 #pragma unroll
       for (int d = 0; d < 4; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[d][r] *= c;
     }
     const float ref = m_run == -INFINITY ? 0.f : m_run;
-    float p[NB * 16];
+    u32x4 pf[TK / 16][PARTS];
 #pragma unroll
-    for (int kb = 0; kb < NB; ++kb)
+    for (int c = 0; c < TK / 16; ++c) {
+      float p[8];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float x = fast_exp2(s[kb][r] - ref);
-        p[kb * 16 + r] = x;
-        l_run += x;
+      for (int j = 0; j < 8; ++j) {
+        p[j] = fast_exp2(fmaf(s[c / 2][8 * (c % 2) + j], scale, -ref));
+        l4[j & 3] += p[j];
       }
+      weight_operands<PARTS>(p, pf[c]);
+    }
+    auto v_operand = [&](int c, int d) __attribute__((always_inline)) -> u32x4 {
+      const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_ptr)(vt + c * 4096 + (v_off ^ (d * 64)))));
+      const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_ptr)(vt + c * 4096 + 2048 + (v_off ^ (d * 64 + 32)))));
+      return u32x4{x.x, x.y, y.x, y.y};
+    };
     // a masked key's weight is 0, but 0 times its value is NaN where that is not
     // finite: such tiles (looked for where something is masked) go another way
     bool odd = false;
     if (masked) {
       uint32_t bad = 0;
-#pragma unroll
+#pragma unroll 4
       for (int i = 0; i < TK * 16 / 64; ++i) {
-        const uint4 w = *reinterpret_cast<const uint4*>(vt + (i * 64 + lane) * 16);
-        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+        const u32x4 w = *(__attribute__((address_space(3))) u32x4*)(vt + (i * 64 + lane) * 16);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          bad |= ((x[j] & 0x7f80u) == 0x7f80u) | ((x[j] & 0x7f800000u) == 0x7f800000u);
+        for (int j = 0; j < 4; ++j) bad |= w[j] ^ finite_halves(w[j]);
       }
       odd = __any(bad != 0);
     }
-    // V^T operand of key chunk c (16 keys) and dimensions 32 d ..: two transposing
-    // reads of 4 keys; lane l of a group of 16 gives the address of row l / 4, 8-byte piece l % 4
-    auto v_operand = [&](int c, int d) __attribute__((always_inline)) -> u32x4 {
-      const int vr = 16 * c + 4 * half + ((lane & 15) >> 2), chunk = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-      const unsigned char* p0 = vt + vr * 256 + ((chunk ^ row_swizzle(vr)) * 16) + (lane & 1) * 8;
-      const unsigned char* p1 = vt + (vr + 8) * 256 + ((chunk ^ row_swizzle(vr + 8)) * 16) + (lane & 1) * 8;
-      typedef __attribute__((address_space(3))) s16x4* lds4;
-      const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)p0));
-      const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)p1));
-      return u32x4{x.x, x.y, y.x, y.y};
-    };
     if (!odd) {
 #pragma unroll
-      for (int c = 0; c < TK / 16; ++c) {
-        bf16x8 pf[PARTS];
-        weight_operands<PARTS>(p + 8 * c, pf);
+      for (int c = 0; c < TK / 16; ++c)
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
           const bf16x8 vf = __builtin_bit_cast(bf16x8, v_operand(c, d));
 #pragma unroll
-          for (int k = PARTS - 1; k >= 0; --k) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[k], o[d], 0, 0, 0);
+          for (int k = PARTS - 1; k >= 0; --k)
+            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, pf[c][k]), o[d], 0, 0, 0);
         }
-      }
     } else {
       // finite values as above; then, for each kind of value that is not finite,
       // whether a key with a weight has it in this dimension
-#pragma unroll 1
-      for (int kind = 0; kind < 4; ++kind) {  // finite, +inf, -inf, NaN
+#pragma unroll
+      for (int c = 0; c < TK / 16; ++c)
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
-          f32x16 seen;
+          u32x4 w = v_operand(c, d);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) seen[r] = 0.f;
+          for (int j = 0; j < 4; ++j) w[j] = finite_halves(w[j]);
+#pragma unroll
+          for (int k = PARTS - 1; k >= 0; --k)
+            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, pf[c][k]), o[d], 0, 0, 0);
+        }
+#pragma unroll 1
+      for (int kind = 1; kind < 4; ++kind) {
+        const float val = kind == 1 ? INFINITY : (kind == 2 ? -INFINITY : NAN);
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          f32x16 hit;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) hit[r] = 0.f;
 #pragma unroll
           for (int c = 0; c < TK / 16; ++c) {
-            u32x4 w = v_operand(c, d);
-            float q[8];
+            u32x4 w = v_operand(c, d), one;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) q[j] = kind == 0 ? p[8 * c + j] : (p[8 * c + j] != 0.f ? 1.f : 0.f);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const uint32_t sh = 16 * (j & 1), v = (w[j >> 1] >> sh) & 0xffffu;
-              const bool inf = (v & 0x7fffu) == 0x7f80u, nan = (v & 0x7fffu) > 0x7f80u;
-              uint32_t use;
-              if (kind == 0) use = inf || nan ? 0u : v;
-              else use = (kind == 3 ? nan : (inf && (v >> 15) == (uint32_t)(kind == 2))) ? 0x3f80u : 0u;
-              w[j >> 1] = (w[j >> 1] & ~(0xffffu << sh)) | (use << sh);
+            for (int j = 0; j < 4; ++j) {
+              w[j] = odd_halves(w[j], kind);
+              one[j] = ((pf[c][0][j] & 0xffffu) ? 0x3f80u : 0u) | ((pf[c][0][j] & 0xffff0000u) ? 0x3f800000u : 0u);
             }
-            bf16x8 pf[PARTS];
-            weight_operands<PARTS>(q, pf);
-#pragma unroll
-            for (int k = PARTS - 1; k >= 0; --k)
-              seen = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pf[k], seen, 0, 0, 0);
+            hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, one), hit, 0, 0, 0);
           }
-          const float val = kind == 1 ? INFINITY : (kind == 2 ? -INFINITY : NAN);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) o[d][r] += kind == 0 ? seen[r] : (seen[r] >= 0.5f ? val : 0.f);
+          for (int r = 0; r < 16; ++r) o[d][r] += hit[r] != 0.f ? val : 0.f;
         }
       }
     }
@@ -452,6 +494,7 @@ void rows_attn_kernel(RowsArgs a) {
   }
 
   // ---- the sums of both halves, then of the KW groups
+  float l_run = (l4[0] + l4[1]) + (l4[2] + l4[3]);
   l_run += swap_half(l_run);
   int d_from = 0, d_to = 4;
   if constexpr (KW > 1) {
@@ -578,24 +621,22 @@ hipError_t launch_doc_range(const RowsArgs& a, int64_t max_tiles, hipStream_t st
   return hipGetLastError();
 }
 
-hipError_t launch_rows_attn(const RowsArgs& a, int variant, bool exact_weights, int64_t items, hipStream_t st) {
+template <int PARTS, bool kPaged, bool kDocs>
+static hipError_t launch_rows_t(const RowsArgs& a, int variant, int64_t items, hipStream_t st) {
   const dim3 grid((unsigned)items);
-  if (exact_weights) {
-    switch (variant) {
-      case 0: hipLaunchKernelGGL((rows_attn_kernel<1, 4, 32, 3>), grid, dim3(256), 0, st, a); break;
-      case 1: hipLaunchKernelGGL((rows_attn_kernel<2, 4, 32, 3>), grid, dim3(512), 0, st, a); break;
-      case 2: hipLaunchKernelGGL((rows_attn_kernel<4, 2, 64, 3>), grid, dim3(512), 0, st, a); break;
-      default: hipLaunchKernelGGL((rows_attn_kernel<8, 1, 64, 3>), grid, dim3(512), 0, st, a); break;
-    }
-  } else {
-    switch (variant) {
-      case 0: hipLaunchKernelGGL((rows_attn_kernel<1, 4, 32, 1>), grid, dim3(256), 0, st, a); break;
-      case 1: hipLaunchKernelGGL((rows_attn_kernel<2, 4, 32, 1>), grid, dim3(512), 0, st, a); break;
-      case 2: hipLaunchKernelGGL((rows_attn_kernel<4, 2, 64, 1>), grid, dim3(512), 0, st, a); break;
-      default: hipLaunchKernelGGL((rows_attn_kernel<8, 1, 64, 1>), grid, dim3(512), 0, st, a); break;
-    }
+  switch (variant) {
+    case 0: hipLaunchKernelGGL((rows_attn_kernel<1, 4, 32, PARTS, kPaged, kDocs>), grid, dim3(256), 0, st, a); break;
+    case 1: hipLaunchKernelGGL((rows_attn_kernel<2, 4, 32, PARTS, kPaged, kDocs>), grid, dim3(512), 0, st, a); break;
+    case 2: hipLaunchKernelGGL((rows_attn_kernel<4, 2, PARTS == 1 ? 64 : 32, PARTS, kPaged, kDocs>), grid, dim3(512), 0, st, a); break;
+    default: hipLaunchKernelGGL((rows_attn_kernel<8, 1, PARTS == 1 ? 64 : 32, PARTS, kPaged, kDocs>), grid, dim3(512), 0, st, a); break;
   }
   return hipGetLastError();
+}
+
+hipError_t launch_rows_attn(const RowsArgs& a, int variant, bool exact_weights, int64_t items, hipStream_t st) {
+  if (exact_weights) return a.paged ? launch_rows_t<3, true, false>(a, variant, items, st) : launch_rows_t<3, false, false>(a, variant, items, st);
+  if (a.documents) return a.paged ? launch_rows_t<1, true, true>(a, variant, items, st) : launch_rows_t<1, false, true>(a, variant, items, st);
+  return a.paged ? launch_rows_t<1, true, false>(a, variant, items, st) : launch_rows_t<1, false, false>(a, variant, items, st);
 }
 
 hipError_t launch_rows_combine(const RowsArgs& a, hipStream_t st) {
