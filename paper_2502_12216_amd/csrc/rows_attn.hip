@@ -69,17 +69,10 @@ __device__ __forceinline__ void weight_operands(const float (&p)[8], u32x4 (&out
   }
 }
 
-// Which halves of the words are infinite or NaN: 0x3f80 (1.0) there, 0 elsewhere.
-// kind 1: +inf, 2: -inf, 3: NaN
-__device__ __forceinline__ uint32_t odd_halves(uint32_t w, int kind) {
-  uint32_t r = 0;
-#pragma unroll
-  for (int sh = 0; sh < 32; sh += 16) {
-    const uint32_t v = (w >> sh) & 0xffffu;
-    const bool hit = kind == 1 ? v == 0x7f80u : (kind == 2 ? v == 0xff80u : (v & 0x7fffu) > 0x7f80u);
-    r |= hit ? 0x3f80u << sh : 0u;
-  }
-  return r;
+// Which halves of a word, under `mask`, lie in [lo, lo + span]: 0x3f80 (1.0) there, 0 elsewhere.
+__device__ __forceinline__ uint32_t halves_in(uint32_t w, uint32_t mask, uint32_t lo, uint32_t span) {
+  const uint32_t a = ((w & mask) - lo) <= span ? 0x3f80u : 0u, b = (((w >> 16) & mask) - lo) <= span ? 0x3f800000u : 0u;
+  return a | b;
 }
 __device__ __forceinline__ uint32_t finite_halves(uint32_t w) {
   const uint32_t lo = (w & 0x7f80u) == 0x7f80u ? 0u : 0xffffu, hi = (w & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u;
@@ -111,7 +104,7 @@ void rows_attn_kernel(RowsArgs a) {
   __shared__ float s_ml[2][NW][32];
   __shared__ __align__(16) int s_doc[kDocs ? KW * kBufs * TK : 4];
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = wave % RW, kg = wave / RW, half = lane >> 5, col = lane & 31;
 
   // ---- the work item: KV head (fastest, so that a head's items share an XCD's L2
@@ -197,11 +190,12 @@ void rows_attn_kernel(RowsArgs a) {
   const float to_cap = capped ? kInvSqrtDim / a.cap : 0.f;
 
   bf16x8 qf[8];
-  {
+  auto load_q = [&]() __attribute__((always_inline)) {
     const uint16_t* qp = a.q + qrow * kHeadDim + 8 * half;
 #pragma unroll
     for (int s = 0; s < 8; ++s) qf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(qp + 16 * s));
-  }
+  };
+  load_q();
 
   // documents: the range of each 64-key tile (from doc_range_kernel) and, for the
   // item's queries, that of the tiles they lie in
@@ -240,32 +234,59 @@ void rows_attn_kernel(RowsArgs a) {
 
   const uint16_t* Kb = a.K + (kPaged ? 0 : ((int64_t)g * a.total + kvb) * kHeadDim);
   const uint16_t* Vb = a.V + (kPaged ? 0 : ((int64_t)g * a.total + kvb) * kHeadDim);
-  uint4 kreg[kLoads], vreg[kLoads];
+  u32x4 kreg[kLoads], vreg[kLoads];
   int doc_r = 0;
   // chunk i of this thread: stored chunk (wr * kLoads + i) * 64 + lane of the group's tile
   const int f_row = wr * kLoads * 4 + (lane >> 4), f_swz = row_swizzle(f_row), f_col = lane & 15;
-  auto fetch = [&](int t) __attribute__((always_inline)) {
+  // element offset of chunk i of tile t: in token order a constant beside the tile's
+  // own (a scalar), in pages by the table
+  auto rows_of = [&](int t, int (&at)[kLoads]) __attribute__((always_inline)) {
+    const int most = n - 1 - t * TK;  // rows past the end repeat the last
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int tok = min(t * TK + f_row + 4 * i, n - 1);
-      const int64_t at = (kPaged ? page_row(a.pk, a.Hkv, src, g, tok) : (int64_t)tok) * kHeadDim + ((f_col ^ f_swz ^ (i & 3)) * 8);
-      kreg[i] = *reinterpret_cast<const uint4*>(Kb + at);
-      vreg[i] = *reinterpret_cast<const uint4*>(Vb + at);
+    for (int i = 0; i < kLoads; ++i) at[i] = (t + 1) * TK <= n ? f_row + 4 * i : min(f_row + 4 * i, most);
+  };
+  auto load = [&](const uint16_t* base, int t, u32x4 (&reg)[kLoads]) __attribute__((always_inline)) {
+    int at[kLoads];
+    rows_of(t, at);
+    if constexpr (kPaged) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        reg[i] = *reinterpret_cast<const u32x4*>(base + page_row(a.pk, a.Hkv, src, g, t * TK + at[i]) * kHeadDim + ((f_col ^ f_swz ^ (i & 3)) * 8));
+    } else {
+      const unsigned char* tile_base = reinterpret_cast<const unsigned char*>(base + (int64_t)t * (TK * kHeadDim));
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        reg[i] = *reinterpret_cast<const u32x4*>(tile_base + (uint32_t)(at[i] * 256 + ((f_col ^ f_swz ^ (i & 3)) * 16)));
     }
+  };
+  auto fetch_k = [&](int t) __attribute__((always_inline)) {
+    load(Kb, t, kreg);
     if constexpr (kDocs) {
       if (wr == 0 && lane < TK) doc_r = a.documents[kvb + min(t * TK + lane, n - 1)];
     }
   };
-  auto store = [&](int buf) __attribute__((always_inline)) {
-    unsigned char* base = smem + (kg * kBufs + buf) * kTileBytes + (wr * kLoads * 64 + lane) * 16;
+  auto fetch_v = [&](int t) __attribute__((always_inline)) { load(Vb, t, vreg); };
+  auto place = [&](int buf) __attribute__((always_inline)) {
+    return smem + (kg * kBufs + buf) * kTileBytes + (wr * kLoads * 64 + lane) * 16;
+  };
+  auto store_k = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      *reinterpret_cast<uint4*>(base + i * 1024) = kreg[i];
-      *reinterpret_cast<uint4*>(base + i * 1024 + TK * 256) = vreg[i];
-    }
+    for (int i = 0; i < kLoads; ++i) *reinterpret_cast<u32x4*>(place(buf) + i * 1024) = kreg[i];
     if constexpr (kDocs) {
       if (wr == 0 && lane < TK) s_doc[(kg * kBufs + buf) * TK + lane] = doc_r;
     }
+  };
+  auto store_v = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) *reinterpret_cast<u32x4*>(place(buf) + i * 1024 + TK * 256) = vreg[i];
+  };
+  auto fetch = [&](int t) __attribute__((always_inline)) {
+    fetch_k(t);
+    fetch_v(t);
+  };
+  auto store = [&](int buf) __attribute__((always_inline)) {
+    store_k(buf);
+    store_v(buf);
     if constexpr (RW == 1) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // one wave writes and reads the tile
   };
 
@@ -286,29 +307,42 @@ void rows_attn_kernel(RowsArgs a) {
   typedef __attribute__((address_space(3))) unsigned char* lds_ptr;
   typedef __attribute__((address_space(3))) s16x4* lds4_ptr;
 
-  auto compute = [&](int t, int buf) __attribute__((always_inline)) {
-    const lds_ptr kt = (lds_ptr)(smem + (kg * kBufs + buf) * kTileBytes), vt = kt + TK * 256;
+  auto tile_lds = [&](int buf) __attribute__((always_inline)) { return (lds_ptr)(smem + (kg * kBufs + buf) * kTileBytes); };
+
+  f32x16 s[NB];           // scores of the tile, then dead
+  u32x4 pf[TK / 16][PARTS];  // its weights
+  enum { kNone = 0, kFull = 1, kMasked = 2 };  // of the wave's rows: none sees the tile, all see all of it, else
+  auto state_of = [&](int t) __attribute__((always_inline)) -> int {
     const int k0 = t * TK;
-    if (k0 >= w_hi) return;  // none of the wave's rows sees the tile
-    bool masked = k0 + TK > w_lo, docs = false;
+    if (k0 >= w_hi) return kNone;
+    bool masked = k0 + TK > w_lo;
     if constexpr (kDocs) {
       const int2 r = dr[k0 / 64];
-      if (r.x > d_hi || r.y < d_lo) return;
-      docs = !(r.x == r.y && d_lo == d_hi);
-      masked |= docs;
+      if (r.x > d_hi || r.y < d_lo) return kNone;
+      masked |= !(r.x == r.y && d_lo == d_hi);
     }
-    f32x16 s[NB];
+    return masked ? kMasked : kFull;
+  };
+
+  auto qk = [&](int buf) __attribute__((always_inline)) {
+    const lds_ptr kt = tile_lds(buf);
+    uint32_t off = k_off;
+    asm volatile("" : "+v"(off));  // (its eight places are made here, not kept in registers over the loop)
 #pragma unroll
     for (int kb = 0; kb < NB; ++kb) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
 #pragma unroll
       for (int st = 0; st < 8; ++st) {
-        const bf16x8 kf = __builtin_bit_cast(bf16x8, *(__attribute__((address_space(3))) u32x4*)(kt + kb * 8192 + (k_off ^ (st * 32))));
+        const bf16x8 kf = __builtin_bit_cast(bf16x8, *(__attribute__((address_space(3))) u32x4*)(kt + kb * 8192 + (off ^ (st * 32))));
         s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[st], s[kb], 0, 0, 0);
       }
     }
-    // accumulator r of block kb is key k0 + 32 kb + 8 (r / 4) + 4 half + r % 4
+  };
+
+  // scores to weights; accumulator r of block kb is key k0 + 32 kb + 8 (r / 4) + 4 half + r % 4
+  auto soft = [&](int t, int buf, bool masked) __attribute__((always_inline)) {
+    const int k0 = t * TK;
     if (capped) {
       float big = 0.f;
 #pragma unroll
@@ -379,7 +413,6 @@ void rows_attn_kernel(RowsArgs a) {
         for (int r = 0; r < 16; ++r) o[d][r] *= c;
     }
     const float ref = m_run == -INFINITY ? 0.f : m_run;
-    u32x4 pf[TK / 16][PARTS];
 #pragma unroll
     for (int c = 0; c < TK / 16; ++c) {
       float p[8];
@@ -390,75 +423,145 @@ void rows_attn_kernel(RowsArgs a) {
       }
       weight_operands<PARTS>(p, pf[c]);
     }
-    auto v_operand = [&](int c, int d) __attribute__((always_inline)) -> u32x4 {
-      const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_ptr)(vt + c * 4096 + (v_off ^ (d * 64)))));
-      const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_ptr)(vt + c * 4096 + 2048 + (v_off ^ (d * 64 + 32)))));
-      return u32x4{x.x, x.y, y.x, y.y};
-    };
-    // a masked key's weight is 0, but 0 times its value is NaN where that is not
-    // finite: such tiles (looked for where something is masked) go another way
-    bool odd = false;
-    if (masked) {
-      uint32_t bad = 0;
-#pragma unroll 4
-      for (int i = 0; i < TK * 16 / 64; ++i) {
-        const u32x4 w = *(__attribute__((address_space(3))) u32x4*)(vt + (i * 64 + lane) * 16);
+  };
+
+  auto v_operand = [&](lds_ptr vt, uint32_t off, int c, int d) __attribute__((always_inline)) -> u32x4 {
+    const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_ptr)(vt + c * 4096 + (off ^ (d * 64)))));
+    const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_ptr)(vt + c * 4096 + 2048 + (off ^ (d * 64 + 32)))));
+    return u32x4{x.x, x.y, y.x, y.y};
+  };
+  auto pv = [&](int buf) __attribute__((always_inline)) {
+    const lds_ptr vt = tile_lds(buf) + TK * 256;
+    uint32_t off = v_off;
+    asm volatile("" : "+v"(off));
 #pragma unroll
-        for (int j = 0; j < 4; ++j) bad |= w[j] ^ finite_halves(w[j]);
+    for (int c = 0; c < TK / 16; ++c)
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, v_operand(vt, off, c, d));
+#pragma unroll
+        for (int k = PARTS - 1; k >= 0; --k)
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, pf[c][k]), o[d], 0, 0, 0);
       }
-      odd = __any(bad != 0);
+  };
+  // A masked key's weight is 0, but 0 times its value is NaN where that is not
+  // finite.  So the values of tiles with something masked are looked over, and where
+  // one is found the item is computed again by a loop that goes by kinds of values.
+  auto any_odd = [&](int buf) __attribute__((always_inline)) -> bool {
+    const lds_ptr vt = tile_lds(buf) + TK * 256;
+    uint32_t bad = 0;
+#pragma unroll 4
+    for (int i = 0; i < TK * 16 / 64; ++i) {
+      const u32x4 w = *(__attribute__((address_space(3))) u32x4*)(vt + (i * 64 + lane) * 16);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) bad |= w[j] ^ finite_halves(w[j]);
     }
-    if (!odd) {
+    return __any(bad != 0);
+  };
+  auto pv_odd = [&](int buf) __attribute__((always_inline)) {
+    const lds_ptr vt = tile_lds(buf) + TK * 256;
+    // finite values as in pv; then, for each kind of value that is not finite,
+    // whether a key with a weight has it in this dimension
 #pragma unroll
-      for (int c = 0; c < TK / 16; ++c)
+    for (int c = 0; c < TK / 16; ++c)
 #pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          const bf16x8 vf = __builtin_bit_cast(bf16x8, v_operand(c, d));
+      for (int d = 0; d < 4; ++d) {
+        u32x4 w = v_operand(vt, v_off, c, d);
 #pragma unroll
-          for (int k = PARTS - 1; k >= 0; --k)
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, pf[c][k]), o[d], 0, 0, 0);
-        }
-    } else {
-      // finite values as above; then, for each kind of value that is not finite,
-      // whether a key with a weight has it in this dimension
+        for (int j = 0; j < 4; ++j) w[j] = finite_halves(w[j]);
 #pragma unroll
-      for (int c = 0; c < TK / 16; ++c)
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          u32x4 w = v_operand(c, d);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) w[j] = finite_halves(w[j]);
-#pragma unroll
-          for (int k = PARTS - 1; k >= 0; --k)
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, pf[c][k]), o[d], 0, 0, 0);
-        }
+        for (int k = PARTS - 1; k >= 0; --k)
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, pf[c][k]), o[d], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);  // one operand at a time: few registers are left here
+      }
 #pragma unroll 1
-      for (int kind = 1; kind < 4; ++kind) {
-        const float val = kind == 1 ? INFINITY : (kind == 2 ? -INFINITY : NAN);
+    for (int kind = 1; kind < 4; ++kind) {
+      const float val = kind == 1 ? INFINITY : (kind == 2 ? -INFINITY : NAN);
+      const uint32_t mask = kind == 3 ? 0x7fffu : 0xffffu, lo = kind == 1 ? 0x7f80u : (kind == 2 ? 0xff80u : 0x7f81u),
+                     span = kind == 3 ? 0x7eu : 0u;
 #pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          f32x16 hit;
+      for (int d = 0; d < 4; ++d) {
+        f32x16 hit;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) hit[r] = 0.f;
+        for (int r = 0; r < 16; ++r) hit[r] = 0.f;
 #pragma unroll
-          for (int c = 0; c < TK / 16; ++c) {
-            u32x4 w = v_operand(c, d), one;
+        for (int c = 0; c < TK / 16; ++c) {
+          u32x4 w = v_operand(vt, v_off, c, d), one;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              w[j] = odd_halves(w[j], kind);
-              one[j] = ((pf[c][0][j] & 0xffffu) ? 0x3f80u : 0u) | ((pf[c][0][j] & 0xffff0000u) ? 0x3f800000u : 0u);
-            }
-            hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, one), hit, 0, 0, 0);
+          for (int j = 0; j < 4; ++j) {
+            w[j] = halves_in(w[j], mask, lo, span);
+            one[j] = ((pf[c][0][j] & 0xffffu) ? 0x3f80u : 0u) | ((pf[c][0][j] & 0xffff0000u) ? 0x3f800000u : 0u);
           }
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[d][r] += hit[r] != 0.f ? val : 0.f;
+          hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, one), hit, 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
         }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] += hit[r] != 0.f ? val : 0.f;
       }
     }
   };
+  bool odd = false;
 
-  // ---- the keys: the next tile's rows are in flight while this one is contracted
-  if constexpr (kSkip) {
+  // ---- the keys
+  if constexpr (RW == 8) {
+    // Eight waves, two per SIMD, take turns: while waves 0 to 3 do the products of a
+    // tile (P V of the one before, then K Q), waves 4 to 7 turn scores into weights,
+    // and the other way round, a barrier between.  In phase 2 i waves 0 to 3 contract
+    // tile i, in phase 2 i + 1 the others do.  Event j of the staging, K of tile j + 1
+    // and V of tile j into the buffers of tiles j - 1 and j - 2, falls into phase
+    // 2 j + 1 for waves 0 to 3 and 2 j for the others: after the last reads of what it
+    // overwrites and before the first of what it brings.
+    int t = next_tile(t_lo);
+    if (t < t_hi) {
+      const bool late = wr >= 4;
+      int t1 = next_tile(t + 1);     // tile of the next K to store
+      int sv = t, ev = 0;            // tile of the next V to store, the event's number
+      fetch_k(t);
+      store_k(0);
+      fetch_v(t);
+      if (t1 < t_hi) fetch_k(t1);
+      __syncthreads();
+      auto stage = [&]() __attribute__((always_inline)) {
+        if (sv < t_hi) {
+          store_v(ev & 1);
+          if (t1 < t_hi) store_k((ev + 1) & 1);
+          ++ev;
+          sv = t1;
+          if (t1 < t_hi) {
+            t1 = next_tile(t1 + 1);
+            fetch_v(sv);
+            if (t1 < t_hi) fetch_k(t1);
+          }
+        }
+      };
+      if (late) {
+        stage();
+        __syncthreads();
+      }
+      // (a tile that none of a wave's rows sees is masked as a whole: the products are
+      // not the wave's to skip, and such tiles are few)
+      int i = 0;
+      bool masked;
+      for (;;) {
+        qk(i & 1);
+        __builtin_amdgcn_s_setprio(0);
+        __syncthreads();
+        stage();
+        masked = state_of(t) != kFull;
+        soft(t, i & 1, masked);
+        t = next_tile(t + 1);
+        if (!(late && t >= t_hi)) __syncthreads();  // (the late waves have made one more)
+        if (masked) odd |= any_odd(i & 1);
+        __builtin_amdgcn_s_setprio(1);
+        if (t >= t_hi) break;
+        pv(i & 1);
+        ++i;
+      }
+      pv(i & 1);
+      __builtin_amdgcn_s_setprio(0);
+    }
+  } else if constexpr (kSkip) {
+    // the next tile's rows are in flight while this one is contracted
     int t = next_tile(t_lo + kg);
     int buf = 0;
     if (t < t_hi) {
@@ -469,7 +572,13 @@ void rows_attn_kernel(RowsArgs a) {
     while (t < t_hi) {
       const int tn = next_tile(t + KW);
       if (tn < t_hi) fetch(tn);
-      compute(t, buf);
+      const int st = state_of(t);
+      if (st != kNone) {
+        qk(buf);
+        soft(t, buf, st == kMasked);
+        if (st == kMasked) odd |= any_odd(buf);
+        pv(buf);
+      }
       if constexpr (RW > 1) buf ^= 1;
       if (tn < t_hi) store(buf);
       if constexpr (RW > 1) __syncthreads();
@@ -486,9 +595,41 @@ void rows_attn_kernel(RowsArgs a) {
     for (int i = 0; i < steps; ++i) {
       const int t = t_lo + i * KW + kg;
       if (t + KW < t_hi) fetch(t + KW);
-      if (t < t_hi) compute(t, buf);
+      const int st = t < t_hi ? state_of(t) : kNone;
+      if (st != kNone) {
+        qk(buf);
+        soft(t, buf, st == kMasked);
+        if (st == kMasked) odd |= any_odd(buf);
+        pv(buf);
+      }
       buf ^= 1;
       if (t + KW < t_hi) store(buf);
+      __syncthreads();
+    }
+  }
+  if (__syncthreads_or(odd)) {  // rare: the whole item again, one tile at a time
+    m_run = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) l4[j] = 0.f;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+    load_q();
+#pragma unroll 1
+    for (int t0 = t_lo; t0 < t_hi; t0 += KW) {
+      const int t = t0 + kg;
+      if (t < t_hi) {
+        fetch(t);
+        store(0);
+      }
+      __syncthreads();
+      const int st = t < t_hi ? state_of(t) : kNone;
+      if (st != kNone) {
+        qk(0);
+        soft(t, 0, st == kMasked);
+        pv_odd(0);
+      }
       __syncthreads();
     }
   }

@@ -27,7 +27,10 @@ __device__ __forceinline__ float tanh_large(float x) {
   const float e = __builtin_amdgcn_exp2f(fabsf(x) * (2.f * kLog2e));
   return copysignf(1.f - 2.f * __builtin_amdgcn_rcpf(1.f + e), x);
 }
-__device__ __forceinline__ float tanh_any(float x) { return fabsf(x) <= 1.f ? tanh_small(x) : tanh_large(x); }
+__device__ __forceinline__ float tanh_any(float x) {  // (both, and no branch per lane)
+  const float a = tanh_small(x), b = tanh_large(x);
+  return fabsf(x) <= 1.f ? a : b;
+}
 
 // tanh(x) for |x| <= kTanhPoly: x times the polynomial of degree 5 in x^2 of the least
 // largest relative error (2.9e-8, by Remez' exchange; with fp32 roundings 1.6e-7):
