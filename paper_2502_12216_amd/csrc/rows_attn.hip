@@ -324,19 +324,30 @@ void rows_attn_kernel(RowsArgs a) {
     return masked ? kMasked : kFull;
   };
 
+  // Operands are read a step ahead of their products and no further (sched_barrier):
+  // left to itself the compiler reads the whole tile ahead and spills the rows in flight.
   auto qk = [&](int buf) __attribute__((always_inline)) {
     const lds_ptr kt = tile_lds(buf);
     uint32_t off = k_off;
     asm volatile("" : "+v"(off));  // (its eight places are made here, not kept in registers over the loop)
+    typedef __attribute__((address_space(3))) u32x4* lds16_ptr;
+    u32x4 kf[2][NB];
 #pragma unroll
     for (int kb = 0; kb < NB; ++kb) {
+      kf[0][kb] = *(lds16_ptr)(kt + kb * 8192 + off);
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+    }
 #pragma unroll
-      for (int st = 0; st < 8; ++st) {
-        const bf16x8 kf = __builtin_bit_cast(bf16x8, *(__attribute__((address_space(3))) u32x4*)(kt + kb * 8192 + (off ^ (st * 32))));
-        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[st], s[kb], 0, 0, 0);
+    for (int st = 0; st < 8; ++st) {
+      if (st < 7) {
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb) kf[(st + 1) & 1][kb] = *(lds16_ptr)(kt + kb * 8192 + (off ^ ((st + 1) * 32)));
       }
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb)
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[st & 1][kb]), qf[st], s[kb], 0, 0, 0);
+      if (st & 1) __builtin_amdgcn_sched_barrier(0);
     }
   };
 
@@ -354,12 +365,18 @@ void rows_attn_kernel(RowsArgs a) {
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[kb][r] = tanh_any(s[kb][r] * to_cap);
+          for (int r = 0; r < 16; ++r) {
+            s[kb][r] = tanh_any(s[kb][r] * to_cap);
+            if (r % 2) __builtin_amdgcn_sched_barrier(0);  // (two at a time: few registers are left here)
+          }
       } else {
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[kb][r] = tanh_poly(s[kb][r] * to_cap);
+          for (int r = 0; r < 16; ++r) {
+            s[kb][r] = tanh_poly(s[kb][r] * to_cap);
+            if (r % 8 == 7) __builtin_amdgcn_sched_barrier(0);
+          }
       }
     }
     if (biased) {
@@ -423,6 +440,12 @@ void rows_attn_kernel(RowsArgs a) {
       }
       weight_operands<PARTS>(p, pf[c]);
     }
+#pragma unroll
+    for (int c = 0; c < TK / 16; ++c)
+#pragma unroll
+      for (int k = 0; k < PARTS; ++k) asm volatile("" : "+v"(pf[c][k]));  // (made here, before the barrier, not at their use)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(l4[j]));
   };
 
   auto v_operand = [&](lds_ptr vt, uint32_t off, int c, int d) __attribute__((always_inline)) -> u32x4 {
@@ -434,15 +457,22 @@ void rows_attn_kernel(RowsArgs a) {
     const lds_ptr vt = tile_lds(buf) + TK * 256;
     uint32_t off = v_off;
     asm volatile("" : "+v"(off));
+    u32x4 vf[2][4];
 #pragma unroll
-    for (int c = 0; c < TK / 16; ++c)
+    for (int d = 0; d < 4; ++d) vf[0][d] = v_operand(vt, off, 0, d);
 #pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        const bf16x8 vf = __builtin_bit_cast(bf16x8, v_operand(vt, off, c, d));
+    for (int c = 0; c < TK / 16; ++c) {
+      if (c + 1 < TK / 16) {
 #pragma unroll
-        for (int k = PARTS - 1; k >= 0; --k)
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, pf[c][k]), o[d], 0, 0, 0);
+        for (int d = 0; d < 4; ++d) vf[(c + 1) & 1][d] = v_operand(vt, off, c + 1, d);
       }
+#pragma unroll
+      for (int k = PARTS - 1; k >= 0; --k)
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[c & 1][d]), __builtin_bit_cast(bf16x8, pf[c][k]), o[d], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
   // A masked key's weight is 0, but 0 times its value is NaN where that is not
   // finite.  So the values of tiles with something masked are looked over, and where
