@@ -79,7 +79,17 @@ __device__ __forceinline__ uint32_t finite_halves(uint32_t w) {
   return w & (lo | hi);
 }
 
-__device__ __forceinline__ float swap_half(float x) { return __shfl_xor(x, 32, 64); }
+// Maximum and sum of the values of lanes l and l ^ 32, the same in both.
+__device__ __forceinline__ float halves_max(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);  // the lower half's value, the upper's
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float halves_sum(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
 
 // Page-table lookup of token `tok` of sequence b (in bounds whatever the table holds).
 __device__ __forceinline__ int64_t page_row(const PagedKV& pk, int Hkv, int b, int kvh, int tok) {
@@ -237,6 +247,7 @@ void rows_attn_kernel(RowsArgs a) {
   u32x4 kreg[kLoads], vreg[kLoads];
   int doc_r = 0;
   // chunk i of this thread: stored chunk (wr * kLoads + i) * 64 + lane of the group's tile
+  const int doc_wave = RW == 8 ? 4 : 0;
   const int f_row = wr * kLoads * 4 + (lane >> 4), f_swz = row_swizzle(f_row), f_col = lane & 15;
   // element offset of chunk i of tile t: in token order a constant beside the tile's
   // own (a scalar), in pages by the table
@@ -262,7 +273,7 @@ void rows_attn_kernel(RowsArgs a) {
   auto fetch_k = [&](int t) __attribute__((always_inline)) {
     load(Kb, t, kreg);
     if constexpr (kDocs) {
-      if (wr == 0 && lane < TK) doc_r = a.documents[kvb + min(t * TK + lane, n - 1)];
+      if (wr == doc_wave && lane < TK) doc_r = a.documents[kvb + min(t * TK + lane, n - 1)];
     }
   };
   auto fetch_v = [&](int t) __attribute__((always_inline)) { load(Vb, t, vreg); };
@@ -273,7 +284,7 @@ void rows_attn_kernel(RowsArgs a) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) *reinterpret_cast<u32x4*>(place(buf) + i * 1024) = kreg[i];
     if constexpr (kDocs) {
-      if (wr == 0 && lane < TK) s_doc[(kg * kBufs + buf) * TK + lane] = doc_r;
+      if (wr == doc_wave && lane < TK) s_doc[(kg * kBufs + buf) * TK + lane] = doc_r;
     }
   };
   auto store_v = [&](int buf) __attribute__((always_inline)) {
@@ -416,7 +427,7 @@ void rows_attn_kernel(RowsArgs a) {
 #pragma unroll
       for (int r = kb == 0 ? 4 : 0; r < 16; ++r) m4[r & 3] = fmaxf(m4[r & 3], s[kb][r]);
     float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-    mx = fmaxf(mx, swap_half(mx)) * scale;
+    mx = halves_max(mx) * scale;
     // the sums keep an old maximum as their reference while no weight exceeds 2^8
     if (__any(mx > m_run + kRescaleSlack)) {
       const float mn = fminf(fmaxf(mx, m_run), kMaxFinite);
@@ -537,49 +548,39 @@ void rows_attn_kernel(RowsArgs a) {
     // Eight waves, two per SIMD, take turns: while waves 0 to 3 do the products of a
     // tile (P V of the one before, then K Q), waves 4 to 7 turn scores into weights,
     // and the other way round, a barrier between.  In phase 2 i waves 0 to 3 contract
-    // tile i, in phase 2 i + 1 the others do.  Event j of the staging, K of tile j + 1
-    // and V of tile j into the buffers of tiles j - 1 and j - 2, falls into phase
-    // 2 j + 1 for waves 0 to 3 and 2 j for the others: after the last reads of what it
-    // overwrites and before the first of what it brings.
+    // tile i, in phase 2 i + 1 the others do.  Each brings its part of K of tile i + 1
+    // and V of tile i to LDS there, between the products: into the buffers of tiles
+    // i - 1 and i - 2, whose last reads are in phase 2 i - 1, for first reads in phase
+    // 2 i + 2.  (A tile's documents are read with the weights, in phases 2 i + 1 and
+    // 2 i + 2, so that a late wave brings them.)
     int t = next_tile(t_lo);
     if (t < t_hi) {
       const bool late = wr >= 4;
-      int t1 = next_tile(t + 1);     // tile of the next K to store
-      int sv = t, ev = 0;            // tile of the next V to store, the event's number
+      int t1 = next_tile(t + 1);
       fetch_k(t);
       store_k(0);
       fetch_v(t);
       if (t1 < t_hi) fetch_k(t1);
       __syncthreads();
-      auto stage = [&]() __attribute__((always_inline)) {
-        if (sv < t_hi) {
-          store_v(ev & 1);
-          if (t1 < t_hi) store_k((ev + 1) & 1);
-          ++ev;
-          sv = t1;
-          if (t1 < t_hi) {
-            t1 = next_tile(t1 + 1);
-            fetch_v(sv);
-            if (t1 < t_hi) fetch_k(t1);
-          }
-        }
-      };
-      if (late) {
-        stage();
-        __syncthreads();
-      }
-      // (a tile that none of a wave's rows sees is masked as a whole: the products are
-      // not the wave's to skip, and such tiles are few)
+      if (late) __syncthreads();
       int i = 0;
       bool masked;
       for (;;) {
+        store_v(i & 1);
+        int t2 = t1;
+        if (t1 < t_hi) {
+          store_k((i + 1) & 1);
+          t2 = next_tile(t1 + 1);
+          fetch_v(t1);
+          if (t2 < t_hi) fetch_k(t2);
+        }
         qk(i & 1);
         __builtin_amdgcn_s_setprio(0);
         __syncthreads();
-        stage();
         masked = state_of(t) != kFull;
         soft(t, i & 1, masked);
-        t = next_tile(t + 1);
+        t = t1;
+        t1 = t2;
         if (!(late && t >= t_hi)) __syncthreads();  // (the late waves have made one more)
         if (masked) odd |= any_odd(i & 1);
         __builtin_amdgcn_s_setprio(1);
@@ -665,8 +666,7 @@ void rows_attn_kernel(RowsArgs a) {
   }
 
   // ---- the sums of both halves, then of the KW groups
-  float l_run = (l4[0] + l4[1]) + (l4[2] + l4[3]);
-  l_run += swap_half(l_run);
+  float l_run = halves_sum((l4[0] + l4[1]) + (l4[2] + l4[3]));
   int d_from = 0, d_to = 4;
   if constexpr (KW > 1) {
     __syncthreads();  // the tiles are dead: their storage takes the groups' sums
