@@ -78,10 +78,12 @@ PromptLayout prompt_layout(const tactic_kv_shape* s, const tactic_query_shape* q
   p.part_ml = p.plan.splits > 1 ? L.take(rows * p.plan.splits * 8) : 0;
   Layout W;
   W.cur = behind;
-  // key tiles of 256 rows: split the queries where they are fewer than two per compute unit
+  // key tiles of 256 rows: the queries are split until there are eight workgroups for
+  // each of the 512 places (an early key is seen by more queries than a late one, so
+  // that they are of many lengths), of at least eight row tiles each
   const int64_t items = std::max<int64_t>(1, (s->total_tokens + 255) / 256) * s->n_kv_heads;
-  const int64_t most = std::max<int64_t>(1, q->max_queries * G / 256);
-  p.wsplits = (int)std::max<int64_t>(1, std::min<int64_t>({512 / items, most, (int64_t)kMaxSplits}));
+  const int64_t most = std::max<int64_t>(1, q->max_queries * G / 512);
+  p.wsplits = (int)std::max<int64_t>(1, std::min<int64_t>({4096 / items, most, (int64_t)kMaxSplits}));
   p.wpart = p.wsplits > 1 ? W.take((int64_t)p.wsplits * s->n_kv_heads * s->total_tokens * 4) : 0;
   p.bytes = std::max<int64_t>(256, std::max(L.cur, W.cur));
   return p;
@@ -138,7 +140,8 @@ tactic_status prompt_impl(const uint16_t* q, const uint16_t* K, const uint16_t* 
   a.out = out;
   a.lse = lse;
   hipError_t e = hipSuccess;
-  if (a.documents && p.range_stride > 0) e = tactic::launch_doc_range(a, p.range_stride, stream);
+  if (a.documents)
+    e = tactic::launch_doc_range(a.documents, a.kv_indptr, a.seq_len, a.n_src, p.range_stride, reinterpret_cast<int2*>(ws + p.ranges), stream);
   if (e == hipSuccess) e = tactic::launch_rows_attn(a, p.plan.variant, false, p.plan.tiles * a.Hkv * a.splits, stream);
   if (e == hipSuccess && !a.direct) e = tactic::launch_rows_combine(a, stream);
   if (e != hipSuccess) return hip_fail(e, "prompt attention launch");
@@ -391,9 +394,15 @@ tactic_status tactic_prompt_weights(const uint16_t* q, const uint16_t* K, const 
     a.documents = mod->documents;
     a.prefix_len = mod->prefix_len;
   }
-  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.wpart);
+  char* ws = static_cast<char*>(workspace);
+  a.doc_range = reinterpret_cast<const int2*>(ws + p.ranges);
+  a.range_stride = p.range_stride;
+  a.part = reinterpret_cast<float*>(ws + p.wpart);
   a.weights = weights;
-  const hipError_t e = tactic::launch_prompt_weights(a, shape->max_seq_len, stream);
+  hipError_t e = hipSuccess;
+  if (a.documents)
+    e = tactic::launch_doc_range(a.documents, a.kv_indptr, a.seq_len, a.B, p.range_stride, reinterpret_cast<int2*>(ws + p.ranges), stream);
+  if (e == hipSuccess) e = tactic::launch_prompt_weights(a, shape->max_seq_len, stream);
   if (e != hipSuccess) return hip_fail(e, "prompt weights launch");
   return TACTIC_OK;
 }

@@ -18,18 +18,22 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 // 2^(s_ij - lse_i).  A workgroup holds 256 keys of a (sequence, KV head), 64 per
 // wave, as the B operands of S = Q K^T and streams the query rows through LDS, 64
 // at a time: a lane's accumulators are the rows of one key, so the sum over rows
-// needs no exchange but one between the halves at the end.  Bound by the matrix
-// unit and by one exponential per score; with few queries by reading K.
+// needs no exchange but one between the halves at the end.  Bound by the vector
+// unit (one exponential, one multiply-add and one add per score, six of its slots
+// where the products take four); with few queries by reading K.
 // grid (key tiles + sequences, Hkv, splits of the rows)
 // ---------------------------------------------------------------------------
 constexpr int kWKeys = 256, kWRows = 64;
 
+template <bool kDocs>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void prompt_weights_kernel(WeightArgs a) {
   __shared__ __align__(16) unsigned char s_q[2][kWRows * 256];
-  __shared__ __align__(16) float s_lse[2][kWRows], s_slope[2][kWRows];
-  __shared__ __align__(16) int s_lim[2][kWRows], s_pos[2][kWRows], s_doc[2][kWRows];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, col = lane & 31;
-  const int g = blockIdx.y, split = blockIdx.z;
+  // per row: the logarithm of its sum, its slope, its position from the first key, the
+  // end of the keys it sees, its document
+  __shared__ __align__(16) float s_lse[2][kWRows], s_slope[2][kWRows], s_pos[2][kWRows];
+  __shared__ __align__(16) int s_lim[2][kWRows], s_doc[2][kDocs ? kWRows : 4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
+  const int tid = threadIdx.x, g = blockIdx.y, split = blockIdx.z;
   int lo = 0, hi = a.B - 1;  // key tiles of sequence b start at floor(rows before it / 256) + b
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -42,71 +46,110 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
   const int64_t k0l = ((int64_t)blockIdx.x - kvb / kWKeys - b) * kWKeys;
   if (k0l < 0 || k0l >= n) return;
   const int k0 = (int)k0l;
-  const int64_t q0 = a.q_indptr[b], m = a.q_indptr[b + 1] - q0;
+  const int64_t q0 = a.q_indptr[b];
+  const int m = (int)(a.q_indptr[b + 1] - q0);
   const int pre = a.prefix_len ? a.prefix_len[b] : 0;
   // tokens [i0, m) of the sequence's queries: within the window, and able to see the tile
-  int64_t i0 = a.window > 0 ? max(m - a.window, (int64_t)0) : 0;
-  if (pre <= k0) i0 = max(i0, (int64_t)k0 - (n - m));
+  int i0 = a.window > 0 ? (int)max((int64_t)m - a.window, (int64_t)0) : 0;
+  if (pre <= k0) i0 = max(i0, k0 - (n - m));
   i0 = max(i0, m - n);  // queries ahead of the first token see nothing
-  const int64_t r0 = i0 * a.G, rows = (m - i0) * a.G;
-  const int tiles = rows > 0 ? (int)((rows + kWRows - 1) / kWRows) : 0;
+  const int lg = a.G == 1 ? 0 : (a.G == 2 ? 1 : (a.G == 4 ? 2 : 3));
+  const int rows = i0 < m ? (m - i0) << lg : 0;
+  const int tiles = (rows + kWRows - 1) / kWRows;
   const int t_lo = (int)((int64_t)tiles * split / a.splits), t_hi = (int)((int64_t)tiles * (split + 1) / a.splits);
 
   // keys of this wave: blocks of 32, a key per column (rows past the end repeat the last)
   bf16x8 kf[2][8];
-  int key[2], kdoc[2];
+  int kdoc[2] = {0, 0};
+  const int key0 = wave * 64 + col;  // from k0; the second block's: 32 more
 #pragma unroll
   for (int bb = 0; bb < 2; ++bb) {
-    key[bb] = k0 + wave * 64 + bb * 32 + col;
-    const int64_t at = ((int64_t)g * a.total + kvb + min(key[bb], n - 1)) * kHeadDim + 8 * half;
-    kdoc[bb] = a.documents ? a.documents[kvb + min(key[bb], n - 1)] : 0;
+    const int key = min(k0 + key0 + bb * 32, n - 1);
+    const uint16_t* at = a.K + ((int64_t)g * a.total + kvb + key) * kHeadDim + 8 * half;
+    if (kDocs) kdoc[bb] = a.documents[kvb + key];
 #pragma unroll
-    for (int s = 0; s < 8; ++s) kf[bb][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(a.K + at + 16 * s));
+    for (int s = 0; s < 8; ++s) kf[bb][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(at + 16 * s));
   }
-  const float to_cap = a.cap > 0.f ? kInvSqrtDim / a.cap : 0.f, cap2 = a.cap * kLog2e;
+  const bool capped = a.cap > 0.f, biased = a.slopes != nullptr;
+  const float scale = capped ? a.cap * kLog2e : kInvSqrtDim * kLog2e, to_cap = capped ? kInvSqrtDim / a.cap : 0.f;
+  const float keyf = (float)key0;
   float sum[2] = {0.f, 0.f};
 
-  uint4 qreg[4];
-  float lse_r = 0.f, slope_r = 0.f;
-  int lim_r = 0, pos_r = 0, doc_r = 0;
+  // documents of the key tile (from doc_range_kernel)
+  const int2* dr = kDocs ? a.doc_range + (int64_t)b * a.range_stride : nullptr;
+  int d_lo = 0, d_hi = 0;
+  if constexpr (kDocs) {
+    d_lo = INT32_MAX;
+    d_hi = INT32_MIN;
+    for (int t = k0 / 64; t <= min(k0 + kWKeys, n) / 64 && t * 64 < n; ++t) {
+      d_lo = min(d_lo, dr[t].x);
+      d_hi = max(d_hi, dr[t].y);
+    }
+  }
+  auto next_tile = [&](int t) __attribute__((always_inline)) -> int {
+    if constexpr (!kDocs) return t;
+    while (t < t_hi) {
+      const int mine = t + lane;
+      bool some = false;
+      if (mine < t_hi) {
+        const int p0 = n - m + i0 + ((mine * kWRows) >> lg), p1 = n - m + i0 + ((min((mine + 1) * kWRows, rows) - 1) >> lg);
+        for (int x = p0 / 64; x <= p1 / 64; ++x) some |= dr[x].x <= d_hi && dr[x].y >= d_lo;
+      }
+      const uint64_t any = __ballot(some);
+      if (any) return t + __ffsll((unsigned long long)any) - 1;
+      t += 64;
+    }
+    return t;
+  };
+
+  u32x4 qreg[4];
+  float lse_r = 0.f, slope_r = 0.f, pos_r = 0.f;
+  int lim_r = 0, doc_r = 0;
+  const uint16_t* qb = a.q + ((q0 + i0) * a.Hq + (int64_t)g * a.G) * kHeadDim;
   auto fetch = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int c = (wave * 4 + i) * 64 + lane, r = c >> 4;
-      const int64_t row = r0 + min((int64_t)t * kWRows + r, rows - 1);
-      const int64_t at = ((q0 + row / a.G) * a.Hq + g * a.G + row % a.G) * kHeadDim;
-      qreg[i] = *reinterpret_cast<const uint4*>(a.q + at + ((c & 15) ^ (4 * (r & 3) + ((r >> 2) & 3))) * 8);
+      const int c = (wave * 4 + i) * 64 + lane, r = c >> 4, row = min(t * kWRows + r, rows - 1);
+      const int64_t at = ((int64_t)(row >> lg) * a.Hq + (row & (a.G - 1))) * kHeadDim;
+      qreg[i] = *reinterpret_cast<const u32x4*>(qb + at + ((c & 15) ^ (4 * (r & 3) + ((r >> 2) & 3))) * 8);
     }
     if (tid < kWRows) {
-      const int64_t x = (int64_t)t * kWRows + tid, row = r0 + min(x, rows - 1), i = row / a.G, h = g * a.G + row % a.G;
-      const int pos = (int)(n - m + i);
-      lse_r = a.lse[h * a.n_queries + q0 + i] * kLog2e;
-      slope_r = a.slopes ? a.slopes[h] * kLog2e : 0.f;
-      pos_r = pos;
+      const int x = t * kWRows + tid, row = min(x, rows - 1), i = i0 + (row >> lg), h = g * a.G + (row & (a.G - 1));
+      const int pos = n - m + i;
+      const float l = a.lse[(int64_t)h * a.n_queries + q0 + i];
       // a row past the end, and one whose sum says that it saw nothing, gives no weight
-      lim_r = x < rows && lse_r != -INFINITY ? min(max(pos + 1, pre), n) : 0;
-      doc_r = a.documents && pos >= 0 ? a.documents[kvb + pos] : 0;
+      lse_r = x < rows && l != -INFINITY ? l * kLog2e : INFINITY;
+      slope_r = biased ? a.slopes[h] * kLog2e / scale : 0.f;
+      pos_r = (float)(pos - k0);
+      lim_r = min(max(pos + 1, pre), n) - k0;
+      if (kDocs) doc_r = a.documents[kvb + max(pos, 0)];
     }
   };
   auto store = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(s_q[buf] + ((wave * 4 + i) * 64 + lane) * 16) = qreg[i];
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x4*>(s_q[buf] + ((wave * 4 + i) * 64 + lane) * 16) = qreg[i];
     if (tid < kWRows) {
       s_lse[buf][tid] = lse_r;
       s_slope[buf][tid] = slope_r;
-      s_lim[buf][tid] = lim_r;
       s_pos[buf][tid] = pos_r;
-      s_doc[buf][tid] = doc_r;
+      s_lim[buf][tid] = lim_r;
+      if (kDocs) s_doc[buf][tid] = doc_r;
     }
   };
-  if (t_lo < t_hi) {
-    fetch(t_lo);
+  const uint32_t q_off = col * 256 + ((half ^ (4 * (col & 3) + ((col >> 2) & 3))) * 16);
+  int t = next_tile(t_lo);
+  if (t < t_hi) {
+    fetch(t);
     store(0);
   }
   __syncthreads();
   int buf = 0;
-  for (int t = t_lo; t < t_hi; ++t) {
-    if (t + 1 < t_hi) fetch(t + 1);
+  while (t < t_hi) {
+    const int tn = next_tile(t + 1);
+    if (tn < t_hi) fetch(tn);
+    // the first token of the tile sees the fewest keys
+    const int lim0 = min(max(n - m + i0 + ((t * kWRows) >> lg) + 1, pre), n);
+    const bool masked = kDocs || k0 + wave * 64 + 64 > lim0;
 #pragma unroll
     for (int rb = 0; rb < 2; ++rb) {
       f32x16 acc[2];
@@ -114,42 +157,95 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
       for (int bb = 0; bb < 2; ++bb)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[bb][r] = 0.f;
-      const unsigned char* qrow = s_q[buf] + (rb * 32 + col) * 256;
+      uint32_t off = q_off + buf * (kWRows * 256) + rb * 8192;
+      asm volatile("" : "+v"(off));
 #pragma unroll
       for (int s = 0; s < 8; ++s) {
-        const bf16x8 qv = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(qrow + ((2 * s + half) ^ (4 * (col & 3) + ((col >> 2) & 3))) * 16));
+        const bf16x8 qv = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(s_q[0] + (off ^ (s * 32))));
         acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qv, kf[0][s], acc[0], 0, 0, 0);
         acc[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qv, kf[1][s], acc[1], 0, 0, 0);
       }
+      // accumulator r is row rb * 32 + 8 (r / 4) + 4 half + r % 4
+      const int at = rb * 32 + 4 * half;
+      if (capped) {
+        float big = 0.f;
 #pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4) {
-        const int at = rb * 32 + 8 * q4 + 4 * half;  // accumulator 4 q4 + j is row at + j
-        const float4 ls = *reinterpret_cast<const float4*>(s_lse[buf] + at);
-        const int4 lm = *reinterpret_cast<const int4*>(s_lim[buf] + at);
+        for (int bb = 0; bb < 2; ++bb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) big = fmaxf(big, fabsf(acc[bb][r]));
+        if (__any(big * to_cap > kTanhPoly)) {
+#pragma unroll
+          for (int bb = 0; bb < 2; ++bb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              acc[bb][r] = tanh_any(acc[bb][r] * to_cap);
+              if (r % 2) __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+#pragma unroll
+          for (int bb = 0; bb < 2; ++bb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              acc[bb][r] = tanh_poly(acc[bb][r] * to_cap);
+              if (r % 8 == 7) __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+      }
+      if (biased) {
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const float4 sl = *reinterpret_cast<const float4*>(s_slope[buf] + at + 2 * r);
+          const float4 ps = *reinterpret_cast<const float4*>(s_pos[buf] + at + 2 * r);
+          const float sla[4] = {sl.x, sl.y, sl.z, sl.w}, psa[4] = {ps.x, ps.y, ps.z, ps.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int bb = 0; bb < 2; ++bb) acc[bb][r + j] = fmaf(-sla[j], fabsf(psa[j] - keyf - 32.f * bb), acc[bb][r + j]);
+        }
+      }
+      if (masked) {
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const int4 lm = *reinterpret_cast<const int4*>(s_lim[buf] + at + 2 * r);
+          const int lma[4] = {lm.x, lm.y, lm.z, lm.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int bb = 0; bb < 2; ++bb) acc[bb][r + j] = key0 + 32 * bb < lma[j] ? acc[bb][r + j] : -INFINITY;
+          if constexpr (kDocs) {
+            const int4 dc = *reinterpret_cast<const int4*>(s_doc[buf] + at + 2 * r);
+            const int dca[4] = {dc.x, dc.y, dc.z, dc.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+              for (int bb = 0; bb < 2; ++bb) acc[bb][r + j] = dca[j] == kdoc[bb] ? acc[bb][r + j] : -INFINITY;
+          }
+        }
+      }
+      float part[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const float4 ls = *reinterpret_cast<const float4*>(s_lse[buf] + at + 2 * r);
         const float lsa[4] = {ls.x, ls.y, ls.z, ls.w};
-        const int lma[4] = {lm.x, lm.y, lm.z, lm.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-          for (int bb = 0; bb < 2; ++bb) {
-            float v = acc[bb][4 * q4 + j];
-            v = a.cap > 0.f ? cap2 * tanh_any(v * to_cap) : v * (kInvSqrtDim * kLog2e);
-            if (a.slopes) v = fmaf(-s_slope[buf][at + j], fabsf((float)(s_pos[buf][at + j] - key[bb])), v);
-            bool seen = key[bb] < lma[j];
-            if (a.documents) seen = seen && s_doc[buf][at + j] == kdoc[bb];
-            sum[bb] += seen ? fast_exp2(v - lsa[j]) : 0.f;
-          }
+          for (int bb = 0; bb < 2; ++bb) part[bb][j & 1] += fast_exp2(fmaf(acc[bb][r + j], scale, -lsa[j]));
       }
+#pragma unroll
+      for (int bb = 0; bb < 2; ++bb) sum[bb] += part[bb][0] + part[bb][1];
     }
-    if (t + 1 < t_hi) store(buf ^ 1);
+    if (tn < t_hi) store(buf ^ 1);
     __syncthreads();
     buf ^= 1;
+    t = tn;
   }
 #pragma unroll
   for (int bb = 0; bb < 2; ++bb) {
     const float s = sum[bb] + __shfl_xor(sum[bb], 32, 64);
-    if (half == 0 && key[bb] < n) {
-      const int64_t at = (int64_t)g * a.total + kvb + key[bb];
+    const int key = k0 + key0 + bb * 32;
+    if (half == 0 && key < n) {
+      const int64_t at = (int64_t)g * a.total + kvb + key;
       if (a.splits == 1) a.weights[at] += s;
       else a.part[(int64_t)split * a.Hkv * a.total + at] = s;
     }
@@ -169,7 +265,9 @@ __global__ __launch_bounds__(256) void sum_weights_kernel(WeightArgs a) {
 
 hipError_t launch_prompt_weights(const WeightArgs& a, int64_t max_len, hipStream_t st) {
   if (max_len == 0) return hipSuccess;
-  hipLaunchKernelGGL(prompt_weights_kernel, dim3((unsigned)(a.total / kWKeys + a.B), a.Hkv, a.splits), dim3(256), 0, st, a);
+  const dim3 grid((unsigned)(a.total / kWKeys + a.B), a.Hkv, a.splits);
+  if (a.documents) hipLaunchKernelGGL(prompt_weights_kernel<true>, grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(prompt_weights_kernel<false>, grid, dim3(256), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && a.splits > 1) {
     hipLaunchKernelGGL(sum_weights_kernel, dim3((unsigned)((max_len + 255) / 256), a.Hkv, a.B), dim3(256), 0, st, a);

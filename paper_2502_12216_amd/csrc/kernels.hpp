@@ -189,6 +189,8 @@ struct WeightArgs {
   const float* slopes;
   const int32_t* documents;
   const int32_t* prefix_len;
+  const int2* doc_range;        // as in RowsArgs
+  int64_t range_stride;
   float* part;                  // [splits][Hkv][total], splits > 1
   float* weights;               // [Hkv][total]
 };
@@ -245,7 +247,8 @@ struct JoinArgs {
 
 // variants 0 to 3: 32, 64, 128 or 256 rows per item
 int rows_per_item(int variant);
-hipError_t launch_doc_range(const RowsArgs& a, int64_t max_tiles, hipStream_t st);
+hipError_t launch_doc_range(const int32_t* documents, const int64_t* kv_indptr, const int64_t* seq_len, int batch,
+                            int64_t max_tiles, int2* out, hipStream_t st);
 hipError_t launch_rows_attn(const RowsArgs& a, int variant, bool exact_weights, int64_t items, hipStream_t st);
 hipError_t launch_rows_combine(const RowsArgs& a, hipStream_t st);
 

@@ -786,9 +786,11 @@ __global__ __launch_bounds__(256) void rows_combine_kernel(RowsArgs a) {
 
 int rows_per_item(int variant) { return 32 << variant; }
 
-hipError_t launch_doc_range(const RowsArgs& a, int64_t max_tiles, hipStream_t st) {
-  hipLaunchKernelGGL(doc_range_kernel, dim3((unsigned)max_tiles, a.n_src), dim3(64), 0, st, a.documents, a.kv_indptr,
-                     a.seq_len, a.range_stride, const_cast<int2*>(a.doc_range));
+hipError_t launch_doc_range(const int32_t* documents, const int64_t* kv_indptr, const int64_t* seq_len, int batch,
+                            int64_t max_tiles, int2* out, hipStream_t st) {
+  if (max_tiles == 0) return hipSuccess;
+  hipLaunchKernelGGL(doc_range_kernel, dim3((unsigned)max_tiles, batch), dim3(64), 0, st, documents, kv_indptr, seq_len,
+                     max_tiles, out);
   return hipGetLastError();
 }
 
