@@ -241,7 +241,7 @@ constexpr int attn_tok(int G) { return G == 8 ? 4 : 2; }
 // scores out (32 bits, a row's heads side by side: 4 G bytes beside its 512).  A
 // row of another document has no weight, whatever its values hold.
 template <int G, int TOK, bool kPaged, int kMod = 0>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(G >= 8 ? 2 : 3)))
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(G >= 8 || (G >= 4 && kMod != 0) ? 2 : 3)))
 void attn_splitk_kernel(AttnArgs a, std::conditional_t<kMod != 0, TokenMod, NoMod> mod) {
   constexpr int LPR = 16;                 // lanes per 256-byte row
   constexpr int kPart = G * (kHeadDim + 2);
@@ -275,6 +275,14 @@ void attn_splitk_kernel(AttnArgs a, std::conditional_t<kMod != 0, TokenMod, NoMo
   __shared__ int64_t s_wsum[4];
   __shared__ int s_wmax[4];
 
+  // kMod: what is the same for all lanes though it came from LDS or a division goes to
+  // scalar registers, which the rules' own registers need (G = 4 had spilled 19: ragged
+  // sequences of 1 to 77777 tokens, 148609 in all, 8 KV heads: 128 us, 107 without a rule)
+  auto uniform = [](auto x) __attribute__((always_inline)) {
+    if constexpr (kMod == 0) return x;
+    else if constexpr (sizeof(x) == 4) return __builtin_bit_cast(decltype(x), __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+    else return (decltype(x))(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+  };
   const int tid = threadIdx.x;
   const int lane = tid & 63, wave = tid >> 6, sl = lane % LPR, grp = lane / LPR;
   const int gid = wave * GPW + grp;
@@ -321,11 +329,12 @@ void attn_splitk_kernel(AttnArgs a, std::conditional_t<kMod != 0, TokenMod, NoMo
     else bgh = mid - 1;
   }
 
-  for (int bg = bg0; bg < BG && s_prefix[bg] < t1; ++bg) {
+  if constexpr (kMod != 0) bg0 = __builtin_amdgcn_readfirstlane(bg0);
+  for (int bg = bg0; bg < BG && uniform(s_prefix[bg]) < uniform(t1); ++bg) {
     // the group's tokens follow its segment cost of setup in the split
-    const int64_t first = s_prefix[bg] + kSegmentCost;
-    const int64_t seg_lo = max(t0, first) - first;
-    const int64_t seg_hi = min(t1, s_prefix[bg + 1]) - first;
+    const int64_t first = uniform(s_prefix[bg]) + kSegmentCost;
+    const int64_t seg_lo = uniform(max(t0, first) - first);
+    const int64_t seg_hi = uniform(min(t1, s_prefix[bg + 1]) - first);
     if (seg_lo >= seg_hi) continue;  // no token of this group in the range
     const int b = bg / a.NV, jg = bg % a.NV, kvh = jg / a.kv_div;
     const int64_t kvb = a.kv_indptr[b];
@@ -365,7 +374,7 @@ void attn_splitk_kernel(AttnArgs a, std::conditional_t<kMod != 0, TokenMod, NoMo
     if constexpr (kMod != 0) {
       const int64_t row0 = (int64_t)kvh * a.total + kvb;
       slope2 = mod.slopes ? mod.slopes[jg * G + hl] * kLog2e : 0.f;
-      to_cap = mod.cap > 0.f ? kInvSqrtDim / mod.cap : 0.f;
+      to_cap = uniform(mod.cap > 0.f ? kInvSqrtDim / mod.cap : 0.f);
       if (mod.pos_base && mod.base_of[b] >= 0)
         base = (int)(mod.pos_base[mod.base_of[b] + 1] - mod.pos_base[mod.base_of[b]]);
       qpos = mod.q_pos ? mod.q_pos[b] : base + nseq - 1;
@@ -374,7 +383,7 @@ void attn_splitk_kernel(AttnArgs a, std::conditional_t<kMod != 0, TokenMod, NoMo
         docp = mod.documents ? mod.documents + kvb : reinterpret_cast<const int32_t*>(a.kv_indptr);
         qdoc = mod.documents ? mod.q_documents[b] : 0;
       }
-      if (mod.scores && sl == (kMatrix ? hl : hl * (16 / G))) scp = mod.scores + row0 * G + hl;
+      if (mod.scores) scp = mod.scores + row0 * G;
     }
     auto sum_of = [&](int h, int e) __attribute__((always_inline)) {
       if constexpr (kMatrix) return accv[h / 4][e][h % 4];
@@ -460,7 +469,11 @@ void attn_splitk_kernel(AttnArgs a, std::conditional_t<kMod != 0, TokenMod, NoMo
         if constexpr (kMod == 0) {
           s[i] = valid ? r * kScaleLog2 : -INFINITY;
         } else {
-          float v = mod.cap > 0.f ? mod.cap * kLog2e * tanh_any(r * to_cap) : r * kScaleLog2;
+          float v = r * kScaleLog2;
+          if (mod.cap > 0.f) {
+            const float y = r * to_cap;
+            v = mod.cap * kLog2e * (__any(fabsf(y) > kTanhPoly) ? tanh_any(y) : tanh_poly(y));
+          }
           if (mod.slopes) {
             int kpos = base + (int)(p0 + t);
             if constexpr (kMod == 2) kpos = mod.positions ? x.pos[i] : kpos;
@@ -471,7 +484,7 @@ void attn_splitk_kernel(AttnArgs a, std::conditional_t<kMod != 0, TokenMod, NoMo
             v = other[i] ? -INFINITY : v;
           }
           s[i] = valid ? v : -INFINITY;
-          if (scp && valid) scp[(p0 + t) * G] = v;
+          if (scp && valid && sl == (kMatrix ? hl : hl * (16 / G))) scp[(p0 + t) * G + hl] = v;
         }
       }
       float mn = m;
@@ -957,31 +970,44 @@ static hipError_t launch_combine_t(const AttnArgs& a, const More& m, int G, hipS
 hipError_t launch_combine(const AttnArgs& a, int G, hipStream_t st) { return launch_combine_t<false>(a, NoMod{}, G, st); }
 hipError_t launch_join(const AttnArgs& a, const JoinArgs& j, int G, hipStream_t st) { return launch_combine_t<true>(a, j, G, st); }
 
-// The running sums of attention weights: one thread per cached row and KV head
-// adds its group's 2^(s - M) / L (s from the decode, M and 1 / L from the
-// combine).  grid (rows / 256, Hkv, B).  Reads 4 G bytes and writes 4 of each row.
+// The running sums of attention weights: a thread per cached row and KV head, four
+// rows each, adds its group's 2^(s - M) / L (s from the decode, M and 1 / L from the
+// combine).  grid (rows / 1024, Hkv, B).  Reads 4 G bytes and writes 4 of each row.
 template <int G>
 __global__ __launch_bounds__(256) void add_weights_kernel(const float* scores, const float* norm, const int64_t* kv_indptr,
                                                           const int64_t* seq_len, int64_t total, float* weights) {
   const int g = blockIdx.y, b = blockIdx.z, Hkv = gridDim.y;
-  const int64_t n = seq_tokens(kv_indptr, seq_len, b), r = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (r >= n) return;
-  const int64_t at = (int64_t)g * total + kv_indptr[b] + r;
+  const int64_t n = seq_tokens(kv_indptr, seq_len, b), r0 = (int64_t)blockIdx.x * 1024 + threadIdx.x;
+  if (r0 >= n) return;
+  const int64_t base = (int64_t)g * total + kv_indptr[b];
   const float* nm = norm + 2 * (((int64_t)b * Hkv + g) * G);
-  float w = weights[at];
-  float x = 0.f;
+  float s[4][G], w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t at = base + min(r0 + 256 * i, n - 1);  // (rows past the end repeat the last and are not stored)
+    w[i] = weights[at];
+#pragma unroll
+    for (int h = 0; h < G; ++h) s[i][h] = scores[at * G + h];
+  }
+  float M[G], inv[G];
 #pragma unroll
   for (int h = 0; h < G; ++h) {
-    const float s = scores[at * G + h];
-    if (s != -INFINITY) x = fmaf(fast_exp2(s - nm[2 * h]), nm[2 * h + 1], x);
+    M[h] = nm[2 * h];
+    inv[h] = nm[2 * h + 1];
   }
-  weights[at] = w + x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float x = 0.f;
+#pragma unroll
+    for (int h = 0; h < G; ++h) x = s[i][h] != -INFINITY ? fmaf(fast_exp2(s[i][h] - M[h]), inv[h], x) : x;
+    if (r0 + 256 * i < n) weights[base + r0 + 256 * i] = w[i] + x;
+  }
 }
 
 hipError_t launch_add_weights(const AttnArgs& a, const float* scores, const float* norm, int64_t max_len, float* weights,
                               int G, hipStream_t st) {
   if (max_len == 0) return hipSuccess;
-  const dim3 grid((unsigned)((max_len + 255) / 256), a.Hkv, a.B);
+  const dim3 grid((unsigned)((max_len + 1023) / 1024), a.Hkv, a.B);
   switch (G) {
     case 1: hipLaunchKernelGGL(add_weights_kernel<1>, grid, dim3(256), 0, st, scores, norm, a.kv_indptr, a.seq_len, a.total, weights); break;
     case 2: hipLaunchKernelGGL(add_weights_kernel<2>, grid, dim3(256), 0, st, scores, norm, a.kv_indptr, a.seq_len, a.total, weights); break;
