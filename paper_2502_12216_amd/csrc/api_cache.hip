@@ -508,7 +508,7 @@ tactic_status tactic_evict(const uint16_t* K, const uint16_t* V, const tactic_kv
   a.positions_out = positions_out;
   a.out_len = out_len;
   a.rows = static_cast<int32_t*>(workspace);
-  const hipError_t e = tactic::launch_evict(a, std::min(out_max, shape->max_seq_len), stream);
+  const hipError_t e = tactic::launch_evict(a, shape->max_seq_len, std::min(out_max, shape->max_seq_len), stream);
   if (e != hipSuccess) return hip_fail(e, "evict launch");
   return TACTIC_OK;
 }

@@ -291,13 +291,22 @@ __device__ __forceinline__ uint32_t rank_key(float w, int64_t pos, int64_t newes
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-// One workgroup per (KV head, sequence) finds the kept rows: the key of the last
-// kept one digit by digit (256 counts of 8 bits each), then the kept rows in
-// ascending order by a running count.
+struct __attribute__((packed, aligned(4))) Four {  // 16 bytes at any 4-byte place
+  uint32_t v[4];
+};
+
+// One workgroup per (KV head, sequence) finds the kept rows: the key of the last kept
+// one digit by digit (11, 11 and 10 bits), then the kept rows in ascending order.
+// Thread t holds rows 4 (1024 j + t) + e, e < 4, j < J, as keys in registers, so that
+// weights and positions are read once (J = 16: 65536 rows); J = 0 makes the keys again
+// in every pass.  Bound by one compute unit's reads and counts: the digits' counts are
+// LDS atomics, of which those on one count take turns.
+template <int J>
 __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
-  __shared__ uint32_t s_hist[256];
-  __shared__ uint32_t s_sum[16], s_eq[16];
-  __shared__ uint32_t s_prefix, s_need;
+  constexpr int kBins = 2048, kHeld = J > 0 ? J : 1;
+  __shared__ uint32_t s_hist[kBins];
+  __shared__ uint32_t s_sum[16];
+  __shared__ uint32_t s_prefix, s_need, s_same;
   const int g = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t kvb = a.kv_indptr[b], outb = a.out_indptr[b];
   const int n = (int)seq_tokens(a.kv_indptr, a.seq_len, b);
@@ -308,72 +317,123 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
   const int64_t newest = a.newest ? a.newest[b] : n - 1;
   const float* w = a.weights + (int64_t)g * a.total + kvb;
   const int32_t* pos = a.positions ? a.positions + (int64_t)g * a.total + kvb : nullptr;
-  auto key_at = [&](int r) { return rank_key(w[r], pos ? pos[r] : r, newest, a.recent); };
-  uint32_t prefix = 0, need = (uint32_t)keep;
-  if (keep < n) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) s_hist[tid] = 0;
-      __syncthreads();
-      for (int r = tid; r < n; r += 1024) {
-        const uint32_t k = key_at(r);
-        if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&s_hist[(k >> shift) & 255], 1u);
-      }
-      __syncthreads();
-      if (wave == 0) {  // the digit that holds the need-th largest, four counts per lane from the top
-        uint32_t c[4], mine = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          c[j] = s_hist[255 - (lane * 4 + j)];
-          mine += c[j];
-        }
-        const uint32_t incl = wave_incl_scan((int)mine), before = incl - mine;
-        if (before < need && need <= incl) {
-          uint32_t run = before;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if (run < need && need <= run + c[j]) {
-              s_prefix = prefix | ((uint32_t)(255 - (lane * 4 + j)) << shift);
-              s_need = need - run;
-            }
-            run += c[j];
-          }
-        }
-      }
-      __syncthreads();
-      prefix = s_prefix;
-      need = s_need;
-      __syncthreads();
-    }
-  }
-  // rows above the key, and the first `need` rows of exactly that key (all kept: key 0, every row)
   int32_t* rows = a.rows + (int64_t)g * a.out_total + outb;
-  uint32_t base = 0, eq_base = 0;
-  for (int r0 = 0; r0 < n; r0 += 1024) {
-    const int r = r0 + tid;
-    const uint32_t k = r < n ? key_at(r) : 0;
-    const bool above = r < n && k > prefix, equal = r < n && k == prefix;
-    const uint64_t em = __ballot(equal), below = (1ull << lane) - 1;
-    if (lane == 0) s_eq[wave] = __popcll(em);
-    __syncthreads();
-    uint32_t e = eq_base + __popcll(em & below), e_all = eq_base;
-    for (int i = 0; i < 16; ++i) {
-      e += i < wave ? s_eq[i] : 0;
-      e_all += s_eq[i];
-    }
-    const bool kept = above || (equal && e < need);
-    const uint64_t km = __ballot(kept);
-    if (lane == 0) s_sum[wave] = __popcll(km);
-    __syncthreads();
-    uint32_t at = base + __popcll(km & below), all = base;
-    for (int i = 0; i < 16; ++i) {
-      at += i < wave ? s_sum[i] : 0;
-      all += s_sum[i];
-    }
-    if (kept && at < (uint32_t)keep) rows[at] = r;
-    base = all;
-    eq_base = e_all;
-    __syncthreads();
+  if (keep == n) {
+    for (int r = tid; r < n; r += 1024) rows[r] = r;
+    return;
   }
+  // the keys of rows r .. r + 3 (past the end: of the last row, never counted)
+  auto keys_at = [&](int64_t r, uint32_t (&k)[4]) __attribute__((always_inline)) {
+    if (r + 4 <= n) {
+      const Four x = *reinterpret_cast<const Four*>(w + r);
+      Four p = {{0, 0, 0, 0}};
+      if (pos) p = *reinterpret_cast<const Four*>(pos + r);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) k[e] = rank_key(__uint_as_float(x.v[e]), pos ? (int)p.v[e] : r + e, newest, a.recent);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int64_t q = min(r + e, (int64_t)n - 1);
+        k[e] = rank_key(w[q], pos ? pos[q] : q, newest, a.recent);
+      }
+    }
+  };
+  const int steps = (int)(((int64_t)n + 4095) / 4096);  // of 4096 rows
+  uint32_t held[kHeld][4];
+  if constexpr (J > 0) {
+#pragma unroll
+    for (int j = 0; j < J; ++j) keys_at(min((int64_t)j * 4096 + tid * 4, (int64_t)n), held[j]);
+  }
+  // f(row, its four keys) for every step of the thread's rows
+  auto each = [&](auto f) __attribute__((always_inline)) {
+    if constexpr (J > 0) {
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+        if (j < steps) f((int64_t)j * 4096 + tid * 4, held[j]);
+    } else {
+      for (int j = 0; j < steps; ++j) {
+        uint32_t k[4];
+        keys_at(min((int64_t)j * 4096 + tid * 4, (int64_t)n), k);
+        f((int64_t)j * 4096 + tid * 4, k);
+      }
+    }
+  };
+  // sum of one value per thread over the threads before it, and of all
+  auto scan = [&](uint32_t x, uint32_t* all) __attribute__((always_inline)) -> uint32_t {
+    const uint32_t incl = (uint32_t)wave_incl_scan((int)x);
+    if (lane == kWave - 1) s_sum[wave] = incl;
+    __syncthreads();
+    uint32_t before = 0, total = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const uint32_t v = s_sum[i];
+      before += i < wave ? v : 0;
+      total += v;
+    }
+    __syncthreads();
+    if (all) *all = total;
+    return before + incl - x;
+  };
+  uint32_t prefix = 0, need = (uint32_t)keep;
+#pragma unroll
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bits = pass == 2 ? 10 : 11;
+    s_hist[tid] = 0;
+    s_hist[tid + 1024] = 0;
+    __syncthreads();
+    each([&](int64_t r, const uint32_t (&k)[4]) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (r + e < n && (pass == 0 || (k[e] >> (shift + bits)) == (prefix >> (shift + bits))))
+          atomicAdd(&s_hist[(k[e] >> shift) & ((1u << bits) - 1)], 1u);
+    });
+    __syncthreads();
+    // the digit that holds the need-th largest: two counts per thread from the top
+    const uint32_t c0 = s_hist[kBins - 1 - 2 * tid], c1 = s_hist[kBins - 2 - 2 * tid];
+    const uint32_t before = scan(c0 + c1, nullptr);
+    if (before < need && need <= before + c0 + c1) {
+      const bool second = need > before + c0;
+      s_prefix = prefix | ((uint32_t)(kBins - 1 - 2 * tid - (second ? 1 : 0)) << shift);
+      s_need = need - before - (second ? c0 : 0);
+      s_same = second ? c1 : c0;
+    }
+    __syncthreads();
+    prefix = s_prefix;
+    need = s_need;
+  }
+  // rows above the key stay, and the first `need` of the s_same rows of exactly that key
+  const bool ties = s_same != need;
+  __syncthreads();
+  uint32_t base = 0, eq_base = 0;
+  each([&](int64_t r, const uint32_t (&k)[4]) {
+    uint32_t kept = 0, eq = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      kept |= (uint32_t)(r + e < n && k[e] > prefix) << e;
+      eq |= (uint32_t)(r + e < n && k[e] == prefix) << e;
+    }
+    if (ties) {
+      uint32_t all;
+      uint32_t rank = eq_base + scan(__popc(eq), &all);
+      eq_base += all;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        kept |= (uint32_t)((eq >> e & 1) && rank < need) << e;
+        rank += eq >> e & 1;
+      }
+    } else {
+      kept |= eq;
+    }
+    uint32_t all;
+    uint32_t at = base + scan(__popc(kept), &all);
+    base += all;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (kept >> e & 1) {
+        if (at < (uint32_t)keep) rows[at] = (int32_t)(r + e);
+        ++at;
+      }
+  });
 }
 
 // Copies the kept rows: 16 lanes per row, K and V.  grid (rows / 64, Hkv, B)
@@ -400,8 +460,12 @@ __global__ __launch_bounds__(256) void evict_gather_kernel(EvictArgs a) {
   }
 }
 
-hipError_t launch_evict(const EvictArgs& a, int64_t max_out, hipStream_t st) {
-  hipLaunchKernelGGL(evict_select_kernel, dim3(a.Hkv, a.B), dim3(1024), 0, st, a);
+hipError_t launch_evict(const EvictArgs& a, int64_t max_len, int64_t max_out, hipStream_t st) {
+  const dim3 grid(a.Hkv, a.B);
+  if (max_len <= 4096) hipLaunchKernelGGL(evict_select_kernel<1>, grid, dim3(1024), 0, st, a);
+  else if (max_len <= 16384) hipLaunchKernelGGL(evict_select_kernel<4>, grid, dim3(1024), 0, st, a);
+  else if (max_len <= 65536) hipLaunchKernelGGL(evict_select_kernel<16>, grid, dim3(1024), 0, st, a);
+  else hipLaunchKernelGGL(evict_select_kernel<0>, grid, dim3(1024), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && max_out > 0) {
     hipLaunchKernelGGL(evict_gather_kernel, dim3((unsigned)((max_out + 63) / 64), a.Hkv, a.B), dim3(256), 0, st, a);
