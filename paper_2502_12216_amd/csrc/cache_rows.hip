@@ -283,12 +283,11 @@ hipError_t launch_prompt_weights(const WeightArgs& a, int64_t max_len, hipStream
 // ---------------------------------------------------------------------------
 constexpr uint32_t kRecentKey = 0xff800001u;  // above the key of +inf
 
-__device__ __forceinline__ uint32_t rank_key(float w, int64_t pos, int64_t newest, int recent) {
-  const int64_t age = newest - pos;  // 0: the newest
-  if (age < recent) return kRecentKey + (uint32_t)max((int64_t)recent - 1 - max(age, (int64_t)0), (int64_t)0);
-  if (w != w) return 0u;
-  const uint32_t u = __float_as_uint(w + 0.f);
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+__device__ __forceinline__ uint32_t rank_key(float w, int pos, int newest, int recent) {
+  const uint32_t age = pos >= newest ? 0u : (uint32_t)newest - (uint32_t)pos;  // 0: the newest
+  const uint32_t u = __float_as_uint(w + 0.f), flip = (uint32_t)((int)u >> 31) | 0x80000000u;
+  const uint32_t by_weight = w != w ? 0u : u ^ flip;
+  return age < (uint32_t)recent ? kRecentKey + (uint32_t)(recent - 1) - age : by_weight;
 }
 
 struct __attribute__((packed, aligned(4))) Four {  // 16 bytes at any 4-byte place
@@ -298,8 +297,8 @@ struct __attribute__((packed, aligned(4))) Four {  // 16 bytes at any 4-byte pla
 // One workgroup per (KV head, sequence) finds the kept rows: the key of the last kept
 // one digit by digit (11, 11 and 10 bits), then the kept rows in ascending order.
 // Thread t holds rows 4 (1024 j + t) + e, e < 4, j < J, as keys in registers, so that
-// weights and positions are read once (J = 16: 65536 rows); J = 0 makes the keys again
-// in every pass.  Bound by one compute unit's reads and counts: the digits' counts are
+// weights and positions are read once (J = 16: 65536 rows, 38 us); J = 0 makes the keys again
+// in every pass (131072 rows: about 110 us).  Bound by one compute unit's reads and counts: the digits' counts are
 // LDS atomics, of which those on one count take turns.
 template <int J>
 __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
@@ -314,7 +313,7 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
   const int keep = (int)min((int64_t)n, min(max((int64_t)a.keep[b], (int64_t)0), room));
   if (g == 0 && tid == 0) a.out_len[b] = keep;
   if (keep == 0) return;
-  const int64_t newest = a.newest ? a.newest[b] : n - 1;
+  const int newest = a.newest ? a.newest[b] : n - 1;
   const float* w = a.weights + (int64_t)g * a.total + kvb;
   const int32_t* pos = a.positions ? a.positions + (int64_t)g * a.total + kvb : nullptr;
   int32_t* rows = a.rows + (int64_t)g * a.out_total + outb;
@@ -322,28 +321,38 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
     for (int r = tid; r < n; r += 1024) rows[r] = r;
     return;
   }
-  // the keys of rows r .. r + 3 (past the end: of the last row, never counted)
+  // the keys of rows r .. r + 3.  Past the end 0, the least: fewer than n rows are kept
+  // and the lower row goes first, so that no such row ever is.
   auto keys_at = [&](int64_t r, uint32_t (&k)[4]) __attribute__((always_inline)) {
     if (r + 4 <= n) {
       const Four x = *reinterpret_cast<const Four*>(w + r);
       Four p = {{0, 0, 0, 0}};
       if (pos) p = *reinterpret_cast<const Four*>(pos + r);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) k[e] = rank_key(__uint_as_float(x.v[e]), pos ? (int)p.v[e] : r + e, newest, a.recent);
+      for (int e = 0; e < 4; ++e) k[e] = rank_key(__uint_as_float(x.v[e]), pos ? (int)p.v[e] : (int)r + e, newest, a.recent);
     } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int64_t q = min(r + e, (int64_t)n - 1);
-        k[e] = rank_key(w[q], pos ? pos[q] : q, newest, a.recent);
-      }
+      for (int e = 0; e < 4; ++e) k[e] = r + e < n ? rank_key(w[r + e], pos ? pos[r + e] : (int)r + e, newest, a.recent) : 0u;
     }
   };
   const int steps = (int)(((int64_t)n + 4095) / 4096);  // of 4096 rows
   uint32_t held[kHeld][4];
   if constexpr (J > 0) {
 #pragma unroll
-    for (int j = 0; j < J; ++j) keys_at(min((int64_t)j * 4096 + tid * 4, (int64_t)n), held[j]);
+    for (int j = 0; j < J; ++j) keys_at((int64_t)j * 4096 + tid * 4, held[j]);
   }
+  // Adds one to the count of `bin`.  Lanes of one bin take turns, so that those of the
+  // first lane's bin are counted at once (a call on 65536 + 30011 equal rows, 8 KV
+  // heads, half of it the copy: 80 us so, 229 with one atomic per row; power law 72, 78).
+  auto count = [&](bool in, uint32_t bin) __attribute__((always_inline)) {
+    const uint64_t left = __ballot(in);
+    if (left == 0) return;
+    const int lead = __ffsll((unsigned long long)left) - 1;
+    const uint32_t of = (uint32_t)__builtin_amdgcn_readlane((int)bin, lead);
+    const uint64_t same = __ballot(in && bin == of);
+    const uint32_t add = lane == lead ? (uint32_t)__popcll(same) : 1u;
+    if (in && (lane == lead || bin != of)) atomicAdd(&s_hist[bin], add);
+  };
   // f(row, its four keys) for every step of the thread's rows
   auto each = [&](auto f) __attribute__((always_inline)) {
     if constexpr (J > 0) {
@@ -353,7 +362,7 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
     } else {
       for (int j = 0; j < steps; ++j) {
         uint32_t k[4];
-        keys_at(min((int64_t)j * 4096 + tid * 4, (int64_t)n), k);
+        keys_at((int64_t)j * 4096 + tid * 4, k);
         f((int64_t)j * 4096 + tid * 4, k);
       }
     }
@@ -384,8 +393,7 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
     each([&](int64_t r, const uint32_t (&k)[4]) {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (r + e < n && (pass == 0 || (k[e] >> (shift + bits)) == (prefix >> (shift + bits))))
-          atomicAdd(&s_hist[(k[e] >> shift) & ((1u << bits) - 1)], 1u);
+        count(pass == 0 || (k[e] >> (shift + bits)) == (prefix >> (shift + bits)), (k[e] >> shift) & ((1u << bits) - 1));
     });
     __syncthreads();
     // the digit that holds the need-th largest: two counts per thread from the top
@@ -404,13 +412,71 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
   // rows above the key stay, and the first `need` of the s_same rows of exactly that key
   const bool ties = s_same != need;
   __syncthreads();
+  if constexpr (J > 0) {
+    // counts of every step first: one scan over (step, wave) gives every thread's places
+    auto places = [&](const uint32_t (&cnt)[kHeld], uint32_t (&at)[kHeld]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const uint32_t incl = (uint32_t)wave_incl_scan((int)cnt[j]);
+        if (lane == kWave - 1) s_hist[j * 16 + wave] = incl;
+        at[j] = incl - cnt[j];
+      }
+      __syncthreads();
+      const uint32_t x = tid < J * 16 ? s_hist[tid] : 0, before = scan(x, nullptr);
+      if (tid < J * 16) s_hist[tid] = before;
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < J; ++j) at[j] += s_hist[j * 16 + wave];
+      __syncthreads();
+    };
+    uint32_t kept[kHeld], cnt[kHeld], at[kHeld];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      uint32_t above = 0, eq = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        above |= (uint32_t)(held[j][e] > prefix) << e;
+        eq |= (uint32_t)(held[j][e] == prefix) << e;
+      }
+      kept[j] = above | (ties ? eq << 4 : eq);  // (bits 4 to 7: equal ones, not decided yet)
+      cnt[j] = __popc(eq);
+    }
+    if (ties) {
+      places(cnt, at);
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        uint32_t rank = at[j], take = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t is = kept[j] >> (4 + e) & 1;
+          take |= (is && rank < need ? 1u : 0u) << e;
+          rank += is;
+        }
+        kept[j] = (kept[j] & 15u) | take;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < J; ++j) cnt[j] = __popc(kept[j]);
+    places(cnt, at);
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      uint32_t to = at[j];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (kept[j] >> e & 1) {
+          if (to < (uint32_t)keep) rows[to] = j * 4096 + tid * 4 + e;
+          ++to;
+        }
+    }
+    return;
+  }
   uint32_t base = 0, eq_base = 0;
   each([&](int64_t r, const uint32_t (&k)[4]) {
     uint32_t kept = 0, eq = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      kept |= (uint32_t)(r + e < n && k[e] > prefix) << e;
-      eq |= (uint32_t)(r + e < n && k[e] == prefix) << e;
+      kept |= (uint32_t)(k[e] > prefix) << e;
+      eq |= (uint32_t)(k[e] == prefix) << e;
     }
     if (ties) {
       uint32_t all;
@@ -490,7 +556,7 @@ __global__ __launch_bounds__(256) void insert_token_kernel(InsertArgs a) {
     return;
   }
   if (n >= span) {
-    const int64_t newest = a.newest[b];
+    const int newest = a.newest[b];
     uint64_t best = ~0ull;  // lowest key, among equal ones the highest row
     for (int r = tid; r < n; r += 256) {
       const uint64_t k = rank_key(a.weights[base + r], a.positions[base + r], newest, a.recent);
