@@ -42,19 +42,51 @@ struct RowsPlan {
   int64_t tiles;  // row tiles of one KV head, at most
 };
 
-// The smallest row tile that holds a source's rows: fewer rows are more waves along
-// the keys.  The splits fill the device's 256 compute units once (32 rows: twice,
-// two workgroups fit) with at least 8 tiles of keys each.
-RowsPlan plan_rows(int64_t total_rows, int64_t max_rows, int n_src, int Hkv, int64_t max_keys) {
-  RowsPlan p;
-  p.variant = max_rows <= 32 ? 0 : (max_rows <= 64 ? 1 : (max_rows <= 128 ? 2 : 3));
-  const int64_t per = tactic::rows_per_item(p.variant);
-  p.tiles = total_rows / per + n_src;
-  const int64_t real = std::max<int64_t>(1, (total_rows + per - 1) / per) * Hkv;
-  const int64_t slots = p.variant == 0 ? 512 : 256;
-  const int64_t step = p.variant == 0 || p.variant == 1 ? 128 : (p.variant == 2 ? 128 : 64);  // keys of a round of tiles
-  const int64_t most = std::max<int64_t>(1, max_keys / (8 * step));
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({slots / real, most, (int64_t)kMaxSplits}));
+// The row tile and the splits with the least estimated time.  A workgroup takes
+// `item` us and `step` us for each round of its waves' tiles (`keys` keys); a compute
+// unit runs one at a time (two of the smallest, at half the pace); the keys come once
+// from memory, half of the shorter of the two hidden behind the longer.  Splits are
+// joined by a second kernel: 4 us, and their sums written and read.  Measured with 32 /
+// 8 and 8 / 2 heads (us a call, tiles of 32, 64, 128, 256 rows with the best splits of
+// each): prompts of 211 tokens 12, 12, 15, 16; 1000 tokens, 2 KV heads 16, 22, 27, 28;
+// 2048 tokens 75, 86, 59, 69; 4096 tokens 243, 270, 185, 153; one token on 32768 34,
+// 36, 39, 47; 20 on 131072 159, 134, 116, 163; 512 on 32768 428, 409, 306, 279.  Shared
+// prefixes of 32768 tokens: 4 sequences 42, 43, 52, 75; 12 50, 45, 54, 76; 64 111, 103,
+// 99, 101.  The choice is within a tenth of the best in most of these.
+struct RowsCost {
+  double item, step;
+  int keys;
+};
+constexpr RowsCost kPromptCost[4] = {{1.3, 0.88, 128}, {2.0, 1.9, 128}, {2.5, 2.3, 128}, {2.0, 1.85, 64}};
+constexpr RowsCost kSharedCost[4] = {{1.3, 1.05, 128}, {2.0, 1.9, 128}, {2.5, 1.7, 64}, {2.0, 1.8, 32}};
+
+RowsPlan plan_rows(int64_t total_rows, int n_src, int Hkv, double mean_keys, int64_t max_keys, int64_t total_keys,
+                   bool shared) {
+  constexpr int kTry[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32, 40, 48, 56, 64};
+  static_assert(kMaxSplits == 64, "the splits tried");
+  const double mem = (double)total_keys * Hkv * 512 / 6e6;  // 6 TB/s
+  double best = INFINITY;
+  RowsPlan p{3, 1, 0};
+  for (int v = 0; v < 4; ++v) {
+    const RowsCost& c = (shared ? kSharedCost : kPromptCost)[v];
+    const int64_t per = tactic::rows_per_item(v);
+    const double items = (double)std::max<int64_t>(n_src, (total_rows + per - 1) / per) * Hkv;
+    for (const int s : kTry) {
+      if (s > 1 && (int64_t)s * c.keys > max_keys) break;
+      const double longest = ceil((double)max_keys / ((double)s * c.keys)), mean = mean_keys / ((double)s * c.keys);
+      const double rounds = ceil(items * s / 256);
+      const double run = std::max(longest * c.step + c.item, rounds * (mean * c.step + c.item));
+      double t = std::max(run, mem) + 0.5 * std::min(run, mem);
+      if (shared) t += 0.1 * s;
+      else if (s > 1) t += 4 + 0.15 * s + (double)total_rows * Hkv * s * (2 * 520) / 4.5e6;
+      if (t < best) {
+        best = t;
+        p.variant = v;
+        p.splits = s;
+      }
+    }
+  }
+  p.tiles = total_rows / tactic::rows_per_item(p.variant) + n_src;
   return p;
 }
 
@@ -68,7 +100,9 @@ struct PromptLayout {
 PromptLayout prompt_layout(const tactic_kv_shape* s, const tactic_query_shape* q) {
   PromptLayout p;
   const int G = s->n_q_heads / s->n_kv_heads;
-  p.plan = plan_rows(q->total_queries * G, q->max_queries * G, s->batch, s->n_kv_heads, s->max_seq_len);
+  // a query sees its own position's keys: on average half its prompt's fewer than all
+  const double mean = std::max(1.0, (double)s->max_seq_len - 0.5 * (double)std::min(q->max_queries, s->max_seq_len));
+  p.plan = plan_rows(q->total_queries * G, s->batch, s->n_kv_heads, mean, s->max_seq_len, s->total_tokens, false);
   const int64_t rows = q->total_queries * s->n_q_heads;
   p.range_stride = (s->max_seq_len + 63) / 64;
   Layout L;
@@ -258,7 +292,8 @@ struct SharedLayout {
 SharedLayout shared_layout(const tactic_kv_shape* s, const tactic_prefixes* p) {
   SharedLayout l;
   const int G = s->n_q_heads / s->n_kv_heads;
-  l.plan = plan_rows((int64_t)p->total_members * G, (int64_t)p->max_members * G, p->n_prefixes, s->n_kv_heads, p->max_len);
+  l.plan = plan_rows((int64_t)p->total_members * G, p->n_prefixes, s->n_kv_heads, (double)p->max_len, p->max_len,
+                     p->total_tokens, true);
   const int64_t rows = (int64_t)s->batch * s->n_q_heads;
   Layout L;
   L.take((int64_t)dense_workspace_bytes(s, tactic::kMaxAttnGrid));

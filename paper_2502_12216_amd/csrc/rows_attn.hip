@@ -239,9 +239,6 @@ void rows_attn_kernel(RowsArgs a) {
     }
     return t;
   };
-  // with several waves to a tile and several tiles at a time all of them step together
-  constexpr bool kSkip = RW == 1 || KW == 1;
-
   const uint16_t* Kb = a.K + (kPaged ? 0 : ((int64_t)g * a.total + kvb) * kHeadDim);
   const uint16_t* Vb = a.V + (kPaged ? 0 : ((int64_t)g * a.total + kvb) * kHeadDim);
   u32x4 kreg[kLoads], vreg[kLoads];
@@ -363,7 +360,7 @@ void rows_attn_kernel(RowsArgs a) {
   };
 
   // scores to weights; accumulator r of block kb is key k0 + 32 kb + 8 (r / 4) + 4 half + r % 4
-  auto soft = [&](int t, int buf, bool masked) __attribute__((always_inline)) {
+  auto soft = [&](int t, int buf, bool masked, bool dead) __attribute__((always_inline)) {
     const int k0 = t * TK;
     if (capped) {
       float big = 0.f;
@@ -399,7 +396,7 @@ void rows_attn_kernel(RowsArgs a) {
           s[kb][r] = fmaf(-slope, fabsf(dist - (float)(kb * 32 + 8 * (r / 4) + r % 4)), s[kb][r]);
     }
     if (masked) {
-      const int lim = klim - k0 - 4 * half;
+      const int lim = dead ? 0 : klim - k0 - 4 * half;  // (dead: nothing of the tile counts)
 #pragma unroll
       for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
@@ -544,23 +541,28 @@ void rows_attn_kernel(RowsArgs a) {
   bool odd = false;
 
   // ---- the keys
-  if constexpr (RW == 8) {
+  if constexpr (RW * KW == 8) {
     // Eight waves, two per SIMD, take turns: while waves 0 to 3 do the products of a
     // tile (P V of the one before, then K Q), waves 4 to 7 turn scores into weights,
     // and the other way round, a barrier between.  In phase 2 i waves 0 to 3 contract
-    // tile i, in phase 2 i + 1 the others do.  Each brings its part of K of tile i + 1
-    // and V of tile i to LDS there, between the products: into the buffers of tiles
-    // i - 1 and i - 2, whose last reads are in phase 2 i - 1, for first reads in phase
-    // 2 i + 2.  (A tile's documents are read with the weights, in phases 2 i + 1 and
-    // 2 i + 2, so that a late wave brings them.)
-    int t = next_tile(t_lo);
+    // their tile i, in phase 2 i + 1 the others do.  Each brings its part of K of tile
+    // i + 1 and V of tile i to LDS there, between the products: into the buffers of
+    // tiles i - 1 and i - 2, whose last reads are in phase 2 i - 1, for first reads in
+    // phase 2 i + 2.  (Documents are read with the weights, in phases 2 i + 1 and
+    // 2 i + 2: where all waves share the tiles a late wave brings them.)  KW = 1: all
+    // waves go by one list of tiles.  Else group kg takes tile first + kg of each round
+    // of KW, and one past the end is the last one again, masked as a whole.
+    constexpr bool kOne = KW == 1;
+    auto round = [&](int t) __attribute__((always_inline)) { return kOne ? next_tile(t) : t; };
+    auto of = [&](int t) __attribute__((always_inline)) { return kOne ? t : min(t + kg, t_hi - 1); };
+    int t = round(t_lo);
     if (t < t_hi) {
-      const bool late = wr >= 4;
-      int t1 = next_tile(t + 1);
-      fetch_k(t);
+      const bool late = wave >= 4;
+      int t1 = round(t + KW);
+      fetch_k(of(t));
       store_k(0);
-      fetch_v(t);
-      if (t1 < t_hi) fetch_k(t1);
+      fetch_v(of(t));
+      if (t1 < t_hi) fetch_k(of(t1));
       __syncthreads();
       if (late) __syncthreads();
       int i = 0;
@@ -570,15 +572,16 @@ void rows_attn_kernel(RowsArgs a) {
         int t2 = t1;
         if (t1 < t_hi) {
           store_k((i + 1) & 1);
-          t2 = next_tile(t1 + 1);
-          fetch_v(t1);
-          if (t2 < t_hi) fetch_k(t2);
+          t2 = round(t1 + KW);
+          fetch_v(of(t1));
+          if (t2 < t_hi) fetch_k(of(t2));
         }
         qk(i & 1);
         __builtin_amdgcn_s_setprio(0);
         __syncthreads();
-        masked = state_of(t) != kFull;
-        soft(t, i & 1, masked);
+        const bool dead = !kOne && t + kg >= t_hi;
+        masked = dead || state_of(of(t)) != kFull;
+        soft(of(t), i & 1, masked, dead);
         t = t1;
         t1 = t2;
         if (!(late && t >= t_hi)) __syncthreads();  // (the late waves have made one more)
@@ -591,51 +594,26 @@ void rows_attn_kernel(RowsArgs a) {
       pv(i & 1);
       __builtin_amdgcn_s_setprio(0);
     }
-  } else if constexpr (kSkip) {
-    // the next tile's rows are in flight while this one is contracted
+  } else {
+    // each wave by itself: the next tile's rows are in flight while this one is contracted
+    static_assert(RW == 1, "waves that share a tile take turns");
     int t = next_tile(t_lo + kg);
-    int buf = 0;
     if (t < t_hi) {
       fetch(t);
       store(0);
     }
-    if constexpr (RW > 1) __syncthreads();
     while (t < t_hi) {
       const int tn = next_tile(t + KW);
       if (tn < t_hi) fetch(tn);
       const int st = state_of(t);
       if (st != kNone) {
-        qk(buf);
-        soft(t, buf, st == kMasked);
-        if (st == kMasked) odd |= any_odd(buf);
-        pv(buf);
+        qk(0);
+        soft(t, 0, st == kMasked, false);
+        if (st == kMasked) odd |= any_odd(0);
+        pv(0);
       }
-      if constexpr (RW > 1) buf ^= 1;
-      if (tn < t_hi) store(buf);
-      if constexpr (RW > 1) __syncthreads();
+      if (tn < t_hi) store(0);
       t = tn;
-    }
-  } else {
-    const int steps = (t_hi - t_lo + KW - 1) / KW;
-    int buf = 0;
-    if (t_lo + kg < t_hi) {
-      fetch(t_lo + kg);
-      store(0);
-    }
-    __syncthreads();
-    for (int i = 0; i < steps; ++i) {
-      const int t = t_lo + i * KW + kg;
-      if (t + KW < t_hi) fetch(t + KW);
-      const int st = t < t_hi ? state_of(t) : kNone;
-      if (st != kNone) {
-        qk(buf);
-        soft(t, buf, st == kMasked);
-        if (st == kMasked) odd |= any_odd(buf);
-        pv(buf);
-      }
-      buf ^= 1;
-      if (t + KW < t_hi) store(buf);
-      __syncthreads();
     }
   }
   if (__syncthreads_or(odd)) {  // rare: the whole item again, one tile at a time
@@ -658,7 +636,7 @@ void rows_attn_kernel(RowsArgs a) {
       const int st = t < t_hi ? state_of(t) : kNone;
       if (st != kNone) {
         qk(0);
-        soft(t, 0, st == kMasked);
+        soft(t, 0, st == kMasked, false);
         pv_odd(0);
       }
       __syncthreads();
@@ -758,25 +736,35 @@ __global__ __launch_bounds__(64) void doc_range_kernel(const int32_t* documents,
   if (threadIdx.x == 0) out[b * stride + t] = make_int2(lo, hi);
 }
 
-// Joins the splits of a row: out = sum_s O_s 2^(m_s - M) / sum_s l_s 2^(m_s - M),
-// in the order of the splits.  One wave per row, two dimensions per lane.
+// Joins the splits of a row: out = sum_s O_s 2^(m_s - M) / sum_s l_s 2^(m_s - M).  One
+// wave per row: lane s has split s's maximum and sum, so that M and the sum of the
+// weights are wave reductions (in one order); then two dimensions per lane, eight
+// splits' sums in flight.
 __global__ __launch_bounds__(256) void rows_combine_kernel(RowsArgs a) {
   const int64_t rows = a.n_queries * a.Hq;
   const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   if (r >= rows) return;
-  float mx = -INFINITY;
-  for (int s = 0; s < a.splits; ++s) mx = fmaxf(mx, a.part_ml[2 * ((int64_t)s * rows + r)]);
-  float x = 0.f, y = 0.f, l = 0.f;
+  static_assert(kMaxSplits <= kWave, "a lane per split");
+  float m = -INFINITY, l = 0.f;
+  if (lane < a.splits) {
+    const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * ((int64_t)lane * rows + r));
+    m = ml.x;
+    l = ml.y;
+  }
+  const float* po = a.part_o + r * kHeadDim + 2 * lane;
+  const float mx = wave_allmax_f(m);
+  const float c = m == -INFINITY ? 0.f : fast_exp2(m - mx);  // (a split without keys wrote no sums)
+  l = wave_allsum_f(m == -INFINITY ? 0.f : l * c);
+  const uint64_t some = __ballot(m != -INFINITY);
+  float x = 0.f, y = 0.f;
+#pragma unroll 8
   for (int s = 0; s < a.splits; ++s) {
-    const int64_t slot = (int64_t)s * rows + r;
-    const float m = a.part_ml[2 * slot];
-    if (m == -INFINITY) continue;
-    const float c = fast_exp2(m - mx);
-    const float2 v = *reinterpret_cast<const float2*>(a.part_o + slot * kHeadDim + 2 * lane);
-    l = fmaf(a.part_ml[2 * slot + 1], c, l);
-    x = fmaf(v.x, c, x);
-    y = fmaf(v.y, c, y);
+    if (!(some >> s & 1)) continue;
+    const float2 v = *reinterpret_cast<const float2*>(po + (int64_t)s * rows * kHeadDim);
+    const float w = readlane_f(c, s);
+    x = fmaf(v.x, w, x);
+    y = fmaf(v.y, w, y);
   }
   const float inv = l != 0.f ? 1.f / l : 0.f;
   *reinterpret_cast<uint32_t*>(a.out + r * kHeadDim + 2 * lane) = pack_bf16(x * inv, y * inv);
