@@ -28,8 +28,9 @@ class _Call:
         """The pointer of tensor t after its checks (None: null, where optional)."""
         if t is None and optional:
             return None
-        _check_tensor(t, name, dtype, shape)
-        if t.device != self.device:
+        if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.device == self.device and t.is_cuda and
+                t.is_contiguous() and (shape is None or t.shape == shape)):
+            _check_tensor(t, name, dtype, shape)  # says which
             raise ValueError(f"{name} is on {t.device}, expected {self.device}")
         # (an empty tensor has no storage: any pointer that is not null stands for it)
         return t.data_ptr() or 16
@@ -44,9 +45,15 @@ class _Call:
         return cache.struct()
 
     def run(self, name: str, *args):
-        with torch.cuda.device(self.device):
-            s = self.stream if self.stream is not None else torch.cuda.current_stream(self.device)
-            C.check(getattr(C.lib(), name)(*args, int(s.cuda_stream)), name)
+        s = self.stream if self.stream is not None else torch.cuda.current_stream(self.device)
+        f = getattr(C.lib(), name)
+        if torch.cuda.current_device() == self.device.index:
+            status = f(*args, s.cuda_stream)
+        else:
+            with torch.cuda.device(self.device):
+                status = f(*args, s.cuda_stream)
+        if status != C.TACTIC_OK:
+            C.check(status, name)
 
 
 def _device(batch: RaggedBatch):
