@@ -91,11 +91,12 @@ __device__ __forceinline__ float halves_sum(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Page-table lookup of token `tok` of sequence b (in bounds whatever the table holds).
-__device__ __forceinline__ int64_t page_row(const PagedKV& pk, int Hkv, int b, int kvh, int tok) {
-  const uint32_t pg = (uint32_t)tok / (uint32_t)pk.page_size;
-  int64_t page = pk.page_table[(int64_t)b * pk.max_pages + pg];
-  page = min(max(page, (int64_t)0), pk.num_pages - 1);
+// Row in the pages of token `tok` of sequence b (in bounds whatever the table holds;
+// the host has checked that the pages hold fewer than 2^31 rows).  `shift`: log2 of the
+// page size, or negative.
+__device__ __forceinline__ int page_row(const PagedKV& pk, int shift, int Hkv, int b, int kvh, int tok) {
+  const uint32_t pg = shift >= 0 ? (uint32_t)tok >> shift : (uint32_t)tok / (uint32_t)pk.page_size;
+  const int page = min(max(pk.page_table[(int64_t)b * pk.max_pages + pg], 0), (int)pk.num_pages - 1);
   return (page * Hkv + kvh) * pk.page_size + (tok - (int)(pg * (uint32_t)pk.page_size));
 }
 
@@ -253,25 +254,40 @@ void rows_attn_kernel(RowsArgs a) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) at[i] = (t + 1) * TK <= n ? f_row + 4 * i : min(f_row + 4 * i, most);
   };
-  auto load = [&](const uint16_t* base, int t, u32x4 (&reg)[kLoads]) __attribute__((always_inline)) {
+  // rows of the pages (paged only)
+  const int page_shift = kPaged && (a.pk.page_size & (a.pk.page_size - 1)) == 0 ? 31 - __clz(a.pk.page_size) : -1;
+  auto page_rows_of = [&](int t, int (&row)[kLoads]) __attribute__((always_inline)) {
     int at[kLoads];
     rows_of(t, at);
-    if constexpr (kPaged) {
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i)
-        reg[i] = *reinterpret_cast<const u32x4*>(base + page_row(a.pk, a.Hkv, src, g, t * TK + at[i]) * kHeadDim + ((f_col ^ f_swz ^ (i & 3)) * 8));
+    for (int i = 0; i < kLoads; ++i) row[i] = page_row(a.pk, page_shift, a.Hkv, src, g, t * TK + at[i]);
+  };
+  auto load_paged = [&](const uint16_t* base, const int (&row)[kLoads], u32x4 (&reg)[kLoads]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      reg[i] = *reinterpret_cast<const u32x4*>(base + (int64_t)row[i] * kHeadDim + ((f_col ^ f_swz ^ (i & 3)) * 8));
+  };
+  auto load = [&](const uint16_t* base, int t, u32x4 (&reg)[kLoads]) __attribute__((always_inline)) {
+    int at[kLoads];
+    if constexpr (kPaged) {
+      page_rows_of(t, at);
+      load_paged(base, at, reg);
     } else {
+      rows_of(t, at);
       const unsigned char* tile_base = reinterpret_cast<const unsigned char*>(base + (int64_t)t * (TK * kHeadDim));
 #pragma unroll
       for (int i = 0; i < kLoads; ++i)
         reg[i] = *reinterpret_cast<const u32x4*>(tile_base + (uint32_t)(at[i] * 256 + ((f_col ^ f_swz ^ (i & 3)) * 16)));
     }
   };
-  auto fetch_k = [&](int t) __attribute__((always_inline)) {
-    load(Kb, t, kreg);
+  auto fetch_doc = [&](int t) __attribute__((always_inline)) {
     if constexpr (kDocs) {
       if (wr == doc_wave && lane < TK) doc_r = a.documents[kvb + min(t * TK + lane, n - 1)];
     }
+  };
+  auto fetch_k = [&](int t) __attribute__((always_inline)) {
+    load(Kb, t, kreg);
+    fetch_doc(t);
   };
   auto fetch_v = [&](int t) __attribute__((always_inline)) { load(Vb, t, vreg); };
   auto place = [&](int buf) __attribute__((always_inline)) {
@@ -289,8 +305,16 @@ void rows_attn_kernel(RowsArgs a) {
     for (int i = 0; i < kLoads; ++i) *reinterpret_cast<u32x4*>(place(buf) + i * 1024 + TK * 256) = vreg[i];
   };
   auto fetch = [&](int t) __attribute__((always_inline)) {
-    fetch_k(t);
-    fetch_v(t);
+    if constexpr (kPaged) {
+      int row[kLoads];
+      page_rows_of(t, row);
+      load_paged(Kb, row, kreg);
+      load_paged(Vb, row, vreg);
+      fetch_doc(t);
+    } else {
+      fetch_k(t);
+      fetch_v(t);
+    }
   };
   auto store = [&](int buf) __attribute__((always_inline)) {
     store_k(buf);
@@ -562,19 +586,44 @@ void rows_attn_kernel(RowsArgs a) {
       fetch_k(of(t));
       store_k(0);
       fetch_v(of(t));
-      if (t1 < t_hi) fetch_k(of(t1));
+      // pages: the rows of a tile are looked up a round before its keys are fetched, and
+      // serve its values a round later (rows1: of t1, rows2: of the tile after)
+      int rows1[kLoads], rows2[kLoads], t2 = t1;
+      if constexpr (kPaged) {
+        if (t1 < t_hi) {
+          page_rows_of(of(t1), rows1);
+          load_paged(Kb, rows1, kreg);
+          fetch_doc(of(t1));
+          t2 = round(t1 + KW);
+          page_rows_of(of(min(t2, t_hi - 1)), rows2);
+        }
+      } else if (t1 < t_hi) {
+        fetch_k(of(t1));
+        t2 = round(t1 + KW);
+      }
       __syncthreads();
       if (late) __syncthreads();
       int i = 0;
       bool masked;
       for (;;) {
         store_v(i & 1);
-        int t2 = t1;
+        int t3 = t2;
         if (t1 < t_hi) {
           store_k((i + 1) & 1);
-          t2 = round(t1 + KW);
-          fetch_v(of(t1));
-          if (t2 < t_hi) fetch_k(of(t2));
+          if (t2 < t_hi) t3 = round(t2 + KW);
+          if constexpr (kPaged) {
+            load_paged(Vb, rows1, vreg);
+            if (t2 < t_hi) {
+              load_paged(Kb, rows2, kreg);
+              fetch_doc(of(t2));
+#pragma unroll
+              for (int j = 0; j < kLoads; ++j) rows1[j] = rows2[j];
+              page_rows_of(of(min(t3, t_hi - 1)), rows2);
+            }
+          } else {
+            fetch_v(of(t1));
+            if (t2 < t_hi) fetch_k(of(t2));
+          }
         }
         qk(i & 1);
         __builtin_amdgcn_s_setprio(0);
@@ -584,6 +633,7 @@ void rows_attn_kernel(RowsArgs a) {
         soft(of(t), i & 1, masked, dead);
         t = t1;
         t1 = t2;
+        t2 = t3;
         if (!(late && t >= t_hi)) __syncthreads();  // (the late waves have made one more)
         if (masked) odd |= any_odd(i & 1);
         __builtin_amdgcn_s_setprio(1);
