@@ -358,7 +358,8 @@ void rows_attn_kernel(RowsArgs a) {
 
   // Operands are read a step ahead of their products and no further (sched_barrier):
   // left to itself the compiler reads the whole tile ahead and spills the rows in flight.
-  auto qk = [&](int buf) __attribute__((always_inline)) {
+  // `beside(step)` is work to place between the products of every second step.
+  auto qk = [&](int buf, auto beside) __attribute__((always_inline)) {
     const lds_ptr kt = tile_lds(buf);
     uint32_t off = k_off;
     asm volatile("" : "+v"(off));  // (its eight places are made here, not kept in registers over the loop)
@@ -379,9 +380,13 @@ void rows_attn_kernel(RowsArgs a) {
 #pragma unroll
       for (int kb = 0; kb < NB; ++kb)
         s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[st & 1][kb]), qf[st], s[kb], 0, 0, 0);
-      if (st & 1) __builtin_amdgcn_sched_barrier(0);
+      if (st & 1) {
+        beside(st / 2);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
   };
+  auto nothing = [](int) __attribute__((always_inline)) {};
 
   // scores to weights; accumulator r of block kb is key k0 + 32 kb + 8 (r / 4) + 4 half + r % 4
   auto soft = [&](int t, int buf, bool masked, bool dead) __attribute__((always_inline)) {
@@ -570,7 +575,8 @@ void rows_attn_kernel(RowsArgs a) {
     // tile (P V of the one before, then K Q), waves 4 to 7 turn scores into weights,
     // and the other way round, a barrier between.  In phase 2 i waves 0 to 3 contract
     // their tile i, in phase 2 i + 1 the others do.  Each brings its part of K of tile
-    // i + 1 and V of tile i to LDS there, between the products: into the buffers of
+    // i + 1 and V of tile i to LDS there, between the products (a block of its own took
+    // 470 of a phase's 2200 cycles): into the buffers of
     // tiles i - 1 and i - 2, whose last reads are in phase 2 i - 1, for first reads in
     // phase 2 i + 2.  (Documents are read with the weights, in phases 2 i + 1 and
     // 2 i + 2: where all waves share the tiles a late wave brings them.)  KW = 1: all
@@ -589,43 +595,41 @@ void rows_attn_kernel(RowsArgs a) {
       // pages: the rows of a tile are looked up a round before its keys are fetched, and
       // serve its values a round later (rows1: of t1, rows2: of the tile after)
       int rows1[kLoads], rows2[kLoads], t2 = t1;
+      if (t1 < t_hi) t2 = round(t1 + KW);
       if constexpr (kPaged) {
-        if (t1 < t_hi) {
-          page_rows_of(of(t1), rows1);
-          load_paged(Kb, rows1, kreg);
-          fetch_doc(of(t1));
-          t2 = round(t1 + KW);
-          page_rows_of(of(min(t2, t_hi - 1)), rows2);
-        }
-      } else if (t1 < t_hi) {
-        fetch_k(of(t1));
-        t2 = round(t1 + KW);
+        page_rows_of(of(min(t1, t_hi - 1)), rows1);
+        load_paged(Kb, rows1, kreg);
+        fetch_doc(of(min(t1, t_hi - 1)));
+        page_rows_of(of(min(t2, t_hi - 1)), rows2);
+      } else {
+        fetch_k(of(min(t1, t_hi - 1)));
       }
       __syncthreads();
       if (late) __syncthreads();
       int i = 0;
       bool masked;
       for (;;) {
-        store_v(i & 1);
         int t3 = t2;
-        if (t1 < t_hi) {
-          store_k((i + 1) & 1);
-          if (t2 < t_hi) t3 = round(t2 + KW);
+        if (t2 < t_hi) t3 = round(t2 + KW);
+        // (past the end the last tile is brought again, which nobody reads)
+        const int tv = of(min(t1, t_hi - 1)), tk = of(min(t2, t_hi - 1)), tr = of(min(t3, t_hi - 1));
+        qk(i & 1, [&](int step) __attribute__((always_inline)) {
+          if (step == 0) store_v(i & 1);
+          if (step == 1) store_k((i + 1) & 1);
           if constexpr (kPaged) {
-            load_paged(Vb, rows1, vreg);
-            if (t2 < t_hi) {
+            if (step == 2) load_paged(Vb, rows1, vreg);
+            if (step == 3) {
               load_paged(Kb, rows2, kreg);
-              fetch_doc(of(t2));
+              fetch_doc(tk);
 #pragma unroll
               for (int j = 0; j < kLoads; ++j) rows1[j] = rows2[j];
-              page_rows_of(of(min(t3, t_hi - 1)), rows2);
+              page_rows_of(tr, rows2);
             }
           } else {
-            fetch_v(of(t1));
-            if (t2 < t_hi) fetch_k(of(t2));
+            if (step == 2) fetch_v(tv);
+            if (step == 3) fetch_k(tk);
           }
-        }
-        qk(i & 1);
+        });
         __builtin_amdgcn_s_setprio(0);
         __syncthreads();
         const bool dead = !kOne && t + kg >= t_hi;
@@ -657,7 +661,7 @@ void rows_attn_kernel(RowsArgs a) {
       if (tn < t_hi) fetch(tn);
       const int st = state_of(t);
       if (st != kNone) {
-        qk(0);
+        qk(0, nothing);
         soft(t, 0, st == kMasked, false);
         if (st == kMasked) odd |= any_odd(0);
         pv(0);
@@ -685,7 +689,7 @@ void rows_attn_kernel(RowsArgs a) {
       __syncthreads();
       const int st = t < t_hi ? state_of(t) : kNone;
       if (st != kNone) {
-        qk(0);
+        qk(0, nothing);
         soft(t, 0, st == kMasked, false);
         pv_odd(0);
       }
