@@ -124,17 +124,19 @@ void rows_attn_kernel(RowsArgs a) {
   int rest = blockIdx.x / a.Hkv;
   const int split = rest % a.splits;
   rest /= a.splits;
+  // the source: tiles of source b start at floor(rows before it / ROWS) + b at the
+  // latest, a lane per candidate (64 at a time: one load where there are few)
   int src = 0;
-  {
-    // tiles of source b start at floor(rows before it / ROWS) + b at the latest
-    int lo = 0, hi = a.n_src - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
+  for (int count = a.n_src; count > 1;) {
+    const int step = (count + 63) / 64, mid = src + lane * step;
+    bool ok = lane * step < count;
+    if (ok) {
       const int64_t before = a.mode == 0 ? a.q_indptr[mid] : (int64_t)a.member_indptr[mid];
-      if (before * a.G / ROWS + mid <= rest) lo = mid;
-      else hi = mid - 1;
+      ok = before * a.G / ROWS + mid <= rest;
     }
-    src = lo;
+    const int at = ((int)__popcll(__ballot(ok)) - 1) * step;  // (candidate 0 always is)
+    src += at;
+    count = min(step, count - at);
   }
   const int64_t q0 = a.mode == 0 ? a.q_indptr[src] : (int64_t)a.member_indptr[src];
   const int64_t q1 = a.mode == 0 ? a.q_indptr[src + 1] : (int64_t)a.member_indptr[src + 1];
@@ -179,19 +181,8 @@ void rows_attn_kernel(RowsArgs a) {
   const int ktiles = (kend + TK - 1) / TK;
   const int t_lo = (int)((int64_t)ktiles * split / a.splits), t_hi = (int)((int64_t)ktiles * (split + 1) / a.splits);
 
-  // uniform limits of the wave's rows
-  int w_lo = klim, w_hi = klim, d_lo = qdoc, d_hi = qdoc;
-#pragma unroll
-  for (int s = 1; s < 32; s <<= 1) {
-    w_lo = min(w_lo, __shfl_xor(w_lo, s, 64));
-    w_hi = max(w_hi, __shfl_xor(w_hi, s, 64));
-    d_lo = min(d_lo, __shfl_xor(d_lo, s, 64));
-    d_hi = max(d_hi, __shfl_xor(d_hi, s, 64));
-  }
-  w_lo = __builtin_amdgcn_readfirstlane(w_lo);
-  w_hi = __builtin_amdgcn_readfirstlane(w_hi);
-  d_lo = __builtin_amdgcn_readfirstlane(d_lo);
-  d_hi = __builtin_amdgcn_readfirstlane(d_hi);
+  // the fewest and the most keys that one of the wave's rows sees (rows ascend)
+  const int w_lo = __builtin_amdgcn_readlane(klim, 0), w_hi = __builtin_amdgcn_readlane(klim, 31);
 
   // Scores stay a factor `scale` below their base-2 value until the exponential,
   // which takes it along with the maximum in one multiply-add.
@@ -208,38 +199,63 @@ void rows_attn_kernel(RowsArgs a) {
   };
   load_q();
 
-  // documents: the range of each 64-key tile (from doc_range_kernel) and, for the
-  // item's queries, that of the tiles they lie in
+  // Documents: ranges of each 64-key tile (from doc_range_kernel).  i_lo, i_hi: of the
+  // tiles that the item's queries lie in; a tile outside is left out.  Ranges are read
+  // 64 tiles at a time, into masks of the tiles that may hold a seen key and of those
+  // whose keys all are of the wave's one document.
   const int2* dr = kDocs ? a.doc_range + (int64_t)src * a.range_stride : nullptr;
-  int i_lo = 0, i_hi = 0;
+  int i_lo = INT32_MAX, i_hi = INT32_MIN, win = INT32_MIN;
+  uint64_t w_some = 0, w_same = 0;
+  const int d_one = __builtin_amdgcn_readfirstlane(qdoc);
+  const bool one_doc = __all(qdoc == d_one);
   if constexpr (kDocs) {
     const int64_t m = q1 - q0;
     const int p0 = max((int)(n - m + row0 / a.G), 0), p1 = (int)(n - m + (min(row0 + ROWS, nrows) - 1) / a.G);
-    i_lo = INT32_MAX;
-    i_hi = INT32_MIN;
-    if (p1 >= 0) {
-      for (int t = p0 / 64; t <= p1 / 64; ++t) {
-        i_lo = min(i_lo, dr[t].x);
-        i_hi = max(i_hi, dr[t].y);
-      }
+    if (p1 >= 0 && p0 / 64 + lane <= p1 / 64) {  // (at most 5 tiles)
+      const int2 r = dr[p0 / 64 + lane];
+      i_lo = r.x;
+      i_hi = r.y;
     }
+#pragma unroll
+    for (int s = 1; s < 8; s <<= 1) {
+      i_lo = min(i_lo, __shfl_xor(i_lo, s, 64));
+      i_hi = max(i_hi, __shfl_xor(i_hi, s, 64));
+    }
+    i_lo = __builtin_amdgcn_readfirstlane(i_lo);
+    i_hi = __builtin_amdgcn_readfirstlane(i_hi);
   }
+  auto look = [&](int t) __attribute__((always_inline)) {
+    if (t >= win && t < win + 64) return;
+    win = t;
+    int2 r = make_int2(INT32_MAX, INT32_MIN);
+    if (t + lane < t_hi) r = dr[(t + lane) * TK / 64];
+    w_some = __ballot(r.x <= i_hi && r.y >= i_lo);
+    w_same = __ballot(one_doc && r.x == r.y && r.x == d_one);
+  };
   // first tile from t on, in steps of KW, that may hold a seen key (t_hi or more: none)
+  constexpr uint64_t kEvery = KW == 1 ? ~0ull : (KW == 2 ? 0x5555555555555555ull : 0x1111111111111111ull);
   auto next_tile = [&](int t) __attribute__((always_inline)) -> int {
     if constexpr (!kDocs) return t;
     while (t < t_hi) {
-      const int mine = t + lane * KW;
-      bool some = false;
-      if (mine < t_hi) {
-        const int2 r = dr[mine * TK / 64];
-        some = r.x <= i_hi && r.y >= i_lo;
-      }
-      const uint64_t any = __ballot(some);
-      if (any) return t + (__ffsll((unsigned long long)any) - 1) * KW;
-      t += 64 * KW;
+      look(t);
+      const uint64_t any = (w_some >> (t - win)) & kEvery;
+      if (any) return t + __ffsll((unsigned long long)any) - 1;
+      t += (win + 64 - t + KW - 1) / KW * KW;
     }
     return t;
   };
+  // whether all of the wave's rows see all of the tile
+  auto is_full = [&](int t) __attribute__((always_inline)) -> bool {
+    bool full = t * TK + TK <= w_lo;
+    if constexpr (kDocs) {
+      if (t < t_hi) {
+        look(t);
+        full = full && (w_same >> (t - win) & 1);
+      }
+    }
+    return full;
+  };
+
   const uint16_t* Kb = a.K + (kPaged ? 0 : ((int64_t)g * a.total + kvb) * kHeadDim);
   const uint16_t* Vb = a.V + (kPaged ? 0 : ((int64_t)g * a.total + kvb) * kHeadDim);
   u32x4 kreg[kLoads], vreg[kLoads];
@@ -343,19 +359,6 @@ void rows_attn_kernel(RowsArgs a) {
 
   f32x16 s[NB];           // scores of the tile, then dead
   u32x4 pf[TK / 16][PARTS];  // its weights
-  enum { kNone = 0, kFull = 1, kMasked = 2 };  // of the wave's rows: none sees the tile, all see all of it, else
-  auto state_of = [&](int t) __attribute__((always_inline)) -> int {
-    const int k0 = t * TK;
-    if (k0 >= w_hi) return kNone;
-    bool masked = k0 + TK > w_lo;
-    if constexpr (kDocs) {
-      const int2 r = dr[k0 / 64];
-      if (r.x > d_hi || r.y < d_lo) return kNone;
-      masked |= !(r.x == r.y && d_lo == d_hi);
-    }
-    return masked ? kMasked : kFull;
-  };
-
   // Operands are read a step ahead of their products and no further (sched_barrier):
   // left to itself the compiler reads the whole tile ahead and spills the rows in flight.
   // `beside(step)` is work to place between the products of every second step.
@@ -588,7 +591,12 @@ void rows_attn_kernel(RowsArgs a) {
     int t = round(t_lo);
     if (t < t_hi) {
       const bool late = wave >= 4;
+      // tiles of this round and the next ones, and whether no row masks any of them
+      // (past the end of the list: dead, and masked as a whole)
+      auto whole = [&](int t) __attribute__((always_inline)) { return t + kg < t_hi && is_full(of(t)); };
+      bool full0 = whole(t);
       int t1 = round(t + KW);
+      bool full1 = whole(t1);
       fetch_k(of(t));
       store_k(0);
       fetch_v(of(t));
@@ -596,6 +604,7 @@ void rows_attn_kernel(RowsArgs a) {
       // serve its values a round later (rows1: of t1, rows2: of the tile after)
       int rows1[kLoads], rows2[kLoads], t2 = t1;
       if (t1 < t_hi) t2 = round(t1 + KW);
+      bool full2 = whole(t2);
       if constexpr (kPaged) {
         page_rows_of(of(min(t1, t_hi - 1)), rows1);
         load_paged(Kb, rows1, kreg);
@@ -611,6 +620,7 @@ void rows_attn_kernel(RowsArgs a) {
       for (;;) {
         int t3 = t2;
         if (t2 < t_hi) t3 = round(t2 + KW);
+        const bool full3 = whole(t3);
         // (past the end the last tile is brought again, which nobody reads)
         const int tv = of(min(t1, t_hi - 1)), tk = of(min(t2, t_hi - 1)), tr = of(min(t3, t_hi - 1));
         qk(i & 1, [&](int step) __attribute__((always_inline)) {
@@ -630,23 +640,23 @@ void rows_attn_kernel(RowsArgs a) {
             if (step == 3) fetch_k(tk);
           }
         });
-        __builtin_amdgcn_s_setprio(0);
         __syncthreads();
         const bool dead = !kOne && t + kg >= t_hi;
-        masked = dead || state_of(of(t)) != kFull;
+        masked = !full0;
         soft(of(t), i & 1, masked, dead);
         t = t1;
         t1 = t2;
         t2 = t3;
+        full0 = full1;
+        full1 = full2;
+        full2 = full3;
         if (!(late && t >= t_hi)) __syncthreads();  // (the late waves have made one more)
         if (masked) odd |= any_odd(i & 1);
-        __builtin_amdgcn_s_setprio(1);
         if (t >= t_hi) break;
         pv(i & 1);
         ++i;
       }
       pv(i & 1);
-      __builtin_amdgcn_s_setprio(0);
     }
   } else {
     // each wave by itself: the next tile's rows are in flight while this one is contracted
@@ -659,13 +669,11 @@ void rows_attn_kernel(RowsArgs a) {
     while (t < t_hi) {
       const int tn = next_tile(t + KW);
       if (tn < t_hi) fetch(tn);
-      const int st = state_of(t);
-      if (st != kNone) {
-        qk(0, nothing);
-        soft(t, 0, st == kMasked, false);
-        if (st == kMasked) odd |= any_odd(0);
-        pv(0);
-      }
+      const bool masked = !is_full(t);
+      qk(0, nothing);
+      soft(t, 0, masked, false);
+      if (masked) odd |= any_odd(0);
+      pv(0);
       if (tn < t_hi) store(0);
       t = tn;
     }
@@ -687,10 +695,9 @@ void rows_attn_kernel(RowsArgs a) {
         store(0);
       }
       __syncthreads();
-      const int st = t < t_hi ? state_of(t) : kNone;
-      if (st != kNone) {
+      if (t < t_hi) {
         qk(0, nothing);
-        soft(t, 0, st == kMasked, false);
+        soft(t, 0, !is_full(t), false);
         pv_odd(0);
       }
       __syncthreads();
