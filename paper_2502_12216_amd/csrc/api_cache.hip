@@ -159,6 +159,7 @@ tactic_status prompt_impl(const uint16_t* q, const uint16_t* K, const uint16_t* 
   a.q_indptr = queries->q_indptr;
   if (mod) {
     a.cap = mod->cap;
+    a.poly = tactic::cap_poly(mod->cap);
     a.slopes = mod->slopes;
     a.documents = mod->documents;
     a.prefix_len = mod->prefix_len;
@@ -335,6 +336,7 @@ tactic_status shared_impl(const uint16_t* q, const uint16_t* Kp, const uint16_t*
   a.own_len = shape->seq_len;
   if (mod) {
     a.cap = mod->cap;
+    a.poly = tactic::cap_poly(mod->cap);
     a.slopes = mod->slopes;
   }
   if (pkp) {
@@ -425,6 +427,7 @@ tactic_status tactic_prompt_weights(const uint16_t* q, const uint16_t* K, const 
   a.window = window;
   if (mod) {
     a.cap = mod->cap;
+    a.poly = tactic::cap_poly(mod->cap);
     a.slopes = mod->slopes;
     a.documents = mod->documents;
     a.prefix_len = mod->prefix_len;

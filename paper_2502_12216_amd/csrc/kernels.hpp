@@ -163,6 +163,7 @@ struct RowsArgs {
   const int64_t* own_indptr;    // mode 1: the sequences' own tokens, for the queries' positions
   const int64_t* own_len;
   float cap;                    // 0: none
+  CapPoly poly;
   const float* slopes;          // [Hq] or null
   const int32_t* documents;     // [total] or null (mode 0)
   const int32_t* prefix_len;    // [n_src] or null (mode 0)
@@ -186,6 +187,7 @@ struct WeightArgs {
   int B, Hq, Hkv, G, splits;
   int64_t total, n_queries, window;  // window 0: every query
   float cap;
+  CapPoly poly;
   const float* slopes;
   const int32_t* documents;
   const int32_t* prefix_len;

@@ -184,12 +184,12 @@ void rows_attn_kernel(RowsArgs a) {
   // the fewest and the most keys that one of the wave's rows sees (rows ascend)
   const int w_lo = __builtin_amdgcn_readlane(klim, 0), w_hi = __builtin_amdgcn_readlane(klim, 31);
 
-  // Scores stay a factor `scale` below their base-2 value until the exponential,
-  // which takes it along with the maximum in one multiply-add.
+  // Scores without a cap stay a factor `scale` below their base-2 value until the
+  // exponential, which takes it along with the maximum in one multiply-add.
   const bool capped = a.cap > 0.f, biased = a.slopes != nullptr;
-  const float scale = capped ? a.cap * kLog2e : kInvSqrtDim * kLog2e;
+  const float scale = capped ? 1.f : kInvSqrtDim * kLog2e;
   const float slope = biased ? a.slopes[g * a.G + h] * kLog2e / scale : 0.f;
-  const float to_cap = capped ? kInvSqrtDim / a.cap : 0.f;
+  const float to_cap = capped ? kInvSqrtDim / a.cap : 0.f, cap2 = a.cap * kLog2e;
 
   bf16x8 qf[8];
   auto load_q = [&]() __attribute__((always_inline)) {
@@ -400,22 +400,30 @@ void rows_attn_kernel(RowsArgs a) {
       for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
         for (int r = 0; r < 16; ++r) big = fmaxf(big, fabsf(s[kb][r]));
-      // (NaN counts as inside: the polynomial keeps it)
-      if (__any(big * to_cap > kTanhPoly)) {
+      // (NaN counts as inside: the polynomials keep it)
+      if (PARTS == 1 && !__any(big > a.poly.near)) {
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            s[kb][r] = tanh_any(s[kb][r] * to_cap);
-            if (r % 2) __builtin_amdgcn_sched_barrier(0);  // (two at a time: few registers are left here)
+            s[kb][r] = cap_near(s[kb][r], a.poly);
+            if (r % 8 == 7) __builtin_amdgcn_sched_barrier(0);
+          }
+      } else if (!__any(big > a.poly.far)) {
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            s[kb][r] = cap_far(s[kb][r], a.poly);
+            if (r % 8 == 7) __builtin_amdgcn_sched_barrier(0);
           }
       } else {
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            s[kb][r] = tanh_poly(s[kb][r] * to_cap);
-            if (r % 8 == 7) __builtin_amdgcn_sched_barrier(0);
+            s[kb][r] = cap2 * tanh_any(s[kb][r] * to_cap);
+            if (r % 2) __builtin_amdgcn_sched_barrier(0);  // (two at a time: few registers are left here)
           }
       }
     }

@@ -46,6 +46,39 @@ __device__ __forceinline__ float tanh_poly(float x) {
   return x * r;
 }
 
+// cap tanh(s / cap) in base 2 for whole tiles of products s = q . k, as s times a
+// polynomial in s^2 whose coefficients hold the scale, the cap and log2(e) (set on the
+// host in 64 bits): of degree 3 up to |s| = near (a relative error of 5.9e-8 with exact
+// arithmetic, 2.2e-7 with fp32's), else of degree 5 up to |s| = far (as tanh_poly).
+struct CapPoly {
+  float near, far;
+  float c3[4], c5[6];
+};
+__host__ inline CapPoly cap_poly(float cap) {
+  CapPoly p{};
+  if (!(cap > 0.f)) return p;
+  const double c3[4] = {0.9999999403953552, -0.333319753408432, 0.13284501433372498, -0.0482722632586956};
+  const double c5[6] = {1.0, -0.33332958817481995, 0.1332540661096573, -0.05334442853927612, 0.019582906737923622,
+                        -0.004716256633400917};
+  const double k = 0.08838834764831845 / cap, out = cap * 1.4426950408889634;
+  double f = k * out;
+  for (int i = 0; i < 6; ++i, f *= k * k) {
+    if (i < 4) p.c3[i] = (float)(c3[i] * f);
+    p.c5[i] = (float)(c5[i] * f);
+  }
+  p.near = (float)(0.375 / k);
+  p.far = (float)(0.75 / k);
+  return p;
+}
+__device__ __forceinline__ float cap_near(float s, const CapPoly& p) {
+  const float z = s * s;
+  return s * fmaf(z, fmaf(z, fmaf(z, p.c3[3], p.c3[2]), p.c3[1]), p.c3[0]);
+}
+__device__ __forceinline__ float cap_far(float s, const CapPoly& p) {
+  const float z = s * s;
+  return s * fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, p.c5[5], p.c5[4]), p.c5[3]), p.c5[2]), p.c5[1]), p.c5[0]);
+}
+
 // Score rules of the single-token form (attn_splitk_kernel); every pointer may be null.
 struct TokenMod {
   float cap;                    // 0: none
