@@ -698,6 +698,9 @@ void attn_splitk_kernel(AttnArgs a, std::conditional_t<kMod != 0, TokenMod, NoMo
     }
 
     // ---- merge the lane-group states: common max, rescale, sum
+    if constexpr (kMod != 0) {  // (a maximum passes NaN over: where no other score was there the sum says that some was)
+      if (m == -INFINITY && l != l) m = 0.f;
+    }
     if (sl == (kMatrix ? hl : hl * (16 / G))) {
       s_ml[gid][0][hl] = m;
       s_ml[gid][1][hl] = l;

@@ -714,6 +714,8 @@ void rows_attn_kernel(RowsArgs a) {
 
   // ---- the sums of both halves, then of the KW groups
   float l_run = halves_sum((l4[0] + l4[1]) + (l4[2] + l4[3]));
+  // (a maximum passes NaN over: where no other score was there the sum says that some was)
+  if (m_run == -INFINITY && l_run != l_run) m_run = 0.f;
   int d_from = 0, d_to = 4;
   if constexpr (KW > 1) {
     __syncthreads();  // the tiles are dead: their storage takes the groups' sums
