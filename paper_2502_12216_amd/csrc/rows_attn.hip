@@ -171,12 +171,14 @@ void rows_attn_kernel(RowsArgs a) {
     qpos = n + (int)seq_tokens(a.own_indptr, a.own_len, b) - 1;
   }
   // the item's keys: those that its last row sees (prompt rows see ever more)
-  int kend = n;
+  int kend = n, kall = n;  // and those that its first row sees
   if (a.mode == 0) {
     const int last = min(row0 + ROWS, nrows) - 1;
     const int lp = (int)(n - (q1 - q0) + last / a.G);
     const int pre = a.prefix_len ? a.prefix_len[src] : 0;
     kend = lp < 0 ? 0 : min(max(lp + 1, pre), n);
+    const int fp = (int)(n - (q1 - q0) + row0 / a.G);
+    kall = fp < 0 ? 0 : min(max(fp + 1, pre), n);
   }
   const int ktiles = (kend + TK - 1) / TK;
   const int t_lo = (int)((int64_t)ktiles * split / a.splits), t_hi = (int)((int64_t)ktiles * (split + 1) / a.splits);
@@ -201,11 +203,11 @@ void rows_attn_kernel(RowsArgs a) {
 
   // Documents: ranges of each 64-key tile (from doc_range_kernel).  i_lo, i_hi: of the
   // tiles that the item's queries lie in; a tile outside is left out.  Ranges are read
-  // 64 tiles at a time, into masks of the tiles that may hold a seen key and of those
-  // whose keys all are of the wave's one document.
+  // 64 tiles at a time, into masks of the tiles that may hold a seen key, of those whose
+  // keys all are of the wave's one document, and of those where that holds for the item.
   const int2* dr = kDocs ? a.doc_range + (int64_t)src * a.range_stride : nullptr;
   int i_lo = INT32_MAX, i_hi = INT32_MIN, win = INT32_MIN;
-  uint64_t w_some = 0, w_same = 0;
+  uint64_t w_some = 0, w_same = 0, w_sure = 0;
   const int d_one = __builtin_amdgcn_readfirstlane(qdoc);
   const bool one_doc = __all(qdoc == d_one);
   if constexpr (kDocs) {
@@ -231,6 +233,7 @@ void rows_attn_kernel(RowsArgs a) {
     if (t + lane < t_hi) r = dr[(t + lane) * TK / 64];
     w_some = __ballot(r.x <= i_hi && r.y >= i_lo);
     w_same = __ballot(one_doc && r.x == r.y && r.x == d_one);
+    w_sure = __ballot(i_lo == i_hi && r.x == r.y && r.x == i_lo);
   };
   // first tile from t on, in steps of KW, that may hold a seen key (t_hi or more: none)
   constexpr uint64_t kEvery = KW == 1 ? ~0ull : (KW == 2 ? 0x5555555555555555ull : 0x1111111111111111ull);
@@ -244,16 +247,17 @@ void rows_attn_kernel(RowsArgs a) {
     }
     return t;
   };
-  // whether all of the wave's rows see all of the tile
-  auto is_full = [&](int t) __attribute__((always_inline)) -> bool {
-    bool full = t * TK + TK <= w_lo;
+  // whether all of the wave's rows see all of the tile (kFull), and all of the item's (kSure)
+  constexpr int kFull = 1, kSure = 2;
+  auto sees_all = [&](int t) __attribute__((always_inline)) -> int {
+    int all = (t * TK + TK <= w_lo ? kFull : 0) | (t * TK + TK <= kall ? kSure : 0);
     if constexpr (kDocs) {
       if (t < t_hi) {
         look(t);
-        full = full && (w_same >> (t - win) & 1);
+        all &= (int)(w_same >> (t - win) & 1) | (int)(w_sure >> (t - win) & 1) << 1;
       }
     }
-    return full;
+    return all;
   };
 
   const uint16_t* Kb = a.K + (kPaged ? 0 : ((int64_t)g * a.total + kvb) * kHeadDim);
@@ -523,13 +527,15 @@ void rows_attn_kernel(RowsArgs a) {
     }
   };
   // A masked key's weight is 0, but 0 times its value is NaN where that is not
-  // finite.  So the values of tiles with something masked are looked over, and where
-  // one is found the item is computed again by a loop that goes by kinds of values.
+  // finite.  So the values of tiles with something masked are looked over, a part by
+  // each wave of the tile, and where one is found the item is computed again by a loop
+  // that goes by kinds of values.
   auto any_odd = [&](int buf) __attribute__((always_inline)) -> bool {
-    const lds_ptr vt = tile_lds(buf) + TK * 256;
+    constexpr int kPart = TK * 16 / 64 / RW;
+    const lds_ptr vt = tile_lds(buf) + TK * 256 + wr * kPart * 1024;
     uint32_t bad = 0;
-#pragma unroll 4
-    for (int i = 0; i < TK * 16 / 64; ++i) {
+#pragma unroll
+    for (int i = 0; i < kPart; ++i) {
       const u32x4 w = *(__attribute__((address_space(3))) u32x4*)(vt + (i * 64 + lane) * 16);
 #pragma unroll
       for (int j = 0; j < 4; ++j) bad |= w[j] ^ finite_halves(w[j]);
@@ -601,10 +607,10 @@ void rows_attn_kernel(RowsArgs a) {
       const bool late = wave >= 4;
       // tiles of this round and the next ones, and whether no row masks any of them
       // (past the end of the list: dead, and masked as a whole)
-      auto whole = [&](int t) __attribute__((always_inline)) { return t + kg < t_hi && is_full(of(t)); };
-      bool full0 = whole(t);
+      auto whole = [&](int t) __attribute__((always_inline)) -> int { return t + kg < t_hi ? sees_all(of(t)) : 0; };
+      int full0 = whole(t);
       int t1 = round(t + KW);
-      bool full1 = whole(t1);
+      int full1 = whole(t1);
       fetch_k(of(t));
       store_k(0);
       fetch_v(of(t));
@@ -612,7 +618,7 @@ void rows_attn_kernel(RowsArgs a) {
       // serve its values a round later (rows1: of t1, rows2: of the tile after)
       int rows1[kLoads], rows2[kLoads], t2 = t1;
       if (t1 < t_hi) t2 = round(t1 + KW);
-      bool full2 = whole(t2);
+      int full2 = whole(t2);
       if constexpr (kPaged) {
         page_rows_of(of(min(t1, t_hi - 1)), rows1);
         load_paged(Kb, rows1, kreg);
@@ -624,11 +630,11 @@ void rows_attn_kernel(RowsArgs a) {
       __syncthreads();
       if (late) __syncthreads();
       int i = 0;
-      bool masked;
+      bool look_over;
       for (;;) {
         int t3 = t2;
         if (t2 < t_hi) t3 = round(t2 + KW);
-        const bool full3 = whole(t3);
+        const int full3 = whole(t3);
         // (past the end the last tile is brought again, which nobody reads)
         const int tv = of(min(t1, t_hi - 1)), tk = of(min(t2, t_hi - 1)), tr = of(min(t3, t_hi - 1));
         qk(i & 1, [&](int step) __attribute__((always_inline)) {
@@ -650,8 +656,8 @@ void rows_attn_kernel(RowsArgs a) {
         });
         __syncthreads();
         const bool dead = !kOne && t + kg >= t_hi;
-        masked = !full0;
-        soft(of(t), i & 1, masked, dead);
+        look_over = !(full0 & kSure);
+        soft(of(t), i & 1, !(full0 & kFull), dead);
         t = t1;
         t1 = t2;
         t2 = t3;
@@ -659,7 +665,7 @@ void rows_attn_kernel(RowsArgs a) {
         full1 = full2;
         full2 = full3;
         if (!(late && t >= t_hi)) __syncthreads();  // (the late waves have made one more)
-        if (masked) odd |= any_odd(i & 1);
+        if (look_over) odd |= any_odd(i & 1);
         if (t >= t_hi) break;
         pv(i & 1);
         ++i;
@@ -677,7 +683,7 @@ void rows_attn_kernel(RowsArgs a) {
     while (t < t_hi) {
       const int tn = next_tile(t + KW);
       if (tn < t_hi) fetch(tn);
-      const bool masked = !is_full(t);
+      const bool masked = !(sees_all(t) & kFull);
       qk(0, nothing);
       soft(t, 0, masked, false);
       if (masked) odd |= any_odd(0);
@@ -705,7 +711,7 @@ void rows_attn_kernel(RowsArgs a) {
       __syncthreads();
       if (t < t_hi) {
         qk(0, nothing);
-        soft(t, 0, !is_full(t), false);
+        soft(t, 0, !(sees_all(t) & kFull), false);
         pv_odd(0);
       }
       __syncthreads();
