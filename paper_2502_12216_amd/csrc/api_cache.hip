@@ -92,7 +92,7 @@ RowsPlan plan_rows(int64_t total_rows, int n_src, int Hkv, double mean_keys, int
 
 struct PromptLayout {
   RowsPlan plan;
-  int64_t part_o, part_ml, ranges, range_stride, bytes;
+  int64_t part_o, part_ml, ranges, range_stride, items, counts, order, bytes;
   int wsplits;  // splits of tactic_prompt_weights
   int64_t wpart;
 };
@@ -110,6 +110,9 @@ PromptLayout prompt_layout(const tactic_kv_shape* s, const tactic_query_shape* q
   const int64_t behind = L.cur;
   p.part_o = p.plan.splits > 1 ? L.take(rows * p.plan.splits * kHeadDim * 4) : 0;
   p.part_ml = p.plan.splits > 1 ? L.take(rows * p.plan.splits * 8) : 0;
+  p.items = L.take(p.plan.tiles * 16);
+  p.counts = L.take(p.plan.tiles * 4);
+  p.order = L.take(p.plan.tiles * 16);
   Layout W;
   W.cur = behind;
   // key tiles of 256 rows: the queries are split until there are eight workgroups for
@@ -177,6 +180,14 @@ tactic_status prompt_impl(const uint16_t* q, const uint16_t* K, const uint16_t* 
   hipError_t e = hipSuccess;
   if (a.documents)
     e = tactic::launch_doc_range(a.documents, a.kv_indptr, a.seq_len, a.n_src, p.range_stride, reinterpret_cast<int2*>(ws + p.ranges), stream);
+  // Documents give row tiles of any length in any order: with more than three for each
+  // compute unit the long ones are started first (two small kernels, 7 us)
+  if (e == hipSuccess && a.documents && p.plan.tiles * a.Hkv * a.splits > 3 * 256) {
+    int4* order = reinterpret_cast<int4*>(ws + p.order);
+    e = tactic::launch_item_order(a, p.plan.variant, (int)p.plan.tiles, reinterpret_cast<int4*>(ws + p.items),
+                                  reinterpret_cast<int32_t*>(ws + p.counts), order, stream);
+    a.order = order;
+  }
   if (e == hipSuccess) e = tactic::launch_rows_attn(a, p.plan.variant, false, p.plan.tiles * a.Hkv * a.splits, stream);
   if (e == hipSuccess && !a.direct) e = tactic::launch_rows_combine(a, stream);
   if (e != hipSuccess) return hip_fail(e, "prompt attention launch");

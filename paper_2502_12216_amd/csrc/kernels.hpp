@@ -169,6 +169,7 @@ struct RowsArgs {
   const int32_t* prefix_len;    // [n_src] or null (mode 0)
   const int2* doc_range;        // [n_src][range_stride]: documents of each 64-row tile
   int64_t range_stride;
+  const int4* order;            // row tiles in the order to start them, or null: tile, source, range of its queries' documents
   PagedKV pk;
   float* part_o;                // [splits][n_queries * Hq][128]
   float* part_ml;               // [splits][n_queries * Hq][2]: reference maximum (base 2), sum
@@ -251,6 +252,8 @@ struct JoinArgs {
 int rows_per_item(int variant);
 hipError_t launch_doc_range(const int32_t* documents, const int64_t* kv_indptr, const int64_t* seq_len, int batch,
                             int64_t max_tiles, int2* out, hipStream_t st);
+hipError_t launch_item_order(const RowsArgs& a, int variant, int tiles, int4* items, int32_t* counts, int4* order,
+                             hipStream_t st);
 hipError_t launch_rows_attn(const RowsArgs& a, int variant, bool exact_weights, int64_t items, hipStream_t st);
 hipError_t launch_rows_combine(const RowsArgs& a, hipStream_t st);
 

@@ -103,6 +103,40 @@ __device__ __forceinline__ int page_row(const PagedKV& pk, int shift, int Hkv, i
 constexpr float kMaxFinite = 3.402823466e38f;  // a score of +inf: the sum becomes inf (its logarithm too), the output NaN
 constexpr float kRescaleSlack = 8.f;  // base-2: a weight may exceed 1 by 2^8 before the sums are rescaled
 
+// Source of row tile `rest`: the tiles of source b start at floor(rows before it / rows)
+// + b at the latest.  A lane per candidate, 64 at a time: one load where there are few.
+__device__ __forceinline__ int source_of(const RowsArgs& a, int rows, int rest, int lane) {
+  int src = 0;
+  for (int count = a.n_src; count > 1;) {
+    const int step = (count + 63) / 64, mid = src + lane * step;
+    bool ok = lane * step < count;
+    if (ok) {
+      const int64_t before = a.mode == 0 ? a.q_indptr[mid] : (int64_t)a.member_indptr[mid];
+      ok = before * a.G / rows + mid <= rest;
+    }
+    const int at = ((int)__popcll(__ballot(ok)) - 1) * step;  // (candidate 0 always is)
+    src += at;
+    count = min(step, count - at);
+  }
+  return src;
+}
+// Range of the documents of tokens [p0, p1] of a sequence, from those of its 64-token
+// tiles (at most 5 of them), the same in all lanes.  Empty where p1 < 0.
+__device__ __forceinline__ int2 docs_of(const int2* dr, int p0, int p1, int lane) {
+  int lo = INT32_MAX, hi = INT32_MIN;
+  if (p1 >= 0 && p0 / 64 + lane <= p1 / 64) {
+    const int2 r = dr[p0 / 64 + lane];
+    lo = r.x;
+    hi = r.y;
+  }
+#pragma unroll
+  for (int s = 1; s < 8; s <<= 1) {
+    lo = min(lo, __shfl_xor(lo, s, 64));
+    hi = max(hi, __shfl_xor(hi, s, 64));
+  }
+  return make_int2(__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readfirstlane(hi));
+}
+
 template <int RW, int KW, int TK, int PARTS, bool kPaged, bool kDocs>
 __global__ __launch_bounds__(RW * KW * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void rows_attn_kernel(RowsArgs a) {
@@ -124,19 +158,16 @@ void rows_attn_kernel(RowsArgs a) {
   int rest = blockIdx.x / a.Hkv;
   const int split = rest % a.splits;
   rest /= a.splits;
-  // the source: tiles of source b start at floor(rows before it / ROWS) + b at the
-  // latest, a lane per candidate (64 at a time: one load where there are few)
-  int src = 0;
-  for (int count = a.n_src; count > 1;) {
-    const int step = (count + 63) / 64, mid = src + lane * step;
-    bool ok = lane * step < count;
-    if (ok) {
-      const int64_t before = a.mode == 0 ? a.q_indptr[mid] : (int64_t)a.member_indptr[mid];
-      ok = before * a.G / ROWS + mid <= rest;
-    }
-    const int at = ((int)__popcll(__ballot(ok)) - 1) * step;  // (candidate 0 always is)
-    src += at;
-    count = min(step, count - at);
+  int src, i_lo = INT32_MAX, i_hi = INT32_MIN;  // and the documents of the item's queries
+  const bool ordered = kDocs && a.order;
+  if (ordered) {
+    const int4 item = a.order[rest];
+    rest = item.x;
+    src = item.y;
+    i_lo = item.z;
+    i_hi = item.w;
+  } else {
+    src = source_of(a, ROWS, rest, lane);
   }
   const int64_t q0 = a.mode == 0 ? a.q_indptr[src] : (int64_t)a.member_indptr[src];
   const int64_t q1 = a.mode == 0 ? a.q_indptr[src + 1] : (int64_t)a.member_indptr[src + 1];
@@ -206,25 +237,15 @@ void rows_attn_kernel(RowsArgs a) {
   // 64 tiles at a time, into masks of the tiles that may hold a seen key, of those whose
   // keys all are of the wave's one document, and of those where that holds for the item.
   const int2* dr = kDocs ? a.doc_range + (int64_t)src * a.range_stride : nullptr;
-  int i_lo = INT32_MAX, i_hi = INT32_MIN, win = INT32_MIN;
+  int win = INT32_MIN;
   uint64_t w_some = 0, w_same = 0, w_sure = 0;
   const int d_one = __builtin_amdgcn_readfirstlane(qdoc);
   const bool one_doc = __all(qdoc == d_one);
-  if constexpr (kDocs) {
+  if (kDocs && !ordered) {
     const int64_t m = q1 - q0;
-    const int p0 = max((int)(n - m + row0 / a.G), 0), p1 = (int)(n - m + (min(row0 + ROWS, nrows) - 1) / a.G);
-    if (p1 >= 0 && p0 / 64 + lane <= p1 / 64) {  // (at most 5 tiles)
-      const int2 r = dr[p0 / 64 + lane];
-      i_lo = r.x;
-      i_hi = r.y;
-    }
-#pragma unroll
-    for (int s = 1; s < 8; s <<= 1) {
-      i_lo = min(i_lo, __shfl_xor(i_lo, s, 64));
-      i_hi = max(i_hi, __shfl_xor(i_hi, s, 64));
-    }
-    i_lo = __builtin_amdgcn_readfirstlane(i_lo);
-    i_hi = __builtin_amdgcn_readfirstlane(i_hi);
+    const int2 r = docs_of(dr, max((int)(n - m + row0 / a.G), 0), (int)(n - m + (min(row0 + ROWS, nrows) - 1) / a.G), lane);
+    i_lo = r.x;
+    i_hi = r.y;
   }
   auto look = [&](int t) __attribute__((always_inline)) {
     if (t >= win && t < win + 64) return;
@@ -813,6 +834,83 @@ __global__ __launch_bounds__(64) void doc_range_kernel(const int32_t* documents,
   if (threadIdx.x == 0) out[b * stride + t] = make_int2(lo, hi);
 }
 
+// Key tiles (of 64) that each row tile's queries may see: what its documents leave of
+// them.  A wave per row tile.
+__global__ __launch_bounds__(256) void doc_items_kernel(RowsArgs a, int rows, int tiles, int4* items, int32_t* counts) {
+  const int lane = threadIdx.x & 63, rest = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (rest >= tiles) return;
+  const int src = source_of(a, rows, rest, lane);
+  const int64_t q0 = a.q_indptr[src], m = a.q_indptr[src + 1] - q0;
+  const int nrows = (int)(m * a.G), ntile = (nrows + rows - 1) / rows;
+  const int tile = ntile - 1 - (rest - (int)(q0 * a.G / rows) - src);  // (as in rows_attn_kernel)
+  int count = 0;
+  int2 own = make_int2(INT32_MAX, INT32_MIN);
+  if (tile >= 0 && tile < ntile) {
+    const int n = (int)seq_tokens(a.kv_indptr, a.seq_len, src);
+    const int2* dr = a.doc_range + (int64_t)src * a.range_stride;
+    const int p0 = max((int)(n - m + tile * rows / a.G), 0), p1 = (int)(n - m + (min(tile * rows + rows, nrows) - 1) / a.G);
+    own = docs_of(dr, p0, p1, lane);
+    const int kend = p1 < 0 ? 0 : min(max(p1 + 1, a.prefix_len ? a.prefix_len[src] : 0), n), kt = (kend + 63) / 64;
+    for (int t = lane; t < kt; t += 64) {
+      const int2 r = dr[t];
+      count += r.x <= own.y && r.y >= own.x;
+    }
+  }
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) count += __shfl_xor(count, s, 64);
+  if (lane == 0) {
+    items[rest] = make_int4(rest, src, own.x, own.y);
+    counts[rest] = count;
+  }
+}
+// The row tiles by falling count, in 32 steps of the largest, in their own order within
+// a step: long ones started last would end after all others (documents of 100 to 8000
+// tokens: the last fifth of the time had idle units), and neighbours share their keys in
+// L2.  One workgroup, a wave for two steps.
+__global__ __launch_bounds__(1024) void item_order_kernel(const int4* items, const int32_t* counts, int tiles, int4* order) {
+  constexpr int kHeld = 8192;  // counts of the first tiles, read again by every wave
+  __shared__ int s_most[16], s_count[32], s_held[kHeld];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int most = 1;
+  for (int t = threadIdx.x; t < tiles; t += 1024) {
+    const int c = counts[t];
+    if (t < kHeld) s_held[t] = c;
+    most = max(most, c);
+  }
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) most = max(most, __shfl_xor(most, s, 64));
+  if (lane == 0) s_most[wave] = most;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 16; ++w) most = max(most, s_most[w]);
+  const float inv = 1.f / (float)most;
+  auto step_of = [&](int t) __attribute__((always_inline)) -> int {  // 0: the longest; -1: none
+    return t < tiles ? 31 - (int)((float)(t < kHeld ? s_held[t] : counts[t]) * 31.f * inv) : -1;
+  };
+  int n0 = 0, n1 = 0;
+  for (int t = 0; t < tiles; t += 64) {
+    const int s = step_of(t + lane);
+    n0 += __popcll(__ballot(s == 2 * wave));
+    n1 += __popcll(__ballot(s == 2 * wave + 1));
+  }
+  if (lane == 0) {
+    s_count[2 * wave] = n0;
+    s_count[2 * wave + 1] = n1;
+  }
+  __syncthreads();
+  int at0 = 0;
+  for (int s = 0; s < 2 * wave; ++s) at0 += s_count[s];
+  int at1 = at0 + n0;
+  for (int t = 0; t < tiles; t += 64) {
+    const int s = step_of(t + lane);
+    const uint64_t in0 = __ballot(s == 2 * wave), in1 = __ballot(s == 2 * wave + 1), before = (1ull << lane) - 1;
+    if (s == 2 * wave) order[at0 + __popcll(in0 & before)] = items[t + lane];
+    if (s == 2 * wave + 1) order[at1 + __popcll(in1 & before)] = items[t + lane];
+    at0 += __popcll(in0);
+    at1 += __popcll(in1);
+  }
+}
+
 // Joins the splits of a row: out = sum_s O_s 2^(m_s - M) / sum_s l_s 2^(m_s - M).  One
 // wave per row: lane s has split s's maximum and sum, so that M and the sum of the
 // weights are wave reductions (in one order); then two dimensions per lane, eight
@@ -856,6 +954,13 @@ hipError_t launch_doc_range(const int32_t* documents, const int64_t* kv_indptr, 
   if (max_tiles == 0) return hipSuccess;
   hipLaunchKernelGGL(doc_range_kernel, dim3((unsigned)max_tiles, batch), dim3(64), 0, st, documents, kv_indptr, seq_len,
                      max_tiles, out);
+  return hipGetLastError();
+}
+
+hipError_t launch_item_order(const RowsArgs& a, int variant, int tiles, int4* items, int32_t* counts, int4* order,
+                             hipStream_t st) {
+  hipLaunchKernelGGL(doc_items_kernel, dim3((tiles + 3) / 4), dim3(256), 0, st, a, rows_per_item(variant), tiles, items, counts);
+  hipLaunchKernelGGL(item_order_kernel, dim3(1), dim3(1024), 0, st, items, counts, tiles, order);
   return hipGetLastError();
 }
 

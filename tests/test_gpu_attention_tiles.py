@@ -41,6 +41,17 @@ def test_prompt_row_tiles_with_values_that_are_not_finite(lens, new, hq, hkv):
     check_prompt(lens, new, hq, hkv, docs=25, spoil=spoil)
 
 
+@pytest.mark.parametrize("lens,new,hq,hkv,docs", [
+    ([120] * 60, [120] * 60, 32, 8, 30), ([3400, 3, 2900], [3400, 3, 2900], 32, 8, 300), ([40, 0] * 40, [42, 1] * 40, 32, 8, 20),
+])
+@pytest.mark.parametrize("kw", [dict(), dict(prefix=True, page=16), dict(spare=3, alibi=True, cap=9.0)])
+def test_prompt_of_many_documents(lens, new, hq, hkv, docs, kw):
+    """Enough row tiles that the long ones are started first."""
+    if "prefix" in kw:
+        kw = dict(kw, prefix=[(37 * b) % 200 for b in range(len(lens))])
+    check_prompt(lens, new, hq, hkv, docs=docs, **kw)
+
+
 @pytest.mark.parametrize("new", [200, 64, 5, 1])
 @pytest.mark.parametrize("rows", [slice(0, 1), slice(0, 64), slice(64, 128), slice(96, 128), slice(0, 200)])
 def test_prompt_tiles_of_nan_keys(new, rows):
