@@ -187,8 +187,10 @@ class EvictingCache:
         """q[b] bf16 [n_b][Hq][128], K[b], V[b] bf16 [Hkv][n_b][128] in token order.  Returns the prompts'
         attention, bf16 [sum n_b][Hq][128]."""
         lens = [int(k.shape[1]) for k in K]
-        if len(lens) != self.batch.batch:
+        if not len(lens) == len(q) == len(V) == self.batch.batch:
             raise ValueError("prefill needs a prompt for every sequence")
+        if [int(x.shape[0]) for x in q] != lens or [int(x.shape[1]) for x in V] != lens:
+            raise ValueError("a prompt's q, K and V must be of one length")
         full = RaggedBatch(lens, self.Hq, self.Hkv, device=self.device)
         Kc, Vc, qc = torch.cat(list(K), 1).contiguous(), torch.cat(list(V), 1).contiguous(), torch.cat(list(q)).contiguous()
         prompt = PromptAttention(full, lens)
@@ -204,6 +206,11 @@ class EvictingCache:
     def append(self, k: torch.Tensor, v: torch.Tensor) -> torch.Tensor:
         """k, v bf16 [B][Hkv][128], the new token of every sequence.  Only device work is enqueued.  Returns
         the rows int32 [B][Hkv] that they went to."""
+        if not k.shape == v.shape == (self.batch.batch, self.Hkv, 128):  # (before anything is changed)
+            raise ValueError(f"k and v must be [{self.batch.batch}][{self.Hkv}][128]")
+        if not (k.is_contiguous() and v.is_contiguous() and k.dtype == v.dtype == torch.bfloat16 and
+                k.device == v.device == self.K.device):
+            raise ValueError(f"k and v must be contiguous bfloat16 tensors on {self.K.device}")
         self.newest += 1
         rows = self.inserter(k, v, self.K, self.V, self.weights, self.positions, self.newest)
         self._set_lens([n + 1 for n in self.batch.seq_lens])

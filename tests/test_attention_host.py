@@ -169,3 +169,28 @@ def test_python_refusals():
         dec(q, kv, kv)
     with pytest.raises(TypeError, match="bfloat16"):
         dec(q.float(), kv.float(), kv)
+
+
+def test_evicting_cache_refuses_before_it_changes():
+    """Prompts whose q, K and V differ in length, and tokens of another shape or type, leave the cache as it was."""
+    import paper_2502_12216_amd as T
+    c = T.EvictingCache(8, 2, 2, 16, recent=4, device="cpu")
+
+    def kv(n):
+        return torch.zeros(2, n, 128, dtype=torch.bfloat16)
+
+    def q(n):
+        return torch.zeros(n, 8, 128, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="every sequence"):
+        c.prefill([q(3)], [kv(3), kv(5)], [kv(3), kv(5)])
+    with pytest.raises(ValueError, match="one length"):
+        c.prefill([q(5), q(3)], [kv(3), kv(5)], [kv(3), kv(5)])
+    with pytest.raises(ValueError, match="one length"):
+        c.prefill([q(3), q(5)], [kv(3), kv(5)], [kv(5), kv(3)])
+    k = torch.zeros(2, 2, 128, dtype=torch.bfloat16)
+    for bad in (k[:1], k.float(), k.transpose(0, 1), torch.zeros(2, 3, 128, dtype=torch.bfloat16)):
+        with pytest.raises(ValueError):
+            c.append(bad, bad)
+        with pytest.raises(ValueError):
+            c.append(k, bad)
+    assert c.newest.tolist() == [-1, -1] and c.batch.seq_lens == [0, 0]
