@@ -97,6 +97,17 @@ struct PromptLayout {
   int64_t wpart;
 };
 
+// Splits of the query rows of tactic_prompt_weights, of which a sequence has at most
+// `rows` for a KV head.  Key tiles have 256 rows: the queries are split until there are
+// eight workgroups for each of the 512 places (an early key is seen by more queries than
+// a late one, so that they are of many lengths), of at least eight tiles of 64 rows each;
+// or of two such tiles until there is one for each place.
+int weight_splits(const tactic_kv_shape* s, int64_t rows) {
+  const int64_t items = std::max<int64_t>(1, (s->total_tokens + 255) / 256) * s->n_kv_heads;
+  const int64_t many = std::min<int64_t>(4096 / items, rows / 512), few = std::min<int64_t>(512 / items, rows / 128);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::max(many, few), kMaxSplits));
+}
+
 PromptLayout prompt_layout(const tactic_kv_shape* s, const tactic_query_shape* q) {
   PromptLayout p;
   const int G = s->n_q_heads / s->n_kv_heads;
@@ -115,12 +126,7 @@ PromptLayout prompt_layout(const tactic_kv_shape* s, const tactic_query_shape* q
   p.order = L.take(p.plan.tiles * 16);
   Layout W;
   W.cur = behind;
-  // key tiles of 256 rows: the queries are split until there are eight workgroups for
-  // each of the 512 places (an early key is seen by more queries than a late one, so
-  // that they are of many lengths), of at least eight row tiles each
-  const int64_t items = std::max<int64_t>(1, (s->total_tokens + 255) / 256) * s->n_kv_heads;
-  const int64_t most = std::max<int64_t>(1, q->max_queries * G / 512);
-  p.wsplits = (int)std::max<int64_t>(1, std::min<int64_t>({4096 / items, most, (int64_t)kMaxSplits}));
+  p.wsplits = weight_splits(s, q->max_queries * G);
   p.wpart = p.wsplits > 1 ? W.take((int64_t)p.wsplits * s->n_kv_heads * s->total_tokens * 4) : 0;
   p.bytes = std::max<int64_t>(256, std::max(L.cur, W.cur));
   return p;
@@ -432,7 +438,7 @@ tactic_status tactic_prompt_weights(const uint16_t* q, const uint16_t* K, const 
   a.Hq = shape->n_q_heads;
   a.Hkv = shape->n_kv_heads;
   a.G = a.Hq / a.Hkv;
-  a.splits = p.wsplits;
+  a.splits = weight_splits(shape, (window > 0 ? std::min(window, (int64_t)queries->max_queries) : queries->max_queries) * a.G);
   a.total = shape->total_tokens;
   a.n_queries = queries->total_queries;
   a.window = window;

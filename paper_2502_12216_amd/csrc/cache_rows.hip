@@ -23,7 +23,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 // where the products take four; the cap adds five); with few queries by reading K.
 // Four waves that run free, two workgroups to a compute unit: eight that take turns at
 // the products, as the attention's do, are slower where the vector unit has more to do
-// (8192 queries, 32 heads on 8, capped: 590 us against 500; not capped 393 against 391).
+// (8192 queries, 32 heads on 8, capped: 590 us against 500; not capped 393 against 391; both before rows of NaN were looked for, 2%).
 // grid (key tiles + sequences, Hkv, splits of the rows)
 // ---------------------------------------------------------------------------
 constexpr int kWKeys = 256, kWRows = 64;
@@ -35,6 +35,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
   // end of the keys it sees, its document
   __shared__ __align__(16) float s_lse[2][kWRows], s_slope[2][kWRows], s_pos[2][kWRows];
   __shared__ __align__(16) int s_lim[2][kWRows], s_doc[2][kDocs ? kWRows : 4];
+  __shared__ uint64_t s_nan[2];  // rows whose logarithm is NaN
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
   const int tid = threadIdx.x, g = blockIdx.y, split = blockIdx.z;
   int lo = 0, hi = a.B - 1;  // key tiles of sequence b start at floor(rows before it / 256) + b
@@ -122,7 +123,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
       const int pos = n - m + i;
       const float l = a.lse[(int64_t)h * a.n_queries + q0 + i];
       // a row past the end, and one whose sum says that it saw nothing, gives no weight
-      lse_r = x < rows && l != -INFINITY ? l * kLog2e : INFINITY;
+      lse_r = x < rows && l != -INFINITY ? l * kLog2e : INFINITY;  // (NaN stays)
       slope_r = biased ? a.slopes[h] * kLog2e / scale : 0.f;
       pos_r = (float)(pos - k0);
       lim_r = min(max(pos + 1, pre), n) - k0;
@@ -133,7 +134,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
 #pragma unroll
     for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x4*>(s_q[buf] + ((wave * 4 + i) * 64 + lane) * 16) = qreg[i];
     if (tid < kWRows) {
-      s_lse[buf][tid] = lse_r;
+      const uint64_t nan_rows = __ballot(lse_r != lse_r);
+      if (tid == 0) s_nan[buf] = nan_rows;
+      s_lse[buf][tid] = lse_r != lse_r ? 0.f : lse_r;
       s_slope[buf][tid] = slope_r;
       s_pos[buf][tid] = pos_r;
       s_lim[buf][tid] = lim_r;
@@ -151,6 +154,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
   while (t < t_hi) {
     const int tn = next_tile(t + 1);
     if (tn < t_hi) fetch(tn);
+    if (__builtin_amdgcn_readfirstlane((int)(s_nan[buf] != 0))) {
+      // rare: such a row gives NaN to the keys it sees, by its scores, which the masks leave out
+      if (tid < kWRows && (s_nan[buf] >> tid & 1)) *reinterpret_cast<uint32_t*>(s_q[buf] + tid * 256) = 0x7fff7fffu;
+      __syncthreads();
+    }
     // the first token of the tile sees the fewest keys
     const int lim0 = min(max(n - m + i0 + ((t * kWRows) >> lg) + 1, pre), n);
     const bool masked = kDocs || k0 + wave * 64 + 64 > lim0;

@@ -203,3 +203,31 @@ def test_insert_beyond_two_to_the_31_elements():
         assert int(rows[0, g]) == 0 and int(rows[1, g]) == at - n
         assert torch.equal(K[g, 0], k[0, g]) and torch.equal(K[g, at], k[1, g]) and torch.equal(V[g, at], v[1, g])
         assert int(p[g, at]) == n + 50 and float(w[g, at]) == 0.0
+
+
+@pytest.mark.parametrize("docs", [0, 70])
+@pytest.mark.parametrize("window", [0, 260])
+def test_weights_of_nan_rows_reach_the_keys_they_see(docs, window):
+    """A query that is NaN gives NaN to the keys it sees, of its KV head, and leaves the others' sums."""
+    import paper_2502_12216_amd as T
+    n, hq, hkv = 300, 8, 2
+    batch = _batch([n], hq, hkv)
+    K, V, q = _randn(1, hkv, n, 128), _randn(2, hkv, n, 128), _randn(3, n, hq, 128)
+    document = torch.arange(n, dtype=torch.int32, device=DEV) // docs if docs else None
+    mod = T.ScoreMod(documents=document)
+    att = T.PromptAttention(batch, [n])
+    results = []
+    for spoil in (False, True):
+        if spoil:
+            q[50, 1], q[210, 6] = float("nan"), float("nan")
+        _, lse = att(q, K, V, mod)
+        assert bool(torch.isnan(lse).any()) == spoil
+        results.append(att.add_weights(q, K, lse, torch.zeros(hkv, n, device=DEV), mod, window=window).clone())
+    torch.cuda.synchronize()
+    clean, got = results
+    seen = torch.zeros(hkv, n, dtype=torch.bool, device=DEV)
+    for g, i in ((0, 50), (1, 210)):
+        if window == 0 or i >= n - window:
+            seen[g, (i // docs * docs if docs else 0):i + 1] = True
+    assert torch.equal(torch.isnan(got), seen)
+    assert torch.equal(got[~seen], clean[~seen])
