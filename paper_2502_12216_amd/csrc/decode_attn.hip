@@ -276,8 +276,10 @@ void attn_splitk_kernel(AttnArgs a, std::conditional_t<kMod != 0, TokenMod, NoMo
   __shared__ int s_wmax[4];
 
   // kMod: what is the same for all lanes though it came from LDS or a division goes to
-  // scalar registers, which the rules' own registers need (G = 4 had spilled 19: ragged
-  // sequences of 1 to 77777 tokens, 148609 in all, 8 KV heads: 128 us, 107 without a rule)
+  // scalar registers, which the rules' own registers need.  G = 4 has two waves per SIMD
+  // as well, not three, where 19 registers were spilled (ragged sequences of 1 to 77777
+  // tokens, 148609 in all, 8 KV heads, cap and slopes: 128 us, now 107 with 256 registers,
+  // and 107 without a rule: the reads of K and V at 5.7 TB/s)
   auto uniform = [](auto x) __attribute__((always_inline)) {
     if constexpr (kMod == 0) return x;
     else if constexpr (sizeof(x) == 4) return __builtin_bit_cast(decltype(x), __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
@@ -975,7 +977,8 @@ hipError_t launch_join(const AttnArgs& a, const JoinArgs& j, int G, hipStream_t 
 
 // The running sums of attention weights: a thread per cached row and KV head, four
 // rows each, adds its group's 2^(s - M) / L (s from the decode, M and 1 / L from the
-// combine).  grid (rows / 1024, Hkv, B).  Reads 4 G bytes and writes 4 of each row.
+// combine).  grid (rows / 1024, Hkv, B).  Reads 4 G bytes and writes 4 of each row, bound
+// by its one round of loads (16 sequences of 2048 rows, 8 KV heads: 4.0 us).
 template <int G>
 __global__ __launch_bounds__(256) void add_weights_kernel(const float* scores, const float* norm, const int64_t* kv_indptr,
                                                           const int64_t* seq_len, int64_t total, float* weights) {

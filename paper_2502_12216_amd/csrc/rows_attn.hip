@@ -12,8 +12,12 @@
 // their order is free as long as V^T has the same, and the transposing LDS read
 // (ds_read_b64_tr_b16) gives four consecutive keys of one dimension, which is the
 // order the accumulators of S^T have.  KW groups of waves take every KW-th tile
-// and are merged at the end; with more items than keys the ranges are split and
-// joined by rows_combine_kernel, in a fixed order.
+// and are merged at the end; where there are few items their keys are split and
+// joined by rows_combine_kernel (the shared prefix by combine_kernel), in a fixed order.
+//
+// Weights go to the matrix unit as bf16 where the output is bf16 (half a step of
+// each, 2^-8, as the output's own rounding; sums in 32 bits), in three parts that hold
+// all 24 bits where it is fp32.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -137,6 +141,17 @@ __device__ __forceinline__ int2 docs_of(const int2* dr, int p0, int p1, int lane
   return make_int2(__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readfirstlane(hi));
 }
 
+// RW waves hold 32 rows each and share a tile of keys, KW such groups take turns at the
+// tiles.  The host takes 32, 64, 128 or 256 rows to an item by an estimate of the time
+// (plan_rows, with the measurements).  Bound by the matrix unit where a prompt is long:
+// 16384 tokens, 32 heads on 8, take 2060 to 2140 us (1.03 to 1.07 PFLOP/s; a library
+// product of 8192^3 reaches 1.11), 2250 to 2320 with slopes, 2480 to 2540 with a cap, whose polynomial
+// competes with the exponential for the vector unit.  512 tokens on 65536 in pages, with
+// slopes: 609 us, 0.90 PFLOP/s.  Packed documents (29193 tokens, 1100 on average, cap):
+// 800 us, 0.60, bound by each item's start and end (12 of 84 us: the chain from the item's
+// record to the first keys, the waves' last turn) and by tiles that are masked in part.  A prefix of 32768 tokens and 32
+// sequences: 47 us, by the matrix unit (the weights' three parts make the products twice as
+// many) and HBM (2.9 TB/s) together.
 template <int RW, int KW, int TK, int PARTS, bool kPaged, bool kDocs>
 __global__ __launch_bounds__(RW * KW * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void rows_attn_kernel(RowsArgs a) {
@@ -866,7 +881,8 @@ __global__ __launch_bounds__(256) void doc_items_kernel(RowsArgs a, int rows, in
 // The row tiles by falling count, in 32 steps of the largest, in their own order within
 // a step: long ones started last would end after all others (documents of 100 to 8000
 // tokens: the last fifth of the time had idle units), and neighbours share their keys in
-// L2.  One workgroup, a wave for two steps.
+// L2.  One workgroup, a wave for two steps, the counts in LDS (460 row tiles: 9 us,
+// bound by its chain; doc_items_kernel 5).
 __global__ __launch_bounds__(1024) void item_order_kernel(const int4* items, const int32_t* counts, int tiles, int4* order) {
   constexpr int kHeld = 8192;  // counts of the first tiles, read again by every wave
   __shared__ int s_most[16], s_count[32], s_held[kHeld];
