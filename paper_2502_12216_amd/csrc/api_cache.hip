@@ -17,6 +17,7 @@ namespace {
 
 constexpr int64_t kMaxInt = ((int64_t)1 << 31) - 1;
 constexpr int kMaxRecent = 1 << 22;
+constexpr int64_t kSliceFrom = 16384, kSliceGroups = 32;
 
 tactic_status check_mod(const tactic_score_mod* m) {
   if (m && !(m->cap >= 0.f && m->cap < INFINITY)) return fail(TACTIC_ERR_INVALID_ARG, "cap must be 0 or positive and finite");
@@ -324,6 +325,25 @@ SharedLayout shared_layout(const tactic_kv_shape* s, const tactic_prefixes* p) {
   return l;
 }
 
+struct EvictLayout {
+  bool sliced;
+  int64_t counts, chosen, ahead, bytes;
+};
+EvictLayout evict_layout(const tactic_kv_shape* s, int64_t out_total) {
+  EvictLayout l{};
+  const int64_t groups = (int64_t)s->batch * s->n_kv_heads;
+  l.sliced = s->max_seq_len > kSliceFrom && groups <= kSliceGroups;
+  Layout L;
+  L.take(out_total * s->n_kv_heads * 4);
+  if (l.sliced) {
+    l.counts = L.take(3 * groups * tactic::kEvictSlices * tactic::kEvictBins * 4);
+    l.chosen = L.take(2 * groups * 8);
+    l.ahead = L.take(2 * groups * tactic::kEvictSlices * 4);
+  }
+  l.bytes = std::max<int64_t>(256, L.cur);
+  return l;
+}
+
 tactic_status shared_impl(const uint16_t* q, const uint16_t* Kp, const uint16_t* Vp, const tactic::PagedKV* pkp,
                           const uint16_t* K, const uint16_t* V, const tactic::PagedKV* pk,
                           const tactic_kv_shape* shape, const tactic_prefixes* pre, const tactic_score_mod* mod,
@@ -523,7 +543,7 @@ tactic_status tactic_shared_decode_paged(const uint16_t* q, const tactic_paged_k
 
 size_t tactic_evict_workspace_size(const tactic_kv_shape* shape, int64_t out_total) {
   if (check_shape(shape) != TACTIC_OK || out_total < 0) return 0;
-  return (size_t)std::max<int64_t>(256, align_up(out_total * shape->n_kv_heads * 4, 256));
+  return (size_t)evict_layout(shape, out_total).bytes;
 }
 
 tactic_status tactic_evict(const uint16_t* K, const uint16_t* V, const tactic_kv_shape* shape, const float* weights,
@@ -565,7 +585,14 @@ tactic_status tactic_evict(const uint16_t* K, const uint16_t* V, const tactic_kv
   a.weights_out = weights_out;
   a.positions_out = positions_out;
   a.out_len = out_len;
-  a.rows = static_cast<int32_t*>(workspace);
+  const EvictLayout l = evict_layout(shape, out_total);
+  char* ws = static_cast<char*>(workspace);
+  a.rows = reinterpret_cast<int32_t*>(ws);
+  if (l.sliced) {
+    a.counts = reinterpret_cast<uint32_t*>(ws + l.counts);
+    a.chosen = reinterpret_cast<uint2*>(ws + l.chosen);
+    a.ahead = reinterpret_cast<uint32_t*>(ws + l.ahead);
+  }
   const hipError_t e = tactic::launch_evict(a, shape->max_seq_len, std::min(out_max, shape->max_seq_len), stream);
   if (e != hipSuccess) return hip_fail(e, "evict launch");
   return TACTIC_OK;

@@ -314,6 +314,50 @@ struct __attribute__((packed, aligned(4))) Four {  // 16 bytes at any 4-byte pla
   uint32_t v[4];
 };
 
+// Keys of rows r .. r + 3.  Past the end 0, the least: fewer than n rows are kept and the
+// lower row goes first, so that no such row ever is.
+__device__ __forceinline__ void rank_keys(const float* w, const int32_t* pos, int n, int newest, int recent, int64_t r,
+                                          uint32_t (&k)[4]) {
+  if (r + 4 <= n) {
+    const Four x = *reinterpret_cast<const Four*>(w + r);
+    Four p = {{0, 0, 0, 0}};
+    if (pos) p = *reinterpret_cast<const Four*>(pos + r);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) k[e] = rank_key(__uint_as_float(x.v[e]), pos ? (int)p.v[e] : (int)r + e, newest, recent);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) k[e] = r + e < n ? rank_key(w[r + e], pos ? pos[r + e] : (int)r + e, newest, recent) : 0u;
+  }
+}
+// Adds one to the count of `bin` in LDS.  Lanes of one bin take turns, so that those of
+// the first lane's bin are counted at once (one workgroup on 65536 + 30011 equal rows, 8 KV
+// heads: 80 us a call so, half of it the copy, 229 with one atomic per row; power law 72, 78).
+__device__ __forceinline__ void count_key(uint32_t* hist, bool in, uint32_t bin, int lane) {
+  const uint64_t left = __ballot(in);
+  if (left == 0) return;
+  const int lead = __ffsll((unsigned long long)left) - 1;
+  const uint32_t of = (uint32_t)__builtin_amdgcn_readlane((int)bin, lead);
+  const uint64_t same = __ballot(in && bin == of);
+  const uint32_t add = lane == lead ? (uint32_t)__popcll(same) : 1u;
+  if (in && (lane == lead || bin != of)) atomicAdd(&hist[bin], add);
+}
+// Sum of one value per thread over the threads before it (1024 of them), and of all.
+__device__ __forceinline__ uint32_t scan_1024(uint32_t* s_sum, uint32_t x, int lane, int wave, uint32_t* all) {
+  const uint32_t incl = (uint32_t)wave_incl_scan((int)x);
+  if (lane == kWave - 1) s_sum[wave] = incl;
+  __syncthreads();
+  uint32_t before = 0, total = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const uint32_t v = s_sum[i];
+    before += i < wave ? v : 0;
+    total += v;
+  }
+  __syncthreads();
+  if (all) *all = total;
+  return before + incl - x;
+}
+
 // One workgroup per (KV head, sequence) finds the kept rows: the key of the last kept
 // one digit by digit (11, 11 and 10 bits), then the kept rows in ascending order.
 // Thread t holds rows 4 (1024 j + t) + e, e < 4, j < J, as keys in registers, so that
@@ -341,19 +385,8 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
     for (int r = tid; r < n; r += 1024) rows[r] = r;
     return;
   }
-  // the keys of rows r .. r + 3.  Past the end 0, the least: fewer than n rows are kept
-  // and the lower row goes first, so that no such row ever is.
   auto keys_at = [&](int64_t r, uint32_t (&k)[4]) __attribute__((always_inline)) {
-    if (r + 4 <= n) {
-      const Four x = *reinterpret_cast<const Four*>(w + r);
-      Four p = {{0, 0, 0, 0}};
-      if (pos) p = *reinterpret_cast<const Four*>(pos + r);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) k[e] = rank_key(__uint_as_float(x.v[e]), pos ? (int)p.v[e] : (int)r + e, newest, a.recent);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) k[e] = r + e < n ? rank_key(w[r + e], pos ? pos[r + e] : (int)r + e, newest, a.recent) : 0u;
-    }
+    rank_keys(w, pos, n, newest, a.recent, r, k);
   };
   const int steps = (int)(((int64_t)n + 4095) / 4096);  // of 4096 rows
   uint32_t held[kHeld][4];
@@ -361,18 +394,7 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
 #pragma unroll
     for (int j = 0; j < J; ++j) keys_at((int64_t)j * 4096 + tid * 4, held[j]);
   }
-  // Adds one to the count of `bin`.  Lanes of one bin take turns, so that those of the
-  // first lane's bin are counted at once (a call on 65536 + 30011 equal rows, 8 KV
-  // heads, half of it the copy: 80 us so, 229 with one atomic per row; power law 72, 78).
-  auto count = [&](bool in, uint32_t bin) __attribute__((always_inline)) {
-    const uint64_t left = __ballot(in);
-    if (left == 0) return;
-    const int lead = __ffsll((unsigned long long)left) - 1;
-    const uint32_t of = (uint32_t)__builtin_amdgcn_readlane((int)bin, lead);
-    const uint64_t same = __ballot(in && bin == of);
-    const uint32_t add = lane == lead ? (uint32_t)__popcll(same) : 1u;
-    if (in && (lane == lead || bin != of)) atomicAdd(&s_hist[bin], add);
-  };
+  auto count = [&](bool in, uint32_t bin) __attribute__((always_inline)) { count_key(s_hist, in, bin, lane); };
   // f(row, its four keys) for every step of the thread's rows
   auto each = [&](auto f) __attribute__((always_inline)) {
     if constexpr (J > 0) {
@@ -387,22 +409,7 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
       }
     }
   };
-  // sum of one value per thread over the threads before it, and of all
-  auto scan = [&](uint32_t x, uint32_t* all) __attribute__((always_inline)) -> uint32_t {
-    const uint32_t incl = (uint32_t)wave_incl_scan((int)x);
-    if (lane == kWave - 1) s_sum[wave] = incl;
-    __syncthreads();
-    uint32_t before = 0, total = 0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const uint32_t v = s_sum[i];
-      before += i < wave ? v : 0;
-      total += v;
-    }
-    __syncthreads();
-    if (all) *all = total;
-    return before + incl - x;
-  };
+  auto scan = [&](uint32_t x, uint32_t* all) __attribute__((always_inline)) { return scan_1024(s_sum, x, lane, wave, all); };
   uint32_t prefix = 0, need = (uint32_t)keep;
 #pragma unroll
   for (int pass = 0; pass < 3; ++pass) {
@@ -522,6 +529,135 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
   });
 }
 
+// The same by several workgroups for a (KV head, sequence), each with a slice of the rows,
+// in four launches: launch P < 3 counts digit P of the slice's keys that have the digits
+// found so far, launch P > 0 first adds the slices' counts of digit P - 1 and finds it, all
+// of them alike, and what of it lies in the slices before.  The last one places the rows.
+// grid (slices, Hkv, B)
+template <int P>
+__global__ __launch_bounds__(1024) void evict_slice_kernel(EvictArgs a) {
+  __shared__ uint32_t s_hist[kEvictBins];
+  __shared__ uint32_t s_sum[16], s_ahead[16];
+  __shared__ uint32_t s_prefix, s_need, s_same, s_before;
+  const int slice = blockIdx.x, g = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t kvb = a.kv_indptr[b], outb = a.out_indptr[b];
+  const int n = (int)seq_tokens(a.kv_indptr, a.seq_len, b);
+  const int64_t room = a.out_indptr[b + 1] - outb;
+  const int keep = (int)min((int64_t)n, min(max((int64_t)a.keep[b], (int64_t)0), room));
+  if (P == 3 && slice == 0 && g == 0 && tid == 0) a.out_len[b] = keep;
+  const int steps = (int)(((int64_t)n + 4096 * kEvictSlices - 1) / (4096 * kEvictSlices));  // of 4096 rows
+  const int64_t r0 = (int64_t)slice * steps * 4096, r1 = min(r0 + (int64_t)steps * 4096, (int64_t)n);
+  if (keep == 0 || r0 >= n) return;
+  int32_t* rows = a.rows + (int64_t)g * a.out_total + outb;
+  if (keep == n) {
+    if (P == 3)
+      for (int64_t r = r0 + tid; r < r1; r += 1024) rows[r] = (int32_t)r;
+    return;
+  }
+  const int newest = a.newest ? a.newest[b] : n - 1;
+  const float* w = a.weights + (int64_t)g * a.total + kvb;
+  const int32_t* pos = a.positions ? a.positions + (int64_t)g * a.total + kvb : nullptr;
+  const int64_t groups = (int64_t)a.B * a.Hkv, group = (int64_t)b * a.Hkv + g;
+  auto counts_of = [&](int pass, int s) __attribute__((always_inline)) {
+    return a.counts + (((int64_t)pass * groups + group) * kEvictSlices + s) * kEvictBins;
+  };
+  uint32_t prefix = 0, need = (uint32_t)keep, ahead = 0, eq_ahead = 0;
+  bool ties = false;
+  if constexpr (P > 0) {
+    constexpr int shift = P == 1 ? 21 : (P == 2 ? 10 : 0);
+    if constexpr (P > 1) {
+      const uint2 c = a.chosen[(P - 2) * groups + group];
+      prefix = c.x;
+      need = c.y;
+      ahead = a.ahead[((P - 2) * groups + group) * kEvictSlices + slice];
+    }
+    const int used = (int)(((int64_t)n + (int64_t)steps * 4096 - 1) / ((int64_t)steps * 4096));
+    // two counts per thread from the top: of all slices, and of those before this one
+    uint32_t c0 = 0, c1 = 0, m0 = 0, m1 = 0;
+    uint2 c[kEvictSlices];
+#pragma unroll
+    for (int s = 0; s < kEvictSlices; ++s)
+      c[s] = s < used ? *reinterpret_cast<const uint2*>(counts_of(P - 1, s) + kEvictBins - 2 - 2 * tid) : make_uint2(0, 0);
+#pragma unroll
+    for (int s = 0; s < kEvictSlices; ++s) {
+      c0 += c[s].y;
+      c1 += c[s].x;
+      m0 += s < slice ? c[s].y : 0;
+      m1 += s < slice ? c[s].x : 0;
+    }
+    const uint32_t before = scan_1024(s_sum, c0 + c1, lane, wave, nullptr);
+    const bool mine = before < need && need <= before + c0 + c1, second = need > before + c0;
+    if (mine) {
+      s_prefix = prefix | ((uint32_t)(kEvictBins - 1 - 2 * tid - (second ? 1 : 0)) << shift);
+      s_need = need - before - (second ? c0 : 0);
+      s_same = second ? c1 : c0;
+      s_before = second ? m1 : m0;
+    }
+    // rows of larger digits in the slices before: whole threads before the digit's, and its first count
+    uint32_t larger = before + c0 + c1 < need ? m0 + m1 : (mine && second ? m0 : 0);
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) larger += __shfl_xor(larger, s, 64);
+    if (lane == 0) s_ahead[wave] = larger;
+    __syncthreads();
+    prefix = s_prefix;
+    need = s_need;
+    ties = s_same != need;
+    eq_ahead = s_before;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) ahead += s_ahead[i];
+    if (P < 3 && tid == 0) {
+      a.ahead[((P - 1) * groups + group) * kEvictSlices + slice] = ahead;
+      if (slice == 0) a.chosen[(P - 1) * groups + group] = make_uint2(prefix, need);
+    }
+  }
+  if constexpr (P < 3) {
+    constexpr int shift = P == 0 ? 21 : (P == 1 ? 10 : 0), bits = P == 2 ? 10 : 11;
+    s_hist[tid] = 0;
+    s_hist[tid + 1024] = 0;
+    __syncthreads();
+    for (int64_t r = r0 + tid * 4; r < r0 + (int64_t)steps * 4096; r += 4096) {
+      uint32_t k[4];
+      rank_keys(w, pos, n, newest, a.recent, r, k);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        count_key(s_hist, P == 0 || (k[e] >> (shift + bits)) == (prefix >> (shift + bits)), (k[e] >> shift) & ((1u << bits) - 1), lane);
+    }
+    __syncthreads();
+    *reinterpret_cast<uint2*>(counts_of(P, slice) + 2 * tid) = make_uint2(s_hist[2 * tid], s_hist[2 * tid + 1]);
+  } else {
+    // rows above the key stay, and the first `need` of those of exactly that key
+    uint32_t at0 = ahead + min(eq_ahead, need), eq0 = eq_ahead;
+    for (int64_t r = r0 + tid * 4; r < r0 + (int64_t)steps * 4096; r += 4096) {
+      uint32_t k[4], kept = 0, eq = 0, all;
+      rank_keys(w, pos, n, newest, a.recent, r, k);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        kept |= (uint32_t)(k[e] > prefix) << e;
+        eq |= (uint32_t)(k[e] == prefix) << e;
+      }
+      if (ties) {
+        uint32_t rank = eq0 + scan_1024(s_sum, __popc(eq), lane, wave, &all);
+        eq0 += all;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          kept |= (uint32_t)((eq >> e & 1) && rank < need) << e;
+          rank += eq >> e & 1;
+        }
+      } else {
+        kept |= eq;
+      }
+      uint32_t at = at0 + scan_1024(s_sum, __popc(kept), lane, wave, &all);
+      at0 += all;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (kept >> e & 1) {
+          if (at < (uint32_t)keep) rows[at] = (int32_t)(r + e);
+          ++at;
+        }
+    }
+  }
+}
+
 // Copies the kept rows: 16 lanes per row, K and V.  grid (rows / 64, Hkv, B).  Bound by
 // HBM, the read rows being 256 bytes each (23884 rows x 8 heads, 196 MB read and written:
 // 35 us, 5.6 TB/s).
@@ -549,8 +685,13 @@ __global__ __launch_bounds__(256) void evict_gather_kernel(EvictArgs a) {
 }
 
 hipError_t launch_evict(const EvictArgs& a, int64_t max_len, int64_t max_out, hipStream_t st) {
-  const dim3 grid(a.Hkv, a.B);
-  if (max_len <= 4096) hipLaunchKernelGGL(evict_select_kernel<1>, grid, dim3(1024), 0, st, a);
+  const dim3 grid(a.Hkv, a.B), slices(kEvictSlices, a.Hkv, a.B);
+  if (a.counts) {
+    hipLaunchKernelGGL(evict_slice_kernel<0>, slices, dim3(1024), 0, st, a);
+    hipLaunchKernelGGL(evict_slice_kernel<1>, slices, dim3(1024), 0, st, a);
+    hipLaunchKernelGGL(evict_slice_kernel<2>, slices, dim3(1024), 0, st, a);
+    hipLaunchKernelGGL(evict_slice_kernel<3>, slices, dim3(1024), 0, st, a);
+  } else if (max_len <= 4096) hipLaunchKernelGGL(evict_select_kernel<1>, grid, dim3(1024), 0, st, a);
   else if (max_len <= 16384) hipLaunchKernelGGL(evict_select_kernel<4>, grid, dim3(1024), 0, st, a);
   else if (max_len <= 65536) hipLaunchKernelGGL(evict_select_kernel<16>, grid, dim3(1024), 0, st, a);
   else hipLaunchKernelGGL(evict_select_kernel<0>, grid, dim3(1024), 0, st, a);

@@ -217,7 +217,12 @@ struct EvictArgs {
   int32_t* positions_out;
   int64_t* out_len;             // [B]
   int32_t* rows;                // [Hkv][out_total] workspace: the kept rows
+  // workspace where a sequence's rows are shared by kEvictSlices workgroups, else null
+  uint32_t* counts;             // [3][B * Hkv][kEvictSlices][2048]
+  uint2* chosen;                // [2][B * Hkv]: key so far, rows needed of it
+  uint32_t* ahead;              // [2][B * Hkv][kEvictSlices]: rows above it in the slices before
 };
+constexpr int kEvictSlices = 16, kEvictBins = 2048;
 struct InsertArgs {
   const uint16_t* k;            // [B][Hkv][128]
   const uint16_t* v;

@@ -253,3 +253,15 @@ def test_evicting_cache_step_captured_and_replayed():
         assert torch.equal(out, ref), step
         for a, b in zip(state, (eager.K, eager.V, eager.weights, eager.positions, eager.newest, eager.batch.seq_len)):
             assert torch.equal(a, b), step
+
+
+@pytest.mark.parametrize("values", ["pareto", "few", "odd"])
+@pytest.mark.parametrize("lens,keep,room,recent,spare", [
+    ([70000, 16385, 0, 5, 4096], [20000, 4000, 3, 3, 4096], [20000, 4000, 3, 5, 4096], 300, 0),  # several workgroups each
+    ([131072, 65537], [131071, 1], [131071, 1], 0, 7),
+    ([40000], [39999], [39999], 39000, 0),
+    ([17000] + [100] * 10, [4000] + [99] * 10, [4000] + [99] * 10, 64, 0),      # many sequences: one workgroup each
+    ([66000] + [90] * 10, [9000] + [50] * 10, [9000] + [50] * 10, 64, 3),
+])
+def test_evict_long_sequences(values, lens, keep, room, recent, spare):
+    test_evict(values, lens, keep, room, recent, spare)
