@@ -17,7 +17,6 @@ namespace {
 
 constexpr int64_t kMaxInt = ((int64_t)1 << 31) - 1;
 constexpr int kMaxRecent = 1 << 22;
-constexpr int64_t kSliceFrom = 16384, kSliceGroups = 32;
 
 tactic_status check_mod(const tactic_score_mod* m) {
   if (m && !(m->cap >= 0.f && m->cap < INFINITY)) return fail(TACTIC_ERR_INVALID_ARG, "cap must be 0 or positive and finite");
@@ -325,6 +324,14 @@ SharedLayout shared_layout(const tactic_kv_shape* s, const tactic_prefixes* p) {
   return l;
 }
 
+// Sequences' rows are ranked by one workgroup for each KV head, or by 16 in four launches,
+// which add up each other's counts: that pays where the one works long and few units are
+// busy otherwise.  One against 16, us a call, 8 KV heads, an eighth kept, weights by a power law
+// (three values): 24000 rows 29 (40) and 29 (31); 4 x 24000 40 (52) and 50 (53); 65536 + 30011
+// 72 (99) and 63 (66); 4 x 65536 84 (114) and 89 (93); past 65536 rows the one makes
+// its keys again in every pass: 131072 122 and 42; 4 x 131072 232 and 162; 8 x 348 and 315.
+bool evict_sliced(int64_t max_len, int64_t groups) { return groups <= (max_len > 65536 ? 64 : 16) && max_len > 16384; }
+
 struct EvictLayout {
   bool sliced;
   int64_t counts, chosen, ahead, bytes;
@@ -332,7 +339,7 @@ struct EvictLayout {
 EvictLayout evict_layout(const tactic_kv_shape* s, int64_t out_total) {
   EvictLayout l{};
   const int64_t groups = (int64_t)s->batch * s->n_kv_heads;
-  l.sliced = s->max_seq_len > kSliceFrom && groups <= kSliceGroups;
+  l.sliced = evict_sliced(s->max_seq_len, groups);
   Layout L;
   L.take(out_total * s->n_kv_heads * 4);
   if (l.sliced) {

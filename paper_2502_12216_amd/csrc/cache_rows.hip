@@ -533,6 +533,7 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
 // in four launches: launch P < 3 counts digit P of the slice's keys that have the digits
 // found so far, launch P > 0 first adds the slices' counts of digit P - 1 and finds it, all
 // of them alike, and what of it lies in the slices before.  The last one places the rows.
+// Bound by the launches' chains, each 5 to 8 us (16 slices' counts are 128 KB to read).
 // grid (slices, Hkv, B)
 template <int P>
 __global__ __launch_bounds__(1024) void evict_slice_kernel(EvictArgs a) {

@@ -262,6 +262,7 @@ def test_evicting_cache_step_captured_and_replayed():
     ([40000], [39999], [39999], 39000, 0),
     ([17000] + [100] * 10, [4000] + [99] * 10, [4000] + [99] * 10, 64, 0),      # many sequences: one workgroup each
     ([66000] + [90] * 10, [9000] + [50] * 10, [9000] + [50] * 10, 64, 3),
+    ([66000] + [9] * 22, [9000] + [5] * 22, [9000] + [5] * 22, 64, 3),
 ])
 def test_evict_long_sequences(values, lens, keep, room, recent, spare):
     test_evict(values, lens, keep, room, recent, spare)
