@@ -231,3 +231,56 @@ def test_weights_of_nan_rows_reach_the_keys_they_see(docs, window):
             seen[g, (i // docs * docs if docs else 0):i + 1] = True
     assert torch.equal(torch.isnan(got), seen)
     assert torch.equal(got[~seen], clean[~seen])
+
+
+def test_graphs_that_share_a_workspace():
+    """Prompts with documents (ranges, order and splits in the workspace), weights and an eviction, captured in two
+    graphs over one workspace and replayed in turn, with eager work between."""
+    import paper_2502_12216_amd as T
+    runs = []
+    ws = None
+    for lens, new, docs in (([3400, 300, 2900], [3400, 300, 2900], 250), ([20000], [64], 9000)):
+        batch = _batch(lens, 32, 8)
+        ws = torch.empty(2 ** 28, dtype=torch.uint8, device=DEV) if ws is None else ws
+        att = T.PromptAttention(batch, new, workspace=ws)
+        assert att.workspace is ws
+        q, K, V = (_randn(i, n, h, 128) for i, n, h in ((1, sum(new), 32), (2, 8, batch.total), (3, 8, batch.total)))
+        mod = T.ScoreMod(cap=30.0, documents=(torch.arange(batch.total, device=DEV) // docs).int())
+        dest = T.RaggedBatch([0] * len(lens), 32, 8, capacities=[100] * len(lens))
+        ev = T.CacheEvictor(batch, dest, 10)
+        assert ws.numel() >= ev.workspace.numel()
+        ev.workspace = ws
+        sums, keep = torch.zeros(8, batch.total, device=DEV), torch.full((len(lens),), 100, dtype=torch.int32, device=DEV)
+        outs = [torch.zeros(8, dest.total, 128, dtype=torch.bfloat16, device=DEV) for _ in range(2)] + \
+            [torch.zeros(8, dest.total, device=DEV), torch.zeros(8, dest.total, dtype=torch.int32, device=DEV)]
+
+        def step(att=att, q=q, K=K, V=V, mod=mod, ev=ev, sums=sums, keep=keep, outs=outs):
+            out, lse = att(q, K, V, mod)
+            sums.zero_()
+            att.add_weights(q, K, lse, sums, mod, window=50)
+            ev(K, V, sums, keep, *outs)
+            return [out, lse, sums] + outs
+        runs.append((step, q))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for step, _ in runs:
+            step()
+    torch.cuda.current_stream().wait_stream(side)
+    graphs = []
+    for step, q in runs:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            kept = step()
+        graphs.append((graph, kept, q, step))
+    for turn in range(4):
+        for i, (graph, kept, q, step) in enumerate(graphs):
+            q.copy_(_randn(100 + 10 * turn + i, *q.shape))
+            want = [x.clone() for x in step()]
+            for x in kept:
+                x.zero_()
+            ws.random_(0, 255)
+            graph.replay()
+            torch.cuda.synchronize()
+            for x, y in zip(kept, want):
+                assert torch.equal(x, y), (turn, i)
