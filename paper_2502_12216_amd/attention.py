@@ -302,6 +302,8 @@ class CacheEvictor:
             raise ValueError("dest must have the same sequences and KV heads")
         if dest.seq_len is None:
             raise ValueError("dest needs capacities")
+        if dest.seq_len is batch.seq_len:
+            raise ValueError("dest must be another batch: its lengths are set while the batch's are read")
         self.batch, self.dest, self.recent = batch, dest, int(recent)
         self._shape = batch.struct()
         name = "tactic_evict_workspace_size"

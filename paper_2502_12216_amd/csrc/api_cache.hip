@@ -566,6 +566,7 @@ tactic_status tactic_evict(const uint16_t* K, const uint16_t* V, const tactic_kv
     return fail(TACTIC_ERR_INVALID_ARG, "null argument");
   if (K && (K == K_out || V == V_out || weights == weights_out || (positions && positions == positions_out)))
     return fail(TACTIC_ERR_INVALID_ARG, "the outputs must not be the inputs");
+  if (out_len == shape->seq_len) return fail(TACTIC_ERR_INVALID_ARG, "out_len must not be the shape's seq_len");
   if (recent < 0 || recent > kMaxRecent) return fail(TACTIC_ERR_INVALID_ARG, "recent must be in [0, 2^22]");
   if (out_total < 0 || out_max < 0 || out_max > out_total)
     return fail(TACTIC_ERR_INVALID_ARG, "inconsistent out_total / out_max");

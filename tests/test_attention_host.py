@@ -194,3 +194,12 @@ def test_evicting_cache_refuses_before_it_changes():
         with pytest.raises(ValueError):
             c.append(k, bad)
     assert c.newest.tolist() == [-1, -1] and c.batch.seq_lens == [0, 0]
+
+
+def test_evict_refuses_lengths_it_reads_while_it_writes_them():
+    import paper_2502_12216_amd as T
+    assert evict(shape=_shape(lens=FAKE), lens=FAKE) == 1
+    assert b"seq_len" in C.lib().tactic_last_error()
+    batch = T.RaggedBatch([3, 5], 2, 2, device="cpu", capacities=[8, 8])
+    with pytest.raises(ValueError, match="another batch"):
+        T.CacheEvictor(batch, batch, 0)
