@@ -241,13 +241,12 @@ hipError_t launch_tokens(tactic::AttnArgs& aa, const tactic::TokenMod& m, bool p
 }
 
 struct ScoredLayout {
-  int64_t norm, scores, bytes;
+  int64_t scores, bytes;
 };
 ScoredLayout scored_layout(const tactic_kv_shape* s, bool weights) {
   ScoredLayout p;
   Layout L;
   L.take((int64_t)dense_workspace_bytes(s, tactic::kMaxAttnGrid));
-  p.norm = L.take((int64_t)s->batch * s->n_q_heads * 8);
   p.scores = weights ? L.take(s->total_tokens * s->n_q_heads * 4) : 0;
   p.bytes = L.cur;
   return p;
@@ -284,12 +283,15 @@ tactic_status scored_impl(const uint16_t* q, const uint16_t* K, const uint16_t* 
   m.scores = weights ? reinterpret_cast<float*>(ws + p.scores) : nullptr;
   tactic::JoinArgs j{};
   j.lse = lse;
-  j.norm = weights ? reinterpret_cast<float*>(ws + p.norm) : nullptr;
+  if (weights && shape->max_seq_len > 0) {
+    j.scores = m.scores;
+    j.weights = weights;
+    j.chunks = (int)std::min<int64_t>((shape->max_seq_len + 2047) / 2048, 4096);
+  }
   j.rows = (int64_t)shape->batch * shape->n_q_heads;
   const int G = aa.Hq / aa.Hkv;
   hipError_t e = launch_tokens(aa, m, pk != nullptr, stream);
   if (e == hipSuccess) e = tactic::launch_join(aa, j, G, stream);
-  if (e == hipSuccess && weights) e = tactic::launch_add_weights(aa, m.scores, j.norm, shape->max_seq_len, weights, G, stream);
   if (e != hipSuccess) return hip_fail(e, "scored decode launch");
   return TACTIC_OK;
 }

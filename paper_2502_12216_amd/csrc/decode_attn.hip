@@ -791,8 +791,69 @@ void attn_splitk_kernel(AttnArgs a, std::conditional_t<kMod != 0, TokenMod, NoMo
 // scheduling.  Groups without tokens get zeros.
 //
 // kMore: the splits of a shared prefix join behind the group's own partials, and
-// the logarithm of the sum and the row's (maximum, 1 / sum) are written too; a row
-// that sees nothing gets zeros and -inf.
+// the logarithm of the sum is written too; a row that sees nothing gets zeros and -inf.
+// Workgroups y >= G add this step's attention weights to the running sums.
+// (16 sequences of 2048 rows, 32 heads on 8: 4.8 us, with the sums 5.0, where a launch
+// of their own behind this one took 4.0.)
+
+// Adds 2^(s - M) / L, summed over the group's heads, to the sums of the cached rows of
+// group bg: s from the attention, M and L from its partials, a wave for each head, in
+// the meantime of the loads of four rows per thread.  Reads 4 G bytes and writes 4 of
+// each row.
+template <int G>
+__device__ void add_weights(const AttnArgs& a, const JoinArgs& more, int bg, const float* pb, int np, float* s_norm) {
+  constexpr int kPart = G * (kHeadDim + 2);
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, b = bg / a.NV, g = bg % a.NV;
+  const int64_t n = seq_tokens(a.kv_indptr, a.seq_len, b), base = (int64_t)g * a.total + a.kv_indptr[b];
+  int64_t r0 = (int64_t)(blockIdx.y - G) * 2048;
+  if (r0 >= n) return;
+  float s[4][G], w[4];
+  auto load = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t at = base + min(r0 + 512 * i + tid, n - 1);  // (rows past the end repeat the last and are not stored)
+      w[i] = more.weights[at];
+#pragma unroll
+      for (int h = 0; h < G; ++h) s[i][h] = more.scores[at * G + h];
+    }
+  };
+  load();
+  if (wave < G) {
+    float m = -INFINITY;
+    for (int c = lane; c < np; c += kWave) m = fmaxf(m, pb[(int64_t)c * kPart + G * kHeadDim + wave]);
+    m = wave_allmax_f(m);
+    float l = 0.f;
+    for (int c = lane; c < np; c += kWave) {
+      const float mc = pb[(int64_t)c * kPart + G * kHeadDim + wave], lc = pb[(int64_t)c * kPart + G * kHeadDim + G + wave];
+      if (mc != -INFINITY) l = fmaf(lc, fast_exp2(mc - m), l);
+    }
+    l = wave_allsum_f(l);
+    if (lane == 0) {
+      s_norm[2 * wave] = m;
+      s_norm[2 * wave + 1] = m == -INFINITY ? 0.f : 1.f / l;
+    }
+  }
+  __syncthreads();
+  float M[G], inv[G];
+#pragma unroll
+  for (int h = 0; h < G; ++h) {
+    M[h] = s_norm[2 * h];
+    inv[h] = s_norm[2 * h + 1];
+  }
+  for (;;) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float x = 0.f;
+#pragma unroll
+      for (int h = 0; h < G; ++h) x = s[i][h] != -INFINITY ? fmaf(fast_exp2(s[i][h] - M[h]), inv[h], x) : x;
+      if (r0 + 512 * i + tid < n) more.weights[base + r0 + 512 * i + tid] = w[i] + x;
+    }
+    r0 += (int64_t)more.chunks * 2048;
+    if (r0 >= n) return;
+    load();
+  }
+}
+
 template <int G, bool kMore>
 __global__ __launch_bounds__(512) void combine_kernel(AttnArgs a, std::conditional_t<kMore, JoinArgs, NoMod> more) {
   constexpr int kPart = G * (kHeadDim + 2);
@@ -823,6 +884,12 @@ __global__ __launch_bounds__(512) void combine_kernel(AttnArgs a, std::condition
     if (more.prefix_of && more.prefix_of[b] >= 0) npre = more.pre_splits;
   }
   const float* pb = a.partials + (bg + w0) * kPart;
+  if constexpr (kMore) {
+    if (blockIdx.y >= G) {
+      add_weights<G>(a, more, bg, pb, np, s_w);
+      return;
+    }
+  }
   const float* pd = pb + h * kHeadDim + d;  // this thread's output dimension of partial 0
   constexpr int kPre = 8;                   // numerator loads issued before the reductions
   float pre[kPre];
@@ -893,10 +960,6 @@ __global__ __launch_bounds__(512) void combine_kernel(AttnArgs a, std::condition
       out[d] = empty ? 0.f : sum / dd;
       if (d == 0) {
         if (more.lse) more.lse[row] = empty ? -INFINITY : (M + __builtin_amdgcn_logf(dd)) * kLn2;
-        if (more.norm) {
-          more.norm[2 * row] = M;
-          more.norm[2 * row + 1] = empty ? 0.f : 1.f / dd;
-        }
       }
     } else {
       out[d] = sum / dd;
@@ -961,7 +1024,8 @@ hipError_t attn_resident_grid(int G, int n_groups, bool paged, int* grid, int* c
 
 template <bool kMore, typename More>
 static hipError_t launch_combine_t(const AttnArgs& a, const More& m, int G, hipStream_t st) {
-  const dim3 grid(a.B * a.NV, G);
+  dim3 grid(a.B * a.NV, G);
+  if constexpr (kMore) grid.y += m.weights ? m.chunks : 0;
   switch (G) {
     case 1: hipLaunchKernelGGL((combine_kernel<1, kMore>), grid, dim3(512), 0, st, a, m); break;
     case 2: hipLaunchKernelGGL((combine_kernel<2, kMore>), grid, dim3(512), 0, st, a, m); break;
@@ -974,54 +1038,5 @@ static hipError_t launch_combine_t(const AttnArgs& a, const More& m, int G, hipS
 
 hipError_t launch_combine(const AttnArgs& a, int G, hipStream_t st) { return launch_combine_t<false>(a, NoMod{}, G, st); }
 hipError_t launch_join(const AttnArgs& a, const JoinArgs& j, int G, hipStream_t st) { return launch_combine_t<true>(a, j, G, st); }
-
-// The running sums of attention weights: a thread per cached row and KV head, four
-// rows each, adds its group's 2^(s - M) / L (s from the decode, M and 1 / L from the
-// combine).  grid (rows / 1024, Hkv, B).  Reads 4 G bytes and writes 4 of each row, bound
-// by its one round of loads (16 sequences of 2048 rows, 8 KV heads: 4.0 us).
-template <int G>
-__global__ __launch_bounds__(256) void add_weights_kernel(const float* scores, const float* norm, const int64_t* kv_indptr,
-                                                          const int64_t* seq_len, int64_t total, float* weights) {
-  const int g = blockIdx.y, b = blockIdx.z, Hkv = gridDim.y;
-  const int64_t n = seq_tokens(kv_indptr, seq_len, b), r0 = (int64_t)blockIdx.x * 1024 + threadIdx.x;
-  if (r0 >= n) return;
-  const int64_t base = (int64_t)g * total + kv_indptr[b];
-  const float* nm = norm + 2 * (((int64_t)b * Hkv + g) * G);
-  float s[4][G], w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int64_t at = base + min(r0 + 256 * i, n - 1);  // (rows past the end repeat the last and are not stored)
-    w[i] = weights[at];
-#pragma unroll
-    for (int h = 0; h < G; ++h) s[i][h] = scores[at * G + h];
-  }
-  float M[G], inv[G];
-#pragma unroll
-  for (int h = 0; h < G; ++h) {
-    M[h] = nm[2 * h];
-    inv[h] = nm[2 * h + 1];
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float x = 0.f;
-#pragma unroll
-    for (int h = 0; h < G; ++h) x = s[i][h] != -INFINITY ? fmaf(fast_exp2(s[i][h] - M[h]), inv[h], x) : x;
-    if (r0 + 256 * i < n) weights[base + r0 + 256 * i] = w[i] + x;
-  }
-}
-
-hipError_t launch_add_weights(const AttnArgs& a, const float* scores, const float* norm, int64_t max_len, float* weights,
-                              int G, hipStream_t st) {
-  if (max_len == 0) return hipSuccess;
-  const dim3 grid((unsigned)((max_len + 1023) / 1024), a.Hkv, a.B);
-  switch (G) {
-    case 1: hipLaunchKernelGGL(add_weights_kernel<1>, grid, dim3(256), 0, st, scores, norm, a.kv_indptr, a.seq_len, a.total, weights); break;
-    case 2: hipLaunchKernelGGL(add_weights_kernel<2>, grid, dim3(256), 0, st, scores, norm, a.kv_indptr, a.seq_len, a.total, weights); break;
-    case 4: hipLaunchKernelGGL(add_weights_kernel<4>, grid, dim3(256), 0, st, scores, norm, a.kv_indptr, a.seq_len, a.total, weights); break;
-    case 8: hipLaunchKernelGGL(add_weights_kernel<8>, grid, dim3(256), 0, st, scores, norm, a.kv_indptr, a.seq_len, a.total, weights); break;
-    default: return hipErrorInvalidValue;
-  }
-  return hipGetLastError();
-}
 
 }  // namespace tactic

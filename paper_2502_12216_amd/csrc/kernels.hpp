@@ -245,12 +245,14 @@ hipError_t launch_insert(const InsertArgs& a, hipStream_t st);
 constexpr int kMaxSplits = 64;  // splits of a row tile's keys
 struct JoinArgs {
   float* lse;                   // [B][Hq] or null
-  float* norm;                  // [B][Hq][2] or null: maximum (base 2), 1 / sum
   const float* pre_o;           // [pre_splits][rows][128]
   const float* pre_ml;          // [pre_splits][rows][2]
   const int32_t* prefix_of;     // [B] or null: negative for a sequence without a prefix
   int pre_splits;
   int64_t rows;                 // B * Hq
+  const float* scores;          // [Hkv][total][G] of the rows, and their running sums [Hkv][total], or null
+  float* weights;
+  int chunks;                   // workgroups of each group for the sums
 };
 
 // variants 0 to 3: 32, 64, 128 or 256 rows per item
@@ -271,8 +273,6 @@ hipError_t launch_combine(const AttnArgs& a, int G, hipStream_t st);
 hipError_t attn_resident_grid(int G, int n_groups, bool paged, int* grid, int* compute_units = nullptr, int mod = 0);
 hipError_t launch_attn_mod(const AttnArgs& a, const TokenMod& m, int G, int grid, bool paged, hipStream_t st);
 hipError_t launch_join(const AttnArgs& a, const JoinArgs& j, int G, hipStream_t st);
-hipError_t launch_add_weights(const AttnArgs& a, const float* scores, const float* norm, int64_t max_len, float* weights,
-                              int G, hipStream_t st);
 hipError_t launch_stream_read(const void* buf, int64_t n16, int workgroups, uint32_t* sink, hipStream_t st);
 
 }  // namespace tactic
