@@ -266,3 +266,35 @@ def test_evicting_cache_step_captured_and_replayed():
 ])
 def test_evict_long_sequences(values, lens, keep, room, recent, spare):
     test_evict(values, lens, keep, room, recent, spare)
+
+
+@pytest.mark.parametrize("hkv", [1, 3, 5, 16, 20])
+@pytest.mark.parametrize("caps,lens", [([40, 300, 0, 7], [40, 299, 0, 7]), ([9000, 5], [9000, 2]), ([5000, 4097], [5000, 4097])])
+def test_insert_heads_and_lengths(hkv, caps, lens):
+    """Heads that do not divide the waves, and caches on both sides of the one-launch limit: two tokens, ties included."""
+    import paper_2502_12216_amd as T
+    B = len(caps)
+    _, K, V, w, pos = _cache_inputs(caps, hkv, 31, 0, "few")
+    batch = T.RaggedBatch(lens, hkv, hkv, capacities=caps)
+    ins = T.TokenInserter(batch, 3)
+    wt, pt = torch.as_tensor(w, device=DEV), torch.as_tensor(pos, device=DEV)
+    for step in range(2):
+        k, v = _randn(70 + step, B, hkv, 128), _randn(80 + step, B, hkv, 128)
+        newest = np.array([2 * c + step for c in caps], np.int32)
+        now, w0, p0 = batch.seq_len.tolist(), wt.cpu().numpy().copy(), pt.cpu().numpy().copy()
+        K0, V0 = K.clone(), V.clone()
+        rows = ins(k, v, K, V, wt, pt, torch.as_tensor(newest, device=DEV)).tolist()
+        torch.cuda.synchronize()
+        for b in range(B):
+            s, n = int(batch.kv_indptr_host[b]), now[b]
+            for g in range(hkv):
+                if caps[b] == 0:
+                    assert rows[b][g] == -1
+                    continue
+                want = n if n < caps[b] else int(R.ranking(w0[g, s:s + n], p0[g, s:s + n], newest[b], 3)[-1])
+                assert rows[b][g] == want, (step, b, g)
+                K0[g, s + want], V0[g, s + want] = k[b, g], v[b, g]
+                w0[g, s + want], p0[g, s + want] = 0.0, newest[b]
+        assert torch.equal(K, K0) and torch.equal(V, V0)
+        assert np.array_equal(wt.cpu().numpy(), w0) and np.array_equal(pt.cpu().numpy(), p0)
+        assert batch.seq_len.tolist() == [min(n + 1, c) for n, c in zip(now, caps)]
