@@ -632,7 +632,7 @@ tactic_status tactic_insert_token(const uint16_t* k, const uint16_t* v, const in
   a.recent = recent;
   a.total = shape->total_tokens;
   a.rows = rows;
-  const hipError_t e = tactic::launch_insert(a, stream);
+  const hipError_t e = tactic::launch_insert(a, shape->max_seq_len, stream);
   if (e != hipSuccess) return hip_fail(e, "insert launch");
   return TACTIC_OK;
 }

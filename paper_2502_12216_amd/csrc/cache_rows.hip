@@ -706,13 +706,30 @@ hipError_t launch_evict(const EvictArgs& a, int64_t max_len, int64_t max_out, hi
 
 // ---------------------------------------------------------------------------
 // One token per sequence: behind the last row while there is room, else in the
-// place of the row that ranks last.  One workgroup per (KV head, sequence), so that a
-// thread reads a few rows' 8 bytes; bound by its chain of loads, reduction and stores (16
-// full sequences of 2048 rows, 8 KV heads: 5.5 us, and 1.4 for the lengths, which wait
-// for every head).
+// place of the row that ranks last.  One workgroup per (KV head, sequence), a thread for
+// four rows at a time; bound by its chain of loads, reduction and stores (full caches of
+// 4 x 16384 rows, 8 KV heads: 7.9 us with the launch that sets the lengths, which waits
+// for every head; with one row at a time and 256 threads 20).
 // ---------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void insert_token_kernel(InsertArgs a) {
-  __shared__ uint64_t s_min[4];
+// Lowest key of rows [0, n), with the highest row of it among equal ones, over the
+// threads whose four-row pieces start at `first`, `step` rows apart: (key, ~row).
+__device__ __forceinline__ uint64_t least_row(const InsertArgs& a, int64_t base, int n, int newest, int64_t first, int step) {
+  uint64_t best = ~0ull;
+#pragma unroll 2
+  for (int64_t r = first; r < n; r += step) {
+    uint32_t k[4];
+    rank_keys(a.weights + base, a.positions + base, n, newest, a.recent, r, k);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (r + e < n) best = min(best, ((uint64_t)k[e] << 32) | (uint32_t)~(uint32_t)(r + e));
+  }
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) best = min(best, (uint64_t)__shfl_xor((unsigned long long)best, s, 64));
+  return best;
+}
+
+__global__ __launch_bounds__(1024) void insert_token_kernel(InsertArgs a) {
+  __shared__ uint64_t s_min[16];
   const int g = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t kvb = a.kv_indptr[b], span = a.kv_indptr[b + 1] - kvb;
   const int n = (int)seq_tokens(a.kv_indptr, a.seq_len, b);
@@ -723,17 +740,11 @@ __global__ __launch_bounds__(256) void insert_token_kernel(InsertArgs a) {
     return;
   }
   if (n >= span) {
-    const int newest = a.newest[b];
-    uint64_t best = ~0ull;  // lowest key, among equal ones the highest row
-    for (int r = tid; r < n; r += 256) {
-      const uint64_t k = rank_key(a.weights[base + r], a.positions[base + r], newest, a.recent);
-      best = min(best, (k << 32) | (uint32_t)~r);
-    }
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) best = min(best, (uint64_t)__shfl_xor((unsigned long long)best, s, 64));
+    uint64_t best = least_row(a, base, n, a.newest[b], tid * 4, 4096);
     if (lane == 0) s_min[wave] = best;
     __syncthreads();
-    best = min(min(s_min[0], s_min[1]), min(s_min[2], s_min[3]));
+#pragma unroll
+    for (int i = 0; i < 16; ++i) best = min(best, s_min[i]);
     row = (int64_t)(uint32_t)~(uint32_t)best;
   }
   const int64_t from = ((int64_t)b * a.Hkv + g) * kHeadDim, to = (base + row) * kHeadDim;
@@ -754,8 +765,43 @@ __global__ __launch_bounds__(256) void advance_lengths_kernel(InsertArgs a) {
   }
 }
 
-hipError_t launch_insert(const InsertArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL(insert_token_kernel, dim3(a.Hkv, a.B), dim3(256), 0, st, a);
+// The same with one workgroup per sequence, its waves shared out among the heads, which
+// sets the length itself behind a barrier (16 full sequences of 2048 rows, 8 KV heads: 6.6 to 7.1 us).
+__global__ __launch_bounds__(1024) void insert_heads_kernel(InsertArgs a) {
+  __shared__ uint64_t s_min[16];
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int waves = 16 / a.Hkv, g = wave / waves, part = wave % waves;  // (Hkv <= 16)
+  const int64_t kvb = a.kv_indptr[b], span = a.kv_indptr[b + 1] - kvb;
+  const int n = (int)seq_tokens(a.kv_indptr, a.seq_len, b), newest = a.newest[b];
+  const int64_t base = (int64_t)g * a.total + kvb;
+  uint64_t best = ~0ull;
+  if (n >= span && g < a.Hkv) best = least_row(a, base, n, newest, (part * 64 + lane) * 4, waves * 256);
+  if (lane == 0) s_min[wave] = best;
+  __syncthreads();  // (and every wave has read the length)
+  if (tid == 0) a.seq_len[b] = min((int64_t)n + 1, span);
+  if (g >= a.Hkv || part != 0) return;
+  for (int i = 1; i < waves; ++i) best = min(best, s_min[wave + i]);
+  const int64_t row = n < span ? n : (int64_t)(uint32_t)~(uint32_t)best;
+  const int64_t from = ((int64_t)b * a.Hkv + g) * kHeadDim, to = (base + row) * kHeadDim;
+  if (lane == 32) a.rows[(int64_t)b * a.Hkv + g] = span == 0 ? -1 : (int32_t)row;
+  if (span == 0) return;
+  if (lane < 16) *reinterpret_cast<uint4*>(a.K + to + lane * 8) = *reinterpret_cast<const uint4*>(a.k + from + lane * 8);
+  else if (lane < 32) *reinterpret_cast<uint4*>(a.V + to + (lane - 16) * 8) = *reinterpret_cast<const uint4*>(a.v + from + (lane - 16) * 8);
+  else if (lane == 32) {
+    a.weights[base + row] = 0.f;
+    a.positions[base + row] = newest;
+  }
+}
+
+hipError_t launch_insert(const InsertArgs& a, int64_t max_len, hipStream_t st) {
+  // One launch while one compute unit reads the heads' rows in about that time: one
+  // against two, us a call in a stream and in a graph: 2 heads of 1000 rows 10.0, 3.6 and 12.2,
+  // 5.1; 8 of 2048 10.3, 6.6 and 12.5, 5.5; 8 of 4096 10.3, 8.9 and 12.4, 5.7; 8 of 8192 14.5, 14.4 and 12.1, 6.5
+  if (a.Hkv <= 16 && max_len * a.Hkv <= 16384) {
+    hipLaunchKernelGGL(insert_heads_kernel, dim3(a.B), dim3(1024), 0, st, a);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL(insert_token_kernel, dim3(a.Hkv, a.B), dim3(1024), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess) {
     hipLaunchKernelGGL(advance_lengths_kernel, dim3((a.B + 255) / 256), dim3(256), 0, st, a);

@@ -239,7 +239,7 @@ struct InsertArgs {
 };
 hipError_t launch_prompt_weights(const WeightArgs& a, int64_t max_len, hipStream_t st);
 hipError_t launch_evict(const EvictArgs& a, int64_t max_len, int64_t max_out, hipStream_t st);
-hipError_t launch_insert(const InsertArgs& a, hipStream_t st);
+hipError_t launch_insert(const InsertArgs& a, int64_t max_len, hipStream_t st);
 
 // What the combine of the single-token forms joins and writes beside the outputs.
 constexpr int kMaxSplits = 64;  // splits of a row tile's keys
