@@ -321,7 +321,9 @@ tactic_status tactic_build_clusters(const uint16_t* K, const uint16_t* V,
  *     minus slope_h * |position of q - position of k|,
  * and a pair that a mask leaves out has no weight, whatever its key and value
  * hold (infinities and NaN too).  A query that sees no key gets zeros and a
- * logarithm of -inf.  bf16 in, sums in 32 bits, one order of every sum. */
+ * logarithm of -inf.  bf16 in, sums in 32 bits, one order of every sum.
+ * q, k, v, K, V, their pages, outputs of rows and the workspace are 16-byte
+ * aligned (else an invalid argument). */
 typedef struct {
   float cap;                   /* 0: none; otherwise positive and finite */
   const float* slopes;         /* device fp32 [Hq] or NULL: none */

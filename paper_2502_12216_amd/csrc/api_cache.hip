@@ -5,6 +5,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "host.hpp"
 #include "plan.hpp"
@@ -20,6 +21,13 @@ constexpr int kMaxRecent = 1 << 22;
 
 tactic_status check_mod(const tactic_score_mod* m) {
   if (m && !(m->cap >= 0.f && m->cap < INFINITY)) return fail(TACTIC_ERR_INVALID_ARG, "cap must be 0 or positive and finite");
+  return TACTIC_OK;
+}
+
+// The kernels read and write rows 16 bytes at a time.
+tactic_status check_rows(std::initializer_list<const void*> arrays) {
+  for (const void* p : arrays)
+    if (reinterpret_cast<uintptr_t>(p) % 16) return fail(TACTIC_ERR_INVALID_ARG, "q, k, v, caches, outputs and workspace must be 16-byte aligned");
   return TACTIC_OK;
 }
 
@@ -146,6 +154,7 @@ tactic_status prompt_impl(const uint16_t* q, const uint16_t* K, const uint16_t* 
   if ((st = check_mod(mod)) != TACTIC_OK || (st = check_queries(queries, shape)) != TACTIC_OK) return st;
   if (queries->total_queries == 0) return TACTIC_OK;
   if (!q || !out || ((!K || !V) && shape->total_tokens > 0)) return fail(TACTIC_ERR_INVALID_ARG, "null argument");
+  if ((st = check_rows({q, K, V, out, workspace})) != TACTIC_OK) return st;
   const PromptLayout p = prompt_layout(shape, queries);
   if ((st = check_workspace(workspace, workspace_bytes, p.bytes)) != TACTIC_OK) return st;
   if (p.plan.tiles * shape->n_kv_heads * p.plan.splits > kMaxInt) return fail(TACTIC_ERR_UNSUPPORTED, "more than 2^31 workgroups");
@@ -264,6 +273,7 @@ tactic_status scored_impl(const uint16_t* q, const uint16_t* K, const uint16_t* 
   if (docs != (rows && rows->q_documents)) return fail(TACTIC_ERR_INVALID_ARG, "documents and q_documents go together");
   if (mod && mod->slopes && rows && rows->positions && !rows->q_pos)
     return fail(TACTIC_ERR_INVALID_ARG, "slopes with positions need q_pos");
+  if ((st = check_rows({q, K, V, out, workspace})) != TACTIC_OK) return st;
   const ScoredLayout p = scored_layout(shape, weights != nullptr);
   if ((st = check_workspace(workspace, workspace_bytes, p.bytes)) != TACTIC_OK) return st;
   char* ws = static_cast<char*>(workspace);
@@ -363,6 +373,7 @@ tactic_status shared_impl(const uint16_t* q, const uint16_t* Kp, const uint16_t*
     return fail(TACTIC_ERR_UNSUPPORTED, "a shared prefix takes a cap and slopes only");
   if (!q || !out || ((!K || !V) && shape->total_tokens > 0) || ((!Kp || !Vp) && pre->total_tokens > 0))
     return fail(TACTIC_ERR_INVALID_ARG, "null argument");
+  if ((st = check_rows({q, Kp, Vp, K, V, out, workspace})) != TACTIC_OK) return st;
   const SharedLayout l = shared_layout(shape, pre);
   if ((st = check_workspace(workspace, workspace_bytes, l.bytes)) != TACTIC_OK) return st;
   char* ws = static_cast<char*>(workspace);
@@ -457,6 +468,7 @@ tactic_status tactic_prompt_weights(const uint16_t* q, const uint16_t* K, const 
   if (window < 0) return fail(TACTIC_ERR_INVALID_ARG, "window must be >= 0");
   if (queries->total_queries == 0 || shape->total_tokens == 0) return TACTIC_OK;
   if (!q || !K || !lse || !weights) return fail(TACTIC_ERR_INVALID_ARG, "null argument");
+  if ((st = check_rows({q, K, workspace})) != TACTIC_OK) return st;
   const PromptLayout p = prompt_layout(shape, queries);
   if ((st = check_workspace(workspace, workspace_bytes, p.bytes)) != TACTIC_OK) return st;
   tactic::WeightArgs a{};
@@ -566,6 +578,7 @@ tactic_status tactic_evict(const uint16_t* K, const uint16_t* V, const tactic_kv
   if ((!K || !V || !weights) && shape->total_tokens > 0) return fail(TACTIC_ERR_INVALID_ARG, "null argument");
   if ((!K_out || !V_out || !weights_out || !positions_out) && out_total > 0)
     return fail(TACTIC_ERR_INVALID_ARG, "null argument");
+  if ((st = check_rows({K, V, K_out, V_out, workspace})) != TACTIC_OK) return st;
   if (K && (K == K_out || V == V_out || weights == weights_out || (positions && positions == positions_out)))
     return fail(TACTIC_ERR_INVALID_ARG, "the outputs must not be the inputs");
   if (out_len == shape->seq_len) return fail(TACTIC_ERR_INVALID_ARG, "out_len must not be the shape's seq_len");
@@ -611,10 +624,11 @@ tactic_status tactic_evict(const uint16_t* K, const uint16_t* V, const tactic_kv
 tactic_status tactic_insert_token(const uint16_t* k, const uint16_t* v, const int32_t* newest, int32_t recent,
                                   const tactic_kv_shape* shape, int64_t* seq_len, uint16_t* K, uint16_t* V,
                                   float* weights, int32_t* positions, int32_t* rows, hipStream_t stream) {
-  const tactic_status st = check_shape(shape);
+  tactic_status st = check_shape(shape);
   if (st != TACTIC_OK) return st;
   if (!k || !v || !newest || !seq_len || !rows) return fail(TACTIC_ERR_INVALID_ARG, "null argument");
   if ((!K || !V || !weights || !positions) && shape->total_tokens > 0) return fail(TACTIC_ERR_INVALID_ARG, "null argument");
+  if ((st = check_rows({k, v, K, V})) != TACTIC_OK) return st;
   if (seq_len != shape->seq_len) return fail(TACTIC_ERR_INVALID_ARG, "seq_len must be the shape's own array");
   if (recent < 0 || recent > kMaxRecent) return fail(TACTIC_ERR_INVALID_ARG, "recent must be in [0, 2^22]");
   tactic::InsertArgs a{};

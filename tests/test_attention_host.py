@@ -203,3 +203,13 @@ def test_evict_refuses_lengths_it_reads_while_it_writes_them():
     batch = T.RaggedBatch([3, 5], 2, 2, device="cpu", capacities=[8, 8])
     with pytest.raises(ValueError, match="another batch"):
         T.CacheEvictor(batch, batch, 0)
+
+
+@pytest.mark.parametrize("call,names", [(prompt, ("q", "K", "V", "out")), (weights, ("q", "K")), (scored, ("q", "K", "out")),
+                                        (shared, ("q", "Kp", "K", "out")), (evict, ("K", "Ko")), (insert, ("k", "K"))])
+def test_rows_off_their_alignment(call, names):
+    """Rows are read 16 bytes at a time."""
+    for name in names:
+        for off in (2, 8):
+            assert call(**{name: FAKE + off}) == 1, name
+            assert b"16-byte" in C.lib().tactic_last_error()
