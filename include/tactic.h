@@ -325,7 +325,7 @@ tactic_status tactic_build_clusters(const uint16_t* K, const uint16_t* V,
  * q, k, v, K, V, their pages, outputs of rows and the workspace are 16-byte
  * aligned (else an invalid argument). */
 typedef struct {
-  float cap;                   /* 0: none; otherwise positive and finite */
+  float cap;                   /* 0: none; otherwise in [2^-120, 2^120] */
   const float* slopes;         /* device fp32 [Hq] or NULL: none */
   const int32_t* documents;    /* device [total_tokens] or NULL: document of each row; a query sees
                                   the rows of its own document only */

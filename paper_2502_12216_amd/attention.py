@@ -76,8 +76,8 @@ class ScoreMod:
     def __init__(self, cap: float = 0.0, slopes: Optional[torch.Tensor] = None,
                  documents: Optional[torch.Tensor] = None, prefix_len: Optional[torch.Tensor] = None):
         self.cap = float(cap)
-        if not 0.0 <= self.cap < float("inf"):
-            raise ValueError("cap must be 0 or positive and finite")
+        if self.cap != 0.0 and not 2.0 ** -120 <= self.cap <= 2.0 ** 120:
+            raise ValueError("cap must be 0 or in [2^-120, 2^120]")
         self.slopes, self.documents, self.prefix_len = slopes, documents, prefix_len
 
     def struct(self, call: _Call, batch: RaggedBatch) -> C.ScoreMod:

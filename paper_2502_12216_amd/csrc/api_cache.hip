@@ -20,7 +20,9 @@ constexpr int64_t kMaxInt = ((int64_t)1 << 31) - 1;
 constexpr int kMaxRecent = 1 << 22;
 
 tactic_status check_mod(const tactic_score_mod* m) {
-  if (m && !(m->cap >= 0.f && m->cap < INFINITY)) return fail(TACTIC_ERR_INVALID_ARG, "cap must be 0 or positive and finite");
+  // (outside, the cap's reciprocal or its value in base 2 would leave the normal numbers)
+  if (m && m->cap != 0.f && !(m->cap >= 0x1p-120f && m->cap <= 0x1p120f))
+    return fail(TACTIC_ERR_INVALID_ARG, "cap must be 0 or in [2^-120, 2^120]");
   return TACTIC_OK;
 }
 

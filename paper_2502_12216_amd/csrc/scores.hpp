@@ -33,8 +33,8 @@ __device__ __forceinline__ float tanh_any(float x) {  // (both, and no branch pe
 }
 
 // tanh(x) for |x| <= kTanhPoly: x times the polynomial of degree 5 in x^2 of the least
-// largest relative error (2.9e-8, by Remez' exchange; with fp32 roundings 1.6e-7):
-// seven operations without a reciprocal, for tiles whose scores all lie inside.
+// largest relative error (by Remez' exchange; with the coefficients in fp32 6.5e-8, with
+// fp32 roundings 1.6e-7): seven operations without a reciprocal, for tiles whose scores all lie inside.
 constexpr float kTanhPoly = 0.75f;
 __device__ __forceinline__ float tanh_poly(float x) {
   const float z = x * x;
@@ -48,8 +48,12 @@ __device__ __forceinline__ float tanh_poly(float x) {
 
 // cap tanh(s / cap) in base 2 for whole tiles of products s = q . k, as s times a
 // polynomial in s^2 whose coefficients hold the scale, the cap and log2(e) (set on the
-// host in 64 bits): of degree 3 up to |s| = near (a relative error of 5.9e-8 with exact
+// host in 64 bits): of degree 3 up to |s| = near (a relative error of 6.1e-8 with exact
 // arithmetic, 2.2e-7 with fp32's), else of degree 5 up to |s| = far (as tanh_poly).
+// near and far are 0.375 and 0.75 of the cap where fp32 holds the coefficients, which go
+// with cap^-2j.  Below a cap of 6e-6 (degree 3: 2.5e-8) the last ones are infinite: no |s|
+// is inside.  Above 280 (8e4) they are below the normal numbers and count as lost, an
+// error of 2^-126 s^2j of the 0.1275 s: within 2^-26 up to |s| = 2^9.5 (2^16).
 struct CapPoly {
   float near, far;
   float c3[4], c5[6];
@@ -66,8 +70,13 @@ __host__ inline CapPoly cap_poly(float cap) {
     if (i < 4) p.c3[i] = (float)(c3[i] * f);
     p.c5[i] = (float)(c5[i] * f);
   }
-  p.near = (float)(0.375 / k);
-  p.far = (float)(0.75 / k);
+  const auto limit = [](double by_cap, const float* c, int n, double by_loss) {
+    for (int i = 0; i < n; ++i)
+      if (!(fabsf(c[i]) < INFINITY)) return -1.f;
+    return (float)(fabsf(c[n - 1]) >= 0x1p-126f || by_cap < by_loss ? by_cap : by_loss);
+  };
+  p.near = limit(0.375 / k, p.c3, 4, 65536.0);
+  p.far = limit(0.75 / k, p.c5, 6, 724.0);
   return p;
 }
 __device__ __forceinline__ float cap_near(float s, const CapPoly& p) {
