@@ -63,7 +63,9 @@ def _device(batch: RaggedBatch):
 def _workspace(nbytes: int, name: str, device, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     if nbytes == 0:
         C.check(1, name)
-    if workspace is not None and workspace.dtype == torch.uint8 and workspace.device == device and workspace.numel() >= nbytes:
+    # (a view that repeats or skips bytes is not as much memory as it has elements)
+    if (workspace is not None and workspace.dtype == torch.uint8 and workspace.device == device and
+            workspace.numel() >= nbytes and workspace.is_contiguous() and workspace.data_ptr() % 16 == 0):
         return workspace
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
@@ -101,7 +103,8 @@ class PromptAttention:
 
     def __init__(self, batch: RaggedBatch, q_lens: Sequence[int], workspace: Optional[torch.Tensor] = None):
         """workspace: a uint8 device tensor to use if it is large enough (for
-        instance that of the chunk before), else a new one is allocated."""
+        instance that of the chunk before), contiguous and 16-byte aligned, else a
+        new one is allocated."""
         self.batch, self.q_lens = batch, [int(x) for x in q_lens]
         if len(self.q_lens) != batch.batch:
             raise ValueError("q_lens must name every sequence")
