@@ -437,8 +437,8 @@ tactic_status tactic_shared_decode_paged(const uint16_t* q, const tactic_paged_k
  *   weights fp32, positions int32 (or NULL: the row) [Hkv][total_tokens]
  *   keep device int32 [B];  newest device int32 [B] or NULL (n_b - 1): no position is above it
  *   out_indptr device [B+1], out_total, out_max host: spans of the other cache, as in tactic_kv_shape
- *   K_out, V_out, weights_out, positions_out [Hkv][out_total]...: must not overlap the inputs; rows
- *   behind the kept ones are left as they were
+ *   K_out, V_out, weights_out, positions_out [Hkv][out_total]...: must not overlap the inputs or
+ *   one another (else an invalid argument); rows behind the kept ones are left as they were
  *   out_len device int64 [B], not the shape's seq_len: rows kept.  recent in [0, 2^22]. */
 size_t tactic_evict_workspace_size(const tactic_kv_shape* shape, int64_t out_total);
 tactic_status tactic_evict(const uint16_t* K, const uint16_t* V, const tactic_kv_shape* shape,

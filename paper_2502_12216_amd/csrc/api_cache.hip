@@ -33,6 +33,16 @@ tactic_status check_rows(std::initializer_list<const void*> arrays) {
   return TACTIC_OK;
 }
 
+// Memory that a call reads or writes; a null or empty one overlaps nothing.
+struct Span {
+  const void* at;
+  int64_t bytes;
+};
+bool overlap(const Span& a, const Span& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+  return x && y && a.bytes > 0 && b.bytes > 0 && x < y + (uintptr_t)b.bytes && y < x + (uintptr_t)a.bytes;
+}
+
 tactic_status check_queries(const tactic_query_shape* q, const tactic_kv_shape* s) {
   if (!q) return fail(TACTIC_ERR_INVALID_ARG, "queries is null");
   if (!q->q_indptr) return fail(TACTIC_ERR_INVALID_ARG, "q_indptr is null");
@@ -581,8 +591,6 @@ tactic_status tactic_evict(const uint16_t* K, const uint16_t* V, const tactic_kv
   if ((!K_out || !V_out || !weights_out || !positions_out) && out_total > 0)
     return fail(TACTIC_ERR_INVALID_ARG, "null argument");
   if ((st = check_rows({K, V, K_out, V_out, workspace})) != TACTIC_OK) return st;
-  if (K && (K == K_out || V == V_out || weights == weights_out || (positions && positions == positions_out)))
-    return fail(TACTIC_ERR_INVALID_ARG, "the outputs must not be the inputs");
   if (out_len == shape->seq_len) return fail(TACTIC_ERR_INVALID_ARG, "out_len must not be the shape's seq_len");
   if (recent < 0 || recent > kMaxRecent) return fail(TACTIC_ERR_INVALID_ARG, "recent must be in [0, 2^22]");
   if (out_total < 0 || out_max < 0 || out_max > out_total)
@@ -590,6 +598,17 @@ tactic_status tactic_evict(const uint16_t* K, const uint16_t* V, const tactic_kv
   if (out_max > kMaxInt) return fail(TACTIC_ERR_UNSUPPORTED, "a span >= 2^31");
   if ((st = check_workspace(workspace, workspace_bytes, (int64_t)tactic_evict_workspace_size(shape, out_total))) != TACTIC_OK)
     return st;
+  // workgroups write rows while others read theirs: no output may lie in an input or in another output
+  const int64_t rows_in = shape->total_tokens * shape->n_kv_heads, rows_out = out_total * shape->n_kv_heads;
+  const Span in[] = {{K, rows_in * kHeadDim * 2}, {V, rows_in * kHeadDim * 2}, {weights, rows_in * 4}, {positions, rows_in * 4}};
+  const Span outs[] = {{K_out, rows_out * kHeadDim * 2}, {V_out, rows_out * kHeadDim * 2}, {weights_out, rows_out * 4},
+                       {positions_out, rows_out * 4}};
+  for (const Span& o : outs) {
+    for (const Span& i : in)
+      if (overlap(o, i)) return fail(TACTIC_ERR_INVALID_ARG, "the outputs must not overlap the inputs");
+    for (const Span& p : outs)
+      if (&o < &p && overlap(o, p)) return fail(TACTIC_ERR_INVALID_ARG, "the outputs must not overlap one another");
+  }
   tactic::EvictArgs a{};
   a.K = K;
   a.V = V;

@@ -32,3 +32,29 @@ def test_a_workspace_that_is_not_one_piece_of_memory_is_not_used():
     for bad in (torch.zeros(1, dtype=torch.uint8).expand(size), whole[::2], whole[1:], whole[:size - 1], whole.float()):
         got = T.PromptAttention(batch, [20, 20], workspace=bad).workspace
         assert got is not bad and got.is_contiguous() and got.numel() == size and got.dtype is torch.uint8
+
+
+KB = 1 << 30  # far apart: eight arrays of at most 1000 x 2 rows
+
+
+def _evict(**at):
+    """tactic_evict over arrays at made-up addresses (1000 rows in, 100 out, 2 KV heads); no refusal, no launch: not called so."""
+    names = ("K", "V", "weights", "positions", "K_out", "V_out", "weights_out", "positions_out")
+    p = {**{x: KB * (i + 1) for i, x in enumerate(names)}, **at}
+    shape = C.KVShape(2, 8, 2, 128, 1000, 700, 0x1000, None)
+    return C.lib().tactic_evict(p["K"], p["V"], C.ctypes.byref(shape), p["weights"], p["positions"], 0x1000, None, 5, 0x1000, 100,
+                                60, p["K_out"], p["V_out"], p["weights_out"], p["positions_out"], 0x1000, 0x1000, 1 << 40, None)
+
+
+@pytest.mark.parametrize("out,size", [("K_out", 100 * 2 * 256), ("V_out", 100 * 2 * 256), ("weights_out", 800), ("positions_out", 800)])
+@pytest.mark.parametrize("other,other_size", [("K", 1000 * 2 * 256), ("V", 1000 * 2 * 256), ("weights", 8000), ("positions", 8000),
+                                              ("K_out", 100 * 2 * 256), ("V_out", 100 * 2 * 256), ("weights_out", 800),
+                                              ("positions_out", 800)])
+def test_evict_refuses_outputs_that_overlap(out, size, other, other_size):
+    """Workgroups write rows while others still read theirs, so that one byte in common is too much."""
+    if out == other:
+        return
+    at = KB * 100
+    for off in (0, 256, other_size - 16, 16 - size):
+        assert _evict(**{other: at, out: at + off}) == 1, off
+        assert b"overlap" in C.lib().tactic_last_error()

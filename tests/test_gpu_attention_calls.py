@@ -1,0 +1,53 @@
+"""Calls beside the sparse decode at the limits of what their arguments may be."""
+import pytest
+import torch
+
+from tests.test_gpu_attention import DEV, _randn
+
+pytestmark = pytest.mark.gpu
+
+
+def test_evict_between_neighbours_in_one_piece_of_memory():
+    """Inputs and outputs that touch, in one buffer, in every order: no byte is in common."""
+    import paper_2502_12216_amd as T
+    hkv, n, m = 2, 200, 50
+    src = T.RaggedBatch([n], hkv, hkv)
+    keep = torch.tensor([m], dtype=torch.int32, device=DEV)
+    K, V = _randn(1, hkv, n, 128), _randn(2, hkv, n, 128)
+    weights, positions = torch.rand(hkv, n, device=DEV), torch.arange(n, dtype=torch.int32, device=DEV).repeat(hkv, 1) + 7
+    inputs, results = [K, V, weights, positions], []
+    shapes = [((hkv, m, 128), torch.bfloat16)] * 2 + [((hkv, m), torch.float32), ((hkv, m), torch.int32)]
+    for turn in range(3):
+        if turn == 0:
+            arrays = inputs + [torch.zeros(s, dtype=d, device=DEV) for s, d in shapes]
+        else:
+            sizes = [x.numel() * x.element_size() for x in inputs] + [torch.Size(s).numel() * d.itemsize for s, d in shapes]
+            order = list(range(8)) if turn == 1 else [4, 0, 5, 1, 6, 2, 7, 3]
+            buf, at, arrays = torch.zeros(sum(sizes), dtype=torch.uint8, device=DEV), 0, [None] * 8
+            for i in order:
+                piece = buf[at:at + sizes[i]]
+                arrays[i] = (piece.view(inputs[i].dtype).view(inputs[i].shape) if i < 4 else
+                             piece.view(shapes[i - 4][1]).view(shapes[i - 4][0]))
+                at += sizes[i]
+            for x, y in zip(arrays, inputs):
+                x.copy_(y)
+        k, v, w, p, ko, vo, wo, po = arrays
+        T.CacheEvictor(src, T.RaggedBatch([0], hkv, hkv, capacities=[m]), 10)(
+            k, v, w, keep, ko, vo, wo, po, positions=p, newest=torch.tensor([n + 6], dtype=torch.int32, device=DEV))
+        torch.cuda.synchronize()
+        results.append([x.clone() for x in arrays])
+    for other in results[1:]:
+        for x, y in zip(results[0], other):
+            assert torch.equal(x, y)
+
+
+def test_evict_of_nothing_into_nothing():
+    """Empty sequences into spans without rows: only the lengths are written."""
+    import paper_2502_12216_amd as T
+    src, dest = T.RaggedBatch([0, 0], 4, 2), T.RaggedBatch([0, 0], 4, 2, capacities=[0, 0])
+    dest.seq_len.fill_(9)
+    rows = torch.zeros(2, 0, 128, dtype=torch.bfloat16, device=DEV)
+    sums, pos = torch.zeros(2, 0, device=DEV), torch.zeros(2, 0, dtype=torch.int32, device=DEV)
+    T.CacheEvictor(src, dest, 3)(rows, rows, sums, torch.tensor([4, 0], dtype=torch.int32, device=DEV), rows, rows, sums, pos)
+    torch.cuda.synchronize()
+    assert dest.seq_len.tolist() == [0, 0]
