@@ -36,12 +36,16 @@ class _Call:
         return t.data_ptr() or 16
 
     def paged(self, cache: PagedCache, batch, name: str, sequences: int):
-        for part in ("K_pages", "V_pages", "page_table"):
-            self.tensor(getattr(cache, part), f"{name}.{part}", getattr(cache, part).dtype)
-        if tuple(cache.K_pages.shape[1:]) != (batch.n_kv_heads, cache.page_size, 128):
-            raise ValueError(f"{name}.K_pages must be [num_pages][{batch.n_kv_heads}][page_size][128]")
-        if cache.page_table.shape[0] != sequences:
-            raise ValueError(f"{name}.page_table has {cache.page_table.shape[0]} sequences, expected {sequences}")
+        # (the attributes may have been replaced since the cache was made, whose sizes bound the kernels' reads)
+        pages = (cache.num_pages, batch.n_kv_heads, cache.page_size, 128)
+        for part in ("K_pages", "V_pages"):
+            if tuple(getattr(cache, part).shape) != pages:
+                raise ValueError(f"{name}.{part} must be {list(pages)}, got {list(getattr(cache, part).shape)}")
+        if tuple(cache.page_table.shape) != (sequences, cache.max_pages):
+            raise ValueError(f"{name}.page_table must be {[sequences, cache.max_pages]}, got {list(cache.page_table.shape)}")
+        self.tensor(cache.K_pages, f"{name}.K_pages", torch.bfloat16)
+        self.tensor(cache.V_pages, f"{name}.V_pages", torch.bfloat16)
+        self.tensor(cache.page_table, f"{name}.page_table", torch.int32)
         return cache.struct()
 
     def run(self, name: str, *args):

@@ -58,3 +58,56 @@ def test_evict_refuses_outputs_that_overlap(out, size, other, other_size):
     for off in (0, 256, other_size - 16, 16 - size):
         assert _evict(**{other: at, out: at + off}) == 1, off
         assert b"overlap" in C.lib().tactic_last_error()
+
+
+def _pages(**other):
+    """A cache of 3 pages of 16 tokens with other parts in place of its own (host memory: no call gets as far as a launch)."""
+    c = object.__new__(T.PagedCache)
+    c.num_pages, c.page_size, c.max_pages, c.perm = 3, 16, 2, None
+    c.K_pages, c.V_pages = (torch.zeros(3, 2, 16, 128, dtype=torch.bfloat16) for _ in range(2))
+    c.page_table = torch.zeros(2, 2, dtype=torch.int32)
+    for part, x in other.items():
+        setattr(c, part, x)
+    return c
+
+
+@pytest.mark.parametrize("part", ["K_pages", "V_pages"])
+@pytest.mark.parametrize("bad,error,match", [
+    (torch.zeros(3, 2, 16, 128, dtype=torch.float16), TypeError, "bfloat16"),
+    (torch.zeros(3, 2, 16, 128, dtype=torch.uint8), TypeError, "bfloat16"),  # half the memory that is read
+    (torch.zeros(2, 2, 16, 128, dtype=torch.bfloat16), ValueError, "must be"),  # fewer pages than the table may name
+    (torch.zeros(3, 2, 8, 128, dtype=torch.bfloat16), ValueError, "must be"),
+    (torch.zeros(3, 1, 16, 128, dtype=torch.bfloat16), ValueError, "must be"),
+])
+def test_pages_that_were_replaced(part, bad, error, match, monkeypatch):
+    """Parts of a paged cache are checked at the call, for every paged form."""
+    _paged_calls_refuse(monkeypatch, {part: bad}, error, match)
+
+
+@pytest.mark.parametrize("bad,error,match", [(torch.zeros(2, 2, dtype=torch.int64), TypeError, "int32"),
+                                             (torch.zeros(2, 1, dtype=torch.int32), ValueError, "must be"),
+                                             (torch.zeros(1, 2, dtype=torch.int32), ValueError, "must be")])
+def test_page_tables_that_were_replaced(bad, error, match, monkeypatch):
+    _paged_calls_refuse(monkeypatch, dict(page_table=bad), error, match)
+
+
+def _paged_calls_refuse(monkeypatch, part, error, match):
+    batch = T.RaggedBatch([20, 30], 8, 2, device="cpu")
+    # (tensors of the host stand in for the device's: only the place is let pass)
+    from paper_2502_12216_amd import attention as A
+    place = A._Call.tensor
+
+    def on_host(self, t, name, dtype, shape=None, optional=False):
+        try:
+            return place(self, t, name, dtype, shape, optional)
+        except ValueError as e:
+            if "must live on the GPU" not in str(e):
+                raise
+    monkeypatch.setattr(A._Call, "tensor", on_host)
+    monkeypatch.setattr(A._Call, "run", lambda self, name, *args: pytest.fail(f"{name} was not refused"))
+    q, prompt_q = torch.zeros(2, 8, 128, dtype=torch.bfloat16), torch.zeros(50, 8, 128, dtype=torch.bfloat16)
+    shared_dec = T.SharedPrefixDecoder(batch, [20, 25], [0, 1])
+    for call in (lambda c: T.PromptAttention(batch, [20, 30]).paged(prompt_q, c), lambda c: T.ScoredDecoder(batch).paged(q, c),
+                 lambda c: shared_dec.paged(q, c, _pages()), lambda c: shared_dec.paged(q, _pages(), c)):
+        with pytest.raises(error, match=match):
+            call(_pages(**part))
