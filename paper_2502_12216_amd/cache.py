@@ -212,7 +212,11 @@ class EvictingCache:
                 k.device == v.device == self.K.device):
             raise ValueError(f"k and v must be contiguous bfloat16 tensors on {self.K.device}")
         self.newest += 1
-        rows = self.inserter(k, v, self.K, self.V, self.weights, self.positions, self.newest)
+        try:
+            rows = self.inserter(k, v, self.K, self.V, self.weights, self.positions, self.newest)
+        except Exception:  # refused, before any of it ran
+            self.newest -= 1
+            raise
         self._set_lens([n + 1 for n in self.batch.seq_lens])
         return rows
 

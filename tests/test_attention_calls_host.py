@@ -111,3 +111,15 @@ def _paged_calls_refuse(monkeypatch, part, error, match):
                  lambda c: shared_dec.paged(q, c, _pages()), lambda c: shared_dec.paged(q, _pages(), c)):
         with pytest.raises(error, match=match):
             call(_pages(**part))
+
+
+def test_append_that_is_refused_leaves_the_positions():
+    """Tokens off their 16-byte alignment, or that the insertion refuses for whatever reason."""
+    c = T.EvictingCache(8, 2, 2, 16, recent=4, device="cpu")
+    k = torch.zeros(2, 2, 128, dtype=torch.bfloat16)
+    off = torch.zeros(2 * 2 * 128 + 1, dtype=torch.bfloat16)[1:].view(2, 2, 128)
+    assert off.is_contiguous() and off.data_ptr() % 16
+    for bad in ((off, k), (k, off), (k, k)):  # (the last: host memory)
+        with pytest.raises((ValueError, C.TacticError)):
+            c.append(*bad)
+        assert c.newest.tolist() == [-1, -1] and c.batch.seq_lens == [0, 0]

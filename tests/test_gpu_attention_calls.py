@@ -51,3 +51,19 @@ def test_evict_of_nothing_into_nothing():
     T.CacheEvictor(src, dest, 3)(rows, rows, sums, torch.tensor([4, 0], dtype=torch.int32, device=DEV), rows, rows, sums, pos)
     torch.cuda.synchronize()
     assert dest.seq_len.tolist() == [0, 0]
+
+
+def test_append_off_its_alignment_leaves_the_cache():
+    import paper_2502_12216_amd as T
+    c = T.EvictingCache(8, 2, 1, 16, recent=4)
+    k = _randn(1, 1, 2, 128)
+    c.append(k, k)
+    state = [x.clone() for x in (c.K, c.V, c.weights, c.positions, c.newest, c.batch.seq_len)]
+    off = torch.zeros(2 * 128 + 1, dtype=torch.bfloat16, device=DEV)[1:].view(1, 2, 128)
+    for bad in ((off, k), (k, off)):
+        with pytest.raises(T.TacticError, match="16-byte"):
+            c.append(*bad)
+    torch.cuda.synchronize()
+    for x, y in zip((c.K, c.V, c.weights, c.positions, c.newest, c.batch.seq_len), state):
+        assert torch.equal(x, y)
+    assert c.batch.seq_lens == [1]
