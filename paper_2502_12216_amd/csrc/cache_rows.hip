@@ -35,7 +35,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
   // end of the keys it sees, its document
   __shared__ __align__(16) float s_lse[2][kWRows], s_slope[2][kWRows], s_pos[2][kWRows];
   __shared__ __align__(16) int s_lim[2][kWRows], s_doc[2][kDocs ? kWRows : 4];
-  __shared__ uint64_t s_nan[2];  // rows whose logarithm is NaN
+  __shared__ uint64_t s_odd[2];  // rows whose logarithm is NaN, or -inf (no weight)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
   const int tid = threadIdx.x, g = blockIdx.y, split = blockIdx.z;
   int lo = 0, hi = a.B - 1;  // key tiles of sequence b start at floor(rows before it / 256) + b
@@ -122,11 +122,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
       const int x = t * kWRows + tid, row = min(x, rows - 1), i = i0 + (row >> lg), h = g * a.G + (row & (a.G - 1));
       const int pos = n - m + i;
       const float l = a.lse[(int64_t)h * a.n_queries + q0 + i];
-      // a row past the end, and one whose sum says that it saw nothing, gives no weight
-      lse_r = x < rows && l != -INFINITY ? l * kLog2e : INFINITY;  // (NaN stays)
+      // a row past the end, and one whose sum says that it saw nothing, gives no weight and
+      // sees no key, whatever the row holds
+      lse_r = x < rows ? l * kLog2e : INFINITY;  // (NaN and -inf stay)
       slope_r = biased ? a.slopes[h] * kLog2e / scale : 0.f;
       pos_r = (float)(pos - k0);
-      lim_r = min(max(pos + 1, pre), n) - k0;
+      lim_r = x >= rows || l == -INFINITY ? INT32_MIN : min(max(pos + 1, pre), n) - k0;
       if (kDocs) doc_r = a.documents[kvb + max(pos, 0)];
     }
   };
@@ -134,9 +135,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
 #pragma unroll
     for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x4*>(s_q[buf] + ((wave * 4 + i) * 64 + lane) * 16) = qreg[i];
     if (tid < kWRows) {
-      const uint64_t nan_rows = __ballot(lse_r != lse_r);
-      if (tid == 0) s_nan[buf] = nan_rows;
-      s_lse[buf][tid] = lse_r != lse_r ? 0.f : lse_r;
+      const uint64_t odd_rows = __ballot(!(lse_r > -INFINITY));
+      if (tid == 0) s_odd[buf] = odd_rows;
+      s_lse[buf][tid] = lse_r > -INFINITY ? lse_r : (lse_r == -INFINITY ? INFINITY : 0.f);
       s_slope[buf][tid] = slope_r;
       s_pos[buf][tid] = pos_r;
       s_lim[buf][tid] = lim_r;
@@ -154,14 +155,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
   while (t < t_hi) {
     const int tn = next_tile(t + 1);
     if (tn < t_hi) fetch(tn);
-    if (__builtin_amdgcn_readfirstlane((int)(s_nan[buf] != 0))) {
-      // rare: such a row gives NaN to the keys it sees, by its scores, which the masks leave out
-      if (tid < kWRows && (s_nan[buf] >> tid & 1)) *reinterpret_cast<uint32_t*>(s_q[buf] + tid * 256) = 0x7fff7fffu;
+    const bool odd = __builtin_amdgcn_readfirstlane((int)(s_odd[buf] != 0));
+    if (odd) {
+      // rare: a row of NaN gives NaN to the keys it sees, by its scores, which the masks leave out
+      if (tid < kWRows && (s_odd[buf] >> tid & 1) && s_lse[buf][tid] != INFINITY)
+        *reinterpret_cast<uint32_t*>(s_q[buf] + tid * 256) = 0x7fff7fffu;
       __syncthreads();
     }
     // the first token of the tile sees the fewest keys
     const int lim0 = min(max(n - m + i0 + ((t * kWRows) >> lg) + 1, pre), n);
-    const bool masked = kDocs || k0 + wave * 64 + 64 > lim0;
+    const bool masked = kDocs || odd || k0 + wave * 64 + 64 > lim0;
 #pragma unroll
     for (int rb = 0; rb < 2; ++rb) {
       f32x16 acc[2];

@@ -92,3 +92,28 @@ def test_caps_beyond_every_score(cap):
     check_prompt([300], [300], 4, 2, cap=cap)
     check_decode([300], 4, 2, cap=cap)
     check_prompt([300], [300], 4, 2, cap=cap, spoil=lambda K, V: K.mul_(1e18))
+
+
+@pytest.mark.parametrize("window", [0, 260])
+@pytest.mark.parametrize("kw", [dict(), dict(docs=70), dict(cap=20.0, alibi=True)])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_weights_of_queries_that_give_none(value, kw, window):
+    """A logarithm of -inf takes a query out whatever the query holds: padding, or heads that a caller leaves out."""
+    import paper_2502_12216_amd as T
+    n, hq, hkv = 300, 8, 2
+    batch = _batch([n], hq, hkv)
+    K, V, q = _randn(1, hkv, n, 128), _randn(2, hkv, n, 128), _randn(3, n, hq, 128)
+    document = torch.arange(n, dtype=torch.int32, device=DEV) // kw["docs"] if "docs" in kw else None
+    mod = T.ScoreMod(cap=kw.get("cap", 0.0), documents=document, slopes=R.slopes(hq) if "alibi" in kw else None)
+    att = T.PromptAttention(batch, [n])
+    _, lse = att(q, K, V, mod)
+    lse = lse.clone()
+    out = torch.zeros(hq, n, dtype=torch.bool, device=DEV)
+    out[1, 50], out[6, 210], out[:, 297:], out[3, 64:192] = True, True, True, True
+    lse[out] = -float("inf")
+    want = att.add_weights(q, K, lse, torch.zeros(hkv, n, device=DEV), mod, window=window).clone()
+    q[out.T] = value
+    got = att.add_weights(q, K, lse, torch.zeros(hkv, n, device=DEV), mod, window=window)
+    torch.cuda.synchronize()
+    assert torch.isfinite(want).all() and torch.equal(got, want)
+    assert not want[:, 297:].any()
