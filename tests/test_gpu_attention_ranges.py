@@ -117,3 +117,27 @@ def test_weights_of_queries_that_give_none(value, kw, window):
     torch.cuda.synchronize()
     assert torch.isfinite(want).all() and torch.equal(got, want)
     assert not want[:, 297:].any()
+
+
+@pytest.mark.parametrize("positions", [True, False])
+@pytest.mark.parametrize("qp", [2 ** 31 - 1, 0, -2 ** 31])
+@pytest.mark.parametrize("hq,hkv", [(2, 2), (8, 2), (16, 2)])
+def test_distances_that_pass_31_bits(hq, hkv, qp, positions):
+    """Positions over the whole range of int32: the bias goes by their true distance."""
+    import paper_2502_12216_amd as T
+    n = 200
+    batch = _batch([n], hq, hkv)
+    K, V, q = _randn(1, hkv, n, 128), _randn(2, hkv, n, 128), _randn(3, 1, hq, 128)
+    slopes = torch.linspace(1.0, 2.0, hq, device=DEV) * 2.0 ** -30
+    pos = torch.linspace(-2.0 ** 31, 2.0 ** 31 - 1, n, dtype=torch.float64, device=DEV).round().to(torch.int64)
+    pos = torch.stack([pos, pos.flip(0)])
+    kw = dict(positions=pos.to(torch.int32).contiguous()) if positions else {}
+    out, lse = T.ScoredDecoder(batch)(q, K, V, T.ScoreMod(slopes=slopes), q_pos=torch.tensor([qp], dtype=torch.int32, device=DEV), **kw)
+    torch.cuda.synchronize()
+    for h in range(hq):
+        g = h * hkv // hq
+        kpos = pos[g] if positions else torch.arange(n, device=DEV)
+        o, l, _, ma, off = R.attend(q[:, h], K[g], V[g], torch.tensor([qp], device=DEV), kpos, torch.ones(1, n, dtype=torch.bool, device=DEV),
+                                    0.0, float(slopes[h]))
+        R.close(out[:, h], o, R.tolerance_fp32(ma, off, o), f"out h={h}")
+        R.close(lse[:, h], l, R.tolerance_lse(off, l), f"lse h={h}")
