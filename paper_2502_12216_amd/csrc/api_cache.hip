@@ -388,6 +388,7 @@ tactic_status shared_impl(const uint16_t* q, const uint16_t* Kp, const uint16_t*
   if ((st = check_rows({q, Kp, Vp, K, V, out, workspace})) != TACTIC_OK) return st;
   const SharedLayout l = shared_layout(shape, pre);
   if ((st = check_workspace(workspace, workspace_bytes, l.bytes)) != TACTIC_OK) return st;
+  if (l.plan.tiles * shape->n_kv_heads * l.plan.splits > kMaxInt) return fail(TACTIC_ERR_UNSUPPORTED, "more than 2^31 workgroups");
   char* ws = static_cast<char*>(workspace);
   tactic::RowsArgs a{};
   a.q = q;

@@ -123,3 +123,10 @@ def test_append_that_is_refused_leaves_the_positions():
         with pytest.raises((ValueError, C.TacticError)):
             c.append(*bad)
         assert c.newest.tolist() == [-1, -1] and c.batch.seq_lens == [0, 0]
+
+
+@pytest.mark.parametrize("n", [1 << 30, (1 << 31) - 1])  # (times two KV heads: 2^31 or more)
+def test_shared_prefixes_of_more_workgroups_than_a_launch_has(n):
+    pre = C.Prefixes(n, 2, 500, 300, 0x1000, 0x1000, 0x1000, 0x1000, 2)
+    assert shared(pre=pre) == 2
+    assert b"workgroups" in C.lib().tactic_last_error()
