@@ -229,8 +229,8 @@ void rows_attn_kernel(RowsArgs a) {
   const int ktiles = (kend + TK - 1) / TK;
   const int t_lo = (int)((int64_t)ktiles * split / a.splits), t_hi = (int)((int64_t)ktiles * (split + 1) / a.splits);
 
-  // the fewest and the most keys that one of the wave's rows sees (rows ascend)
-  const int w_lo = __builtin_amdgcn_readlane(klim, 0), w_hi = __builtin_amdgcn_readlane(klim, 31);
+  // the fewest keys that one of the wave's rows sees (rows ascend)
+  const int w_lo = __builtin_amdgcn_readlane(klim, 0);
 
   // Scores without a cap stay a factor `scale` below their base-2 value until the
   // exponential, which takes it along with the maximum in one multiply-add.
@@ -578,10 +578,31 @@ void rows_attn_kernel(RowsArgs a) {
     }
     return __any(bad != 0);
   };
-  auto pv_odd = [&](int buf) __attribute__((always_inline)) {
+  auto pv_odd = [&](int t, int buf) __attribute__((always_inline)) {
     const lds_ptr vt = tile_lds(buf) + TK * 256;
-    // finite values as in pv; then, for each kind of value that is not finite,
-    // whether a key with a weight has it in this dimension
+    // which keys the row sees, by the masks: a weight may be 0 without one (bit r + 16 kb as
+    // in soft; by arithmetic and four at a time, since the masks of comparisons and more
+    // registers here are spilled by the loops above: 128 rows with documents in pages, 3001
+    // tokens, 32 heads on 8, 218 us that way, 200 now, 193 where a weight of 0 counted as masked)
+    static_assert(NB <= 2, "a bit per key");
+    const int lim = klim - t * TK - 4 * half;
+    uint32_t seen = 0;
+#pragma unroll 1
+    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll 1
+      for (int r = 0; r < 16; r += 4) {
+        uint32_t in = (1u << min(max(lim - kb * 32 - 2 * r, 0), 4)) - 1u;
+        if constexpr (kDocs) {
+          const int4 d = *reinterpret_cast<const int4*>(s_doc + (kg * kBufs + buf) * TK + 4 * half + kb * 32 + 2 * r);
+          const uint32_t other = min((uint32_t)(d.x ^ qdoc), 1u) | min((uint32_t)(d.y ^ qdoc), 1u) << 1 |
+                                 min((uint32_t)(d.z ^ qdoc), 1u) << 2 | min((uint32_t)(d.w ^ qdoc), 1u) << 3;
+          in &= ~other;
+        }
+        seen |= in << (kb * 16 + r);
+      }
+    // finite values as in pv; then, for each kind of value that is not finite, whether a
+    // seen key has it in this dimension: an infinity (1, 2) with a weight, NaN (3), an
+    // infinity without a weight, which gives NaN as 0 times it does in pv (4)
 #pragma unroll
     for (int c = 0; c < TK / 16; ++c)
 #pragma unroll
@@ -595,10 +616,11 @@ void rows_attn_kernel(RowsArgs a) {
         __builtin_amdgcn_sched_barrier(0);  // one operand at a time: few registers are left here
       }
 #pragma unroll 1
-    for (int kind = 1; kind < 4; ++kind) {
+    for (int kind = 1; kind < 5; ++kind) {
       const float val = kind == 1 ? INFINITY : (kind == 2 ? -INFINITY : NAN);
-      const uint32_t mask = kind == 3 ? 0x7fffu : 0xffffu, lo = kind == 1 ? 0x7f80u : (kind == 2 ? 0xff80u : 0x7f81u),
+      const uint32_t mask = kind >= 3 ? 0x7fffu : 0xffffu, lo = kind == 2 ? 0xff80u : (kind == 3 ? 0x7f81u : 0x7f80u),
                      span = kind == 3 ? 0x7eu : 0u;
+      const uint32_t by_weight = kind < 3 ? ~0u : 0u, no_weight = kind == 4 ? ~0u : 0u;
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
         f32x16 hit;
@@ -610,7 +632,9 @@ void rows_attn_kernel(RowsArgs a) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             w[j] = halves_in(w[j], mask, lo, span);
-            one[j] = ((pf[c][0][j] & 0xffffu) ? 0x3f80u : 0u) | ((pf[c][0][j] & 0xffff0000u) ? 0x3f800000u : 0u);
+            const uint32_t weight = ((pf[c][0][j] & 0xffffu) ? 0x3f80u : 0u) | ((pf[c][0][j] & 0xffff0000u) ? 0x3f800000u : 0u);
+            const uint32_t bits = seen >> (8 * c + 2 * j), sees = (bits & 1u) * 0x3f80u | (bits >> 1 & 1u) * 0x3f800000u;
+            one[j] = (weight & by_weight) | (sees & ~by_weight & ~(weight & no_weight));
           }
           hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, one), hit, 0, 0, 0);
           __builtin_amdgcn_sched_barrier(0);
@@ -748,7 +772,7 @@ void rows_attn_kernel(RowsArgs a) {
       if (t < t_hi) {
         qk(0, nothing);
         soft(t, 0, !(sees_all(t) & kFull), false);
-        pv_odd(0);
+        pv_odd(t, 0);
       }
       __syncthreads();
     }
