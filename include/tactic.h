@@ -320,9 +320,9 @@ tactic_status tactic_build_clusters(const uint16_t* K, const uint16_t* V,
  *     s = q . k / sqrt(128),   capped: cap * tanh(s / cap),
  *     minus slope_h * |position of q - position of k|,
  * and a pair that a mask leaves out has no weight, whatever its key and value
- * hold (infinities and NaN too).  A seen value of NaN gives NaN, and so does an
- * infinite one whose weight is too small for 32 bits.  A query that sees no key
- * gets zeros and a logarithm of -inf.  bf16 in, sums in 32 bits, one order of every sum.
+ * hold (infinities and NaN too).  A seen value of NaN gives NaN; an infinite one
+ * whose weight is too small for 32 bits gives itself or NaN.  A query that sees
+ * no key gets zeros and a logarithm of -inf.  bf16 in, sums in 32 bits, one order of every sum.
  * q, k, v, K, V, their pages, outputs of rows and the workspace are 16-byte
  * aligned (else an invalid argument). */
 typedef struct {

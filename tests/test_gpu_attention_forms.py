@@ -1,0 +1,180 @@
+"""Every form of the prompt attention (32, 64, 128 or 256 rows to an item, keys split among workgroups or not) against
+the plain 64-bit implementation.  The host takes the form by an estimate of the time, which is worked out here
+again: each case names its form, and the size of the workspace, which follows from it, has to agree."""
+import math
+
+import pytest
+import torch
+
+from tests import attention_ref as R
+from tests.test_gpu_attention import DEV, _documents, _randn, check_prompt
+
+SPLITS = (1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32, 40, 48, 56, 64)
+COSTS = ((1.3, 0.88, 128), (2.0, 1.9, 128), (2.5, 2.3, 128), (2.0, 1.85, 64))  # item, round (us), keys of a round
+
+
+def form(lens, new, hq, hkv):
+    """(rows to an item, splits of the keys) with the least estimated time."""
+    rows, total, most = sum(new) * (hq // hkv), sum(lens), max(lens)
+    mean = max(1.0, most - 0.5 * min(max(new), most))
+    memory = total * hkv * 512 / 6e6
+    best = None
+    for v, (item, step, keys) in enumerate(COSTS):
+        items = max(len(lens), -(-rows // (32 << v))) * hkv
+        for s in SPLITS:
+            if s > 1 and s * keys > most:
+                break
+            run = max(math.ceil(most / (s * keys)) * step + item, math.ceil(items * s / 256) * (mean / (s * keys) * step + item))
+            t = max(run, memory) + 0.5 * min(run, memory)
+            if s > 1:
+                t += 4 + 0.15 * s + rows * hkv * s * (2 * 520) / 4.5e6
+            if best is None or t < best[0]:
+                best = (t, 32 << v, s)
+    return best[1:]
+
+
+def tiles(lens, new, hq, hkv):
+    return sum(new) * (hq // hkv) // form(lens, new, hq, hkv)[0] + len(lens)
+
+
+def workspace(lens, new, hq, hkv):
+    G, total, splits = hq // hkv, sum(lens), form(lens, new, hq, hkv)[1]
+
+    def take(at, size):
+        return -(-(at + size) // 256) * 256
+    at = behind = take(0, -(-max(lens) // 64) * len(lens) * 8)
+    for size in ([sum(new) * hq * splits * 512, sum(new) * hq * splits * 8] if splits > 1 else []):
+        at = take(at, size)
+    for size in (16, 4, 16):
+        at = take(at, tiles(lens, new, hq, hkv) * size)
+    items, rows = max(1, (total + 255) // 256) * hkv, max(new) * G  # the sums of the accumulated weights' splits
+    weight_splits = max(1, min(max(min(4096 // items, rows // 512), min(512 // items, rows // 128)), 64))
+    if weight_splits > 1:
+        behind = take(behind, weight_splits * hkv * total * 4)
+    return max(256, at, behind)
+
+
+# form, split or not, whether the row tiles of documents are put in order first (more than 768 items)
+CASES = [
+    ((32, False, False), [300, 200], [300, 200], 4, 2),
+    ((32, False, True), [82, 80, 82, 1, 82, 77, 82, 82, 82], [82, 80, 82, 1, 82, 77, 82, 82, 82], 32, 16),
+    ((32, True, False), [2100, 900], [64, 5], 8, 2),
+    ((64, False, False), [700, 700, 701], [700, 700, 690], 12, 6),
+    ((64, False, False), [400, 333, 397], [300, 290, 299], 32, 8),
+    ((128, False, False), [400, 1, 0, 399, 400, 380], [200, 1, 0, 200, 200, 199], 32, 8),
+    ((128, False, False), [2100, 2033, 2055], [1500, 1400, 1499], 6, 6),
+    ((128, False, True), [1026, 1000] * 6, [115, 114] * 6, 64, 16),
+    ((128, True, False), [3999], [301], 16, 2),
+    ((128, True, True), [3558] * 12, [56] * 12, 32, 8),
+    ((256, False, False), [400, 390, 400, 400, 370, 400], [200, 190, 200, 200, 170, 200], 32, 8),
+    ((256, False, True), [120] * 60, [120] * 60, 32, 8),
+    ((256, True, False), [6000], [3000], 4, 2),
+    ((256, True, False), [20000], [520], 16, 2),
+]
+MASKS = [dict(), dict(cap=30.0, page=16), dict(alibi=True, prefix=100, spare=3), dict(docs=60), dict(page=64, alibi=True),
+         dict(docs=300, page=7, alibi=True, cap=3.0), dict(docs=2000, prefix=700)]
+
+
+def _known(case):
+    (rows, split, ordered), *shape = case
+    r, s = form(*shape)
+    assert (r, s > 1, tiles(*shape) * shape[3] * s > 768) == (rows, split, ordered)
+    return shape
+
+
+@pytest.mark.parametrize("case", CASES)
+def test_cases_take_the_forms_that_they_name(case):
+    """(On the CPU: the workspace's size is worked out on the host.)"""
+    import paper_2502_12216_amd as T
+    lens, new, hq, hkv = _known(case)
+    att = T.PromptAttention(T.RaggedBatch(lens, hq, hkv, device="cpu"), new)
+    assert att.workspace.numel() == workspace(lens, new, hq, hkv)
+
+
+def test_cases_cover_every_form():
+    assert {case[0][:2] for case in CASES} == {(r, s) for r in (32, 64, 128, 256) for s in (False, True)} - {(64, True)}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kw", MASKS)
+@pytest.mark.parametrize("case", CASES)
+def test_prompt_forms(case, kw):
+    lens, new, hq, hkv = _known(case)
+    if "prefix" in kw:
+        kw = dict(kw, prefix=[kw["prefix"] + 37 * b for b in range(len(lens))])
+    check_prompt(lens, new, hq, hkv, **kw)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("page", [0, 24])
+@pytest.mark.parametrize("kw", [dict(docs=25), dict(), dict(alibi=True)])
+@pytest.mark.parametrize("case", [c for c in CASES if c[0] in ((32, True, False), (64, False, False), (128, False, False), (128, True, False),
+                                                               (256, False, False), (256, True, False)) and max(c[1]) < 5000])
+def test_prompt_forms_with_values_that_are_not_finite(case, kw, page):
+    """In places that some queries see, that others do not, and that nobody sees: the items are computed again."""
+    lens, new, hq, hkv = _known(case)
+
+    def spoil(K, V):
+        n = lens[0]
+        for i, value in enumerate((float("nan"), float("inf"), -float("inf"))):
+            V[i::3, n // 2 + 11 + i, 5 * i:5 * i + 2] = value
+            V[0, n - 60 + 3 * i] = value
+            K[1, n - 100 + 7 * i, 3] = value
+    check_prompt(lens, new, hq, hkv, spoil=spoil, page=page, **kw)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("docs,alibi", [(200, False), (0, True)])
+def test_split_256_row_form_with_values_that_are_not_finite(docs, alibi):
+    """The last queries of a long sequence in pages, of which some see what is spoilt.  With a bias by distance the
+    weights of early keys leave the range of 32 bits (2^-149): their infinities give themselves or NaN."""
+    import paper_2502_12216_amd as T
+    case = next(c for c in CASES if c[0] == (256, True, False) and c[2] == [520])
+    (n,), (m,), hq, hkv = _known(case)
+    K, V, q = _randn(1, hkv, n, 128), _randn(2, hkv, n, 128), _randn(3, m, hq, 128, scale=2.0)
+    V[0, 19990, 7] = float("nan")
+    V[1, 19000:19900:50, 9] = float("inf")
+    V[1, 5, 30] = -float("inf")
+    K[1, 19970, 3] = float("nan")
+    document = torch.as_tensor(_documents(n, docs, 1), device=DEV) if docs else None
+    sl = R.slopes(hq) if alibi else None
+    kp, table = R.pages(K, [n], 64, 1)
+    out, lse = T.PromptAttention(T.RaggedBatch([n], hq, hkv), [m]).paged(
+        q, T.PagedCache(kp, R.pages(V, [n], 64, 1)[0], table), T.ScoreMod(slopes=sl, documents=document))
+    torch.cuda.synchronize()
+    kpos, qpos = torch.arange(n, device=DEV), torch.arange(n - m, n, device=DEV)
+    seen = kpos[None] <= qpos[:, None]
+    if docs:
+        seen = seen & (document[qpos][:, None] == document[None])
+    for h in range(hq):
+        g = h * hkv // hq
+        v = V[g].double()
+        odd = ~torch.isfinite(v)
+        o, l, p, ma, off = R.attend(q[:, h], K[g], torch.where(odd, 0.0, v), qpos, kpos, seen, 0.0, float(sl[h]) if alibi else 0.0)
+        R.close(lse[h], l, R.tolerance_lse(off, l), f"lse h={h}")
+
+        def some(keys, value):  # whether one of a query's `keys` has the value, per dimension
+            return keys.double() @ value.double() > 0
+        nan = torch.isnan(l)[:, None] | some(seen, torch.isnan(v))
+        got, finite = out[:, h].double(), ~nan
+        for value in (float("inf"), -float("inf")):
+            sure, any_seen = some(p > 2.0 ** -100, v == value) & ~nan, some(seen, v == value) & ~nan
+            assert (got[sure] == value).all()
+            assert (torch.isnan(got[any_seen]) | (got[any_seen] == value)).all()
+            finite &= ~any_seen
+        assert torch.isnan(got[nan]).all()
+        R.close(torch.where(finite, got, 0.0), torch.where(finite, o, 0.0), torch.where(finite, R.tolerance_bf16(ma, off, o), 1e-30),
+                f"out h={h}")
+
+
+@pytest.mark.gpu
+def test_lengths_that_are_nothing():
+    """No queries at all, or queries without any tokens: nothing written, and zeros."""
+    import paper_2502_12216_amd as T
+    batch = T.RaggedBatch([0, 0], 8, 2)
+    rows = torch.zeros(2, 0, 128, dtype=torch.bfloat16, device="cuda")
+    out, lse = T.PromptAttention(batch, [0, 0])(torch.zeros(0, 8, 128, dtype=torch.bfloat16, device="cuda"), rows, rows)
+    assert out.shape == (0, 8, 128) and lse.shape == (8, 0)
+    out, lse = T.PromptAttention(batch, [3, 0])(torch.ones(3, 8, 128, dtype=torch.bfloat16, device="cuda"), rows, rows)
+    torch.cuda.synchronize()
+    assert not out.any() and (lse == -float("inf")).all()
