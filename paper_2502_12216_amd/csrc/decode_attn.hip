@@ -929,7 +929,7 @@ __global__ __launch_bounds__(512) void combine_kernel(AttnArgs a, std::condition
   for (int c = tid; c < np + npre; c += 512) {  // (not kMore: the entries this thread wrote)
     const float mc = s_w[c];
     const float wc = mc == -INFINITY ? 0.f : fast_exp2(mc - M);
-    s_w[c] = wc;
+    s_w[c] = kMore && c >= np && mc == -INFINITY ? -1.f : wc;  // (a prefix's split without keys wrote no sums)
     den = fmaf(s_l[c], wc, den);
   }
   den = wave_allsum_f(den);
@@ -947,8 +947,8 @@ __global__ __launch_bounds__(512) void combine_kernel(AttnArgs a, std::condition
   if constexpr (kMore) {
     const float* pre_o = more.pre_o + row * kHeadDim + d;
 #pragma unroll 4
-    for (int c = slice; c < npre; c += 4)  // (a split without keys wrote no sums)
-      if (s_w[np + c] != 0.f) num = fmaf(s_w[np + c], pre_o[(int64_t)c * more.rows * kHeadDim], num);
+    for (int c = slice; c < npre; c += 4)  // (a weight of 0 counts: 0 times NaN)
+      if (s_w[np + c] >= 0.f) num = fmaf(s_w[np + c], pre_o[(int64_t)c * more.rows * kHeadDim], num);
   }
   s_num[slice][d] = num;
   __syncthreads();

@@ -1,5 +1,5 @@
-"""Every form of the prompt attention (32, 64, 128 or 256 rows to an item, keys split among workgroups or not) against
-the plain 64-bit implementation.  The host takes the form by an estimate of the time, which is worked out here
+"""Every form of the prompt attention and of a shared prefix's (32, 64, 128 or 256 rows to an item, keys split among
+workgroups or not) against the plain 64-bit implementation.  The host takes the form by an estimate of the time, which is worked out here
 again: each case names its form, and the size of the workspace, which follows from it, has to agree."""
 import math
 
@@ -8,25 +8,36 @@ import torch
 
 from tests import attention_ref as R
 from tests.test_gpu_attention import DEV, _documents, _randn, check_prompt
+from tests.test_gpu_attention_tiles import test_shared_prefix_row_tiles as _shared_row_tiles
 
 SPLITS = (1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32, 40, 48, 56, 64)
 COSTS = ((1.3, 0.88, 128), (2.0, 1.9, 128), (2.5, 2.3, 128), (2.0, 1.85, 64))  # item, round (us), keys of a round
+SHARED_COSTS = ((1.3, 1.05, 128), (2.0, 1.9, 128), (2.5, 1.7, 64), (2.0, 1.8, 32))
 
 
 def form(lens, new, hq, hkv):
     """(rows to an item, splits of the keys) with the least estimated time."""
-    rows, total, most = sum(new) * (hq // hkv), sum(lens), max(lens)
-    mean = max(1.0, most - 0.5 * min(max(new), most))
+    most = max(lens)
+    return _least(sum(new) * (hq // hkv), len(lens), hkv, max(1.0, most - 0.5 * min(max(new), most)), most, sum(lens), COSTS)
+
+
+def shared_form(prefix, members, hq, hkv):
+    return _least(members * (hq // hkv), 1, hkv, prefix, prefix, prefix, SHARED_COSTS)
+
+
+def _least(rows, sources, hkv, mean, most, total, costs):
     memory = total * hkv * 512 / 6e6
     best = None
-    for v, (item, step, keys) in enumerate(COSTS):
-        items = max(len(lens), -(-rows // (32 << v))) * hkv
+    for v, (item, step, keys) in enumerate(costs):
+        items = max(sources, -(-rows // (32 << v))) * hkv
         for s in SPLITS:
             if s > 1 and s * keys > most:
                 break
             run = max(math.ceil(most / (s * keys)) * step + item, math.ceil(items * s / 256) * (mean / (s * keys) * step + item))
             t = max(run, memory) + 0.5 * min(run, memory)
-            if s > 1:
+            if costs is SHARED_COSTS:
+                t += 0.1 * s
+            elif s > 1:
                 t += 4 + 0.15 * s + rows * hkv * s * (2 * 520) / 4.5e6
             if best is None or t < best[0]:
                 best = (t, 32 << v, s)
@@ -165,6 +176,87 @@ def test_split_256_row_form_with_values_that_are_not_finite(docs, alibi):
         assert torch.isnan(got[nan]).all()
         R.close(torch.where(finite, got, 0.0), torch.where(finite, o, 0.0), torch.where(finite, R.tolerance_bf16(ma, off, o), 1e-30),
                 f"out h={h}")
+
+
+SHARED = [  # form, tokens of the prefix, its sequences, heads
+    ((32, False), 5, 300, 8, 8), ((32, True), 333, 3, 8, 2), ((64, False), 100, 512, 32, 8), ((64, True), 1000, 150, 32, 8),
+    ((128, False), 45, 262, 64, 8), ((128, True), 1000, 200, 32, 8), ((256, False), 17, 262, 64, 8), ((256, True), 100, 512, 64, 8),
+]
+
+
+def _known_shared(case):
+    (rows, split), *shape = case
+    r, s = shared_form(*shape)
+    assert (r, s > 1) == (rows, split)
+    return shape
+
+
+@pytest.mark.parametrize("case", SHARED)
+def test_shared_cases_take_the_forms_that_they_name(case):
+    """(On the CPU.)  The workspace is that of a decode and the sums of every split."""
+    import ctypes
+
+    import paper_2502_12216_amd as T
+    prefix, members, hq, hkv = _known_shared(case)
+    batch = T.RaggedBatch([i % 4 for i in range(members)], hq, hkv, device="cpu")
+    shape = batch.struct()
+    rest = T.SharedPrefixDecoder(batch, [prefix], [0] * members).workspace.numel() - \
+        T.lib().tactic_scored_decode_workspace_size(ctypes.byref(shape), 0)
+    assert 0 <= rest - shared_form(prefix, members, hq, hkv)[1] * members * hq * (512 + 8) < 512
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kw", [dict(), dict(cap=20.0), dict(page=16, alibi=True)])
+@pytest.mark.parametrize("case", [c for c in SHARED if c[0] in ((32, False), (32, True), (128, False), (256, False))])
+def test_shared_forms(case, kw):
+    _shared_row_tiles(*_known_shared(case), kw)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("page", [0, 24])
+@pytest.mark.parametrize("scale", [1.0, 64.0])
+@pytest.mark.parametrize("case", SHARED)
+def test_shared_forms_with_values_that_are_not_finite(case, scale, page):
+    """Every sequence sees all of the prefix: what is not finite there reaches each of them, in full tiles and in the
+    last one, which is looked over; with scores of hundreds (scale) most weights are below the range of 32 bits."""
+    import paper_2502_12216_amd as T
+    n, members, hq, hkv = _known_shared(case)
+    lens = [i % 3 for i in range(members)]
+    batch = T.RaggedBatch(lens, hq, hkv)
+    Kp, Vp, q = _randn(1, hkv, n, 128, scale=scale), _randn(2, hkv, n, 128), _randn(3, members, hq, 128, scale=2.0)
+    K, V = _randn(4, hkv, batch.total, 128, scale=scale), _randn(5, hkv, batch.total, 128)
+    Vp[0, n - 1, 3] = float("inf")
+    Vp[0, n // 2, 7] = float("nan")
+    Vp[1, 0, 9] = -float("inf")
+    Vp[1, n - 2, 11], Vp[1, n // 3, 11] = float("inf"), -float("inf")
+    dec = T.SharedPrefixDecoder(batch, [n], [0] * members)
+    if page:
+        parts = []
+        for k, v, m in ((Kp, Vp, [n]), (K, V, lens)):
+            a, table = R.pages(k, m, page, 1)
+            parts.append(T.PagedCache(a, R.pages(v, m, page, 1)[0], table))
+        out, lse = dec.paged(q, *parts)
+    else:
+        out, lse = dec(q, Kp, Vp, K, V)
+    torch.cuda.synchronize()
+    own = torch.as_tensor(lens, device=DEV)
+    of = torch.repeat_interleave(torch.arange(members, device=DEV), own)
+    seen = torch.cat([torch.ones(members, n, dtype=torch.bool, device=DEV), of[None] == torch.arange(members, device=DEV)[:, None]], 1)
+    pos = torch.zeros(max(members, n + len(of)), dtype=torch.int64, device=DEV)
+    for h in range(hq):
+        g = h * hkv // hq
+        v = torch.cat([Vp[g], V[g]]).double()
+        o, l, p, ma, off = R.attend(q[:, h], torch.cat([Kp[g], K[g]]), torch.nan_to_num(v, 0.0, 0.0, 0.0), pos[:members],
+                                    pos[:n + len(of)], seen)
+        R.close(lse[:, h], l, R.tolerance_lse(off, l), f"lse h={h}")
+        got, nan = out[:, h].double(), torch.isnan(v).any(0)
+        up, down = (v == float("inf")).any(0), (v == -float("inf")).any(0)
+        assert torch.isnan(got[:, nan | (up & down)]).all()
+        finite = ~(nan | up | down)
+        R.close(got[:, finite], o[:, finite], R.tolerance_fp32(ma, off, o)[:, finite], f"out h={h}")
+        for value, only in ((float("inf"), up & ~down), (-float("inf"), down & ~up)):
+            x, weight = got[:, only], (p @ (v == value).double())[:, only]
+            assert ((x == value) | (torch.isnan(x) & (weight < 2.0 ** -100))).all(), h
 
 
 @pytest.mark.gpu
