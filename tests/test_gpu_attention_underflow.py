@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from tests import attention_ref as R
-from tests.test_gpu_attention import DEV, _batch, _randn, check_prompt
+from tests.test_gpu_attention import DEV, _batch, _randn, check_decode, check_prompt
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +55,23 @@ def test_seen_infinity_without_a_weight(value, odd):
     for h in range(hq):
         o, _, _, ma, off = R.attend(q[:, h], K[h // 2], clean[h // 2], pos, pos, seen)
         R.close(ref[:, h], o, R.tolerance_bf16(ma, off, o), f"h={h}")
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(docs=90), dict(alibi=True, positions=True, add=True), dict(page=16, cap=500.0), dict(page=7, docs=300)])
+@pytest.mark.parametrize("lens", [[700, 1, 0, 2049], [33000]])
+@pytest.mark.parametrize("hq,hkv", [(2, 2), (4, 2), (8, 2), (16, 2)])
+def test_decode_of_seen_nan_without_a_weight(hq, hkv, lens, kw):
+    """Scores of hundreds: a NaN value reaches the query that sees it from any lane group, wave or split."""
+    def spoil(K, V, document, qd):
+        K.mul_(64.0)
+        V[0, 3, 5], V[0, 500, 6], V[0, 640:699, 8] = (float("nan"),) * 3
+        V[1, 650, 64] = float("nan")
+    check_decode(lens, hq, hkv, spoil=spoil, **kw)
+
+
+def test_decode_of_seen_nan_where_the_last_rows_have_all_the_weight():
+    """A share of the rows, and every lane group of it but the last, has a weight of 0."""
+    def spoil(K, V, document, qd):
+        K[:, :-1] *= 200.0
+        V[:, 10::1000, 3] = float("nan")
+    check_decode([33000], 8, 2, spoil=spoil)
