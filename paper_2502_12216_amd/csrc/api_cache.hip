@@ -207,14 +207,19 @@ tactic_status prompt_impl(const uint16_t* q, const uint16_t* K, const uint16_t* 
   hipError_t e = hipSuccess;
   if (a.documents)
     e = tactic::launch_doc_range(a.documents, a.kv_indptr, a.seq_len, a.n_src, p.range_stride, reinterpret_cast<int2*>(ws + p.ranges), stream);
-  // Documents give row tiles of any length in any order: with more than three for each
-  // compute unit the long ones are started first (two small kernels, 14 us; capped, 32
-  // heads on 8, without and with: 3 x 2500 tokens, documents of 500 on average, 149 and
-  // 131 us; 4 x 1500, of 300, 122 and 113; 16000 + 8192 + 5001, of 1100, 1147 and 1099;
-  // 8 x 800, of 100, 80 and 81)
-  if (e == hipSuccess && a.documents && p.plan.tiles * a.Hkv * a.splits > 3 * 256) {
+  // Documents give row tiles of any length in any order.  Where the form that skips what
+  // they leave out (256 rows to an item, keys not split) has more than one and a half
+  // items for each compute unit, and sequences of more than four key tiles, the long ones
+  // are started first: two small kernels, 14 us, part of them beside the attention.
+  // Without and with, us a call, cap, 32 heads on 8: 16000 + 8192 + 5001 tokens, documents of 1100 on
+  // average 840, 808; of 300 484, 444; 3 x 2500 (of 500) 147, 121; 5000 (of 500) 114, 97;
+  // 4096 (of 300) 85, 84; 3 x 1200 (of 300) 72, 57; 6 x 800 (of 200) 67, 69; 8 x 800 (of 100) 87, 79;
+  // 30 x 250 84, 90; 20 x 120 36, 40; one item a unit: 2000 on 12000 79, 86.  The other forms go
+  // through every tile and lose by it: 12000 tokens in three, 8 heads on 2, 234, 287; 8192 267, 416.
+  const bool in_order = a.documents && p.plan.variant == 3 && a.splits == 1 && p.plan.tiles * a.Hkv > 384 && shape->max_seq_len > 256;
+  if (e == hipSuccess && in_order) {
     int4* order = reinterpret_cast<int4*>(ws + p.order);
-    e = tactic::launch_item_order(a, p.plan.variant, (int)p.plan.tiles, reinterpret_cast<int4*>(ws + p.items),
+    e = tactic::launch_item_order(a, (int)p.plan.tiles, reinterpret_cast<int4*>(ws + p.items),
                                   reinterpret_cast<int32_t*>(ws + p.counts), order, stream);
     a.order = order;
   }

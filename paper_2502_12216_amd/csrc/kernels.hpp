@@ -259,8 +259,7 @@ struct JoinArgs {
 int rows_per_item(int variant);
 hipError_t launch_doc_range(const int32_t* documents, const int64_t* kv_indptr, const int64_t* seq_len, int batch,
                             int64_t max_tiles, int2* out, hipStream_t st);
-hipError_t launch_item_order(const RowsArgs& a, int variant, int tiles, int4* items, int32_t* counts, int4* order,
-                             hipStream_t st);
+hipError_t launch_item_order(const RowsArgs& a, int tiles, int4* items, int32_t* counts, int4* order, hipStream_t st);
 hipError_t launch_rows_attn(const RowsArgs& a, int variant, bool exact_weights, int64_t items, hipStream_t st);
 hipError_t launch_rows_combine(const RowsArgs& a, hipStream_t st);
 

@@ -174,7 +174,7 @@ void rows_attn_kernel(RowsArgs a) {
   const int split = rest % a.splits;
   rest /= a.splits;
   int src, i_lo = INT32_MAX, i_hi = INT32_MIN;  // and the documents of the item's queries
-  const bool ordered = kDocs && a.order;
+  const bool ordered = kDocs && RW == 8 && a.order;  // (only the form of 256 rows is started in order)
   if (ordered) {
     const int4 item = a.order[rest];
     rest = item.x;
@@ -583,7 +583,7 @@ void rows_attn_kernel(RowsArgs a) {
     // which keys the row sees, by the masks: a weight may be 0 without one (bit r + 16 kb as
     // in soft; by arithmetic and four at a time, since the masks of comparisons and more
     // registers here are spilled by the loops above: 128 rows with documents in pages, 3001
-    // tokens, 32 heads on 8, 218 us that way, 200 now, 193 where a weight of 0 counted as masked)
+    // tokens, 32 heads on 8, 218 us that way, 196 now, 193 where a weight of 0 counted as masked)
     static_assert(NB <= 2, "a bit per key");
     const int lim = klim - t * TK - 4 * half;
     uint32_t seen = 0;
@@ -875,7 +875,8 @@ __global__ __launch_bounds__(64) void doc_range_kernel(const int32_t* documents,
 
 // Key tiles (of 64) that each row tile's queries may see: what its documents leave of
 // them.  A wave per row tile.
-__global__ __launch_bounds__(256) void doc_items_kernel(RowsArgs a, int rows, int tiles, int4* items, int32_t* counts) {
+__global__ __launch_bounds__(256) void doc_items_kernel(RowsArgs a, int tiles, int4* items, int32_t* counts) {
+  constexpr int rows = 256;  // of an item
   const int lane = threadIdx.x & 63, rest = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (rest >= tiles) return;
   const int src = source_of(a, rows, rest, lane);
@@ -997,9 +998,8 @@ hipError_t launch_doc_range(const int32_t* documents, const int64_t* kv_indptr, 
   return hipGetLastError();
 }
 
-hipError_t launch_item_order(const RowsArgs& a, int variant, int tiles, int4* items, int32_t* counts, int4* order,
-                             hipStream_t st) {
-  hipLaunchKernelGGL(doc_items_kernel, dim3((tiles + 3) / 4), dim3(256), 0, st, a, rows_per_item(variant), tiles, items, counts);
+hipError_t launch_item_order(const RowsArgs& a, int tiles, int4* items, int32_t* counts, int4* order, hipStream_t st) {
+  hipLaunchKernelGGL(doc_items_kernel, dim3((tiles + 3) / 4), dim3(256), 0, st, a, tiles, items, counts);
   hipLaunchKernelGGL(item_order_kernel, dim3(1), dim3(1024), 0, st, items, counts, tiles, order);
   return hipGetLastError();
 }
