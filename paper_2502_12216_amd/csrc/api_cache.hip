@@ -66,7 +66,8 @@ struct RowsPlan {
 // `item` us and `step` us for each round of its waves' tiles (`keys` keys); a compute
 // unit runs one at a time (two of the smallest, at half the pace); the keys come once
 // from memory, half of the shorter of the two hidden behind the longer.  Splits are
-// joined by a second kernel: 4 us, and their sums written and read.  Measured with 32 /
+// joined by a second kernel: 4 us, and their sums written and read.  Every sequence counts as
+// the longest, and documents as all seen.  Measured with 32 /
 // 8 and 8 / 2 heads (us a call, tiles of 32, 64, 128, 256 rows with the best splits of
 // each): prompts of 211 tokens 11, 12, 14, 15; 1000 tokens, 2 KV heads 16, 21, 24, 24;
 // 2048 tokens 74, 85, 56, 65; 4096 tokens 245, 263, 180, 151; one token on 32768 34,

@@ -797,9 +797,11 @@ __global__ __launch_bounds__(1024) void insert_heads_kernel(InsertArgs a) {
 }
 
 hipError_t launch_insert(const InsertArgs& a, int64_t max_len, hipStream_t st) {
-  // One launch while one compute unit reads the heads' rows in about that time: one
-  // against two, us a call in a stream and in a graph: 2 heads of 1000 rows 10.0, 3.6 and 12.2,
-  // 5.1; 8 of 2048 10.3, 6.6 and 12.5, 5.5; 8 of 4096 10.3, 8.9 and 12.4, 5.7; 8 of 8192 14.5, 14.4 and 12.1, 6.5
+  // One launch or two, us a call in a stream and in a graph: 2 heads of 1000 rows 10.0, 3.6 and
+  // 12.2, 5.1; 8 of 2048 10.3, 6.6 and 12.5, 5.5; 8 of 4096 10.3, 8.9 and 12.4, 5.7; 8 of 8192 14.5,
+  // 14.4 and 12.1, 6.5.  In a stream the second launch costs the host 2 us up to 8 of 4096, in
+  // a graph the one launch's compute unit is the slower from 8 of about 1500 on: the limit lies
+  // between, where the one gains 2.2 in a stream and loses 1.1 in a graph.
   if (a.Hkv <= 16 && max_len * a.Hkv <= 16384) {
     hipLaunchKernelGGL(insert_heads_kernel, dim3(a.B), dim3(1024), 0, st, a);
     return hipGetLastError();

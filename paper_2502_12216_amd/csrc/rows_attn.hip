@@ -148,8 +148,9 @@ __device__ __forceinline__ int2 docs_of(const int2* dr, int p0, int p1, int lane
 // product of 8192^3 reaches 1.11), 2250 to 2320 with slopes, 2480 to 2540 with a cap, whose polynomial
 // competes with the exponential for the vector unit.  512 tokens on 65536 in pages, with
 // slopes: 609 us, 0.90 PFLOP/s.  Packed documents (29193 tokens, 1100 on average, cap):
-// 800 us, 0.60, bound by each item's start and end (12 of 84 us: the chain from the item's
-// record to the first keys, the waves' last turn) and by tiles that are masked in part.  A prefix of 32768 tokens and 32
+// 800 us, 0.60: the tiles hold 1.09 of the pairs that count, the cap takes a sixth, each item's
+// start and end 12 of its 84 us (the chain from the item's record to the first keys, the waves'
+// last turn), the kernels ahead 14, the tiles masked in part (16%) and uneven ends the rest.  A prefix of 32768 tokens and 32
 // sequences: 47 us, by the matrix unit (the weights' three parts make the products twice as
 // many) and HBM (2.9 TB/s) together.
 template <int RW, int KW, int TK, int PARTS, bool kPaged, bool kDocs>
@@ -248,7 +249,9 @@ void rows_attn_kernel(RowsArgs a) {
   load_q();
 
   // Documents: ranges of each 64-key tile (from doc_range_kernel).  i_lo, i_hi: of the
-  // tiles that the item's queries lie in; a tile outside is left out.  Ranges are read
+  // tiles that the item's queries lie in; a tile outside is left out by the forms of 32
+  // and 256 rows, and masked by the others, whose groups of waves go by fixed rounds (8192
+  // tokens, 8 heads on 2, documents of 300: 237 us, 178 without documents).  Ranges are read
   // 64 tiles at a time, into masks of the tiles that may hold a seen key, of those whose
   // keys all are of the wave's one document, and of those where that holds for the item.
   const int2* dr = kDocs ? a.doc_range + (int64_t)src * a.range_stride : nullptr;
