@@ -200,7 +200,7 @@ class SparseDecoder:
     def __init__(self, batch: RaggedBatch, n_clusters: Sequence[int], params: Optional[C.DecodeParams] = None,
                  device="cuda", workspace: Optional[torch.Tensor] = None):
         """workspace: a uint8 device tensor to use if it is large enough (for
-        instance a previous decoder's), else a new one is allocated."""
+        instance a previous decoder's) and contiguous, else a new one is allocated."""
         self.batch = batch
         self.params = params if params is not None else decode_params()
         self.n_clusters = [int(x) for x in n_clusters]
@@ -212,7 +212,9 @@ class SparseDecoder:
                                                   ctypes.byref(self.params), ctypes.byref(self.plan),
                                                   ctypes.byref(nbytes)), "tactic_sparse_decode_plan")
         need = max(1, nbytes.value)
-        if workspace is not None and workspace.dtype == torch.uint8 and workspace.is_cuda and workspace.numel() >= need:
+        # (a view that repeats or skips bytes is not as much memory as it has elements)
+        if (workspace is not None and workspace.dtype == torch.uint8 and workspace.is_cuda and workspace.numel() >= need and
+                workspace.is_contiguous()):
             self.workspace = workspace
         else:
             self.workspace = torch.empty(need, dtype=torch.uint8, device=device)

@@ -67,3 +67,14 @@ def test_append_off_its_alignment_leaves_the_cache():
     for x, y in zip((c.K, c.V, c.weights, c.positions, c.newest, c.batch.seq_len), state):
         assert torch.equal(x, y)
     assert c.batch.seq_lens == [1]
+
+
+def test_sparse_decoder_takes_a_workspace_of_one_piece_only():
+    import paper_2502_12216_amd as T
+    batch = T.RaggedBatch([900, 300], 8, 2)
+    size = T.SparseDecoder(batch, [20, 10]).workspace.numel()
+    whole = torch.zeros(2 * size, dtype=torch.uint8, device=DEV)
+    assert T.SparseDecoder(batch, [20, 10], workspace=whole).workspace is whole
+    for bad in (torch.zeros(1, dtype=torch.uint8, device=DEV).expand(size), whole[::2], whole[:size - 1]):
+        got = T.SparseDecoder(batch, [20, 10], workspace=bad).workspace
+        assert got is not bad and got.is_contiguous() and got.numel() == size
