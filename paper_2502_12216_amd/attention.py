@@ -49,7 +49,11 @@ class _Call:
         return cache.struct()
 
     def run(self, name: str, *args):
-        s = self.stream if self.stream is not None else torch.cuda.current_stream(self.device)
+        s = self.stream
+        if s is None:
+            s = torch.cuda.current_stream(self.device)
+        elif s.device != self.device:
+            raise ValueError(f"the stream is on {s.device}, expected {self.device}")
         f = getattr(C.lib(), name)
         if torch.cuda.current_device() == self.device.index:
             status = f(*args, s.cuda_stream)

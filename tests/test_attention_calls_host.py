@@ -130,3 +130,14 @@ def test_shared_prefixes_of_more_workgroups_than_a_launch_has(n):
     pre = C.Prefixes(n, 2, 500, 300, 0x1000, 0x1000, 0x1000, 0x1000, 2)
     assert shared(pre=pre) == 2
     assert b"workgroups" in C.lib().tactic_last_error()
+
+
+def test_a_stream_of_another_device_is_refused(monkeypatch):
+    from types import SimpleNamespace
+
+    from paper_2502_12216_amd import attention as A
+    here, there = torch.device("cuda", 0), torch.device("cuda", 1)
+    call = A._Call(here, SimpleNamespace(device=there, cuda_stream=0))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(ValueError, match="stream"):
+        call.run("tactic_last_error")
