@@ -170,10 +170,10 @@ class EvictingCache:
         self.Hq, self.Hkv, self.budget, self.recent = int(n_q_heads), int(n_kv_heads), int(budget), int(recent)
         self.window = int(window)
         self.mod = ScoreMod(cap=cap, slopes=slopes)
-        self.device = device
         self.batch = RaggedBatch([0] * int(batch), self.Hq, self.Hkv, device=device, capacities=[self.budget] * int(batch))
         self.K = torch.zeros(self.Hkv, self.batch.total, 128, dtype=torch.bfloat16, device=device)
         self.V = torch.zeros_like(self.K)
+        self.device = self.K.device  # ("cuda" is the device that is current now)
         self.weights = torch.zeros(self.Hkv, self.batch.total, dtype=torch.float32, device=device)
         self.positions = torch.zeros(self.Hkv, self.batch.total, dtype=torch.int32, device=device)
         self.newest = torch.full((int(batch),), -1, dtype=torch.int32, device=device)  # the last token's position

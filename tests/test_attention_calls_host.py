@@ -141,3 +141,9 @@ def test_a_stream_of_another_device_is_refused(monkeypatch):
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     with pytest.raises(ValueError, match="stream"):
         call.run("tactic_last_error")
+
+
+def test_evicting_cache_stays_on_the_device_it_was_made_on():
+    """Not on whichever is current at a later prefill ("cuda" names that one)."""
+    c = T.EvictingCache(8, 2, 2, 16, recent=4, device="cpu")
+    assert isinstance(c.device, torch.device) and c.device == c.K.device
