@@ -78,3 +78,12 @@ def test_sparse_decoder_takes_a_workspace_of_one_piece_only():
     for bad in (torch.zeros(1, dtype=torch.uint8, device=DEV).expand(size), whole[::2], whole[:size - 1]):
         got = T.SparseDecoder(batch, [20, 10], workspace=bad).workspace
         assert got is not bad and got.is_contiguous() and got.numel() == size
+
+
+@pytest.mark.parametrize("lens", [[0, 50, 1], [0, 0, 70]])
+def test_evicting_cache_of_empty_prompts(lens):
+    """Sequences that start from nothing beside others, through prompt, eviction, insertion and decode."""
+    import paper_2502_12216_amd as T
+    from tests import attention_ref as R
+    from tests.test_gpu_evict import _loop
+    _loop(T.EvictingCache(8, 2, 3, 8, recent=3, cap=30.0, slopes=R.slopes(8)), lens, 8, 2, 12)
