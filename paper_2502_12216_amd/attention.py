@@ -79,7 +79,7 @@ def _workspace(nbytes: int, name: str, device, workspace: Optional[torch.Tensor]
 
 
 class ScoreMod:
-    """How scores are formed (see tactic_score_mod): cap > 0 caps them by cap tanh(s / cap);
+    """How scores are formed (see tactic_score_mod): cap in [2^-120, 2^120] caps them by cap tanh(s / cap), 0 is none;
     slopes fp32 [Hq] subtract slope |distance|; documents int32 [total] let a query see its own
     document only; prefix_len int32 [B] (prompts) lets every query see so many first tokens."""
 

@@ -23,7 +23,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 // where the products take four; the cap adds five); with few queries by reading K.
 // Four waves that run free, two workgroups to a compute unit: eight that take turns at
 // the products, as the attention's do, are slower where the vector unit has more to do
-// (8192 queries, 32 heads on 8, capped: 590 us against 500; not capped 393 against 391; both before rows of NaN were looked for, 2%).
+// (8192 queries, 32 heads on 8, capped: 590 us against 500; not capped 393 against 391; both before rows of NaN and left-out ones were looked for, 3%).
 // grid (key tiles + sequences, Hkv, splits of the rows)
 // ---------------------------------------------------------------------------
 constexpr int kWKeys = 256, kWRows = 64;

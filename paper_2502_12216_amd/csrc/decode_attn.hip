@@ -479,7 +479,7 @@ void attn_splitk_kernel(AttnArgs a, std::conditional_t<kMod != 0, TokenMod, NoMo
           if (mod.slopes) {
             int kpos = base + (int)(p0 + t);
             if constexpr (kMod == 2) kpos = mod.positions ? x.pos[i] : kpos;
-            uint32_t dist;  // of any two positions, from the least one: |x - y| of 32 bits, one instruction
+            uint32_t dist;  // of any two positions: |x - y| of both counted from the least int32
             asm("v_sad_u32 %0, %1, %2, 0" : "=v"(dist) : "v"((uint32_t)qpos ^ 0x80000000u), "v"((uint32_t)kpos ^ 0x80000000u));
             v = fmaf(-slope2, (float)dist, v);
           }
