@@ -458,6 +458,73 @@ tactic_status tactic_insert_token(const uint16_t* k, const uint16_t* v, const in
                                   const tactic_kv_shape* shape, int64_t* seq_len, uint16_t* K, uint16_t* V,
                                   float* weights, int32_t* positions, int32_t* rows, hipStream_t stream);
 
+/* ---- A cache of 8 or 4 bits a value: half or a quarter of the bytes that a decode
+ * reads.  A row of 128 values is four groups of 32 with a power of two each, the byte
+ * s + 127: the least s whose largest number M 2^s is not below the group's largest
+ * value.  8 bits: e4m3 (M = 448), s in [-117, 119]; 4 bits: e2m1 (M = 6), s in
+ * [-125, 125], the first of two values in the lower half of a byte.  A value is the
+ * number nearest to it, ties to even, held to M 2^s; a group with a value that is not
+ * finite has the byte 255 and reads as NaN.  Every value read is a bf16 exactly.
+ *
+ * Blocks: rows [j block, (j + 1) block) of a sequence.  bounds holds the least and the
+ * largest value of every dimension of a block's keys, as they read; the blocks of
+ * sequence b are at kv_indptr[b] / block + b and on. */
+typedef struct {
+  uint8_t* K;                  /* device [Hkv][total_tokens][16 * bits], or pages
+                                  [num_pages][Hkv][page_size][16 * bits] */
+  uint8_t* K_scale;            /* device [..][4] of the same rows */
+  uint8_t* V;
+  uint8_t* V_scale;
+  uint16_t* bounds;            /* device bf16 [Hkv][total_tokens / block + B][2][128] or NULL */
+  const int32_t* page_table;   /* device [B][max_pages] as in tactic_paged_kv, or NULL: no pages */
+  int32_t bits;                /* 8 or 4 */
+  int32_t block;               /* 16, 32, 64 or 128; 0 without bounds */
+  int32_t page_size;           /* the next three as in tactic_paged_kv, with page_table only */
+  int32_t max_pages;
+  int64_t num_pages;
+} tactic_quant_kv;
+
+/* Writes the last m_b rows of every sequence (rows->q_indptr counts them, as queries in
+ * tactic_prompt_attention: row i of m is row n_b - m + i, those ahead of the first are
+ * left out): a prompt, a chunk, or a new token behind lengths that were advanced.
+ * k, v: bf16 [rows->total_queries][Hkv][128].  With bounds, those of every block that has
+ * a new row are set from the rows of the block up to the sequence's last.  A row whose
+ * table entry is out of range is not written; no two sequences may write one page row. */
+tactic_status tactic_quant_write(const uint16_t* k, const uint16_t* v, const tactic_kv_shape* shape,
+                                 const tactic_query_shape* rows, const tactic_quant_kv* kv, hipStream_t stream);
+/* The same rows in bf16 again, [Hkv][rows->total_queries][128] each (as the attention of a
+ * prompt takes them); rows ahead of a sequence's first, and of pages that are not there, are zeros. */
+tactic_status tactic_quant_read(const tactic_quant_kv* kv, const tactic_kv_shape* shape,
+                                const tactic_query_shape* rows, uint16_t* K_out, uint16_t* V_out,
+                                hipStream_t stream);
+
+/* The blocks that a token looks at: those of the `budget` largest scores of every KV
+ * head, the `first` first and `last` last ones of the sequence always among them.
+ *     u_hj  = sum over d of max(q_d lo_jd, q_d hi_jd)      (products and sums in 64 bits)
+ *     score = max over the group's heads of u_hj - max_i u_hi
+ * Ties go to the lower block; a score of NaN is above all others. */
+typedef struct {
+  int32_t budget;              /* blocks at most, >= 1 */
+  int32_t first, last;         /* >= 0, together at most budget */
+} tactic_block_params;
+/* kv: the bounds and the block are read, not the rows.
+ *   blocks int32 [B][Hkv][budget]: the chosen ones, ascending, then -1
+ *   counts int32 [B][Hkv]: how many */
+size_t tactic_block_select_workspace_size(const tactic_kv_shape* shape, int32_t block);
+tactic_status tactic_block_select(const uint16_t* q, const tactic_quant_kv* kv, const tactic_kv_shape* shape,
+                                  const tactic_block_params* params, int32_t* blocks, int32_t* counts,
+                                  void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Single tokens over such a cache: out fp32 [B][Hq][128], lse fp32 [B][Hq] or NULL, scores
+ * as above (mod, or NULL, may hold a cap and slopes; the query is at position n_b - 1).
+ * blocks, counts (both or neither): only the rows of these blocks of kv->block rows, as
+ * tactic_block_select gives them with this budget (0 without); other lists have to be
+ * ascending and without -1 up to the count.  Workspace: as tactic_dense_decode_workspace_size. */
+tactic_status tactic_quant_decode(const uint16_t* q, const tactic_quant_kv* kv, const tactic_kv_shape* shape,
+                                  const tactic_score_mod* mod, const int32_t* blocks, const int32_t* counts,
+                                  int32_t budget, float* out, float* lse, void* workspace,
+                                  size_t workspace_bytes, hipStream_t stream);
+
 /* Measurement helper, not part of the method: reads every 16-byte word of
  * `buf` (bytes, a multiple of 16) once with streaming loads from `workgroups`
  * workgroups of 256 threads (0: as many as fit on the device at once) and

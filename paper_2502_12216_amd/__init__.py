@@ -8,4 +8,5 @@ from .tactic import (ClusterBuild, ClusterBuilder, ClusterSet, DenseDecoder, Pag
                      SparseDecoder, decode_params, sparse_decode_workspace_bytes, stream_read_gbps)
 from .attention import (CacheEvictor, PromptAttention, ScoredDecoder, ScoreMod, SharedPrefixDecoder,  # noqa: F401
                         TokenInserter)
-from .cache import EvictingCache, RecentTailCache  # noqa: F401
+from .quant import BlockSelector, CacheQuantizer, QuantizedCache, QuantizedDecoder  # noqa: F401
+from .cache import EvictingCache, QuantizingCache, RecentTailCache  # noqa: F401

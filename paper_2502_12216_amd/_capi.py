@@ -29,6 +29,8 @@ EXPORTS = (
     "tactic_prompt_weights", "tactic_scored_decode_workspace_size", "tactic_scored_decode",
     "tactic_scored_decode_paged", "tactic_shared_decode_workspace_size", "tactic_shared_decode",
     "tactic_shared_decode_paged", "tactic_evict_workspace_size", "tactic_evict", "tactic_insert_token",
+    "tactic_quant_write", "tactic_quant_read", "tactic_quant_decode", "tactic_block_select_workspace_size",
+    "tactic_block_select",
 )
 
 
@@ -86,6 +88,16 @@ class Prefixes(ctypes.Structure):
                 ("member_indptr", c_void_p), ("total_members", c_int32)]
 
 
+class QuantKV(ctypes.Structure):
+    _fields_ = [("K", c_void_p), ("K_scale", c_void_p), ("V", c_void_p), ("V_scale", c_void_p), ("bounds", c_void_p),
+                ("page_table", c_void_p), ("bits", c_int32), ("block", c_int32), ("page_size", c_int32),
+                ("max_pages", c_int32), ("num_pages", c_int64)]
+
+
+class BlockParams(ctypes.Structure):
+    _fields_ = [("budget", c_int32), ("first", c_int32), ("last", c_int32)]
+
+
 class TacticError(RuntimeError):
     pass
 
@@ -141,6 +153,7 @@ def lib() -> ctypes.CDLL:
     L.tactic_probe_stream_read.restype = c_int
     shape, mod, ws = POINTER(KVShape), POINTER(ScoreMod), [c_void_p, c_size_t, c_void_p]
     queries, rows, pre, paged = POINTER(QueryShape), POINTER(TokenRows), POINTER(Prefixes), POINTER(PagedKV)
+    quant, blocks = POINTER(QuantKV), POINTER(BlockParams)
     for name, args in {
             "tactic_prompt_attention": [c_void_p] * 3 + [shape, queries, mod, c_void_p, c_void_p] + ws,
             "tactic_prompt_attention_paged": [c_void_p, paged, shape, queries, mod, c_void_p, c_void_p] + ws,
@@ -152,6 +165,10 @@ def lib() -> ctypes.CDLL:
             "tactic_evict": [c_void_p, c_void_p, shape] + [c_void_p] * 4 + [c_int32, c_void_p, c_int64, c_int64] +
                             [c_void_p] * 5 + ws,
             "tactic_insert_token": [c_void_p] * 3 + [c_int32, shape] + [c_void_p] * 7,
+            "tactic_quant_write": [c_void_p, c_void_p, shape, queries, quant, c_void_p],
+            "tactic_quant_read": [quant, shape, queries] + [c_void_p] * 3,
+            "tactic_quant_decode": [c_void_p, quant, shape, mod, c_void_p, c_void_p, c_int32, c_void_p, c_void_p] + ws,
+            "tactic_block_select": [c_void_p, quant, shape, blocks, c_void_p, c_void_p] + ws,
     }.items():
         getattr(L, name).argtypes = args
         getattr(L, name).restype = c_int
@@ -160,6 +177,7 @@ def lib() -> ctypes.CDLL:
             "tactic_scored_decode_workspace_size": [shape, c_int32],
             "tactic_shared_decode_workspace_size": [shape, pre],
             "tactic_evict_workspace_size": [shape, c_int64],
+            "tactic_block_select_workspace_size": [shape, c_int32],
     }.items():
         getattr(L, name).argtypes = args
         getattr(L, name).restype = c_size_t
@@ -178,6 +196,6 @@ def check(status: int, what: str) -> None:
                           f"{L.tactic_last_error().decode()} (status {status})")
 
 
-__all__ = ["KVShape", "ScoreMod", "QueryShape", "TokenRows", "Prefixes", "ClusterMeta", "DecodeParams", "DecodePlan", "DecodeView", "KMeansParams", "PagedKV",
+__all__ = ["KVShape", "ScoreMod", "QueryShape", "TokenRows", "Prefixes", "QuantKV", "BlockParams", "ClusterMeta", "DecodeParams", "DecodePlan", "DecodeView", "KMeansParams", "PagedKV",
            "TacticError", "lib", "check", "EXPORTS", "LIB_PATH", "FIT_FIELDS", "FIT_NAMES", "NOALLOC_SCRATCH_BYTES",
            "c_double"]

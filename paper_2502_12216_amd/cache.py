@@ -17,7 +17,8 @@ import numpy as np
 import torch
 
 from .attention import CacheEvictor, PromptAttention, ScoredDecoder, ScoreMod, TokenInserter
-from .tactic import (ClusterBuilder, ClusterSet, DenseDecoder, RaggedBatch, SparseDecoder, decode_params,
+from .quant import BlockSelector, CacheQuantizer, QuantizedCache, QuantizedDecoder
+from .tactic import (ClusterBuilder, ClusterSet, DenseDecoder, RaggedBatch, SparseDecoder, _check_tensor, decode_params,
                      sparse_decode_workspace_bytes)
 
 
@@ -226,3 +227,67 @@ class EvictingCache:
         out, _ = self.decoder(q, self.K, self.V, self.mod, positions=self.positions, q_pos=self.newest,
                               weights=self.weights)
         return out
+
+
+class QuantizingCache:
+    """One layer's KV cache of 8 or 4 bits a value, for a batch decoded in lockstep.
+
+    extend() attends a chunk of every prompt in bf16 - its own tokens and the cached ones as the cache
+    holds them - and keeps it; append() adds one token per sequence; decode() attends all rows, or with a
+    `budget` those of the blocks of `block` rows that the token's cheap score chooses."""
+
+    def __init__(self, n_q_heads: int, n_kv_heads: int, capacities: Sequence[int], bits: int = 8, block: int = 64,
+                 budget: int = 0, first: int = 1, last: int = 2, cap: float = 0.0,
+                 slopes: Optional[torch.Tensor] = None, device="cuda"):
+        self.Hq, self.Hkv = int(n_q_heads), int(n_kv_heads)
+        self.capacities = [int(c) for c in capacities]
+        self.batch = RaggedBatch([0] * len(self.capacities), self.Hq, self.Hkv, device=device, capacities=self.capacities)
+        self.device = self.batch.kv_indptr.device
+        self.cache = QuantizedCache.empty(self.batch, bits, block)
+        self.mod = ScoreMod(cap=cap, slopes=slopes)
+        self.token = CacheQuantizer(self.batch, [1] * self.batch.batch)
+        self.decoder = QuantizedDecoder(self.batch)
+        self.selector = BlockSelector(self.batch, block, budget, first, last) if budget else None
+
+    def _grow(self, new: Sequence[int]) -> List[int]:
+        lens = [n + m for n, m in zip(self.batch.seq_lens, new)]
+        if any(n > c for n, c in zip(lens, self.capacities)):
+            raise ValueError("a sequence outgrew its capacity")
+        return lens
+
+    def extend(self, q: Sequence[torch.Tensor], K: Sequence[torch.Tensor], V: Sequence[torch.Tensor]) -> torch.Tensor:
+        """q[b] bf16 [m_b][Hq][128], K[b], V[b] bf16 [m_b][Hkv][128], the next tokens of every prompt.  Returns their
+        attention, bf16 [sum m_b][Hq][128]."""
+        new = [int(k.shape[0]) for k in K]
+        if not len(new) == len(q) == len(V) == self.batch.batch:
+            raise ValueError("extend needs tokens for every sequence")
+        if [int(x.shape[0]) for x in q] != new or [int(x.shape[0]) for x in V] != new:
+            raise ValueError("a prompt's q, K and V must be of one length")
+        lens = self._grow(new)
+        qc, Kc, Vc = (torch.cat(list(x)).contiguous() for x in (q, K, V))
+        rows, held = CacheQuantizer(self.batch, new), CacheQuantizer(self.batch, lens)
+        for name, x, heads in (("q", qc, self.Hq), ("K", Kc, self.Hkv), ("V", Vc, self.Hkv)):  # (before anything is changed)
+            _check_tensor(x, name, torch.bfloat16, (rows.total, heads, 128))
+        self.batch.seq_len.copy_(torch.as_tensor(np.asarray(lens, dtype=np.int64)))
+        self.batch.seq_lens = lens
+        rows.write(Kc, Vc, self.cache)
+        full = RaggedBatch(lens, self.Hq, self.Hkv, device=self.device)
+        return PromptAttention(full, new)(qc, *held.read(self.cache), self.mod)[0]
+
+    def append(self, k: torch.Tensor, v: torch.Tensor) -> None:
+        """k, v bf16 [B][Hkv][128], the new token of every sequence.  Only device work is enqueued."""
+        lens = self._grow([1] * self.batch.batch)
+        self.batch.seq_len += 1
+        try:
+            self.token.write(k, v, self.cache)
+        except Exception:  # refused, before any of it ran
+            self.batch.seq_len -= 1
+            raise
+        self.batch.seq_lens = lens
+
+    def decode(self, q: torch.Tensor) -> torch.Tensor:
+        """Attention of q (bf16 [B][Hq][128], the last token's queries), fp32 [B][Hq][128]."""
+        if self.selector is None:
+            return self.decoder(q, self.cache, self.mod)[0]
+        blocks, counts = self.selector(q, self.cache)
+        return self.decoder(q, self.cache, self.mod, blocks=blocks, counts=counts)[0]

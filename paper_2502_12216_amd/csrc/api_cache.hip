@@ -19,13 +19,6 @@ namespace {
 constexpr int64_t kMaxInt = ((int64_t)1 << 31) - 1;
 constexpr int kMaxRecent = 1 << 22;
 
-tactic_status check_mod(const tactic_score_mod* m) {
-  // (outside, the cap's reciprocal or its value in base 2 would leave the normal numbers)
-  if (m && m->cap != 0.f && !(m->cap >= 0x1p-120f && m->cap <= 0x1p120f))
-    return fail(TACTIC_ERR_INVALID_ARG, "cap must be 0 or in [2^-120, 2^120]");
-  return TACTIC_OK;
-}
-
 // The kernels read and write rows 16 bytes at a time.
 tactic_status check_rows(std::initializer_list<const void*> arrays) {
   for (const void* p : arrays)
@@ -448,6 +441,13 @@ tactic_status shared_impl(const uint16_t* q, const uint16_t* Kp, const uint16_t*
 }
 
 }  // namespace
+
+tactic_status tactic_host::check_mod(const tactic_score_mod* m) {
+  // (outside, the cap's reciprocal or its value in base 2 would leave the normal numbers)
+  if (m && m->cap != 0.f && !(m->cap >= 0x1p-120f && m->cap <= 0x1p120f))
+    return fail(TACTIC_ERR_INVALID_ARG, "cap must be 0 or in [2^-120, 2^120]");
+  return TACTIC_OK;
+}
 
 extern "C" {
 

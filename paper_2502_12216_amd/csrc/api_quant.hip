@@ -1,0 +1,234 @@
+// Host side of the quantised cache: rows in and out, chosen blocks, single-token decode.
+#include <hip/hip_runtime.h>
+#include <string.h>
+
+#include <algorithm>
+#include <initializer_list>
+
+#include "host.hpp"
+#include "plan.hpp"
+
+using namespace tactic_host;
+using tactic::kHeadDim;
+
+namespace {
+
+constexpr int64_t kMaxInt = ((int64_t)1 << 31) - 1;
+
+tactic_status check_aligned(std::initializer_list<const void*> arrays, int bytes) {
+  for (const void* p : arrays)
+    if (reinterpret_cast<uintptr_t>(p) % bytes) return fail(TACTIC_ERR_INVALID_ARG, "an array is not %d-byte aligned", bytes);
+  return TACTIC_OK;
+}
+
+// Checks of the cache; `rows`: whether its rows are used, and not its bounds alone.
+tactic_status quant_args(const tactic_quant_kv* kv, const tactic_kv_shape* s, bool rows, tactic::QuantKV* out) {
+  if (!kv) return fail(TACTIC_ERR_INVALID_ARG, "kv is null");
+  if (kv->bits != 8 && kv->bits != 4) return fail(TACTIC_ERR_INVALID_ARG, "bits must be 8 or 4 (got %d)", kv->bits);
+  if (kv->block != 0 && kv->block != 16 && kv->block != 32 && kv->block != 64 && kv->block != 128)
+    return fail(TACTIC_ERR_INVALID_ARG, "block must be 16, 32, 64 or 128, or 0 without bounds (got %d)", kv->block);
+  if (kv->bounds && kv->block == 0) return fail(TACTIC_ERR_INVALID_ARG, "bounds need a block");
+  if (rows && s->total_tokens > 0 && (!kv->K || !kv->K_scale || !kv->V || !kv->V_scale))
+    return fail(TACTIC_ERR_INVALID_ARG, "null cache array");
+  tactic_status st;
+  if ((st = check_aligned({kv->K, kv->V, kv->bounds}, 16)) != TACTIC_OK || (st = check_aligned({kv->K_scale, kv->V_scale}, 4)) != TACTIC_OK)
+    return st;
+  *out = tactic::QuantKV{};
+  out->K = kv->K;
+  out->K_scale = kv->K_scale;
+  out->V = kv->V;
+  out->V_scale = kv->V_scale;
+  out->bounds = kv->bounds;
+  out->bits = kv->bits;
+  out->block = kv->block;
+  if (kv->page_table && rows) {
+    const tactic_paged_kv pages{reinterpret_cast<const uint16_t*>(kv->K), reinterpret_cast<const uint16_t*>(kv->V),
+                                kv->page_table, nullptr, kv->page_size, kv->max_pages, kv->num_pages};
+    if ((st = paged_args(&pages, s, &out->pk)) != TACTIC_OK) return st;
+    out->paged = 1;
+  }
+  return TACTIC_OK;
+}
+
+tactic_status check_new_rows(const tactic_query_shape* q, const tactic_kv_shape* s) {
+  if (!q) return fail(TACTIC_ERR_INVALID_ARG, "rows is null");
+  if (!q->q_indptr) return fail(TACTIC_ERR_INVALID_ARG, "q_indptr is null");
+  if (q->total_queries < 0 || q->max_queries < 0 || q->max_queries > q->total_queries || q->total_queries > q->max_queries * s->batch)
+    return fail(TACTIC_ERR_INVALID_ARG, "inconsistent total_queries / max_queries");
+  if (q->total_queries * s->n_kv_heads > kMaxInt) return fail(TACTIC_ERR_UNSUPPORTED, "total_queries * n_kv_heads >= 2^31");
+  return TACTIC_OK;
+}
+
+tactic::QuantRowsArgs rows_args(const tactic_kv_shape* s, const tactic_query_shape* rows, const tactic::QuantKV& kv) {
+  tactic::QuantRowsArgs a{};
+  a.kv_indptr = s->kv_indptr;
+  a.seq_len = s->seq_len;
+  a.row_indptr = rows->q_indptr;
+  a.B = s->batch;
+  a.Hkv = s->n_kv_heads;
+  a.total = s->total_tokens;
+  a.n_rows = rows->total_queries;
+  a.kv = kv;
+  return a;
+}
+
+struct SelectLayout {
+  int64_t max_blocks, tops, scores, top, keys, bytes;
+};
+SelectLayout select_layout(const tactic_kv_shape* s, int block) {
+  SelectLayout l{};
+  l.max_blocks = std::max<int64_t>(1, (s->max_seq_len + block - 1) / block);
+  l.tops = (l.max_blocks + tactic::kSelectRows - 1) / tactic::kSelectRows;
+  Layout L;
+  const int64_t heads = (int64_t)s->batch * s->n_q_heads;
+  l.scores = L.take(heads * l.max_blocks * 8);
+  l.top = L.take(heads * l.tops * 8);
+  l.keys = l.max_blocks > tactic::kSelectHeld ? L.take((int64_t)s->batch * s->n_kv_heads * l.max_blocks * 8) : 0;
+  l.bytes = L.cur;
+  return l;
+}
+
+bool is_block(int block) { return block == 16 || block == 32 || block == 64 || block == 128; }
+
+}  // namespace
+
+extern "C" {
+
+tactic_status tactic_quant_write(const uint16_t* k, const uint16_t* v, const tactic_kv_shape* shape,
+                                 const tactic_query_shape* rows, const tactic_quant_kv* kv, hipStream_t stream) {
+  tactic_status st;
+  tactic::QuantKV c;
+  if ((st = check_shape(shape)) != TACTIC_OK || (st = check_new_rows(rows, shape)) != TACTIC_OK ||
+      (st = quant_args(kv, shape, true, &c)) != TACTIC_OK)
+    return st;
+  if (rows->total_queries == 0 || shape->total_tokens == 0) return TACTIC_OK;
+  if (!k || !v) return fail(TACTIC_ERR_INVALID_ARG, "null argument");
+  if ((st = check_aligned({k, v}, 16)) != TACTIC_OK) return st;
+  tactic::QuantRowsArgs a = rows_args(shape, rows, c);
+  a.k = k;
+  a.v = v;
+  const hipError_t e = tactic::launch_quant_write(a, stream);
+  return e == hipSuccess ? TACTIC_OK : hip_fail(e, "quantised write launch");
+}
+
+tactic_status tactic_quant_read(const tactic_quant_kv* kv, const tactic_kv_shape* shape,
+                                const tactic_query_shape* rows, uint16_t* K_out, uint16_t* V_out,
+                                hipStream_t stream) {
+  tactic_status st;
+  tactic::QuantKV c;
+  if ((st = check_shape(shape)) != TACTIC_OK || (st = check_new_rows(rows, shape)) != TACTIC_OK ||
+      (st = quant_args(kv, shape, true, &c)) != TACTIC_OK)
+    return st;
+  if (rows->total_queries == 0) return TACTIC_OK;
+  if (!K_out || !V_out) return fail(TACTIC_ERR_INVALID_ARG, "null argument");
+  if ((st = check_aligned({K_out, V_out}, 16)) != TACTIC_OK) return st;
+  tactic::QuantRowsArgs a = rows_args(shape, rows, c);
+  a.K_out = K_out;
+  a.V_out = V_out;
+  const hipError_t e = tactic::launch_quant_read(a, stream);
+  return e == hipSuccess ? TACTIC_OK : hip_fail(e, "quantised read launch");
+}
+
+size_t tactic_block_select_workspace_size(const tactic_kv_shape* shape, int32_t block) {
+  if (check_shape(shape) != TACTIC_OK) return 0;
+  if (!is_block(block)) {
+    fail(TACTIC_ERR_INVALID_ARG, "block must be 16, 32, 64 or 128 (got %d)", block);
+    return 0;
+  }
+  return (size_t)select_layout(shape, block).bytes;
+}
+
+tactic_status tactic_block_select(const uint16_t* q, const tactic_quant_kv* kv, const tactic_kv_shape* shape,
+                                  const tactic_block_params* params, int32_t* blocks, int32_t* counts,
+                                  void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  tactic_status st;
+  tactic::QuantKV c;
+  if ((st = check_shape(shape)) != TACTIC_OK || (st = quant_args(kv, shape, false, &c)) != TACTIC_OK) return st;
+  if (!params) return fail(TACTIC_ERR_INVALID_ARG, "params is null");
+  if (params->budget < 1 || params->first < 0 || params->last < 0 || (int64_t)params->first + params->last > params->budget)
+    return fail(TACTIC_ERR_INVALID_ARG, "budget must be >= 1 and at least first + last");
+  if (!q || !blocks || !counts || !c.bounds) return fail(TACTIC_ERR_INVALID_ARG, "null argument");
+  if ((st = check_aligned({q, workspace}, 16)) != TACTIC_OK || (st = check_aligned({blocks, counts}, 4)) != TACTIC_OK) return st;
+  const SelectLayout l = select_layout(shape, c.block);
+  if (!workspace || (int64_t)workspace_bytes < l.bytes)
+    return fail(TACTIC_ERR_WORKSPACE, "workspace has %zu bytes, needs %lld", workspace_bytes, (long long)l.bytes);
+  char* ws = static_cast<char*>(workspace);
+  tactic::SelectArgs a{};
+  a.q = q;
+  a.bounds = c.bounds;
+  a.kv_indptr = shape->kv_indptr;
+  a.seq_len = shape->seq_len;
+  a.B = shape->batch;
+  a.Hq = shape->n_q_heads;
+  a.Hkv = shape->n_kv_heads;
+  a.G = a.Hq / a.Hkv;
+  a.block = c.block;
+  a.budget = params->budget;
+  a.first = params->first;
+  a.last = params->last;
+  a.total = shape->total_tokens;
+  a.max_blocks = l.max_blocks;
+  a.tops = l.tops;
+  a.scores = reinterpret_cast<double*>(ws + l.scores);
+  a.top = reinterpret_cast<double*>(ws + l.top);
+  a.keys = reinterpret_cast<uint64_t*>(ws + l.keys);
+  a.blocks = blocks;
+  a.counts = counts;
+  hipError_t e = hipSuccess;
+  if (l.max_blocks > a.budget) e = tactic::launch_block_scores(a, stream);  // (else every block is chosen)
+  if (e == hipSuccess) e = tactic::launch_block_select(a, stream);
+  return e == hipSuccess ? TACTIC_OK : hip_fail(e, "block selection launch");
+}
+
+tactic_status tactic_quant_decode(const uint16_t* q, const tactic_quant_kv* kv, const tactic_kv_shape* shape,
+                                  const tactic_score_mod* mod, const int32_t* blocks, const int32_t* counts,
+                                  int32_t budget, float* out, float* lse, void* workspace,
+                                  size_t workspace_bytes, hipStream_t stream) {
+  tactic_status st;
+  tactic::QuantAttnArgs x{};
+  if ((st = check_shape(shape)) != TACTIC_OK || (st = quant_args(kv, shape, true, &x.kv)) != TACTIC_OK || (st = check_mod(mod)) != TACTIC_OK)
+    return st;
+  if (mod && (mod->documents || mod->prefix_len)) return fail(TACTIC_ERR_UNSUPPORTED, "a quantised cache takes a cap and slopes only");
+  if (!q || !out) return fail(TACTIC_ERR_INVALID_ARG, "null argument");
+  if (!blocks != !counts) return fail(TACTIC_ERR_INVALID_ARG, "blocks and counts go together");
+  if (blocks && (!is_block(x.kv.block) || budget < 1)) return fail(TACTIC_ERR_INVALID_ARG, "blocks need a block size and a budget >= 1");
+  if ((st = check_aligned({q, out, workspace}, 16)) != TACTIC_OK || (st = check_aligned({blocks, counts, lse}, 4)) != TACTIC_OK) return st;
+  const int64_t need = (int64_t)dense_workspace_bytes(shape, tactic::kMaxAttnGrid);
+  if (!workspace || (int64_t)workspace_bytes < need)
+    return fail(TACTIC_ERR_WORKSPACE, "workspace has %zu bytes, needs %lld", workspace_bytes, (long long)need);
+  char* ws = static_cast<char*>(workspace);
+  const int G = shape->n_q_heads / shape->n_kv_heads;
+  const int64_t groups = (int64_t)shape->batch * shape->n_kv_heads;
+  x.a.q = q;
+  x.a.kv_indptr = shape->kv_indptr;
+  x.a.seq_len = shape->seq_len;
+  x.a.B = shape->batch;
+  x.a.Hq = shape->n_q_heads;
+  x.a.Hkv = shape->n_kv_heads;
+  x.a.dense = 1;
+  x.a.NV = shape->n_kv_heads;
+  x.a.kv_div = 1;
+  x.a.total = shape->total_tokens;
+  Layout L;  // as in dense_workspace_bytes
+  x.a.partials = reinterpret_cast<float*>(ws + L.take((groups + tactic::kMaxAttnGrid) * G * (kHeadDim + 2) * 4));
+  x.a.ameta = reinterpret_cast<int64_t*>(ws + L.take((groups + 2) * 8));
+  x.a.out = out;
+  x.blocks = blocks;
+  x.counts = counts;
+  x.budget = budget;
+  x.block = x.kv.block;
+  if (mod) {
+    x.cap = mod->cap;
+    x.slopes = mod->slopes;
+  }
+  tactic::JoinArgs j{};
+  j.lse = lse;
+  j.rows = (int64_t)shape->batch * shape->n_q_heads;
+  int grid = 0;
+  hipError_t e = tactic::quant_resident_grid(x, G, &grid);
+  if (e == hipSuccess) e = tactic::launch_quant_attn(x, G, std::min(grid, tactic::kMaxAttnGrid), stream);
+  if (e == hipSuccess) e = tactic::launch_join(x.a, j, G, stream);
+  return e == hipSuccess ? TACTIC_OK : hip_fail(e, "quantised decode launch");
+}
+
+}  // extern "C"

@@ -45,7 +45,6 @@ __device__ __forceinline__ int64_t group_tokens(const AttnArgs& a, int bg) {
 // attention: 14.4 us at 256 / 96 units, 11.7 at 64 / 32, 8.4 at 64 / 128 to
 // 256; 1M tokens 19.1 -> 17.1, 4 x 131072 at 25%: 87.4 -> 85.8 to 87.2).  Shares
 // below 64 units gain nothing and give the combine more partials.
-constexpr int64_t kSegmentCost = 192;
 constexpr int64_t kSparseShare = 64;
 // A dense share has no range lookup to spread: 256 units, and where that makes
 // only a few shares more than a whole number per compute unit, that whole number

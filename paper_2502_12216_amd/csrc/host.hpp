@@ -26,6 +26,7 @@ struct Layout {
 };
 
 tactic_status check_shape(const tactic_kv_shape* s);
+tactic_status check_mod(const tactic_score_mod* m);
 tactic_status paged_args(const tactic_paged_kv* kv, const tactic_kv_shape* s, tactic::PagedKV* pk);
 size_t dense_workspace_bytes(const tactic_kv_shape* s, int64_t grid);
 

@@ -125,6 +125,7 @@ struct FitArgs {
   PagedKV pk;                 // used by the paged launches (K then points at the pages)
 };
 
+constexpr int64_t kSegmentCost = 192;  // rows that a segment of a group counts more (decode_attn.hip)
 struct AttnArgs {
   const uint16_t* q;
   const uint16_t* K;
@@ -240,6 +241,65 @@ struct InsertArgs {
 hipError_t launch_prompt_weights(const WeightArgs& a, int64_t max_len, hipStream_t st);
 hipError_t launch_evict(const EvictArgs& a, int64_t max_len, int64_t max_out, hipStream_t st);
 hipError_t launch_insert(const InsertArgs& a, int64_t max_len, hipStream_t st);
+
+// A cache of 8 or 4 bits a value (quant.hpp), in spans or pages.
+struct QuantKV {
+  uint8_t* K;                   // [Hkv][total][16 bits] or [num_pages][Hkv][page_size][16 bits]
+  uint8_t* K_scale;             // [..][4]
+  uint8_t* V;
+  uint8_t* V_scale;
+  uint16_t* bounds;             // bf16 [Hkv][total / block + B][2][128] or null
+  int bits, block, paged;
+  PagedKV pk;
+};
+
+// New rows of a quantised cache, and rows of it in bf16 again (quant_cache.hip).
+struct QuantRowsArgs {
+  const uint16_t* k;            // writing: bf16 [n_rows][Hkv][128]
+  const uint16_t* v;
+  uint16_t* K_out;              // reading: bf16 [Hkv][n_rows][128]
+  uint16_t* V_out;
+  const int64_t* kv_indptr;
+  const int64_t* seq_len;
+  const int64_t* row_indptr;    // [B+1]: the last so many rows of each sequence
+  int B, Hkv;
+  int64_t total, n_rows;
+  QuantKV kv;
+};
+hipError_t launch_quant_write(const QuantRowsArgs& a, hipStream_t st);
+hipError_t launch_quant_read(const QuantRowsArgs& a, hipStream_t st);
+
+// Scores of blocks from their bounds, and the best of them (block_select.hip).
+constexpr int kSelectRows = 64;     // blocks per scoring workgroup
+struct SelectArgs {
+  const uint16_t* q;
+  const uint16_t* bounds;
+  const int64_t* kv_indptr;
+  const int64_t* seq_len;
+  int B, Hq, Hkv, G, block, budget, first, last;
+  int64_t total, max_blocks, tops;  // tops: scoring workgroups of a sequence's head
+  double* scores;               // [B][Hq][max_blocks]
+  double* top;                  // [B][Hq][tops]: the largest score of each scoring workgroup
+  uint64_t* keys;               // [B][Hkv][max_blocks] where a workgroup's registers do not hold them
+  int32_t* blocks;              // [B][Hkv][budget]
+  int32_t* counts;              // [B][Hkv]
+};
+constexpr int kSelectHeld = 16384;  // blocks whose keys a workgroup holds in registers
+hipError_t launch_block_scores(const SelectArgs& a, hipStream_t st);
+hipError_t launch_block_select(const SelectArgs& a, hipStream_t st);
+
+// One token per sequence over a quantised cache, all of it or the chosen blocks (quant_attn.hip).
+struct QuantAttnArgs {
+  AttnArgs a;                   // sizes, partials and outputs (K, V unused)
+  QuantKV kv;
+  const int32_t* blocks;        // [B][Hkv][budget] or null: every row
+  const int32_t* counts;        // [B][Hkv]
+  int budget, block;
+  float cap;
+  const float* slopes;
+};
+hipError_t quant_resident_grid(const QuantAttnArgs& a, int G, int* grid);
+hipError_t launch_quant_attn(const QuantAttnArgs& a, int G, int grid, hipStream_t st);
 
 // What the combine of the single-token forms joins and writes beside the outputs.
 constexpr int kMaxSplits = 64;  // splits of a row tile's keys
