@@ -2,18 +2,16 @@
 // blocks, split over the workgroups and joined by the combine of the dense decode.
 //
 // A row of K and V is 264 or 136 bytes for 512 G operations: bound by HBM as long as
-// codes become products in few instructions.  A wave takes 32 rows a step, and
+// codes become products in few instructions.  A wave takes two tiles of 16 rows a step, and
 // everything stays in the lanes that loaded it:
-//  - Scores: two tiles of 16 rows, each four v_mfma_f32_16x16x32_bf16 with the rows of K as
-//    the first operand - lane l has row l % 16, dimensions 32 (l / 16) .. + 31, which is one
-//    group and one power, converted to bf16 exactly - and four query heads as the columns,
-//    repeated four times.  So lane l receives the scores of head l % 4 for the rows
-//    4 (l / 16) .. + 3 of either tile, exactly once for each lane that needs them.
-//  - Values: lanes with l % 16 < 8 take the first tile, the others the second: rows
-//    4 (l / 16) .. + 3 of it, 16 dimensions each, so that a quad of lanes has the weights of
-//    four heads and the values of four dimensions of the same four rows: one block of
-//    v_mfma_f32_4x4x4_16b_bf16 for each of the lane's dimensions, with the weights split
-//    into three bf16 parts whose sum is exact.
+//  - Scores: v_mfma_f32_16x16x32_bf16 with the rows of K as the first operand - lane l has
+//    row l % 16 and 32 of its dimensions, made bf16 exactly by one conversion for two of
+//    them - and four query heads as the columns, repeated four times.  So lane l receives the
+//    scores of head l % 4 for the rows 4 (l / 16) .. + 3 of both tiles.
+//  - Values: the same instruction with the weights as the first operand: its row l % 16
+//    is head l % 4 and the part (l % 16) / 4 of the weight, three bf16 parts whose sum is
+//    exact, so that one instruction takes all parts of four heads; its columns are lane l's
+//    dimensions 8 (l % 16) .. + 7, one to an instruction, for the same eight rows.
 // (The instructions that multiply 8 and 4 bit codes themselves add with fewer bits: 9e-5
 // of the absolute sum for a row of 128 codes, where fp32 has 6e-8.)
 #include <hip/hip_runtime.h>
@@ -34,33 +32,21 @@ constexpr float kScaleLog2 = kLog2e * kInvSqrtDim;
 constexpr int64_t kQuantShare = 256;  // rows of the least share
 constexpr int kTableRows = 2048;      // rows looked up at once
 
-typedef short bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
-__device__ __forceinline__ bf16x4 four(uint32_t lo, uint32_t hi) {
-  u32x2 w;
-  w.x = lo;
-  w.y = hi;
-  return __builtin_bit_cast(bf16x4, w);
-}
 
-// Four fp32 weights as three bf16 operands whose sum is exact: the upper 8 bits of the
-// significand, the next 8 of the rest, the rest
-__device__ __forceinline__ void three_parts(const float (&p)[4], bf16x4 (&part)[3]) {
-  uint32_t h[4], m[4], r[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    h[i] = __float_as_uint(p[i]);
-    const float x = p[i] - __uint_as_float(h[i] & 0xffff0000u);
-    m[i] = __float_as_uint(x);
-    r[i] = __float_as_uint(x - __uint_as_float(m[i] & 0xffff0000u));
-  }
-  part[0] = four(high_halves(h[0], h[1]), high_halves(h[2], h[3]));
-  part[1] = four(high_halves(m[0], m[1]), high_halves(m[2], m[3]));
-  part[2] = four(high_halves(r[0], r[1]), high_halves(r[2], r[3]));
+// The power of group g of a row from the word of its four bytes: rotated to where a float has
+// its exponent, the only part that the conversions read
+__device__ __forceinline__ float power_in(uint32_t word, int turn) { return __uint_as_float(__builtin_amdgcn_alignbit(word, word, turn)); }
+__device__ __forceinline__ int turn_of(int g) { return 9 + 8 * g; }
+
+template <typename T>
+__device__ __forceinline__ T uniform(T x) {
+  if constexpr (sizeof(T) == 4) return __builtin_bit_cast(T, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+  else return (T)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)((uint64_t)x >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
 }
 
 // Rows that group bg attends: its sequence's, or those of its chosen blocks (ascending, so
@@ -76,33 +62,37 @@ __device__ __forceinline__ int64_t rows_of(const QuantAttnArgs& x, int bg) {
   return ((int64_t)(count - 1) << lb) + min(max(n - (last << lb), (int64_t)1), (int64_t)x.block);
 }
 
-// kTable: rows are looked up (pages or chosen blocks), else they are the positions
-template <int G, int kBits, bool kTable, bool kMod>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(G == 8 ? 1 : 2)))
+// kRows: 0 rows lie at their positions; 1 every 16 positions from a multiple of 16 lie together
+// (chosen blocks, pages of a multiple of 16 rows); 2 rows lie anywhere
+template <int G, int kBits, int kRows, bool kMod>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
 void quant_attn_kernel(QuantAttnArgs x) {
   constexpr int kPart = G * (kHeadDim + 2);
-  constexpr int S = G == 8 ? 2 : 1;         // sets of four heads
+  constexpr int S = G == 8 ? 2 : 1;           // sets of four heads
   constexpr int RB = kRowBytes<kBits>;
-  constexpr int KW = kBits == 8 ? 2 : 1;    // 16-byte words of a lane's group of K
-  constexpr int VW = kBits == 8 ? 4 : 2;    // 4-byte words of a lane's 16 values
-  constexpr int kAhead = kBits == 8 ? 1 : 2;  // steps loaded ahead
+  constexpr int KW = kBits == 8 ? 2 : 1;      // 16-byte words of a lane's dimensions of K
+  constexpr int VW = kBits == 8 ? 2 : 1;      // 4-byte words of its 8 values
+  constexpr int kAhead = 1;  // steps loaded ahead
   const AttnArgs& a = x.a;
-  extern __shared__ int64_t s_prefix[];     // [B * NV + 1] units before each group
+  extern __shared__ int64_t s_prefix[];       // [B * NV + 1] units before each group
   union Shared {
     struct {
-      int place[kTableRows];                // row in the arrays, from the head's (spans) or their start (pages)
-      int row[kMod ? kTableRows : 1];       // row of the sequence
+      int tile[kTableRows / 16];              // place of 16 positions (kRows 1)
+      int row[kTableRows / 16];               // their rows of the sequence
+      __align__(16) int place[kRows == 2 ? kTableRows : 1];
     } t;
-    float red[16][G][kHeadDim];             // the merge: four row groups of four waves
+    float red[12][G][kHeadDim];               // the merge: three parts of four waves
   };
   __shared__ __align__(16) Shared sh;
-  __shared__ float s_ml[32][2][G];
-  __shared__ float s_M[G], s_L[G];
+  __shared__ float s_ml[4][2][G], s_scale[4][G];
   __shared__ int64_t s_wsum[4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int sl = lane & 15, grp = lane >> 4, half = sl >> 3, hd = sl & 3;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int sl = lane & 15, grp = lane >> 4, hd = sl & 3;
+  // what a lane takes off its weights: the upper 8 bits from the second part on, the next from the third on
+  const uint32_t off1 = sl >= 4 ? 0xffff0000u : 0u, off2 = sl >= 8 ? 0xffff0000u : 0u;
   const int BG = a.B * a.NV;
-  auto units = [&](int bg) { const int64_t n = rows_of(x, bg); return n > 0 ? n + kSegmentCost : 0; };
+  // segments begin at multiples of 32 rows of their group
+  auto units = [&](int bg) { const int64_t n = rows_of(x, bg); return n > 0 ? ((n + 31) & ~(int64_t)31) + kSegmentCost : 0; };
   {
     const int per = (BG + 255) / 256, g0 = min(BG, tid * per), g1 = min(BG, g0 + per);
     const int64_t u_first = g0 < g1 ? units(g0) : 0;
@@ -120,8 +110,8 @@ void quant_attn_kernel(QuantAttnArgs x) {
     if (tid == 255) s_prefix[BG] = run;
     __syncthreads();
   }
-  const int64_t total = s_prefix[BG];
-  const int64_t share = max((total + gridDim.x - 1) / gridDim.x, kQuantShare);
+  const int64_t total = uniform(s_prefix[BG]);
+  const int64_t share = max(((total + gridDim.x - 1) / gridDim.x + 31) & ~(int64_t)31, kQuantShare);
   if (blockIdx.x == 0) {  // for the combine
     if (tid == 0) a.ameta[0] = share;
     for (int bg = tid; bg <= BG; bg += 256) a.ameta[1 + bg] = s_prefix[bg];
@@ -136,21 +126,22 @@ void quant_attn_kernel(QuantAttnArgs x) {
   }
   bg0 = __builtin_amdgcn_readfirstlane(bg0);
 
-  for (int bg = bg0; bg < BG && s_prefix[bg] < t1; ++bg) {
-    const int64_t first = s_prefix[bg] + kSegmentCost;
-    const int64_t seg_lo = max(t0, first) - first, seg_hi = min(t1, s_prefix[bg + 1]) - first;
+  for (int bg = bg0; bg < BG && uniform(s_prefix[bg]) < t1; ++bg) {
+    const int64_t first = uniform(s_prefix[bg]) + kSegmentCost;
+    const int64_t seg_lo = max(t0, first) - first, seg_hi = min(uniform(rows_of(x, bg)), t1 - first);
     if (seg_lo >= seg_hi) continue;
     const int b = bg / a.NV, kvh = bg % a.NV;
     const int64_t kvb = a.kv_indptr[b];
     const int nseq = (int)seq_tokens(a.kv_indptr, a.seq_len, b);
 
-    // the queries: dimensions 32 grp .. + 31 of head hd of each set
+    // the queries, in the dimensions that the lane has of K
     bf16x8 qv[S][4];
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-      const uint16_t* qp = a.q + ((int64_t)b * a.Hq + kvh * G + (G >= 4 ? 4 * s + hd : hd % G)) * kHeadDim + grp * 32;
+      const uint16_t* qp = a.q + ((int64_t)b * a.Hq + kvh * G + (G >= 4 ? 4 * s + hd : hd % G)) * kHeadDim;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) qv[s][j] = *reinterpret_cast<const bf16x8*>(qp + 8 * j);
+      for (int j = 0; j < 4; ++j)
+        qv[s][j] = *reinterpret_cast<const bf16x8*>(qp + (kBits == 8 ? (j >> 1) * 64 + grp * 16 + (j & 1) * 8 : grp * 32 + j * 8));
     }
     float slope2[S], to_cap = 0.f;
 #pragma unroll
@@ -161,56 +152,92 @@ void quant_attn_kernel(QuantAttnArgs x) {
         slope2[s] = x.slopes ? x.slopes[kvh * G + (G >= 4 ? 4 * s + hd : hd % G)] * kLog2e : 0.f;
       to_cap = x.cap > 0.f ? kInvSqrtDim / x.cap : 0.f;
     }
-    // reference maximum and sum of this lane's heads over its rows; sums of values, a
-    // vector of four heads for each of the lane's 16 dimensions
+    // a head's reference maximum (the same in all lanes of the wave that have the head) and the sum
+    // over this lane's rows; sums of values: element i of lane group p is part p of head i
     float m[S], l[S];
-    f32x4 acc[S][16];
+    f32x4 acc[S][8];
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-      m[s] = -INFINITY;
+      m[s] = -3.402823466e38f;
       l[s] = 0.f;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc[s][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int e = 0; e < 8; ++e) acc[s][e] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     const int64_t base = x.kv.paged ? 0 : (int64_t)kvh * a.total + kvb;
-    const uint8_t* Kb = x.kv.K + base * RB + grp * (RB / 4);
-    const uint8_t* Ks = x.kv.K_scale + base * 4 + grp;
-    const uint8_t* Vb = x.kv.V + base * RB + (sl & 7) * (RB / 8);
-    const uint8_t* Vs = x.kv.V_scale + base * 4 + ((sl & 7) >> 1);
+    const uint8_t* const Kb = x.kv.K + base * RB;
+    const uint8_t* const Vb = x.kv.V + base * RB;
+    const uint8_t* const Ks = x.kv.K_scale + base * 4;
+    const uint8_t* const Vs = x.kv.V_scale + base * 4;
+    // the groups of the lane's dimensions
+    const int k_turn = kBits == 8 ? turn_of(grp >> 1) : turn_of(grp), k_turn2 = turn_of(2 + (grp >> 1)), v_turn = turn_of(sl >> 2);
     int cnt = 0;
     int64_t p0 = 0;
     struct Tile {
       u32x4 k[2][KW];
-      uint32_t v[4][VW];
-      uint8_t ks[2], vs[4];
+      uint32_t v[8][VW];   // rows 4 grp .. + 3 of the first tile, then of the second
+      uint32_t ks[2], vs[8];
+    };
+    auto load_k = [&](Tile& r, int t, const uint8_t* p, const uint8_t* ps) __attribute__((always_inline)) {
+#pragma unroll
+      for (int w = 0; w < KW; ++w) r.k[t][w] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 64 * w));
+      r.ks[t] = *reinterpret_cast<const uint32_t*>(ps);
+    };
+    auto load_v = [&](Tile& r, int i, const uint8_t* p) __attribute__((always_inline)) {
+      if constexpr (kBits == 8) {
+        const u32x2 w = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
+        r.v[i][0] = w.x;
+        r.v[i][1] = w.y;
+      } else {
+        r.v[i][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p));
+      }
     };
     // step `step` of this wave: positions 128 step + 32 wave .. + 31 of the sub-range; those
     // past its end read its last row, which the group attends anyway
     auto load_tile = [&](int step) __attribute__((always_inline)) -> Tile {
       Tile r;
       const int at = step * 128 + wave * 32;
+      if constexpr (kRows == 2) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int pos = min(at + 16 * t + sl, cnt - 1);
-        const int64_t row = kTable ? (int64_t)sh.t.place[pos] : p0 + pos;
-        const uint8_t* p = Kb + row * RB;
+        for (int t = 0; t < 2; ++t) {
+          const int64_t row = sh.t.place[min(at + 16 * t + sl, cnt - 1)];
+          load_k(r, t, Kb + row * RB + grp * 16, Ks + row * 4);
 #pragma unroll
-        for (int w = 0; w < KW; ++w) r.k[t][w] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p) + w);
-        r.ks[t] = Ks[row * 4];
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int pos = min(at + 16 * half + 4 * grp + i, cnt - 1);
-        const int64_t row = kTable ? (int64_t)sh.t.place[pos] : p0 + pos;
-        const uint8_t* p = Vb + row * RB;
-        if constexpr (kBits == 8) {
-          const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
-          r.v[i][0] = w.x; r.v[i][1] = w.y; r.v[i][2] = w.z; r.v[i][3] = w.w;
-        } else {
-          const u32x2 w = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
-          r.v[i][0] = w.x; r.v[i][1] = w.y;
+          for (int i = 0; i < 4; ++i) {
+            const int64_t vrow = sh.t.place[min(at + 16 * t + 4 * grp + i, cnt - 1)];
+            load_v(r, 4 * t + i, Vb + vrow * RB + sl * (RB / 16));
+            r.vs[4 * t + i] = *reinterpret_cast<const uint32_t*>(Vs + vrow * 4);
+          }
         }
-        r.vs[i] = Vs[row * 4];
+      } else {
+        auto place = [&](int pos) -> int64_t {  // of 16 positions
+          if constexpr (kRows == 0) return p0 + pos;
+          else return (int64_t)__builtin_amdgcn_readfirstlane(sh.t.tile[pos >> 4]);
+        };
+        if (at + 32 <= cnt) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const int64_t row = place(at + 16 * t);
+            load_k(r, t, Kb + row * RB + (uint32_t)(sl * RB + grp * 16), Ks + row * 4 + (uint32_t)(sl * 4));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) load_v(r, 4 * t + i, Vb + row * RB + (uint32_t)(grp * (4 * RB) + sl * (RB / 16)) + i * RB);
+            const u32x4 w = *reinterpret_cast<const u32x4*>(Vs + row * 4 + (uint32_t)(grp * 16));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r.vs[4 * t + i] = w[i];
+          }
+        } else {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const int from = min(at + 16 * t, (cnt - 1) & ~15), most = min(cnt - 1 - from, 15);
+            const int64_t row = place(from);
+            load_k(r, t, Kb + row * RB + (uint32_t)(min(sl, most) * RB + grp * 16), Ks + row * 4 + (uint32_t)(min(sl, most) * 4));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int in = min(4 * grp + i, most);
+              load_v(r, 4 * t + i, Vb + row * RB + (uint32_t)(in * RB + sl * (RB / 16)));
+              r.vs[4 * t + i] = *reinterpret_cast<const uint32_t*>(Vs + row * 4 + (uint32_t)(in * 4));
+            }
+          }
+        }
       }
       return r;
     };
@@ -218,7 +245,7 @@ void quant_attn_kernel(QuantAttnArgs x) {
       f32x4 d[S][2];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const float power = power_of(y.ks[t]);
+        const float power = power_in(y.ks[t], k_turn), power2 = power_in(y.ks[t], k_turn2);
 #pragma unroll
         for (int s = 0; s < S; ++s) d[s][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -226,10 +253,11 @@ void quant_attn_kernel(QuantAttnArgs x) {
           u32x4 w;
           if constexpr (kBits == 8) {
             const uint32_t c0 = y.k[t][j >> 1][2 * (j & 1)], c1 = y.k[t][j >> 1][2 * (j & 1) + 1];
-            w.x = decode_pair<8>(c0, 0, power);
-            w.y = decode_pair<8>(c0, 1, power);
-            w.z = decode_pair<8>(c1, 0, power);
-            w.w = decode_pair<8>(c1, 1, power);
+            const float pw = j < 2 ? power : power2;
+            w.x = decode_pair<8>(c0, 0, pw);
+            w.y = decode_pair<8>(c0, 1, pw);
+            w.z = decode_pair<8>(c1, 0, pw);
+            w.w = decode_pair<8>(c1, 1, pw);
           } else {
             const uint32_t c = y.k[t][0][j];
             w.x = decode_pair<4>(c, 0, power);
@@ -242,111 +270,125 @@ void quant_attn_kernel(QuantAttnArgs x) {
           for (int s = 0; s < S; ++s) d[s][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qv[s][j], d[s][t], 0, 0, 0);
         }
       }
-      const int pos0 = step * 128 + wave * 32 + 16 * half + 4 * grp;
-      const bool whole = step * 128 + wave * 32 + 32 <= cnt;
-      bf16x4 part[S][3];
+      const int at = step * 128 + wave * 32;
+      bf16x8 part[S];
 #pragma unroll
       for (int s = 0; s < S; ++s) {
-        float v[4];
+        constexpr float kTo2 = kMod ? 1.f : kScaleLog2;
+        float v[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float r = half ? d[s][1][i] : d[s][0][i];
-          v[i] = r * kScaleLog2;
-          if constexpr (kMod) {
+        for (int i = 0; i < 8; ++i) v[i] = d[s][i >> 2][i & 3];
+        if constexpr (kMod) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float r = v[i];
+            v[i] = r * kScaleLog2;
             if (x.cap > 0.f) {
               const float z = r * to_cap;
               v[i] = x.cap * kLog2e * (__any(fabsf(z) > kTanhPoly) ? tanh_any(z) : tanh_poly(z));
             }
-            if (x.slopes) {
-              const int pos = min(pos0 + i, cnt - 1);
-              const int row = kTable ? sh.t.row[pos] : (int)(p0 + pos);
-              v[i] = fmaf(-slope2[s], (float)(nseq - 1 - row), v[i]);
+          }
+          if (x.slopes) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              int row;  // of the tile's first position
+              if constexpr (kRows == 0) row = (int)p0 + at + 16 * t;
+              else row = sh.t.row[min(at + 16 * t, cnt - 1) >> 4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) v[4 * t + i] = fmaf(-slope2[s], (float)(nseq - 1 - row - 4 * grp - i), v[4 * t + i]);
             }
           }
         }
-        if (!whole) {
+        if (at + 32 > cnt) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = pos0 + i < cnt ? v[i] : -INFINITY;
+          for (int i = 0; i < 8; ++i) v[i] = at + 16 * (i >> 2) + 4 * grp + (i & 3) < cnt ? v[i] : -INFINITY;
         }
+        float mx = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7]))) * kTo2;
         // the reference is raised only where a weight would pass 2^8
-        float mn = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
-        mn = fminf(mn, 3.402823466e38f);  // a score of +inf: the sum is inf, the output NaN
-        if (__any(mn > m[s] + 8.f)) {
-          const float to = fmaxf(m[s], mn);
-          const float corr = to > m[s] ? fast_exp2(m[s] - to) : 1.f;
+        if (__any(mx > m[s] + 8.f)) {
+          mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+          mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+          const float to = fmaxf(m[s], fminf(mx, 3.402823466e38f));  // (a score of +inf: the sum is inf, the output NaN)
+          const float corr = fast_exp2(m[s] - to);
           m[s] = to;
           l[s] *= corr;
           const f32x4 c = {dpp<0x00>(corr), dpp<0x55>(corr), dpp<0xAA>(corr), dpp<0xFF>(corr)};  // of the quad's four heads
 #pragma unroll
-          for (int e = 0; e < 16; ++e) acc[s][e] *= c;
+          for (int e = 0; e < 8; ++e) acc[s][e] *= c;
         }
-        float p[4];
+        u32x4 w;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          p[i] = v[i] == -INFINITY ? 0.f : fast_exp2(v[i] - m[s]);
-          l[s] += p[i];
-        }
-        three_parts(p, part[s]);
-      }
-      // the values, eight dimensions at a time
+        for (int i = 0; i < 8; i += 2) {
+          float p[2];
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        bf16x4 vt[8];
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {  // pairs 4 c + w of the 8
-          uint32_t z[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float power = power_of(y.vs[i]);
-            if constexpr (kBits == 8) z[i] = w & 1 ? decode_pair<8>(y.v[i][2 * c + (w >> 1)], 1, power) : decode_pair<8>(y.v[i][2 * c + (w >> 1)], 0, power);
-            else z[i] = w == 0 ? decode_pair<4>(y.v[i][c], 0, power) : w == 1 ? decode_pair<4>(y.v[i][c], 1, power)
-                        : w == 2 ? decode_pair<4>(y.v[i][c], 2, power) : decode_pair<4>(y.v[i][c], 3, power);
+          for (int k = 0; k < 2; ++k) {
+            p[k] = fast_exp2(fmaf(v[i + k], kTo2, -m[s]));
+            l[s] += p[k];
+            p[k] -= __uint_as_float(__float_as_uint(p[k]) & off1);
+            p[k] -= __uint_as_float(__float_as_uint(p[k]) & off2);
           }
-          vt[2 * w] = four(low_halves(z[0], z[1]), low_halves(z[2], z[3]));
-          vt[2 * w + 1] = four(high_halves(z[0], z[1]), high_halves(z[2], z[3]));
+          w[i >> 1] = high_halves(__float_as_uint(p[0]), __float_as_uint(p[1]));
         }
+        part[s] = __builtin_bit_cast(bf16x8, w);
+      }
+      float power[8];
 #pragma unroll
-        for (int s = 0; s < S; ++s)
+      for (int i = 0; i < 8; ++i) power[i] = power_in(y.vs[i], v_turn);
 #pragma unroll
-          for (int k = 2; k >= 0; --k)
+      for (int e = 0; e < 4; ++e) {  // two dimensions at a time
+        uint32_t z[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              acc[s][8 * c + e] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(part[s][k], vt[e], acc[s][8 * c + e], 0, 0, 0);
+        for (int i = 0; i < 8; ++i) {
+          if constexpr (kBits == 8) z[i] = e & 1 ? decode_pair<8>(y.v[i][e >> 1], 1, power[i]) : decode_pair<8>(y.v[i][e >> 1], 0, power[i]);
+          else z[i] = e == 0 ? decode_pair<4>(y.v[i][0], 0, power[i]) : e == 1 ? decode_pair<4>(y.v[i][0], 1, power[i])
+                      : e == 2 ? decode_pair<4>(y.v[i][0], 2, power[i]) : decode_pair<4>(y.v[i][0], 3, power[i]);
+        }
+        const u32x4 lo = {low_halves(z[0], z[1]), low_halves(z[2], z[3]), low_halves(z[4], z[5]), low_halves(z[6], z[7])};
+        const u32x4 hi = {high_halves(z[0], z[1]), high_halves(z[2], z[3]), high_halves(z[4], z[5]), high_halves(z[6], z[7])};
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+          acc[s][2 * e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part[s], __builtin_bit_cast(bf16x8, lo), acc[s][2 * e], 0, 0, 0);
+          acc[s][2 * e + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part[s], __builtin_bit_cast(bf16x8, hi), acc[s][2 * e + 1], 0, 0, 0);
+        }
       }
     };
     for (int64_t p = seg_lo; p < seg_hi; p += cnt) {
       p0 = p;
-      if constexpr (!kTable) {
+      if constexpr (kRows == 0) {
         cnt = (int)(seg_hi - p);
       } else {
         cnt = (int)min(seg_hi - p, (int64_t)kTableRows);
-        constexpr int kPer = kTableRows / 256;
-        int rr[kPer];
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) {
-          const int64_t pos = p + min(tid + e * 256, cnt - 1);
-          if (x.blocks) {
-            const int lb = __builtin_ctz(x.block);
-            const int64_t at = x.blocks[(int64_t)bg * x.budget + (pos >> lb)];
-            rr[e] = (int)min(max((at << lb) + (pos & (x.block - 1)), (int64_t)0), (int64_t)nseq - 1);
-          } else {
-            rr[e] = (int)pos;
+        auto row_at = [&](int64_t pos) -> int {
+          if (!x.blocks) return (int)pos;
+          const int lb = __builtin_ctz(x.block);
+          const int64_t at = x.blocks[(int64_t)bg * x.budget + (pos >> lb)];
+          return (int)min(max((at << lb) + (pos & (x.block - 1)), (int64_t)0), (int64_t)nseq - 1);
+        };
+        if (tid * 16 < cnt) {
+          int row[1] = {row_at(p + tid * 16)};
+          sh.t.row[tid] = row[0];
+          if constexpr (kRows == 1) {
+            // (a list that is not as it should be: 16 rows stay inside the sequence's first ones or its last)
+            if (x.blocks && cnt - tid * 16 >= 16) row[0] = max(0, min(row[0], nseq - 16)) & ~(x.kv.paged ? 15 : 0);
+            if (x.kv.paged) {
+              int64_t at[1];
+              paged_rows(x.kv.pk, a.Hkv, a.total, kvb, b, kvh, row, 0, at);
+              row[0] = (int)at[0];
+            }
+            sh.t.tile[tid] = row[0];
           }
         }
-        if constexpr (kMod) {
-#pragma unroll
-          for (int e = 0; e < kPer; ++e)
-            if (tid + e * 256 < cnt) sh.t.row[tid + e * 256] = rr[e];
-        }
-        if (x.kv.paged) {
+        if constexpr (kRows == 2) {
+          constexpr int kPer = kTableRows / 256;
+          int rr[kPer];
           int64_t pr[kPer];
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) rr[e] = row_at(p + min(tid + e * 256, cnt - 1));
           paged_rows(x.kv.pk, a.Hkv, a.total, kvb, b, kvh, rr, 0, pr);
 #pragma unroll
-          for (int e = 0; e < kPer; ++e) rr[e] = (int)pr[e];
+          for (int e = 0; e < kPer; ++e)
+            if (tid + e * 256 < cnt) sh.t.place[tid + e * 256] = (int)pr[e];
         }
-#pragma unroll
-        for (int e = 0; e < kPer; ++e)
-          if (tid + e * 256 < cnt) sh.t.place[tid + e * 256] = rr[e];
         __syncthreads();
       }
       const int steps = (max(cnt - wave * 32, 0) + 127) / 128;
@@ -356,9 +398,11 @@ void quant_attn_kernel(QuantAttnArgs x) {
 #pragma unroll 1
           for (int s = 0; s < steps; s += 2) {
             const Tile y1 = load_tile(s + 1);
+            __builtin_amdgcn_sched_barrier(0);
             consume(y0, s);
             if (s + 1 >= steps) break;
             y0 = load_tile(s + 2);
+            __builtin_amdgcn_sched_barrier(0);
             consume(y1, s + 1);
           }
         } else {
@@ -366,82 +410,77 @@ void quant_attn_kernel(QuantAttnArgs x) {
 #pragma unroll 1
           for (int s = 0; s < steps; s += 3) {
             Tile y2 = load_tile(s + 2);
+            __builtin_amdgcn_sched_barrier(0);
             consume(y0, s);
             if (s + 1 >= steps) break;
             y0 = load_tile(s + 3);
+            __builtin_amdgcn_sched_barrier(0);
             consume(y1, s + 1);
             if (s + 2 >= steps) break;
             y1 = load_tile(s + 4);
+            __builtin_amdgcn_sched_barrier(0);
             consume(y2, s + 2);
           }
         }
       }
-      if constexpr (kTable) __syncthreads();  // the next sub-range, or the merge, rewrites the table
+      if constexpr (kRows != 0) __syncthreads();  // the next sub-range, or the merge, rewrites the table
     }
 
-    // ---- merge: 32 states of every head (wave, row group, half): common maximum, rescale, sum
-    const int state = wave * 8 + grp * 2 + half;
+    // ---- merge the four waves: common maximum, rescale, sum
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-      if (m[s] == -INFINITY && l[s] != l[s]) m[s] = 0.f;  // (a maximum passes NaN over: where no other score was there the sum says that some was)
-      if ((sl & 7) < 4 && hd < G) {
-        s_ml[state][0][4 * s + hd] = m[s];
-        s_ml[state][1][4 * s + hd] = l[s];
+      l[s] += __shfl_xor(l[s], 16, 64);
+      l[s] += __shfl_xor(l[s], 32, 64);
+      if (lane < 4 && hd < G) {
+        s_ml[wave][0][4 * s + hd] = m[s];
+        s_ml[wave][1][4 * s + hd] = l[s];
       }
-    }
-    __syncthreads();
-    if (tid < G) {
-      float mm = -INFINITY;
-      for (int q = 0; q < 32; ++q) mm = fmaxf(mm, s_ml[q][0][tid]);
-      float ll = 0.f;
-      for (int q = 0; q < 32; ++q) {
-        const float mq = s_ml[q][0][tid];
-        ll += mq == -INFINITY ? 0.f : s_ml[q][1][tid] * fast_exp2(mq - mm);
-      }
-      s_M[tid] = mm;
-      s_L[tid] = ll;
-    }
-    __syncthreads();
-    float* part = a.partials + ((int64_t)bg + blockIdx.x) * kPart;
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      const float sc = m[s] == -INFINITY ? 0.f : fast_exp2(m[s] - s_M[G >= 4 ? 4 * s + hd : hd % G]);
-      const f32x4 c = {dpp<0x00>(sc), dpp<0x55>(sc), dpp<0xAA>(sc), dpp<0xFF>(sc)};
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        f32x4 y = acc[s][e] * c;
-#pragma unroll
-        for (int h = 0; h < (G < 4 ? G : 4); ++h) {
-          const float z = y[h] + dpp<0x128>(y[h]);  // row_ror:8, the other half's rows
-          acc[s][e][h] = z;
-        }
-      }
-      if (half == 0) {
+      if (grp < 3) {
 #pragma unroll
         for (int h = 0; h < (G < 4 ? G : 4); ++h)
 #pragma unroll
-          for (int e = 0; e < 16; e += 4)
-            *reinterpret_cast<float4*>(&sh.red[wave * 4 + grp][4 * s + h][(sl & 7) * 16 + e]) =
+          for (int e = 0; e < 8; e += 4)
+            *reinterpret_cast<float4*>(&sh.red[wave * 3 + grp][4 * s + h][sl * 8 + e]) =
                 make_float4(acc[s][e][h], acc[s][e + 1][h], acc[s][e + 2][h], acc[s][e + 3][h]);
       }
+    }
+    __syncthreads();
+    float* part = a.partials + ((int64_t)bg + blockIdx.x) * kPart;
+    if (tid < G) {
+      float mm = -INFINITY, ll = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) mm = fmaxf(mm, s_ml[w][1][tid] == 0.f ? -INFINITY : s_ml[w][0][tid]);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float lw = s_ml[w][1][tid], f = lw == 0.f ? 0.f : fast_exp2(s_ml[w][0][tid] - mm);
+        s_scale[w][tid] = f;
+        ll = fmaf(lw, f, ll);
+      }
+      part[G * kHeadDim + tid] = mm;
+      part[G * kHeadDim + G + tid] = ll;
     }
     __syncthreads();
     if (tid * 4 < G * kHeadDim) {
       const int h = tid * 4 / kHeadDim, e = tid * 4 % kHeadDim;
       float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int q = 0; q < 16; ++q) {
-        const float4 v = *reinterpret_cast<const float4*>(&sh.red[q][h][e]);
-        sum.x += v.x;
-        sum.y += v.y;
-        sum.z += v.z;
-        sum.w += v.w;
+      for (int w = 0; w < 4; ++w) {
+        const float f = s_scale[w][h];
+        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int q = 2; q >= 0; --q) {  // the small parts first
+          const float4 v = *reinterpret_cast<const float4*>(&sh.red[w * 3 + q][h][e]);
+          y.x += v.x;
+          y.y += v.y;
+          y.z += v.z;
+          y.w += v.w;
+        }
+        sum.x = fmaf(y.x, f, sum.x);
+        sum.y = fmaf(y.y, f, sum.y);
+        sum.z = fmaf(y.z, f, sum.z);
+        sum.w = fmaf(y.w, f, sum.w);
       }
       *reinterpret_cast<float4*>(part + tid * 4) = sum;
-    }
-    if (tid < G) {
-      part[G * kHeadDim + tid] = s_M[tid];
-      part[G * kHeadDim + G + tid] = s_L[tid];
     }
     __syncthreads();
   }
@@ -450,9 +489,10 @@ void quant_attn_kernel(QuantAttnArgs x) {
 // Calls f with the kernel of these arguments.
 template <int G, int kBits, typename F>
 static hipError_t with_kernel_g(const QuantAttnArgs& x, F f) {
-  const bool table = x.blocks || x.kv.paged, mod = x.cap > 0.f || x.slopes;
-  if (table) return mod ? f(quant_attn_kernel<G, kBits, true, true>) : f(quant_attn_kernel<G, kBits, true, false>);
-  return mod ? f(quant_attn_kernel<G, kBits, false, true>) : f(quant_attn_kernel<G, kBits, false, false>);
+  const bool mod = x.cap > 0.f || x.slopes;
+  if (x.kv.paged && x.kv.pk.page_size % 16) return mod ? f(quant_attn_kernel<G, kBits, 2, true>) : f(quant_attn_kernel<G, kBits, 2, false>);
+  if (x.blocks || x.kv.paged) return mod ? f(quant_attn_kernel<G, kBits, 1, true>) : f(quant_attn_kernel<G, kBits, 1, false>);
+  return mod ? f(quant_attn_kernel<G, kBits, 0, true>) : f(quant_attn_kernel<G, kBits, 0, false>);
 }
 template <typename F>
 static hipError_t with_kernel(const QuantAttnArgs& x, int G, F f) {
