@@ -14,6 +14,8 @@ using tactic::kHeadDim;
 namespace {
 
 constexpr int64_t kMaxInt = ((int64_t)1 << 31) - 1;
+constexpr int64_t kDirectRows = 1024;
+constexpr int64_t kScoreGroups = 1024;
 
 tactic_status check_aligned(std::initializer_list<const void*> arrays, int bytes) {
   for (const void* p : arrays)
@@ -73,12 +75,15 @@ tactic::QuantRowsArgs rows_args(const tactic_kv_shape* s, const tactic_query_sha
 }
 
 struct SelectLayout {
-  int64_t max_blocks, tops, scores, top, keys, bytes;
+  int64_t max_blocks, per, tops, scores, top, keys, bytes;
 };
 SelectLayout select_layout(const tactic_kv_shape* s, int block) {
   SelectLayout l{};
   l.max_blocks = std::max<int64_t>(1, (s->max_seq_len + block - 1) / block);
-  l.tops = (l.max_blocks + tactic::kSelectRows - 1) / tactic::kSelectRows;
+  // scoring workgroups of whole 16 blocks, about four for each compute unit if the sequences are as long as the longest
+  const int64_t all = l.max_blocks * s->batch * s->n_kv_heads;
+  l.per = std::min<int64_t>(1024, std::max<int64_t>(16, (all / kScoreGroups + 15) / 16 * 16));
+  l.tops = (l.max_blocks + l.per - 1) / l.per;
   Layout L;
   const int64_t heads = (int64_t)s->batch * s->n_q_heads;
   l.scores = L.take(heads * l.max_blocks * 8);
@@ -168,6 +173,7 @@ tactic_status tactic_block_select(const uint16_t* q, const tactic_quant_kv* kv, 
   a.last = params->last;
   a.total = shape->total_tokens;
   a.max_blocks = l.max_blocks;
+  a.per = (int)l.per;
   a.tops = l.tops;
   a.scores = reinterpret_cast<double*>(ws + l.scores);
   a.top = reinterpret_cast<double*>(ws + l.top);
@@ -224,10 +230,21 @@ tactic_status tactic_quant_decode(const uint16_t* q, const tactic_quant_kv* kv, 
   tactic::JoinArgs j{};
   j.lse = lse;
   j.rows = (int64_t)shape->batch * shape->n_q_heads;
-  int grid = 0;
-  hipError_t e = tactic::quant_resident_grid(x, G, &grid);
-  if (e == hipSuccess) e = tactic::launch_quant_attn(x, G, std::min(grid, tactic::kMaxAttnGrid), stream);
-  if (e == hipSuccess) e = tactic::launch_join(x.a, j, G, stream);
+  // few rows for every group: one workgroup takes them, and no combine follows
+  const int64_t most = blocks ? std::min<int64_t>(shape->max_seq_len, (int64_t)budget * x.block) : shape->max_seq_len;
+  x.direct = most <= kDirectRows;
+  x.lse = lse;
+  hipError_t e = hipSuccess;
+  if (x.direct) {
+    e = tactic::launch_quant_attn(x, G, (int)groups, stream);
+  } else {
+    int grid = 0;
+    e = tactic::quant_resident_grid(x, G, &grid);
+    grid = std::min(grid, tactic::kMaxAttnGrid);
+    x.per_grid = 1.0 / std::max(grid, 1);
+    if (e == hipSuccess) e = tactic::launch_quant_attn(x, G, grid, stream);
+    if (e == hipSuccess) e = tactic::launch_join(x.a, j, G, stream);
+  }
   return e == hipSuccess ? TACTIC_OK : hip_fail(e, "quantised decode launch");
 }
 

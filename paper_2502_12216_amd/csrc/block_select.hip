@@ -9,81 +9,114 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "common.hpp"
 #include "kernels.hpp"
 #include "quant.hpp"
 
 namespace tactic {
 
-// 64 blocks of one KV head for its G query heads, four heads at a time (their queries are 128
-// registers).  A block is 512 bytes and 2 G 128 fused operations in 64 bits.
+// Sums over the 16 lanes of a DPP row of four values per lane, in every lane the total of value
+// sl / 4: each step pairs lanes over one lane bit, and while more than one value is left the lower
+// lane of a pair keeps the lower half of them and takes its partner's copy.  (Both partners
+// add the same two numbers, so lanes that end on the same value hold the same bits.)
+__device__ __forceinline__ double reduce4(const double (&v)[4], int sl) {
+  const bool up8 = sl & 8, up4 = sl & 4;
+  double c[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) c[i] = (up8 ? v[2 + i] : v[i]) + dpp<0x140>(up8 ? v[i] : v[2 + i]);  // row_mirror
+  double x = (up4 ? c[1] : c[0]) + dpp<0x141>(up4 ? c[0] : c[1]);  // row_half_mirror
+  x += dpp<0x4E>(x);
+  return x + dpp<0xB1>(x);
+}
+__device__ __forceinline__ double reduce2(const double (&v)[2], int sl) {  // of value sl / 8
+  const bool up8 = sl & 8;
+  double x = (up8 ? v[1] : v[0]) + dpp<0x140>(up8 ? v[0] : v[1]);
+  x += dpp<0x141>(x);
+  x += dpp<0x4E>(x);
+  return x + dpp<0xB1>(x);
+}
+
+// a.per blocks of one KV head for its G query heads, 16 at a time with the next ones on their way, four
+// heads at a time.  The larger of q lo and q hi is q (hi + lo) / 2 + |q| (hi - lo) / 2, whose
+// sums are exact as well: that needs half the registers of the positive and negative parts of
+// q (64 for four heads), so that four waves fit a SIMD.  A block is 512 bytes and 2 G 128 fused
+// operations in 64 bits, and about as many to make 64 bits of the bounds and to add up over the
+// lanes: bound by these from four heads on.
 template <int G>
 __global__ __launch_bounds__(256) void block_score_kernel(SelectArgs a) {
-  constexpr int H = G < 4 ? G : 4;
+  constexpr int H = G < 4 ? G : 4, kSpan = 16 / H;  // a head's score ends in kSpan lanes
+  constexpr int kAhead = 1;  // loads of 16 blocks on their way (2, 3 and 4 are slower: 10.4 against 11.8 us for 4 x 2048 blocks of 8 heads)
   __shared__ double s_top[16][G];
   const int tid = threadIdx.x, sl = tid & 15, sub = tid >> 4;
   const int g = blockIdx.y, b = blockIdx.z;
   const int lb = __builtin_ctz(a.block);
   const int64_t kvb = a.kv_indptr[b], n = seq_tokens(a.kv_indptr, a.seq_len, b);
   const int64_t nb = (n + a.block - 1) >> lb;
-  const int64_t j0 = (int64_t)blockIdx.x * kSelectRows;
+  const int64_t j0 = (int64_t)blockIdx.x * a.per, j1 = min(nb, j0 + a.per);
   if (j0 >= nb || nb <= a.budget) return;  // (all of them are chosen)
   const uint16_t* bounds = a.bounds + ((int64_t)g * ((a.total >> lb) + a.B) + first_block(kvb, lb, b)) * (2 * kHeadDim) + sl * 8;
-  uint4 lo[4], hi[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int64_t j = min(j0 + 16 * i + sub, nb - 1);
-    lo[i] = load_stream16(bounds + j * (2 * kHeadDim));
-    hi[i] = load_stream16(bounds + j * (2 * kHeadDim) + kHeadDim);
-  }
 #pragma unroll 1
   for (int h0 = 0; h0 < G; h0 += H) {
     const int64_t head = (int64_t)b * a.Hq + g * G + h0;
-    double pos[H][8], neg[H][8], best[H];
+    auto load = [&](int64_t j, uint4& lo, uint4& hi) __attribute__((always_inline)) {
+      const uint16_t* p = bounds + min(j + sub, j1 - 1) * (2 * kHeadDim);
+      lo = *reinterpret_cast<const uint4*>(p);
+      hi = *reinterpret_cast<const uint4*>(p + kHeadDim);
+    };
+    uint4 lo[kAhead], hi[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) load(min(j0 + 16 * k, j1 - 1), lo[k], hi[k]);
+    double q[H][8], best = -INFINITY;
 #pragma unroll
     for (int h = 0; h < H; ++h) {
       const uint4 w = *reinterpret_cast<const uint4*>(a.q + (head + h) * kHeadDim + sl * 8);
       const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-      best[h] = -INFINITY;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float q = e & 1 ? bf16hi(u[e >> 1]) : bf16lo(u[e >> 1]);
-        pos[h][e] = q < 0.f ? 0.0 : (double)q;
-        neg[h][e] = q < 0.f ? (double)q : 0.0;
+        q[h][e] = 0.5 * (double)(e & 1 ? bf16hi(u[e >> 1]) : bf16lo(u[e >> 1]));
       }
     }
-    double* scores = a.scores + head * a.max_blocks;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t j = j0 + 16 * i + sub;
+    double* scores = a.scores + (head + sl / kSpan) * a.max_blocks;
+    auto score = [&](const uint4& lw, const uint4& tw, int64_t j) __attribute__((always_inline)) {
       double u[H];
 #pragma unroll
       for (int h = 0; h < H; ++h) u[h] = 0.0;
-      const uint32_t l[4] = {lo[i].x, lo[i].y, lo[i].z, lo[i].w}, t[4] = {hi[i].x, hi[i].y, hi[i].z, hi[i].w};
+      const uint32_t l[4] = {lw.x, lw.y, lw.z, lw.w}, t[4] = {tw.x, tw.y, tw.z, tw.w};
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const double x = (double)(e & 1 ? bf16hi(l[e >> 1]) : bf16lo(l[e >> 1]));
         const double y = (double)(e & 1 ? bf16hi(t[e >> 1]) : bf16lo(t[e >> 1]));
+        const double sum = y + x, span = y - x;
 #pragma unroll
-        for (int h = 0; h < H; ++h) u[h] = fma(neg[h][e], x, fma(pos[h][e], y, u[h]));
+        for (int h = 0; h < H; ++h) u[h] = fma(fabs(q[h][e]), span, fma(q[h][e], sum, u[h]));
       }
+      double v;
+      if constexpr (H == 4) v = reduce4(u, sl);
+      else if constexpr (H == 2) v = reduce2(u, sl);
+      else v = sum16d(u[0]);
+      if (j + sub < j1) {
+        best = fmax(best, v);  // (NaN is passed over, and stored as what it counts as)
+        if (sl % kSpan == 0) scores[j + sub] = v != v ? INFINITY : v;
+      }
+    };
+#pragma unroll 1
+    for (int64_t j = j0; j < j1; j += 16 * kAhead) {
 #pragma unroll
-      for (int h = 0; h < H; ++h) {
-        u[h] = sum16d(u[h]);
-        if (j < nb) {
-          best[h] = fmax(best[h], u[h]);  // (NaN is passed over)
-          if (sl == 0) scores[(int64_t)h * a.max_blocks + j] = u[h];
-        }
+      for (int k = 0; k < kAhead; ++k) {
+        if (j + 16 * k >= j1) break;
+        const uint4 lw = lo[k], tw = hi[k];
+        load(min(j + 16 * (k + kAhead), j1 - 1), lo[k], hi[k]);
+        score(lw, tw, j + 16 * k);
       }
     }
-    if (sl == 0) {
-#pragma unroll
-      for (int h = 0; h < H; ++h) s_top[sub][h0 + h] = best[h];
-    }
+    if (sl % kSpan == 0) s_top[sub][h0 + sl / kSpan] = best;
   }
   __syncthreads();
   if (tid < G) {
     double v = s_top[0][tid];
+#pragma unroll
     for (int i = 1; i < 16; ++i) v = fmax(v, s_top[i][tid]);
     a.top[((int64_t)b * a.Hq + g * G + tid) * a.tops + blockIdx.x] = v;
   }
@@ -96,19 +129,45 @@ __device__ __forceinline__ uint64_t order_key(double x) {
   return u >> 63 ? ~u : u | 0x8000000000000000ull;
 }
 
-// The `budget` blocks of the largest keys of one KV head, ascending.  A radix selection:
-// digits of 11 bits from the first bit in which the keys differ (so that a digit spreads over
-// the scores there are), each with a histogram in LDS of the keys still level; it ends
-// as soon as all keys of the digit that holds the last one are wanted.  Thread t has blocks t kPer ..,
-// so that ranks and places are one scan; kPer = 0: the keys lie in the workspace.
+// Largest and smallest of a 32-bit word over the wave, in its last lane, by DPP
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+  auto step = [](uint32_t x, uint32_t y) { return max(x, y); };
+  v = step(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x111, 0xF, 0xF, false));
+  v = step(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x112, 0xF, 0xF, false));
+  v = step(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x114, 0xF, 0xF, false));
+  v = step(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x118, 0xF, 0xF, false));
+  v = step(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x142, 0xA, 0xF, false));
+  return step(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x143, 0xC, 0xF, false));
+}
+
+// The score of a key, and where it lies in the range of the free blocks' scores [-width, 0], as a number
+// that rises with it: equal ones are told apart by their keys.
+__device__ __forceinline__ double score_of(uint64_t key) {
+  return __builtin_bit_cast(double, key >> 63 ? key & 0x7fffffffffffffffull : ~key);
+}
+__device__ __forceinline__ uint32_t place_in_range(uint64_t key, double per_width) {
+  return (uint32_t)fmin(fmax(fma(score_of(key), per_width, 4294966784.0), 0.0), 4294967295.0);
+}
+
+// The `budget` blocks of the largest keys of one KV head, ascending.  A radix selection
+// in digits of 11 bits, each with a histogram in LDS of the keys still level, that ends as
+// soon as all keys of the digit that holds the last one are wanted: first over a key's place
+// in the range of scores, 32 bits linear (the bits of the scores themselves fill few bins, whose
+// counts wait for one another: the first digit of 8192 blocks took 8 us), then, where that
+// does not tell, over the keys from the first bit in which they differ.  Block j is thread
+// j mod 1024's; chosen ones find their places by one scan over the ballots of 64 blocks.
+// kPer = 0: the keys lie in the workspace and are gone through 16384 at a time.
+// Bound by its chain of loads, scans and barriers.
 template <int kPer>
 __global__ __launch_bounds__(1024) void block_select_kernel(SelectArgs a) {
-  constexpr int kBins = 2048, kThreads = 1024;
+  constexpr int kBins = 2048, kThreads = 1024, kHeld = kPer ? kPer : 16, kWords = kHeld * 16;
   __shared__ uint32_t s_hist[kBins];
   __shared__ double s_best[8];
-  __shared__ uint64_t s_min[16], s_max[16];
+  __shared__ uint32_t s_max[16];
+  __shared__ uint64_t s_least[16], s_most[16];
   __shared__ uint32_t s_wave[16][2];
   __shared__ uint32_t s_digit, s_above, s_in;
+  __shared__ uint32_t s_ahead[kWords][2];  // chosen and level blocks before each 64
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int g = blockIdx.x, b = blockIdx.y;
   const int lb = __builtin_ctz(a.block), G = a.G;
@@ -121,92 +180,130 @@ __global__ __launch_bounds__(1024) void block_select_kernel(SelectArgs a) {
     for (int i = tid; i < want; i += kThreads) out[i] = i;
     return;
   }
+  const double* scores = a.scores + ((int64_t)b * a.Hq + g * G) * a.max_blocks;
+  uint64_t* stored = a.keys + ((int64_t)b * a.Hkv + g) * a.max_blocks;
   // every head's best score: a wave for each
   if (wave < G) {
     const double* top = a.top + ((int64_t)b * a.Hq + g * G + wave) * a.tops;
     double v = -INFINITY;
-    for (int i = lane; i < (nb + kSelectRows - 1) / kSelectRows; i += kWave) v = fmax(v, top[i]);
+    for (int i = lane; i < (nb + a.per - 1) / a.per; i += kWave) v = fmax(v, top[i]);
     v = wave_allmax_d(v);
     if (lane == 0) s_best[wave] = v;
   }
+  for (int i = tid; i < kBins; i += kThreads) s_hist[i] = 0;
   __syncthreads();
-  const double* scores = a.scores + ((int64_t)b * a.Hq + g * G) * a.max_blocks;
-  uint64_t* stored = a.keys + ((int64_t)b * a.Hkv + g) * a.max_blocks;
-  const int per = kPer ? kPer : (nb + kThreads - 1) / kThreads;
-  const int j0 = tid * per;
-  auto key_of = [&](int j) -> uint64_t {
-    if (j < a.first || j >= nb - a.last) return ~0ull;
-    double best = -INFINITY;
-    bool odd = false;
-    for (int h = 0; h < G; ++h) {
-      const double d = scores[(int64_t)h * a.max_blocks + j] - s_best[h];
-      odd |= d != d;
-      best = fmax(best, d);
+  bool finite = true;  // else a difference may be NaN, which counts as +inf
+  for (int h = 0; h < G; ++h) finite &= fabs(s_best[h]) < INFINITY;
+  // the keys of K blocks from j on, kThreads apart, all loads first
+  auto keys_g = [&](auto count, auto heads, int j, uint64_t* keys) __attribute__((always_inline)) {
+    constexpr int K = decltype(count)::value, H = decltype(heads)::value;
+    double d[H][K];
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int i = 0; i < K; ++i) d[h][i] = scores[(int64_t)h * a.max_blocks + min(j + i * kThreads, nb - 1)];
+    double from[H];
+#pragma unroll
+    for (int h = 0; h < H; ++h) from[h] = s_best[h];
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+      double best = d[0][i] - from[0];
+      if (finite) {
+#pragma unroll
+        for (int h = 1; h < H; ++h) best = fmax(best, d[h][i] - from[h]);
+      } else {
+        bool odd = best != best;
+#pragma unroll
+        for (int h = 1; h < H; ++h) {
+          const double y = d[h][i] - from[h];
+          odd |= y != y;
+          best = fmax(best, y);
+        }
+        best = odd ? INFINITY : best;
+      }
+      keys[i] = order_key(best + 0.0);  // (-0 as 0)
     }
-    return order_key(odd ? INFINITY : best);
   };
-  uint64_t held[kPer ? kPer : 1];
-  uint64_t least = ~0ull, most = 0;
+  auto keys_of = [&](auto count, int j, uint64_t* keys) __attribute__((always_inline)) {
+    switch (G) {
+      case 1: keys_g(count, std::integral_constant<int, 1>{}, j, keys); break;
+      case 2: keys_g(count, std::integral_constant<int, 2>{}, j, keys); break;
+      case 4: keys_g(count, std::integral_constant<int, 4>{}, j, keys); break;
+      default: keys_g(count, std::integral_constant<int, 8>{}, j, keys); break;
+    }
+  };
+  // the first and the last blocks are chosen whatever their scores: they take no part in the selection
+  const int begin = min(a.first, nb), end = max(begin, nb - a.last), forced = nb - (end - begin);
+  auto free_block = [&](int j) { return j >= begin && j < end; };
+  uint64_t held[kHeld];
+  uint32_t place[kHeld];
+  uint32_t width = 0;  // the least finite score, its size as the bits of a float
+  {
+    constexpr int K = kHeld < 4 ? kHeld : 4;
+    for (int c = 0; c < nb; c += kHeld * kThreads) {  // (once with kPer)
+#pragma unroll
+      for (int i = 0; i < kHeld; i += K) {
+        if (c + i * kThreads >= nb) break;
+        keys_of(std::integral_constant<int, K>{}, c + i * kThreads + tid, held + i);
+#pragma unroll
+        for (int k = i; k < i + K; ++k) {
+          const int j = c + k * kThreads + tid;
+          const float x = -(float)score_of(held[k]);
+          if (free_block(j) && x < INFINITY) width = max(width, __float_as_uint(fmaxf(x, 0.f)));
+          if constexpr (kPer == 0) {  // (read back by the thread that wrote it)
+            if (j < nb) stored[j] = held[k];
+          }
+        }
+      }
+      if constexpr (kPer > 0) break;
+    }
+  }
+  width = wave_max_u32(width);
+  if (lane == kWave - 1) s_max[wave] = width;
+  __syncthreads();
+  width = s_max[0];
+#pragma unroll
+  for (int w = 1; w < 16; ++w) width = max(width, s_max[w]);
+  const double per_width = width ? 4294966784.0 / (double)__uint_as_float(width) : 1.0;
+  // f(block, key, place) of this thread's free blocks
+  auto fetch = [&](int c) __attribute__((always_inline)) {
+    if constexpr (kPer == 0) {
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) held[i] = stored[min(c + i * kThreads + tid, nb - 1 - (nb - 1 - tid) % kThreads)];
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) place[i] = place_in_range(held[i], per_width);
+    }
+  };
+  auto each = [&](auto f) __attribute__((always_inline)) {
+    for (int c = 0; c < nb; c += kHeld * kThreads) {
+      fetch(c);
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) {
+        if (c + i * kThreads >= nb) break;
+        if (free_block(c + i * kThreads + tid)) f(held[i], place[i]);
+      }
+      if constexpr (kPer > 0) break;
+    }
+  };
   if constexpr (kPer > 0) {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int j = j0 + i;
-      held[i] = j < nb ? key_of(j) : 0;
-      if (j < nb) {
-        least = min(least, held[i]);
-        most = max(most, held[i]);
-      }
-    }
-  } else {
-    for (int j = tid; j < nb; j += kThreads) {  // (written and read by the same workgroup only)
-      const uint64_t k = key_of(j);
-      stored[j] = k;
-      least = min(least, k);
-      most = max(most, k);
-    }
-    __threadfence_block();
-    __syncthreads();
+    for (int i = 0; i < kHeld; ++i) place[i] = place_in_range(held[i], per_width);
   }
-  auto each = [&](auto f) __attribute__((always_inline)) {  // (block, key) of this thread's blocks in order
-    if constexpr (kPer > 0) {
-#pragma unroll
-      for (int i = 0; i < kPer; ++i)
-        if (j0 + i < nb) f(j0 + i, held[i]);
-    } else {
-      for (int j = j0; j < min(nb, j0 + per); ++j) f(j, stored[j]);
-    }
-  };
-  for (int d = 32; d >= 1; d /= 2) {
-    least = min(least, (uint64_t)__shfl_xor((unsigned long long)least, d, 64));
-    most = max(most, (uint64_t)__shfl_xor((unsigned long long)most, d, 64));
-  }
-  if (lane == 0) {
-    s_min[wave] = least;
-    s_max[wave] = most;
-  }
-  __syncthreads();
-  for (int w = 0; w < 16; ++w) {
-    least = min(least, s_min[w]);
-    most = max(most, s_max[w]);
-  }
-  // keys agree above bit `low` with `prefix`; of those `need` are wanted
-  int low = least == most ? 0 : 64 - __clzll((long long)(least ^ most));
-  uint64_t prefix = low >= 64 ? 0 : most >> low;
-  uint32_t need = (uint32_t)want;
-  bool all = least == most ? (uint32_t)nb == need : false;
-  auto level = [&](uint64_t k) { return low >= 64 || k >> low == prefix; };
-  while (!all && low > 0) {
-    const int bits = min(low, 11), shift = low - bits;
-    for (int i = tid; i < kBins; i += kThreads) s_hist[i] = 0;
-    __syncthreads();
-    each([&](int, uint64_t k) {
-      if (level(k)) atomicAdd(&s_hist[(k >> shift) & ((1u << bits) - 1)], 1u);
+  uint32_t need = (uint32_t)(want - forced);  // wanted of the free blocks that are level so far
+  bool all = need == 0;
+  // a digit: counts of the level keys' digits, and the one that holds the last wanted key
+  auto digit = [&](auto digit_of) __attribute__((always_inline)) -> uint32_t {
+    each([&](uint64_t k, uint32_t p) {
+      const int d = digit_of(k, p);
+      if (d >= 0) atomicAdd(&s_hist[d], 1u);
     });
     __syncthreads();
     // thread t: bins 2 t and 2 t + 1 counted from the top
     const uint32_t c0 = s_hist[kBins - 1 - 2 * tid], c1 = s_hist[kBins - 2 - 2 * tid];
     const uint32_t incl = wave_incl_scan(c0 + c1);
     if (lane == 63) s_wave[wave][0] = incl;
+    s_hist[kBins - 1 - 2 * tid] = 0;  // for the next digit
+    s_hist[kBins - 2 - 2 * tid] = 0;
     __syncthreads();
     uint32_t ahead = incl - c0 - c1;
     for (int w = 0; w < wave; ++w) ahead += s_wave[w][0];
@@ -220,36 +317,112 @@ __global__ __launch_bounds__(1024) void block_select_kernel(SelectArgs a) {
       s_in = c1;
     }
     __syncthreads();
-    prefix = low >= 64 ? (uint64_t)s_digit : prefix << bits | s_digit;
     need -= s_above;
     all = s_in == need;
+    return s_digit;
+  };
+  // places agree above bit `low` with `prefix`
+  int low = 32;
+  uint32_t prefix = 0;
+  while (!all && low > 0) {
+    const int bits = min(low, 11), shift = low - bits;
+    const uint32_t d = digit([&](uint64_t, uint32_t p) {
+      return low == 32 || p >> low == prefix ? (int)(p >> shift & ((1u << bits) - 1)) : -1;
+    });
+    prefix = prefix << bits | d;
     low = shift;
   }
-  // chosen: keys above the prefix, and of those level with it all or the first `need`
-  uint32_t above = 0, same = 0;
-  each([&](int, uint64_t k) {
-    const uint64_t p = low >= 64 ? 0 : k >> low;
-    above += p > prefix;
-    same += p == prefix;
-  });
-  const uint32_t ia = wave_incl_scan(above), is = wave_incl_scan(same);
-  if (lane == 63) {
-    s_wave[wave][0] = ia;
-    s_wave[wave][1] = is;
+  auto level = [&](uint32_t p) { return low == 32 || p >> low == prefix; };
+  // the level keys agree above bit `key_low` with `key_prefix` (64: nothing said of them)
+  int key_low = 64;
+  uint64_t key_prefix = 0;
+  if (!all) {
+    uint64_t least = ~0ull, most = 0;
+    each([&](uint64_t k, uint32_t p) {
+      if (level(p)) {
+        least = min(least, k);
+        most = max(most, k);
+      }
+    });
+    for (int d = 32; d >= 1; d /= 2) {
+      least = min(least, (uint64_t)__shfl_xor((unsigned long long)least, d, 64));
+      most = max(most, (uint64_t)__shfl_xor((unsigned long long)most, d, 64));
+    }
+    if (lane == 0) {
+      s_least[wave] = least;
+      s_most[wave] = most;
+    }
+    __syncthreads();
+    for (int w = 0; w < 16; ++w) {
+      least = min(least, s_least[w]);
+      most = max(most, s_most[w]);
+    }
+    key_low = least == most ? 0 : 64 - __clzll((long long)(least ^ most));
+    key_prefix = key_low >= 64 ? 0 : most >> key_low;
+    while (!all && key_low > 0) {
+      const int bits = min(key_low, 11), shift = key_low - bits;
+      const uint32_t d = digit([&](uint64_t k, uint32_t p) {
+        return level(p) && (key_low >= 64 || k >> key_low == key_prefix) ? (int)(k >> shift & ((1u << bits) - 1)) : -1;
+      });
+      key_prefix = key_low >= 64 ? (uint64_t)d : key_prefix << bits | d;
+      key_low = shift;
+    }
   }
-  __syncthreads();
-  uint32_t pa = ia - above, ps = is - same;
-  for (int w = 0; w < wave; ++w) {
-    pa += s_wave[w][0];
-    ps += s_wave[w][1];
+  // chosen: the blocks that always are, those above the prefixes, and of those level with them the first `need`
+  uint32_t done_above = 0, done_same = 0;
+  for (int c = 0; c < nb; c += kHeld * kThreads) {
+    fetch(c);
+    uint64_t above[kHeld], same[kHeld];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      above[i] = same[i] = 0;
+      if (c + i * kThreads < nb) {
+        const int j = c + i * kThreads + tid;
+        const bool is_free = free_block(j), on = level(place[i]);
+        const uint64_t k = key_low >= 64 ? 0 : held[i] >> key_low;
+        const bool over = (low < 32 && place[i] >> low > prefix) || (on && k > key_prefix);
+        above[i] = __ballot(j < nb && (!is_free || (over && want > forced)));
+        same[i] = __ballot(is_free && on && k == key_prefix);
+      }
+      if (lane == 0) {
+        s_ahead[i * 16 + wave][0] = __popcll(above[i]);
+        s_ahead[i * 16 + wave][1] = __popcll(same[i]);
+      }
+    }
+    __syncthreads();
+    const bool mine = tid < kWords;
+    const uint32_t ca = mine ? s_ahead[tid][0] : 0, cs = mine ? s_ahead[tid][1] : 0;
+    const uint32_t ia = wave_incl_scan(ca), is = wave_incl_scan(cs);
+    if (lane == 63) {
+      s_wave[wave][0] = ia;
+      s_wave[wave][1] = is;
+    }
+    __syncthreads();
+    uint32_t pa = done_above + ia - ca, ps = done_same + is - cs;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+      const uint32_t wa = s_wave[w][0], ws = s_wave[w][1];
+      done_above += wa;
+      done_same += ws;
+      pa += w < wave ? wa : 0;
+      ps += w < wave ? ws : 0;
+    }
+    if (mine) {
+      s_ahead[tid][0] = pa;
+      s_ahead[tid][1] = ps;
+    }
+    __syncthreads();
+    const uint64_t before = (1ull << lane) - 1;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      if ((above[i] | same[i]) == 0) continue;  // (the wave has none)
+      const uint32_t at = s_ahead[i * 16 + wave][0] + __popcll(above[i] & before);
+      const uint32_t level_at = s_ahead[i * 16 + wave][1] + __popcll(same[i] & before);
+      if ((above[i] >> lane & 1) || ((same[i] >> lane & 1) && level_at < need)) out[at + min(level_at, need)] = c + i * kThreads + tid;
+    }
+    if constexpr (kPer > 0) break;
+    __syncthreads();
   }
-  each([&](int j, uint64_t k) {
-    const uint64_t p = low >= 64 ? 0 : k >> low;
-    const bool level_here = p == prefix, take = p > prefix || (level_here && ps < need);
-    if (take) out[pa + min(ps, need)] = j;
-    pa += p > prefix;
-    ps += level_here;
-  });
 }
 
 hipError_t launch_block_scores(const SelectArgs& a, hipStream_t st) {

@@ -270,13 +270,13 @@ hipError_t launch_quant_write(const QuantRowsArgs& a, hipStream_t st);
 hipError_t launch_quant_read(const QuantRowsArgs& a, hipStream_t st);
 
 // Scores of blocks from their bounds, and the best of them (block_select.hip).
-constexpr int kSelectRows = 64;     // blocks per scoring workgroup
 struct SelectArgs {
   const uint16_t* q;
   const uint16_t* bounds;
   const int64_t* kv_indptr;
   const int64_t* seq_len;
   int B, Hq, Hkv, G, block, budget, first, last;
+  int per;                      // blocks per scoring workgroup
   int64_t total, max_blocks, tops;  // tops: scoring workgroups of a sequence's head
   double* scores;               // [B][Hq][max_blocks]
   double* top;                  // [B][Hq][tops]: the largest score of each scoring workgroup
@@ -295,6 +295,9 @@ struct QuantAttnArgs {
   const int32_t* blocks;        // [B][Hkv][budget] or null: every row
   const int32_t* counts;        // [B][Hkv]
   int budget, block;
+  int direct;                   // a workgroup for each group, which writes the outputs itself
+  double per_grid;              // 1 / workgroups, else
+  float* lse;                   // [B][Hq] or null, direct
   float cap;
   const float* slopes;
 };

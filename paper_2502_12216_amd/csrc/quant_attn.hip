@@ -31,6 +31,11 @@ namespace tactic {
 constexpr float kScaleLog2 = kLog2e * kInvSqrtDim;
 constexpr int64_t kQuantShare = 256;  // rows of the least share
 constexpr int kTableRows = 2048;      // rows looked up at once
+#ifndef QWAVES
+#define QWAVES 4
+#endif
+constexpr int kWaves = QWAVES;        // waves of a workgroup
+constexpr int kStep = 32 * kWaves;    // rows of a step of all of them
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -65,7 +70,7 @@ __device__ __forceinline__ int64_t rows_of(const QuantAttnArgs& x, int bg) {
 // kRows: 0 rows lie at their positions; 1 every 16 positions from a multiple of 16 lie together
 // (chosen blocks, pages of a multiple of 16 rows); 2 rows lie anywhere
 template <int G, int kBits, int kRows, bool kMod>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ __launch_bounds__(kWave * kWaves) __attribute__((amdgpu_waves_per_eu(2)))
 void quant_attn_kernel(QuantAttnArgs x) {
   constexpr int kPart = G * (kHeadDim + 2);
   constexpr int S = G == 8 ? 2 : 1;           // sets of four heads
@@ -73,63 +78,81 @@ void quant_attn_kernel(QuantAttnArgs x) {
   constexpr int KW = kBits == 8 ? 2 : 1;      // 16-byte words of a lane's dimensions of K
   constexpr int VW = kBits == 8 ? 2 : 1;      // 4-byte words of its 8 values
   constexpr int kAhead = 1;  // steps loaded ahead
+  constexpr int kThreads = kWave * kWaves;
   const AttnArgs& a = x.a;
-  extern __shared__ int64_t s_prefix[];       // [B * NV + 1] units before each group
+  extern __shared__ int64_t s_prefix[];       // [B * NV + 1] units before each group, then int32 [B * NV] its rows
   union Shared {
     struct {
       int tile[kTableRows / 16];              // place of 16 positions (kRows 1)
       int row[kTableRows / 16];               // their rows of the sequence
       __align__(16) int place[kRows == 2 ? kTableRows : 1];
     } t;
-    float red[12][G][kHeadDim];               // the merge: three parts of four waves
+    float red[3 * kWaves][G][kHeadDim];       // the merge: three parts of every wave
   };
   __shared__ __align__(16) Shared sh;
-  __shared__ float s_ml[4][2][G], s_scale[4][G];
-  __shared__ int64_t s_wsum[4];
+  __shared__ float s_ml[kWaves][2][G];
+  __shared__ int64_t s_wsum[kWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int sl = lane & 15, grp = lane >> 4, hd = sl & 3;
   // what a lane takes off its weights: the upper 8 bits from the second part on, the next from the third on
   const uint32_t off1 = sl >= 4 ? 0xffff0000u : 0u, off2 = sl >= 8 ? 0xffff0000u : 0u;
   const int BG = a.B * a.NV;
-  // segments begin at multiples of 32 rows of their group
-  auto units = [&](int bg) { const int64_t n = rows_of(x, bg); return n > 0 ? ((n + 31) & ~(int64_t)31) + kSegmentCost : 0; };
-  {
-    const int per = (BG + 255) / 256, g0 = min(BG, tid * per), g1 = min(BG, g0 + per);
-    const int64_t u_first = g0 < g1 ? units(g0) : 0;
-    int64_t loc = u_first;
-    for (int bg = g0 + 1; bg < g1; ++bg) loc += units(bg);
+  // The rows of group bg, [seg_lo, seg_hi): all of them where every group has a workgroup of its
+  // own, else this workgroup's share of the units (rows plus the cost of a segment) of all groups,
+  // of which segments begin at multiples of 32 rows.
+  int bg = blockIdx.x, bg_end = bg + 1;
+  int64_t t0 = 0, t1 = INT64_MAX;
+  if (!x.direct) {
+    const int per = (BG + kThreads - 1) / kThreads, g0 = min(BG, tid * per), g1 = min(BG, g0 + per);
+    auto units = [&](int64_t n) { return n > 0 ? ((n + 31) & ~(int64_t)31) + kSegmentCost : 0; };
+    int32_t* const s_rows = reinterpret_cast<int32_t*>(s_prefix + BG + 1);
+    int64_t loc = 0;
+    for (int g = g0; g < g1; ++g) {
+      const int64_t n = rows_of(x, g);
+      s_rows[g] = (int32_t)n;
+      loc += units(n);
+    }
     const int64_t incl = wave_incl_scan(loc);
     if (lane == kWave - 1) s_wsum[wave] = incl;
     __syncthreads();
     int64_t run = incl - loc;
     for (int w = 0; w < wave; ++w) run += s_wsum[w];
-    for (int bg = g0; bg < g1; ++bg) {
-      s_prefix[bg] = run;
-      run += bg == g0 ? u_first : units(bg);
+    for (int g = g0; g < g1; ++g) {
+      s_prefix[g] = run;
+      run += units(s_rows[g]);
     }
-    if (tid == 255) s_prefix[BG] = run;
+    if (tid == kThreads - 1) s_prefix[BG] = run;
     __syncthreads();
+    const int64_t total = uniform(s_prefix[BG]);
+    // (at least the quotient: its error is far below the least fraction that it can have)
+    const int64_t even = (int64_t)((double)total * x.per_grid) + 1;
+    const int64_t share = max((even + 31) & ~(int64_t)31, kQuantShare);
+    if (blockIdx.x == 0) {  // for the combine
+      if (tid == 0) a.ameta[0] = share;
+      for (int g = tid; g <= BG; g += kThreads) a.ameta[1 + g] = s_prefix[g];
+    }
+    t0 = (int64_t)blockIdx.x * share;
+    t1 = min(total, t0 + share);
+    if (t0 >= t1) return;
+    // the largest group that starts at or before t0: 64 of them looked at in one step, then those between
+    const int stride = (BG + 63) / 64;
+    bg = (__popcll(__ballot(lane * stride < BG && s_prefix[min(lane * stride, BG)] <= t0)) - 1) * stride;
+    if (stride > 1) bg += __popcll(__ballot(lane < stride && bg + lane < BG && s_prefix[min(bg + lane, BG)] <= t0)) - 1;
+    bg = __builtin_amdgcn_readfirstlane(bg);
+    bg_end = BG;
   }
-  const int64_t total = uniform(s_prefix[BG]);
-  const int64_t share = max(((total + gridDim.x - 1) / gridDim.x + 31) & ~(int64_t)31, kQuantShare);
-  if (blockIdx.x == 0) {  // for the combine
-    if (tid == 0) a.ameta[0] = share;
-    for (int bg = tid; bg <= BG; bg += 256) a.ameta[1 + bg] = s_prefix[bg];
-  }
-  const int64_t t0 = (int64_t)blockIdx.x * share, t1 = min(total, t0 + share);
-  if (t0 >= t1) return;
-  int bg0 = 0, bgh = BG - 1;  // the largest group that starts at or before t0
-  while (bg0 < bgh) {
-    const int mid = (bg0 + bgh + 1) >> 1;
-    if (s_prefix[mid] <= t0) bg0 = mid;
-    else bgh = mid - 1;
-  }
-  bg0 = __builtin_amdgcn_readfirstlane(bg0);
 
-  for (int bg = bg0; bg < BG && uniform(s_prefix[bg]) < t1; ++bg) {
-    const int64_t first = uniform(s_prefix[bg]) + kSegmentCost;
-    const int64_t seg_lo = max(t0, first) - first, seg_hi = min(uniform(rows_of(x, bg)), t1 - first);
-    if (seg_lo >= seg_hi) continue;
+  for (; bg < bg_end; ++bg) {
+    int64_t seg_lo = 0, seg_hi;
+    if (x.direct) {
+      seg_hi = uniform(rows_of(x, bg));
+    } else {
+      const int64_t start = uniform(s_prefix[bg]);
+      if (start >= t1) break;
+      seg_lo = max(t0 - start - kSegmentCost, (int64_t)0);
+      seg_hi = min((int64_t)uniform(reinterpret_cast<const int32_t*>(s_prefix + BG + 1)[bg]), t1 - start - kSegmentCost);
+      if (seg_lo >= seg_hi) continue;
+    }
     const int b = bg / a.NV, kvh = bg % a.NV;
     const int64_t kvb = a.kv_indptr[b];
     const int nseq = (int)seq_tokens(a.kv_indptr, a.seq_len, b);
@@ -191,11 +214,11 @@ void quant_attn_kernel(QuantAttnArgs x) {
         r.v[i][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p));
       }
     };
-    // step `step` of this wave: positions 128 step + 32 wave .. + 31 of the sub-range; those
+    // step `step` of this wave: positions kStep step + 32 wave .. + 31 of the sub-range; those
     // past its end read its last row, which the group attends anyway
     auto load_tile = [&](int step) __attribute__((always_inline)) -> Tile {
       Tile r;
-      const int at = step * 128 + wave * 32;
+      const int at = step * kStep + wave * 32;
       if constexpr (kRows == 2) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -270,7 +293,7 @@ void quant_attn_kernel(QuantAttnArgs x) {
           for (int s = 0; s < S; ++s) d[s][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qv[s][j], d[s][t], 0, 0, 0);
         }
       }
-      const int at = step * 128 + wave * 32;
+      const int at = step * kStep + wave * 32;
       bf16x8 part[S];
 #pragma unroll
       for (int s = 0; s < S; ++s) {
@@ -379,19 +402,19 @@ void quant_attn_kernel(QuantAttnArgs x) {
           }
         }
         if constexpr (kRows == 2) {
-          constexpr int kPer = kTableRows / 256;
+          constexpr int kPer = kTableRows / kThreads;
           int rr[kPer];
           int64_t pr[kPer];
 #pragma unroll
-          for (int e = 0; e < kPer; ++e) rr[e] = row_at(p + min(tid + e * 256, cnt - 1));
+          for (int e = 0; e < kPer; ++e) rr[e] = row_at(p + min(tid + e * kThreads, cnt - 1));
           paged_rows(x.kv.pk, a.Hkv, a.total, kvb, b, kvh, rr, 0, pr);
 #pragma unroll
           for (int e = 0; e < kPer; ++e)
-            if (tid + e * 256 < cnt) sh.t.place[tid + e * 256] = (int)pr[e];
+            if (tid + e * kThreads < cnt) sh.t.place[tid + e * kThreads] = (int)pr[e];
         }
         __syncthreads();
       }
-      const int steps = (max(cnt - wave * 32, 0) + 127) / 128;
+      const int steps = (max(cnt - wave * 32, 0) + kStep - 1) / kStep;
       if (steps > 0) {
         Tile y0 = load_tile(0);
         if constexpr (kAhead == 1) {
@@ -426,7 +449,7 @@ void quant_attn_kernel(QuantAttnArgs x) {
       if constexpr (kRows != 0) __syncthreads();  // the next sub-range, or the merge, rewrites the table
     }
 
-    // ---- merge the four waves: common maximum, rescale, sum
+    // ---- merge the waves: common maximum, rescale, sum
 #pragma unroll
     for (int s = 0; s < S; ++s) {
       l[s] += __shfl_xor(l[s], 16, 64);
@@ -445,27 +468,16 @@ void quant_attn_kernel(QuantAttnArgs x) {
       }
     }
     __syncthreads();
-    float* part = a.partials + ((int64_t)bg + blockIdx.x) * kPart;
-    if (tid < G) {
-      float mm = -INFINITY, ll = 0.f;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) mm = fmaxf(mm, s_ml[w][1][tid] == 0.f ? -INFINITY : s_ml[w][0][tid]);
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float lw = s_ml[w][1][tid], f = lw == 0.f ? 0.f : fast_exp2(s_ml[w][0][tid] - mm);
-        s_scale[w][tid] = f;
-        ll = fmaf(lw, f, ll);
-      }
-      part[G * kHeadDim + tid] = mm;
-      part[G * kHeadDim + G + tid] = ll;
-    }
-    __syncthreads();
     if (tid * 4 < G * kHeadDim) {
       const int h = tid * 4 / kHeadDim, e = tid * 4 % kHeadDim;
+      float mm = -INFINITY, ll = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, s_ml[w][1][h] == 0.f ? -INFINITY : s_ml[w][0][h]);
       float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float f = s_scale[w][h];
+      for (int w = 0; w < kWaves; ++w) {
+        const float lw = s_ml[w][1][h], f = lw == 0.f ? 0.f : fast_exp2(s_ml[w][0][h] - mm);
+        ll = fmaf(lw, f, ll);
         float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int q = 2; q >= 0; --q) {  // the small parts first
@@ -480,9 +492,22 @@ void quant_attn_kernel(QuantAttnArgs x) {
         sum.z = fmaf(y.z, f, sum.z);
         sum.w = fmaf(y.w, f, sum.w);
       }
-      *reinterpret_cast<float4*>(part + tid * 4) = sum;
+      if (x.direct) {
+        const int64_t row = (int64_t)b * a.Hq + kvh * G + h;
+        const bool empty = mm == -INFINITY;
+        if (empty) sum = make_float4(0.f, 0.f, 0.f, 0.f), ll = 1.f;
+        *reinterpret_cast<float4*>(a.out + row * kHeadDim + e) = make_float4(sum.x / ll, sum.y / ll, sum.z / ll, sum.w / ll);
+        if (e == 0 && x.lse) x.lse[row] = empty ? -INFINITY : (mm + __builtin_amdgcn_logf(ll)) * kLn2;
+      } else {
+        float* part = a.partials + ((int64_t)bg + blockIdx.x) * kPart;
+        *reinterpret_cast<float4*>(part + tid * 4) = sum;
+        if (e == 0) {
+          part[G * kHeadDim + h] = mm;
+          part[G * kHeadDim + G + h] = ll;
+        }
+      }
     }
-    __syncthreads();
+    if (bg + 1 < bg_end) __syncthreads();
   }
 }
 
@@ -506,21 +531,25 @@ static hipError_t with_kernel(const QuantAttnArgs& x, int G, F f) {
   }
 }
 
+// Dynamic LDS of the units before each group and of the groups' rows
+static size_t prefix_lds(const QuantAttnArgs& x) {
+  const size_t groups = (size_t)x.a.B * x.a.NV;
+  return x.direct ? 0 : (groups + 1) * sizeof(int64_t) + groups * sizeof(int32_t);
+}
+
 hipError_t quant_resident_grid(const QuantAttnArgs& x, int G, int* grid) {
   int dev = 0, cus = 0, per = 0;
-  const size_t lds = ((size_t)x.a.B * x.a.NV + 1) * sizeof(int64_t);
   hipError_t e = hipGetDevice(&dev);
   if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
   if (e == hipSuccess)
-    e = with_kernel(x, G, [&](auto kernel) { return hipOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, 256, lds); });
+    e = with_kernel(x, G, [&](auto kernel) { return hipOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, kWave * kWaves, prefix_lds(x)); });
   *grid = std::max(per, 1) * std::max(cus, 1);
   return e;
 }
 
 hipError_t launch_quant_attn(const QuantAttnArgs& x, int G, int grid, hipStream_t st) {
-  const size_t lds = ((size_t)x.a.B * x.a.NV + 1) * sizeof(int64_t);
   return with_kernel(x, G, [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), lds, st, x);
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(kWave * kWaves), prefix_lds(x), st, x);
     return hipGetLastError();
   });
 }

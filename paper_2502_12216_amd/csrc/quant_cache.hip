@@ -13,19 +13,39 @@
 
 namespace tactic {
 
-// The sequence of work item `item` where sequence b's items start at at(b), which rises
-// with b: 64 of them looked at in one step, a lane each.  Uniform over the workgroup.
-template <typename At>
-__device__ __forceinline__ int source_of(int64_t item, int B, At at) {
+// A work item's sequence and what is known of it, the same in all lanes.
+struct Source {
+  int b;
+  int64_t first, rows, kvb, n;  // its rows among all, how many; its span's start, its length
+};
+
+// The sequence of work item `item` where the items of one that starts at row r of all are from
+// r / kRows + extra b on: 64 sequences looked at in one step, a lane each, with all that
+// is read of them loaded at once.
+template <int kRows, int kExtra>
+__device__ __forceinline__ Source source_of(const QuantRowsArgs& a, int64_t item) {
   const int lane = threadIdx.x & (kWave - 1);
-  int b = 0;
-  for (int b0 = 0; b0 < B; b0 += kWave) {
-    const bool before = b0 + lane < B && at(min(b0 + lane, B - 1)) <= item;
-    const int n = __popcll(__ballot(before));
-    if (n > 0) b = b0 + n - 1;
+  Source s{};
+  for (int b0 = 0; b0 < a.B; b0 += kWave) {
+    const int b = min(b0 + lane, a.B - 1);
+    const int64_t r0 = a.row_indptr[b], r1 = a.row_indptr[b + 1], k0 = a.kv_indptr[b], k1 = a.kv_indptr[b + 1];
+    const int64_t len = a.seq_len ? a.seq_len[b] : k1 - k0;
+    const int n = __popcll(__ballot(b0 + lane < a.B && r0 / kRows + kExtra * (int64_t)b <= item));
+    if (n > 0) {
+      auto of = [&](int64_t x) {
+        return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), n - 1) << 32 |
+                         (uint32_t)__builtin_amdgcn_readlane((int)x, n - 1));
+      };
+      s.b = b0 + n - 1;
+      s.first = of(r0);
+      s.rows = of(r1 - r0);
+      s.kvb = of(k0);
+      s.n = of(max((int64_t)0, min(len, k1 - k0)));
+    }
     if (n < kWave) break;
   }
-  return __builtin_amdgcn_readfirstlane(b);
+  s.b = __builtin_amdgcn_readfirstlane(s.b);
+  return s;
 }
 
 // Index of sequence row `row` among the rows of [Hkv][total] or [num_pages][Hkv][page_size];
@@ -55,18 +75,16 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
 template <int kBits, int kPass, bool kBounds>
 __global__ __launch_bounds__(256) void quant_write_kernel(QuantRowsArgs a) {
   constexpr int kRows = 16 * kPass, kWaveRows = 4 * kPass;
-  __shared__ float s_lo[4][kHeadDim], s_hi[4][kHeadDim];
+  __shared__ __align__(16) float s_bound[2][16][kHeadDim];  // of the rows of four lane groups of four waves
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, sl = lane & 15, grp = lane >> 4;
   const int g = blockIdx.y >> 1;
   const bool values = blockIdx.y & 1;
-  const int64_t item = blockIdx.x;
   // a sequence of m new rows meets at most m / kRows + 2 pieces of its cache
-  auto at = [&](int b) { return a.row_indptr[b] / kRows + 2 * (int64_t)b; };
-  const int b = source_of(item, a.B, at);
-  const int64_t r0 = a.row_indptr[b], m = a.row_indptr[b + 1] - r0, kvb = a.kv_indptr[b];
-  const int64_t n = seq_tokens(a.kv_indptr, a.seq_len, b);
+  const Source src = source_of<kRows, 2>(a, blockIdx.x);
+  const int b = src.b;
+  const int64_t r0 = src.first, m = src.rows, kvb = src.kvb, n = src.n;
   const int64_t start = max(n - m, (int64_t)0);  // the first row that is written
-  const int64_t piece = start / kRows + (item - at(b));
+  const int64_t piece = start / kRows + ((int64_t)blockIdx.x - (r0 / kRows + 2 * (int64_t)b));
   if (m <= 0 || piece * kRows >= n) return;
   const int row0 = (int)(piece * kRows) + wave * kWaveRows + grp;
   // rows before the new ones count for the bounds from the first touched block on
@@ -144,36 +162,30 @@ __global__ __launch_bounds__(256) void quant_write_kernel(QuantRowsArgs a) {
   if constexpr (kBounds) {
     if (values) return;  // (the whole workgroup)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < 8; ++e)
       if (odd) lo[e] = hi[e] = __builtin_nanf("");
 #pragma unroll
-      for (int d = 16; d <= 32; d *= 2) {
-        const float l = __shfl_xor(lo[e], d, 64), h = __shfl_xor(hi[e], d, 64);
-        // (NaN stays)
-        lo[e] = l != l || lo[e] != lo[e] ? __builtin_nanf("") : fminf(lo[e], l);
-        hi[e] = h != h || hi[e] != hi[e] ? __builtin_nanf("") : fmaxf(hi[e], h);
-      }
-      if (grp == 0) {
-        s_lo[wave][sl * 8 + e] = lo[e];
-        s_hi[wave][sl * 8 + e] = hi[e];
-      }
+    for (int e = 0; e < 8; e += 4) {
+      *reinterpret_cast<float4*>(&s_bound[0][wave * 4 + grp][sl * 8 + e]) = make_float4(lo[e], lo[e + 1], lo[e + 2], lo[e + 3]);
+      *reinterpret_cast<float4*>(&s_bound[1][wave * 4 + grp][sl * 8 + e]) = make_float4(hi[e], hi[e + 1], hi[e + 2], hi[e + 3]);
     }
     __syncthreads();
     // block j of the piece: the waves of its rows; a thread takes one dimension of one side
-    const int per = max(1, a.kv.block / kWaveRows), blocks = kRows >> log_block;
+    const int per = 4 * max(1, a.kv.block / kWaveRows), blocks = kRows >> log_block;
     const int64_t out = (int64_t)g * ((a.total >> log_block) + a.B) + first_block(kvb, log_block, b);
     const int side = tid >> 7, d = tid & 127;
-    const float(*src)[kHeadDim] = side ? s_hi : s_lo;
     for (int j = 0; j < blocks; ++j) {
       const int64_t block = piece * blocks + j;
       if (block << log_block < from || block << log_block >= n) continue;
-      float v = src[j * per][d];
-      for (int w = 1; w < per; ++w) {
-        const float y = src[j * per + w][d];
-        v = v != v || y != y ? __builtin_nanf("") : side ? fmaxf(v, y) : fminf(v, y);
+      float v = side ? -INFINITY : INFINITY;
+      bool odd_here = false;
+      for (int w = 0; w < per; ++w) {
+        const float y = s_bound[side][j * per + w][d];
+        odd_here |= y != y;
+        v = side ? fmaxf(v, y) : fminf(v, y);
       }
       // exact: every value read from the cache is a bf16
-      a.kv.bounds[((out + block) * 2 + side) * kHeadDim + d] = v != v ? (uint16_t)0x7fc0 : (uint16_t)(__float_as_uint(v) >> 16);
+      a.kv.bounds[((out + block) * 2 + side) * kHeadDim + d] = odd_here ? (uint16_t)0x7fc0 : (uint16_t)(__float_as_uint(v) >> 16);
     }
   }
 }
@@ -185,11 +197,10 @@ __global__ __launch_bounds__(256) void quant_read_kernel(QuantRowsArgs a) {
   const int tid = threadIdx.x, sl = tid & 15, sub = tid >> 4;
   const int g = blockIdx.y >> 1;
   const bool values = blockIdx.y & 1;
-  const int64_t item = blockIdx.x;
-  auto at = [&](int b) { return a.row_indptr[b] / 64 + (int64_t)b; };
-  const int b = source_of(item, a.B, at);
-  const int64_t r0 = a.row_indptr[b], m = a.row_indptr[b + 1] - r0, kvb = a.kv_indptr[b];
-  const int64_t n = seq_tokens(a.kv_indptr, a.seq_len, b), i0 = (item - at(b)) * 64;
+  const Source src = source_of<64, 1>(a, blockIdx.x);
+  const int b = src.b;
+  const int64_t r0 = src.first, m = src.rows, kvb = src.kvb, n = src.n;
+  const int64_t i0 = ((int64_t)blockIdx.x - (r0 / 64 + b)) * 64;
   const uint8_t* codes = values ? a.kv.V : a.kv.K;
   const uint8_t* scales = values ? a.kv.V_scale : a.kv.K_scale;
   uint16_t* out = (values ? a.V_out : a.K_out) + (int64_t)g * a.n_rows * kHeadDim;
