@@ -1,5 +1,6 @@
 // Host side of the quantised cache: rows in and out, chosen blocks, single-token decode.
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <string.h>
 
 #include <algorithm>
@@ -14,7 +15,6 @@ using tactic::kHeadDim;
 namespace {
 
 constexpr int64_t kMaxInt = ((int64_t)1 << 31) - 1;
-constexpr int64_t kDirectRows = 1024;
 constexpr int64_t kScoreGroups = 1024;
 
 tactic_status check_aligned(std::initializer_list<const void*> arrays, int bytes) {
@@ -91,6 +91,25 @@ SelectLayout select_layout(const tactic_kv_shape* s, int block) {
   l.keys = l.max_blocks > tactic::kSelectHeld ? L.take((int64_t)s->batch * s->n_kv_heads * l.max_blocks * 8) : 0;
   l.bytes = L.cur;
   return l;
+}
+
+// Whether the decode gives every KV head one workgroup, which joins its own waves and writes the
+// outputs, or splits all rows evenly and joins the parts in a second launch.  One workgroup takes 5.5 us
+// and `step` us for 128 rows of its four waves, or what memory gives it; the split 11 to 14.5
+// us (a start that looks at every group, the second launch) and the bytes at 6 TB/s.  Measured, one
+// against split, us a call, rows of 8 KV heads, 8 bits and 4 heads each: one sequence
+// of 256 rows 7.2, 11.3; 512 9.7, 11.7; 768 12.3, 11.9; 1024 15.1, 12.1; 32 sequences of 256 8.4,
+// 16.5; 1024 17.2, 25.9; 2048 28.6, 36.6; 8 sequences at 4 bits 512 8.0, 11.1; 1024 11.1,
+// 12.5; 1536 14.3, 12.9; with 8 heads at 8 bits 512 12.3, 14.4; 1024 18.4, 18.6.  One workgroup
+// is as slow as its longest sequence, so that it is not used from 2048 rows on.
+bool one_workgroup(const tactic_kv_shape* s, int bits, int64_t most) {
+  if (most > 2048) return false;
+  const double groups = (double)s->batch * s->n_kv_heads, row = 2 * (16.0 * bits + 4) / 6e6;
+  const double step = (bits == 8 ? 1.25 : 0.8) * (s->n_q_heads / s->n_kv_heads == 8 ? 1.2 : 1.0);
+  const double rounds = std::max(1.0, ceil(groups / 512));
+  const double all = std::min((double)s->total_tokens * s->n_kv_heads, groups * (double)most);
+  const double one = 5.5 + (double)most * rounds * std::max(step / 128, std::min(groups, 512.0) * row);
+  return one <= 11 + 3.5 * std::min(1.0, groups / 256) + all * row;
 }
 
 bool is_block(int block) { return block == 16 || block == 32 || block == 64 || block == 128; }
@@ -230,9 +249,8 @@ tactic_status tactic_quant_decode(const uint16_t* q, const tactic_quant_kv* kv, 
   tactic::JoinArgs j{};
   j.lse = lse;
   j.rows = (int64_t)shape->batch * shape->n_q_heads;
-  // few rows for every group: one workgroup takes them, and no combine follows
   const int64_t most = blocks ? std::min<int64_t>(shape->max_seq_len, (int64_t)budget * x.block) : shape->max_seq_len;
-  x.direct = most <= kDirectRows;
+  x.direct = one_workgroup(shape, x.kv.bits, most);
   x.lse = lse;
   hipError_t e = hipSuccess;
   if (x.direct) {

@@ -31,10 +31,7 @@ namespace tactic {
 constexpr float kScaleLog2 = kLog2e * kInvSqrtDim;
 constexpr int64_t kQuantShare = 256;  // rows of the least share
 constexpr int kTableRows = 2048;      // rows looked up at once
-#ifndef QWAVES
-#define QWAVES 4
-#endif
-constexpr int kWaves = QWAVES;        // waves of a workgroup
+constexpr int kWaves = 4;             // waves of a workgroup (eight: 3 to 11% slower)
 constexpr int kStep = 32 * kWaves;    // rows of a step of all of them
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -77,7 +74,6 @@ void quant_attn_kernel(QuantAttnArgs x) {
   constexpr int RB = kRowBytes<kBits>;
   constexpr int KW = kBits == 8 ? 2 : 1;      // 16-byte words of a lane's dimensions of K
   constexpr int VW = kBits == 8 ? 2 : 1;      // 4-byte words of its 8 values
-  constexpr int kAhead = 1;  // steps loaded ahead
   constexpr int kThreads = kWave * kWaves;
   const AttnArgs& a = x.a;
   extern __shared__ int64_t s_prefix[];       // [B * NV + 1] units before each group, then int32 [B * NV] its rows
@@ -417,33 +413,16 @@ void quant_attn_kernel(QuantAttnArgs x) {
       const int steps = (max(cnt - wave * 32, 0) + kStep - 1) / kStep;
       if (steps > 0) {
         Tile y0 = load_tile(0);
-        if constexpr (kAhead == 1) {
+        // (one step ahead; two: at most 8% faster for short sequences, 10% to 60% slower with eight heads)
 #pragma unroll 1
-          for (int s = 0; s < steps; s += 2) {
-            const Tile y1 = load_tile(s + 1);
-            __builtin_amdgcn_sched_barrier(0);
-            consume(y0, s);
-            if (s + 1 >= steps) break;
-            y0 = load_tile(s + 2);
-            __builtin_amdgcn_sched_barrier(0);
-            consume(y1, s + 1);
-          }
-        } else {
-          Tile y1 = load_tile(1);
-#pragma unroll 1
-          for (int s = 0; s < steps; s += 3) {
-            Tile y2 = load_tile(s + 2);
-            __builtin_amdgcn_sched_barrier(0);
-            consume(y0, s);
-            if (s + 1 >= steps) break;
-            y0 = load_tile(s + 3);
-            __builtin_amdgcn_sched_barrier(0);
-            consume(y1, s + 1);
-            if (s + 2 >= steps) break;
-            y1 = load_tile(s + 4);
-            __builtin_amdgcn_sched_barrier(0);
-            consume(y2, s + 2);
-          }
+        for (int s = 0; s < steps; s += 2) {
+          const Tile y1 = load_tile(s + 1);  // (a load past the last step reads its row again)
+          __builtin_amdgcn_sched_barrier(0);
+          consume(y0, s);
+          if (s + 1 >= steps) break;
+          y0 = load_tile(s + 2);
+          __builtin_amdgcn_sched_barrier(0);
+          consume(y1, s + 1);
         }
       }
       if constexpr (kRows != 0) __syncthreads();  // the next sub-range, or the merge, rewrites the table

@@ -12,7 +12,7 @@ from typing import Optional, Sequence
 import torch
 
 from . import _capi as C
-from .attention import ScoreMod, _Call, _device, _mod, _workspace
+from .attention import ScoreMod, _Call, _device, _workspace
 from .tactic import RaggedBatch, _indptr
 
 BLOCKS = (16, 32, 64, 128)
@@ -66,25 +66,23 @@ class QuantizedCache:
 
     def struct(self, call: _Call, batch: RaggedBatch, rows: bool = True) -> C.QuantKV:
         """The C struct after its checks against a batch (rows: its rows are used, not the bounds alone)."""
-        kv = C.QuantKV(bits=self.bits, block=self.block)
-        t = call.tensor
-        if rows:
-            if self.page_table is None:
-                shape = (batch.n_kv_heads, batch.total)
-            else:
-                shape = (self.K.shape[0], batch.n_kv_heads, self.K.shape[2])
-                kv.page_table = t(self.page_table, "cache.page_table", torch.int32)
-                if tuple(self.page_table.shape) != (batch.batch, self.page_table.shape[-1]):
-                    raise ValueError(f"cache.page_table must be [{batch.batch}][..], got {list(self.page_table.shape)}")
-                kv.num_pages, kv.page_size, kv.max_pages = shape[0], shape[2], self.page_table.shape[1]
-            wide, scale = shape + (16 * self.bits,), shape + (4,)
-            kv.K, kv.V = t(self.K, "cache.K", torch.uint8, wide), t(self.V, "cache.V", torch.uint8, wide)
-            kv.K_scale = t(self.K_scale, "cache.K_scale", torch.uint8, scale)
-            kv.V_scale = t(self.V_scale, "cache.V_scale", torch.uint8, scale)
+        t, u8, heads, bits, block = call.tensor, torch.uint8, batch.n_kv_heads, self.bits, self.block
+        bounds = None
         if self.bounds is not None:
-            kv.bounds = t(self.bounds, "cache.bounds", torch.bfloat16,
-                          (batch.n_kv_heads, batch.total // self.block + batch.batch, 2, 128))
-        return kv
+            bounds = t(self.bounds, "cache.bounds", torch.bfloat16, (heads, batch.total // block + batch.batch, 2, 128))
+        if not rows:
+            return C.QuantKV(None, None, None, None, bounds, None, bits, block, 0, 0, 0)
+        table, pages = self.page_table, (0, 0, 0)
+        if table is None:
+            wide, scale = (heads, batch.total, 16 * bits), (heads, batch.total, 4)
+        else:
+            num_pages, _, page_size, _ = self.K.shape
+            wide, scale = (num_pages, heads, page_size, 16 * bits), (num_pages, heads, page_size, 4)
+            pages = (page_size, table.shape[-1], num_pages)
+            table = t(table, "cache.page_table", torch.int32, (batch.batch, pages[1]))
+        return C.QuantKV(t(self.K, "cache.K", u8, wide), t(self.K_scale, "cache.K_scale", u8, scale),
+                         t(self.V, "cache.V", u8, wide), t(self.V_scale, "cache.V_scale", u8, scale), bounds, table, bits, block,
+                         *pages)
 
 
 class CacheQuantizer:
@@ -195,9 +193,10 @@ class QuantizedDecoder:
             if blocks.dim() != 3:
                 raise ValueError(f"blocks must be [{b.batch}][{b.n_kv_heads}][budget], got {list(blocks.shape)}")
             budget = int(blocks.shape[2])
-        kv, m = cache.struct(call, b), _mod(mod, call, b)
+        kv = cache.struct(call, b)
+        m = None if mod is None else ctypes.byref(mod.struct(call, b))
         call.run("tactic_quant_decode", t(q, "q", torch.bfloat16, (b.batch, b.n_q_heads, 128)), ctypes.byref(kv),
-                 ctypes.byref(self._shape), ctypes.byref(m),
+                 ctypes.byref(self._shape), m,
                  t(blocks, "blocks", torch.int32, (b.batch, b.n_kv_heads, budget), True),
                  t(counts, "counts", torch.int32, (b.batch, b.n_kv_heads), True), budget,
                  t(out, "out", torch.float32, (b.batch, b.n_q_heads, 128)),
