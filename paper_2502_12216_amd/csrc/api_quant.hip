@@ -94,9 +94,10 @@ SelectLayout select_layout(const tactic_kv_shape* s, int block) {
 }
 
 // Whether the decode gives every KV head one workgroup, which joins its own waves and writes the
-// outputs, or splits all rows evenly and joins the parts in a second launch.  One workgroup takes 5.5 us
+// outputs, or splits all rows evenly and joins the parts in a second launch.  One workgroup takes 4.7 us
 // and `step` us for 128 rows of its four waves, or what memory gives it; the split 11 to 14.5
-// us (a start that looks at every group, the second launch) and the bytes at 6 TB/s.  Measured, one
+// us (a start that looks at every group, the second launch, and 4 us more on the host) and the
+// bytes at 6 TB/s.  Measured, one
 // against split, us a call, rows of 8 KV heads, 8 bits and 4 heads each: one sequence
 // of 256 rows 7.2, 11.3; 512 9.7, 11.7; 768 12.3, 11.9; 1024 15.1, 12.1; 32 sequences of 256 8.4,
 // 16.5; 1024 17.2, 25.9; 2048 28.6, 36.6; 8 sequences at 4 bits 512 8.0, 11.1; 1024 11.1,
@@ -108,8 +109,8 @@ bool one_workgroup(const tactic_kv_shape* s, int bits, int64_t most) {
   const double step = (bits == 8 ? 1.25 : 0.8) * (s->n_q_heads / s->n_kv_heads == 8 ? 1.2 : 1.0);
   const double rounds = std::max(1.0, ceil(groups / 512));
   const double all = std::min((double)s->total_tokens * s->n_kv_heads, groups * (double)most);
-  const double one = 5.5 + (double)most * rounds * std::max(step / 128, std::min(groups, 512.0) * row);
-  return one <= 11 + 3.5 * std::min(1.0, groups / 256) + all * row;
+  const double one = 4.7 + (double)most * rounds * std::max(step / 128, std::min(groups, 512.0) * row);
+  return one <= 12 + 3.5 * std::min(1.0, groups / 256) + all * row;
 }
 
 bool is_block(int block) { return block == 16 || block == 32 || block == 64 || block == 128; }
