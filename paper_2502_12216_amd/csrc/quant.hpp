@@ -17,6 +17,8 @@
 namespace tactic {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
 template <int kBits>
 constexpr int kRowBytes = 16 * kBits;
@@ -30,33 +32,38 @@ __device__ __forceinline__ int scale_byte(uint32_t top) {
 }
 __device__ __forceinline__ float power_of(int byte) { return __uint_as_float((uint32_t)byte << 23); }  // (255: inf, makes NaN of any code)
 
-// Codes of 8 values (words of two bf16) of a group: 8 or 4 bytes.  The product with the
-// power is exact, the conversion rounds to nearest, ties to even; values above the largest
-// number (where the power is at its limit) are held to it, a group of NaN has codes 0.
+// Codes of 8 values (words of two bf16) of a group: 8 or 4 bytes.  The conversions divide by the power
+// and round to nearest, ties to even (checked for every bf16).  Values above the largest number
+// (where the power is at its limit) are held to it: e2m1's conversion does, e4m3's gives NaN
+// beyond 464.  A group of NaN has codes 0.
 template <int kBits>
 __device__ __forceinline__ uint2 encode8(const uint4& x, int byte) {
-  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-  const float inv = byte == 255 ? 0.f : __uint_as_float((uint32_t)(254 - byte) << 23);
-  constexpr float kTop = kBits == 8 ? 448.f : 6.f;
-  float y[8];
+  uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  const uint32_t keep = byte == 255 ? 0u : ~0u;
+  const float power = power_of(byte == 255 ? 127 : byte);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    y[2 * i] = bf16lo(w[i]) * inv;
-    y[2 * i + 1] = bf16hi(w[i]) * inv;
+  for (int i = 0; i < 4; ++i) w[i] &= keep;
+  if (kBits == 8 && __any(byte == 246)) {
+    constexpr uint32_t kTop = 0x7f60u;  // 448 2^119
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t lo = min(w[i] & 0x7fffu, kTop), hi = min(w[i] >> 16 & 0x7fffu, kTop);
+      if (byte == 246) w[i] = (w[i] & 0x80008000u) | hi << 16 | lo;
+    }
   }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = byte == 255 ? 0.f : fminf(fmaxf(y[i], -kTop), kTop);
   uint2 c = make_uint2(0u, 0u);
   if constexpr (kBits == 8) {
-    c.x = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-    c.x = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], (int)c.x, true);
-    c.y = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], 0, false);
-    c.y = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], (int)c.y, true);
+    i16x2 lo = {0, 0}, hi = {0, 0};
+    lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, __builtin_bit_cast(bf16x2, w[0]), power, false);
+    lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, __builtin_bit_cast(bf16x2, w[1]), power, true);
+    hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2, w[2]), power, false);
+    hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2, w[3]), power, true);
+    c = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
   } else {
-    c.x = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, y[0], y[1], 1.f, 0);
-    c.x = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c.x, y[2], y[3], 1.f, 1);
-    c.x = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c.x, y[4], y[5], 1.f, 2);
-    c.x = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c.x, y[6], y[7], 1.f, 3);
+    c.x = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0u, __builtin_bit_cast(bf16x2, w[0]), power, 0);
+    c.x = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c.x, __builtin_bit_cast(bf16x2, w[1]), power, 1);
+    c.x = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c.x, __builtin_bit_cast(bf16x2, w[2]), power, 2);
+    c.x = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c.x, __builtin_bit_cast(bf16x2, w[3]), power, 3);
   }
   return c;
 }

@@ -52,9 +52,12 @@ __device__ __forceinline__ Source source_of(const QuantRowsArgs& a, int64_t item
 // -1: a page that is not there
 __device__ __forceinline__ int64_t place_of(const QuantKV& kv, int Hkv, int64_t total, int64_t kvb, int b, int g, int row) {
   if (!kv.paged) return (int64_t)g * total + kvb + row;
-  const int64_t page = kv.pk.page_table[(int64_t)b * kv.pk.max_pages + min(row / kv.pk.page_size, kv.pk.max_pages - 1)];
+  const int size = kv.pk.page_size;
+  // (sizes are powers of two as a rule: a division is 20 instructions)
+  const int at = (size & (size - 1)) == 0 ? row >> __builtin_ctz(size) : row / size;
+  const int page = kv.pk.page_table[(int64_t)b * kv.pk.max_pages + min(at, kv.pk.max_pages - 1)];
   if (page < 0 || page >= kv.pk.num_pages) return -1;
-  return (page * Hkv + g) * kv.pk.page_size + row % kv.pk.page_size;
+  return (int64_t)((page * Hkv + g) * size + (row - at * size));  // (fewer than 2^31 rows)
 }
 
 template <int kBits>
@@ -63,9 +66,26 @@ __device__ __forceinline__ uint2 load_codes(const uint8_t* p) {
   else return make_uint2(*reinterpret_cast<const uint32_t*>(p), 0u);
 }
 
-__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
-  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, false));
-  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, false));
+__device__ __forceinline__ uint32_t pk_max(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+// Largest |bf16| of a group, as its bits, from the words of four lanes
+__device__ __forceinline__ uint32_t largest(const uint4& x) {
+  uint32_t t = pk_max(pk_max(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), pk_max(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
+  t = pk_max(t, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)t, 0x4E, 0xF, 0xF, false));
+  t = pk_max(t, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)t, 0xB1, 0xF, 0xF, false));
+  return max(t & 0xffffu, t >> 16);
+}
+// Two bf16 as 16-bit integers that order as they do, and back: an involution
+__device__ __forceinline__ uint32_t ordered(uint32_t w) {
+  const i16x2 x = __builtin_bit_cast(i16x2, w);
+  return w ^ (__builtin_bit_cast(uint32_t, x >> 15) & 0x7fff7fffu);
+}
+__device__ __forceinline__ uint32_t pk_least(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(i16x2, a), __builtin_bit_cast(i16x2, b)));
+}
+__device__ __forceinline__ uint32_t pk_most(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(i16x2, a), __builtin_bit_cast(i16x2, b)));
 }
 
 // Writes the last row_indptr[b + 1] - row_indptr[b] rows of every sequence.  A workgroup
@@ -75,7 +95,8 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
 template <int kBits, int kPass, bool kBounds>
 __global__ __launch_bounds__(256) void quant_write_kernel(QuantRowsArgs a) {
   constexpr int kRows = 16 * kPass, kWaveRows = 4 * kPass;
-  __shared__ __align__(16) float s_bound[2][16][kHeadDim];  // of the rows of four lane groups of four waves
+  __shared__ __align__(16) uint32_t s_bound[2][16][kHeadDim / 2];  // of the rows of four lane groups of four waves, ordered
+  __shared__ uint32_t s_odd[16];                                   // bit g: group g of them has a row of NaN
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, sl = lane & 15, grp = lane >> 4;
   const int g = blockIdx.y >> 1;
   const bool values = blockIdx.y & 1;
@@ -101,28 +122,29 @@ __global__ __launch_bounds__(256) void quant_write_kernel(QuantRowsArgs a) {
 #pragma unroll
   for (int i = 0; i < kPass; ++i) {
     const int row = row0 + 4 * i;
-    place[i] = -1;
     x[i] = make_uint4(0u, 0u, 0u, 0u);
-    old[i] = make_uint2(0u, 0u);
-    byte[i] = 127;
-    if (row >= from && row < n) place[i] = place_of(a.kv, a.Hkv, a.total, kvb, b, g, row);
     if (row >= start && row < n) x[i] = load_stream16(in + ((r0 + row - (n - m)) * a.Hkv + g) * kHeadDim + sl * 8);
   }
-  if constexpr (kBounds) {
 #pragma unroll
-    for (int i = 0; i < kPass; ++i) {
-      if (place[i] >= 0 && row0 + 4 * i < start) {
-        old[i] = load_codes<kBits>(codes + place[i] * kRowBytes<kBits> + sl * kBits);
-        byte[i] = scales[place[i] * 4 + (sl >> 2)];
-      }
+  for (int i = 0; i < kPass; ++i) {  // (behind the loads: a page's place is one more)
+    const int row = row0 + 4 * i;
+    place[i] = row >= from && row < n ? place_of(a.kv, a.Hkv, a.total, kvb, b, g, row) : -1;
+  }
+#pragma unroll
+  for (int i = 0; i < kPass; ++i) {
+    old[i] = make_uint2(0u, 0u);
+    byte[i] = 127;
+    if (kBounds && place[i] >= 0 && row0 + 4 * i < start) {
+      old[i] = load_codes<kBits>(codes + place[i] * kRowBytes<kBits> + sl * kBits);
+      byte[i] = scales[place[i] * 4 + (sl >> 2)];
     }
   }
-  float lo[8], hi[8];
+  uint32_t lo[4], hi[4];  // of two dimensions each
   bool odd = false;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    lo[e] = INFINITY;
-    hi[e] = -INFINITY;
+  for (int e = 0; e < 4; ++e) {
+    lo[e] = 0x7fff7fffu;
+    hi[e] = 0x80008000u;
   }
 #pragma unroll
   for (int i = 0; i < kPass; ++i) {
@@ -131,11 +153,7 @@ __global__ __launch_bounds__(256) void quant_write_kernel(QuantRowsArgs a) {
     uint2 c = old[i];
     int s = byte[i];
     if (row >= start) {
-      uint32_t top = 0;
-      const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7fffu, (w[e] >> 16) & 0x7fffu));
-      s = scale_byte<kBits>(quad_max(top));
+      s = scale_byte<kBits>(largest(x[i]));
       c = encode8<kBits>(x[i], s);
       if (place[i] >= 0) {
         uint8_t* to = codes + place[i] * kRowBytes<kBits> + sl * kBits;
@@ -148,44 +166,39 @@ __global__ __launch_bounds__(256) void quant_write_kernel(QuantRowsArgs a) {
       if (!values) {
         odd |= s == 255;
         const uint4 d = decode8<kBits>(c, power_of(s));
-        const uint32_t w[4] = {d.x, d.y, d.z, d.w};
+        const uint32_t w[4] = {ordered(d.x), ordered(d.y), ordered(d.z), ordered(d.w)};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          lo[2 * e] = fminf(lo[2 * e], bf16lo(w[e]));
-          hi[2 * e] = fmaxf(hi[2 * e], bf16lo(w[e]));
-          lo[2 * e + 1] = fminf(lo[2 * e + 1], bf16hi(w[e]));
-          hi[2 * e + 1] = fmaxf(hi[2 * e + 1], bf16hi(w[e]));
+          lo[e] = pk_least(lo[e], w[e]);
+          hi[e] = pk_most(hi[e], w[e]);
         }
       }
     }
   }
   if constexpr (kBounds) {
     if (values) return;  // (the whole workgroup)
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (odd) lo[e] = hi[e] = __builtin_nanf("");
-#pragma unroll
-    for (int e = 0; e < 8; e += 4) {
-      *reinterpret_cast<float4*>(&s_bound[0][wave * 4 + grp][sl * 8 + e]) = make_float4(lo[e], lo[e + 1], lo[e + 2], lo[e + 3]);
-      *reinterpret_cast<float4*>(&s_bound[1][wave * 4 + grp][sl * 8 + e]) = make_float4(hi[e], hi[e + 1], hi[e + 2], hi[e + 3]);
-    }
+    *reinterpret_cast<uint4*>(&s_bound[0][wave * 4 + grp][sl * 4]) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    *reinterpret_cast<uint4*>(&s_bound[1][wave * 4 + grp][sl * 4]) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    const uint64_t odd_lanes = __ballot(odd) >> (16 * grp);
+    if (sl == 0) s_odd[wave * 4 + grp] = (uint32_t)(odd_lanes & 1) | (uint32_t)(odd_lanes >> 3 & 2) | (uint32_t)(odd_lanes >> 6 & 4) | (uint32_t)(odd_lanes >> 9 & 8);
     __syncthreads();
-    // block j of the piece: the waves of its rows; a thread takes one dimension of one side
+    // block j of the piece: the lane groups of its rows; a thread takes two dimensions of one side
+    if (tid >= kHeadDim) return;
     const int per = 4 * max(1, a.kv.block / kWaveRows), blocks = kRows >> log_block;
     const int64_t out = (int64_t)g * ((a.total >> log_block) + a.B) + first_block(kvb, log_block, b);
-    const int side = tid >> 7, d = tid & 127;
+    const int side = tid >> 6, d = tid & 63;
     for (int j = 0; j < blocks; ++j) {
       const int64_t block = piece * blocks + j;
       if (block << log_block < from || block << log_block >= n) continue;
-      float v = side ? -INFINITY : INFINITY;
-      bool odd_here = false;
+      uint32_t v = side ? 0x80008000u : 0x7fff7fffu, bad = 0;
+#pragma unroll 4
       for (int w = 0; w < per; ++w) {
-        const float y = s_bound[side][j * per + w][d];
-        odd_here |= y != y;
-        v = side ? fmaxf(v, y) : fminf(v, y);
+        const uint32_t y = s_bound[side][j * per + w][d];
+        bad |= s_odd[j * per + w];
+        v = side ? pk_most(v, y) : pk_least(v, y);
       }
-      // exact: every value read from the cache is a bf16
-      a.kv.bounds[((out + block) * 2 + side) * kHeadDim + d] = odd_here ? (uint16_t)0x7fc0 : (uint16_t)(__float_as_uint(v) >> 16);
+      // (exact: every value read from the cache is a bf16)
+      reinterpret_cast<uint32_t*>(a.kv.bounds)[((out + block) * 2 + side) * (kHeadDim / 2) + d] = bad >> (d >> 4) & 1 ? 0x7fc07fc0u : ordered(v);
     }
   }
 }
