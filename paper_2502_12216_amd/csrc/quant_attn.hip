@@ -51,17 +51,24 @@ __device__ __forceinline__ T uniform(T x) {
   else return (T)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)((uint64_t)x >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
 }
 
-// Rows that group bg attends: its sequence's, or those of its chosen blocks (ascending, so
-// that only the last one may be the sequence's last, of fewer rows).
-__device__ __forceinline__ int64_t rows_of(const QuantAttnArgs& x, int bg) {
+// What a workgroup knows of a group: where its sequence's rows begin, the sequence's length, and
+// the rows attended: all, or those of its chosen blocks (ascending, so that only the last one
+// may be the sequence's last, of fewer rows).
+struct Group {
+  int64_t kvb;
+  int32_t n, rows;
+};
+__device__ __forceinline__ Group group_of(const QuantAttnArgs& x, int bg) {
   const int b = bg / x.a.NV;
-  const int64_t n = seq_tokens(x.a.kv_indptr, x.a.seq_len, b);
-  if (!x.blocks) return n;
-  const int count = min(max(x.counts[bg], 0), x.budget);
-  if (count == 0 || n == 0) return 0;
-  const int lb = __builtin_ctz(x.block);
-  const int64_t last = x.blocks[(int64_t)bg * x.budget + count - 1];
-  return ((int64_t)(count - 1) << lb) + min(max(n - (last << lb), (int64_t)1), (int64_t)x.block);
+  const int count = x.blocks ? min(max(x.counts[bg], 0), x.budget) : 0;
+  const int64_t kvb = x.a.kv_indptr[b], n = seq_tokens(x.a.kv_indptr, x.a.seq_len, b);
+  Group g{kvb, (int32_t)n, (int32_t)n};
+  if (x.blocks) {
+    const int lb = __builtin_ctz(x.block);
+    const int64_t last = x.blocks[(int64_t)bg * x.budget + max(count - 1, 0)];
+    g.rows = count == 0 || n == 0 ? 0 : (int32_t)(((int64_t)(count - 1) << lb) + min(max(n - (last << lb), (int64_t)1), (int64_t)x.block));
+  }
+  return g;
 }
 
 // kRows: 0 rows lie at their positions; 1 every 16 positions from a multiple of 16 lie together
@@ -76,7 +83,7 @@ void quant_attn_kernel(QuantAttnArgs x) {
   constexpr int VW = kBits == 8 ? 2 : 1;      // 4-byte words of its 8 values
   constexpr int kThreads = kWave * kWaves;
   const AttnArgs& a = x.a;
-  extern __shared__ int64_t s_prefix[];       // [B * NV + 1] units before each group, then int32 [B * NV] its rows
+  extern __shared__ int64_t s_prefix[];       // [B * NV + 1] units before each group, then [B * NV] the groups
   union Shared {
     struct {
       int tile[kTableRows / 16];              // place of 16 positions (kRows 1)
@@ -101,12 +108,11 @@ void quant_attn_kernel(QuantAttnArgs x) {
   if (!x.direct) {
     const int per = (BG + kThreads - 1) / kThreads, g0 = min(BG, tid * per), g1 = min(BG, g0 + per);
     auto units = [&](int64_t n) { return n > 0 ? ((n + 31) & ~(int64_t)31) + kSegmentCost : 0; };
-    int32_t* const s_rows = reinterpret_cast<int32_t*>(s_prefix + BG + 1);
+    Group* const groups = reinterpret_cast<Group*>(s_prefix + BG + 1);
     int64_t loc = 0;
     for (int g = g0; g < g1; ++g) {
-      const int64_t n = rows_of(x, g);
-      s_rows[g] = (int32_t)n;
-      loc += units(n);
+      groups[g] = group_of(x, g);
+      loc += units(groups[g].rows);
     }
     const int64_t incl = wave_incl_scan(loc);
     if (lane == kWave - 1) s_wsum[wave] = incl;
@@ -115,7 +121,7 @@ void quant_attn_kernel(QuantAttnArgs x) {
     for (int w = 0; w < wave; ++w) run += s_wsum[w];
     for (int g = g0; g < g1; ++g) {
       s_prefix[g] = run;
-      run += units(s_rows[g]);
+      run += units(groups[g].rows);
     }
     if (tid == kThreads - 1) s_prefix[BG] = run;
     __syncthreads();
@@ -139,19 +145,24 @@ void quant_attn_kernel(QuantAttnArgs x) {
   }
 
   for (; bg < bg_end; ++bg) {
-    int64_t seg_lo = 0, seg_hi;
+    int64_t seg_lo = 0, seg_hi, kvb;
+    int nseq;
     if (x.direct) {
-      seg_hi = uniform(rows_of(x, bg));
+      const Group g = group_of(x, bg);
+      seg_hi = uniform(g.rows);
+      kvb = uniform(g.kvb);
+      nseq = uniform(g.n);
     } else {
       const int64_t start = uniform(s_prefix[bg]);
       if (start >= t1) break;
+      const Group g = reinterpret_cast<const Group*>(s_prefix + BG + 1)[bg];  // (no more loads before the rows')
       seg_lo = max(t0 - start - kSegmentCost, (int64_t)0);
-      seg_hi = min((int64_t)uniform(reinterpret_cast<const int32_t*>(s_prefix + BG + 1)[bg]), t1 - start - kSegmentCost);
+      seg_hi = min((int64_t)uniform(g.rows), t1 - start - kSegmentCost);
       if (seg_lo >= seg_hi) continue;
+      kvb = uniform(g.kvb);
+      nseq = uniform(g.n);
     }
     const int b = bg / a.NV, kvh = bg % a.NV;
-    const int64_t kvb = a.kv_indptr[b];
-    const int nseq = (int)seq_tokens(a.kv_indptr, a.seq_len, b);
 
     // the queries, in the dimensions that the lane has of K
     bf16x8 qv[S][4];
@@ -513,7 +524,7 @@ static hipError_t with_kernel(const QuantAttnArgs& x, int G, F f) {
 // Dynamic LDS of the units before each group and of the groups' rows
 static size_t prefix_lds(const QuantAttnArgs& x) {
   const size_t groups = (size_t)x.a.B * x.a.NV;
-  return x.direct ? 0 : (groups + 1) * sizeof(int64_t) + groups * sizeof(int32_t);
+  return x.direct ? 0 : (groups + 1) * sizeof(int64_t) + groups * sizeof(Group);
 }
 
 hipError_t quant_resident_grid(const QuantAttnArgs& x, int G, int* grid) {
