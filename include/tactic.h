@@ -489,11 +489,13 @@ typedef struct {
  * left out): a prompt, a chunk, or a new token behind lengths that were advanced.
  * k, v: bf16 [rows->total_queries][Hkv][128].  With bounds, those of every block that has
  * a new row are set from the rows of the block up to the sequence's last.  A row whose
- * table entry is out of range is not written; no two sequences may write one page row. */
+ * table entry is out of range is not written; no two sequences may write one page row.  k, v and
+ * the cache's arrays must not overlap (else an invalid argument). */
 tactic_status tactic_quant_write(const uint16_t* k, const uint16_t* v, const tactic_kv_shape* shape,
                                  const tactic_query_shape* rows, const tactic_quant_kv* kv, hipStream_t stream);
 /* The same rows in bf16 again, [Hkv][rows->total_queries][128] each (as the attention of a
- * prompt takes them); rows ahead of a sequence's first, and of pages that are not there, are zeros. */
+ * prompt takes them); rows ahead of a sequence's first, and of pages that are not there, are zeros.  The outputs
+ * overlap neither the cache nor one another. */
 tactic_status tactic_quant_read(const tactic_quant_kv* kv, const tactic_kv_shape* shape,
                                 const tactic_query_shape* rows, uint16_t* K_out, uint16_t* V_out,
                                 hipStream_t stream);

@@ -26,16 +26,6 @@ tactic_status check_rows(std::initializer_list<const void*> arrays) {
   return TACTIC_OK;
 }
 
-// Memory that a call reads or writes; a null or empty one overlaps nothing.
-struct Span {
-  const void* at;
-  int64_t bytes;
-};
-bool overlap(const Span& a, const Span& b) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
-  return x && y && a.bytes > 0 && b.bytes > 0 && x < y + (uintptr_t)b.bytes && y < x + (uintptr_t)a.bytes;
-}
-
 tactic_status check_queries(const tactic_query_shape* q, const tactic_kv_shape* s) {
   if (!q) return fail(TACTIC_ERR_INVALID_ARG, "queries is null");
   if (!q->q_indptr) return fail(TACTIC_ERR_INVALID_ARG, "q_indptr is null");

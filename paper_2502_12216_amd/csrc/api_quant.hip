@@ -74,6 +74,26 @@ tactic::QuantRowsArgs rows_args(const tactic_kv_shape* s, const tactic_query_sha
   return a;
 }
 
+// The arrays of a cache
+struct CacheSpans {
+  Span s[5];
+};
+CacheSpans spans_of(const tactic::QuantKV& c, const tactic_kv_shape* s) {
+  const int64_t rows = c.paged ? c.pk.num_pages * s->n_kv_heads * c.pk.page_size : s->total_tokens * s->n_kv_heads;
+  const int64_t bounds = c.bounds ? (s->total_tokens / c.block + s->batch) * s->n_kv_heads * (4 * kHeadDim) : 0;
+  return {{{c.K, rows * 16 * c.bits}, {c.V, rows * 16 * c.bits}, {c.K_scale, rows * 4}, {c.V_scale, rows * 4}, {c.bounds, bounds}}};
+}
+// Workgroups write some arrays while others read and write theirs: no two may overlap.
+tactic_status check_apart(const CacheSpans& cache, bool cache_written, const Span& x, const Span& y, bool written) {
+  for (const Span& c : cache.s) {
+    if (overlap(c, x) || overlap(c, y)) return fail(TACTIC_ERR_INVALID_ARG, "rows must not overlap the cache");
+    for (const Span& d : cache.s)
+      if (cache_written && &c < &d && overlap(c, d)) return fail(TACTIC_ERR_INVALID_ARG, "the cache's arrays must not overlap one another");
+  }
+  if (written && overlap(x, y)) return fail(TACTIC_ERR_INVALID_ARG, "the outputs must not overlap one another");
+  return TACTIC_OK;
+}
+
 struct SelectLayout {
   int64_t max_blocks, per, tops, scores, top, keys, bytes;
 };
@@ -128,7 +148,9 @@ tactic_status tactic_quant_write(const uint16_t* k, const uint16_t* v, const tac
     return st;
   if (rows->total_queries == 0 || shape->total_tokens == 0) return TACTIC_OK;
   if (!k || !v) return fail(TACTIC_ERR_INVALID_ARG, "null argument");
-  if ((st = check_aligned({k, v}, 16)) != TACTIC_OK) return st;
+  const int64_t bytes = rows->total_queries * shape->n_kv_heads * kHeadDim * 2;
+  if ((st = check_aligned({k, v}, 16)) != TACTIC_OK || (st = check_apart(spans_of(c, shape), true, {k, bytes}, {v, bytes}, false)) != TACTIC_OK)
+    return st;
   tactic::QuantRowsArgs a = rows_args(shape, rows, c);
   a.k = k;
   a.v = v;
@@ -146,7 +168,10 @@ tactic_status tactic_quant_read(const tactic_quant_kv* kv, const tactic_kv_shape
     return st;
   if (rows->total_queries == 0) return TACTIC_OK;
   if (!K_out || !V_out) return fail(TACTIC_ERR_INVALID_ARG, "null argument");
-  if ((st = check_aligned({K_out, V_out}, 16)) != TACTIC_OK) return st;
+  const int64_t bytes = rows->total_queries * shape->n_kv_heads * kHeadDim * 2;
+  if ((st = check_aligned({K_out, V_out}, 16)) != TACTIC_OK ||
+      (st = check_apart(spans_of(c, shape), false, {K_out, bytes}, {V_out, bytes}, true)) != TACTIC_OK)
+    return st;
   tactic::QuantRowsArgs a = rows_args(shape, rows, c);
   a.K_out = K_out;
   a.V_out = V_out;

@@ -25,6 +25,16 @@ struct Layout {
   }
 };
 
+// Memory that a call reads or writes; a null or empty one overlaps nothing.
+struct Span {
+  const void* at;
+  int64_t bytes;
+};
+inline bool overlap(const Span& a, const Span& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+  return x && y && a.bytes > 0 && b.bytes > 0 && x < y + (uintptr_t)b.bytes && y < x + (uintptr_t)a.bytes;
+}
+
 tactic_status check_shape(const tactic_kv_shape* s);
 tactic_status check_mod(const tactic_score_mod* m);
 tactic_status paged_args(const tactic_paged_kv* kv, const tactic_kv_shape* s, tactic::PagedKV* pk);

@@ -60,13 +60,14 @@ struct Group {
 };
 __device__ __forceinline__ Group group_of(const QuantAttnArgs& x, int bg) {
   const int b = bg / x.a.NV;
-  const int count = x.blocks ? min(max(x.counts[bg], 0), x.budget) : 0;
+  const int listed = x.blocks ? x.counts[bg] : 0;
   const int64_t kvb = x.a.kv_indptr[b], n = seq_tokens(x.a.kv_indptr, x.a.seq_len, b);
   Group g{kvb, (int32_t)n, (int32_t)n};
-  if (x.blocks) {
+  if (x.blocks) {  // (whatever a list holds, the rows are among the sequence's)
     const int lb = __builtin_ctz(x.block);
-    const int64_t last = x.blocks[(int64_t)bg * x.budget + max(count - 1, 0)];
-    g.rows = count == 0 || n == 0 ? 0 : (int32_t)(((int64_t)(count - 1) << lb) + min(max(n - (last << lb), (int64_t)1), (int64_t)x.block));
+    const int64_t nb = (n + x.block - 1) >> lb, count = min((int64_t)min(max(listed, 0), x.budget), nb);
+    const int64_t last = min(max((int64_t)x.blocks[(int64_t)bg * x.budget + max(count - 1, (int64_t)0)], (int64_t)0), nb - 1);
+    g.rows = count == 0 ? 0 : (int32_t)(((count - 1) << lb) + min(n - (last << lb), (int64_t)x.block));
   }
   return g;
 }
@@ -398,8 +399,8 @@ void quant_attn_kernel(QuantAttnArgs x) {
           int row[1] = {row_at(p + tid * 16)};
           sh.t.row[tid] = row[0];
           if constexpr (kRows == 1) {
-            // (a list that is not as it should be: 16 rows stay inside the sequence's first ones or its last)
-            if (x.blocks && cnt - tid * 16 >= 16) row[0] = max(0, min(row[0], nseq - 16)) & ~(x.kv.paged ? 15 : 0);
+            // (a list that is not as it should be: the rows stay inside the sequence and their page)
+            if (x.blocks) row[0] = max(min(row[0], nseq - min(16, cnt - tid * 16)), 0) & ~(x.kv.paged ? 15 : 0);
             if (x.kv.paged) {
               int64_t at[1];
               paged_rows(x.kv.pk, a.Hkv, a.total, kvb, b, kvh, row, 0, at);

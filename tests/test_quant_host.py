@@ -101,6 +101,27 @@ def test_unsupported_scores_and_small_workspaces():
     assert decode(n=need - 1) == 3 and decode(ws=None) == 3
 
 
+def test_arrays_that_overlap():
+    """k, v and the cache's arrays (of 2000 rows of 128 bytes), each a byte too near to the next."""
+    at = {"k": 1 << 24, "v": 2 << 24, "K": 3 << 24, "Ks": 4 << 24, "V": 5 << 24, "Vs": 6 << 24, "bounds": 7 << 24}
+    size = {"k": 100 * 512, "v": 100 * 512, "K": 2000 * 128, "V": 2000 * 128, "Ks": 8000, "Vs": 8000, "bounds": (1000 // 64 + 2) * 1024}
+    lib = C.lib()
+
+    def refused(call, **over):  # (only calls that are: the pointers mean nothing)
+        p = {**at, **over}
+        kv = _kv(K=p["K"], Ks=p["Ks"], V=p["V"], Vs=p["Vs"], bounds=p["bounds"])
+        status = (lib.tactic_quant_write(p["k"], p["v"], R(_shape()), R(_rows()), R(kv), None) if call == "write" else
+                  lib.tactic_quant_read(R(kv), R(_shape()), R(_rows()), p["k"], p["v"], None))
+        return status == 1 and "overlap" in lib.tactic_last_error().decode()
+
+    for x in at:
+        for y in at:
+            if x != y:
+                near, rows = at[y] + size[y] - 16, {x, y} & {"k", "v"}
+                assert rows == {"k", "v"} or refused("write", **{x: near}), (x, y)  # (k and v of a write are both read)
+                assert not rows or refused("read", **{x: near}), (x, y)
+
+
 def test_nothing_to_do():
     assert write(rows=_rows(0, 0), k=None, v=None) == 0 and read(rows=_rows(0, 0), K=None, V=None) == 0
     assert write(shape=_shape(total=0, nmax=0), kv=_kv(K=None, Ks=None, V=None, Vs=None)) == 0
