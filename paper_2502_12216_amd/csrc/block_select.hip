@@ -43,7 +43,8 @@ __device__ __forceinline__ double reduce2(const double (&v)[2], int sl) {  // of
 // sums are exact as well: that needs half the registers of the positive and negative parts of
 // q (64 for four heads), so that four waves fit a SIMD.  A block is 512 bytes and 2 G 128 fused
 // operations in 64 bits, and about as many to make 64 bits of the bounds and to add up over the
-// lanes: bound by these from four heads on.
+// lanes: bound by these from four heads on (65536 blocks of four heads each 8.9 us, 3.8 TB/s; with the
+// positive and negative parts 11 to 13).
 template <int G>
 __global__ __launch_bounds__(256) void block_score_kernel(SelectArgs a) {
   constexpr int H = G < 4 ? G : 4, kSpan = 16 / H;  // a head's score ends in kSpan lanes
@@ -157,7 +158,8 @@ __device__ __forceinline__ uint32_t place_in_range(uint64_t key, double per_widt
 // does not tell, over the keys from the first bit in which they differ.  Block j is thread
 // j mod 1024's; chosen ones find their places by one scan over the ballots of 64 blocks.
 // kPer = 0: the keys lie in the workspace and are gone through 16384 at a time.
-// Bound by its chain of loads, scans and barriers.
+// Bound by its chain of loads, scans and barriers: 188 blocks 5.1 us, 2048 (32 groups) 7.8, 8192 (8
+// groups) 13.6, 16400 22, 40000 77.
 template <int kPer>
 __global__ __launch_bounds__(1024) void block_select_kernel(SelectArgs a) {
   constexpr int kBins = 2048, kThreads = 1024, kHeld = kPer ? kPer : 16, kWords = kHeld * 16;

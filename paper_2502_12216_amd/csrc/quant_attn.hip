@@ -14,6 +14,11 @@
 //    dimensions 8 (l % 16) .. + 7, one to an instruction, for the same eight rows.
 // (The instructions that multiply 8 and 4 bit codes themselves add with fewer bits: 9e-5
 // of the absolute sum for a row of 128 codes, where fp32 has 6e-8.)
+//
+// 4 x 131072 rows, 8 KV heads of 4 query heads: 8 bits 172 us (6.4 TB/s), 4 bits 95 (6.0; 89 of
+// them at that rate, the rest the start and the merge; a step of 32 rows is 200 vector and 16 matrix
+// instructions, two thirds of the time that its bytes take).  Two waves per SIMD: three spill
+// (119 us), one has nothing to run beside its waits (102).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -29,7 +34,11 @@
 namespace tactic {
 
 constexpr float kScaleLog2 = kLog2e * kInvSqrtDim;
-constexpr int64_t kQuantShare = 256;  // rows of the least share
+// Rows of the least share of a workgroup.  Shares of 128, 192, 256, 384 rows, us a call: 8 bits, 8 KV heads,
+// one sequence of 4096 rows 13.2, 11.9, 12.4, 13.9; two of 2300 13.1, 12.0, 12.4, 13.4; 3000 + 2500 with eight
+// heads each 15.3, 13.9, 15.9, 17.6; 4 bits, 8192 rows 13.6, 13.3, 12.5, 13.1.
+template <int kBits>
+constexpr int64_t kQuantShare = kBits == 8 ? 192 : 256;
 constexpr int kTableRows = 2048;      // rows looked up at once
 constexpr int kWaves = 4;             // waves of a workgroup (eight: 3 to 11% slower)
 constexpr int kStep = 32 * kWaves;    // rows of a step of all of them
@@ -129,7 +138,7 @@ void quant_attn_kernel(QuantAttnArgs x) {
     const int64_t total = uniform(s_prefix[BG]);
     // (at least the quotient: its error is far below the least fraction that it can have)
     const int64_t even = (int64_t)((double)total * x.per_grid) + 1;
-    const int64_t share = max((even + 31) & ~(int64_t)31, kQuantShare);
+    const int64_t share = max((even + 31) & ~(int64_t)31, kQuantShare<kBits>);
     if (blockIdx.x == 0) {  // for the combine
       if (tid == 0) a.ameta[0] = share;
       for (int g = tid; g <= BG; g += kThreads) a.ameta[1 + g] = s_prefix[g];
