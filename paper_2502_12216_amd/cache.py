@@ -268,6 +268,8 @@ class QuantizingCache:
         rows, held = CacheQuantizer(self.batch, new), CacheQuantizer(self.batch, lens)
         for name, x, heads in (("q", qc, self.Hq), ("K", Kc, self.Hkv), ("V", Vc, self.Hkv)):  # (before anything is changed)
             _check_tensor(x, name, torch.bfloat16, (rows.total, heads, 128))
+            if x.device != self.device:
+                raise ValueError(f"{name} is on {x.device}, expected {self.device}")
         self.batch.seq_len.copy_(torch.as_tensor(np.asarray(lens, dtype=np.int64)))
         self.batch.seq_lens = lens
         rows.write(Kc, Vc, self.cache)

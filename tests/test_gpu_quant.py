@@ -344,6 +344,69 @@ def test_cache_past_2_31_bytes(bits):
     assert np.array_equal(K.double().cpu().numpy(), ref) and torch.equal(K, V)
 
 
+@pytest.mark.parametrize("longest", [40, 2100])
+@pytest.mark.parametrize("blocks", [False, True])
+def test_as_many_groups_as_there_may_be(longest, blocks):
+    """512 sequences of 8 KV heads, most of a few rows or none: by one workgroup each, and split."""
+    lens = [longest] + [i % 6 for i in range(511)]
+    h = Held(lens, lens, 64, 8, 8, block=16)
+    h.fill()
+    q = torch.randn(512, 64, D, generator=gen(3), device="cuda").to(torch.bfloat16)
+    dec, sel = T.QuantizedDecoder(h.batch), T.BlockSelector(h.batch, 16, 131, 0, 1)
+    b, c = sel(q, h.cache)
+    out, lse = dec(q, h.cache, blocks=b, counts=c) if blocks else dec(q, h.cache)
+    few = [0, 1, 2, 3, 4, 5, 6, 511]
+    assert not out[[i for i, n in enumerate(lens) if n == 0]].any()
+    sub = Held([lens[i] for i in few], [lens[i] for i in few], 64, 8, 8, block=16)
+    for at, i in enumerate(few):  # the same rows in a cache of their own
+        a, z, n = int(h.batch.kv_indptr_host[i]), int(sub.batch.kv_indptr_host[at]), lens[i]
+        for x in ("K", "V", "K_scale", "V_scale"):
+            getattr(sub.cache, x)[:, z:z + n] = getattr(h.cache, x)[:, a:a + n]
+        if lens[i]:
+            f = h.first_block(i)
+            sub.cache.bounds[:, sub.first_block(at):sub.first_block(at) + -(-n // 16)] = h.cache.bounds[:, f:f + -(-n // 16)]
+    want = choices(sub, q[few], 131, 0, 1)  # (132 blocks of the long one)
+    check_choice(want, b[few], c[few])
+    check_decode(sub, q[few], out[few], lse[few], want if blocks else None)
+
+
+@pytest.mark.parametrize("page", [0, 16])
+def test_spans_without_spare_rows(page):
+    """No device lengths: every span is full."""
+    lens = [130, 1, 64]
+    h = Held(lens, lens, 8, 2, 8, page, 32)
+    full = T.RaggedBatch(lens, 8, 2)
+    assert full.seq_len is None
+    g = gen(1)
+    k, v = rows_like(g, 195, 2), rows_like(g, 195, 2)
+    rows = T.CacheQuantizer(full, lens)
+    rows.write(k, v, h.cache)
+    got = [x.clone() for x in rows.read(h.cache)]
+    assert all(torch.equal(x, y) for x, y in zip(got, T.CacheQuantizer(h.batch, lens).read(h.cache)))
+    q = torch.randn(3, 8, D, generator=g, device="cuda").to(torch.bfloat16)
+    b, c = T.BlockSelector(full, 32, 3)(q, h.cache)
+    want = choices(h, q, 3, 1, 2)
+    check_choice(want, b, c)
+    out, lse = T.QuantizedDecoder(full)(q, h.cache, blocks=b, counts=c)
+    check_decode(h, q, out, lse, want)
+
+
+def test_empty_chunks_and_refused_ones():
+    c = T.QuantizingCache(4, 2, [40, 40], bits=8, block=32)
+    def some(m, heads, dtype=torch.bfloat16):
+        return torch.randn(m, heads, D, generator=gen(m + heads), device="cuda").to(dtype)
+    assert c.extend([some(0, 4)] * 2, [some(0, 2)] * 2, [some(0, 2)] * 2).shape == (0, 4, D)
+    assert c.batch.seq_lens == [0, 0] and not c.decode(some(2, 4)).any()
+    for bad in (([some(3, 4)] * 2, [some(3, 2)] * 2, [some(2, 2)] * 2), ([some(3, 4)], [some(3, 2)], [some(3, 2)]),
+                ([some(3, 4)] * 2, [some(3, 2, torch.float32)] * 2, [some(3, 2)] * 2),
+                ([some(3, 2)] * 2, [some(3, 2)] * 2, [some(3, 2)] * 2)):
+        with pytest.raises((TypeError, ValueError)):
+            c.extend(*bad)
+    assert c.batch.seq_lens == [0, 0] and c.batch.seq_len.tolist() == [0, 0]
+    assert c.extend([some(3, 4), some(0, 4)], [some(3, 2), some(0, 2)], [some(3, 2), some(0, 2)]).shape == (3, 4, D)
+    assert c.batch.seq_len.tolist() == [3, 0]
+
+
 def test_captured_steps_and_streams():
     """A step (length, write, choice, decode) captured, replayed with eager work between, on another stream, and beside a
     second captured step of the same objects."""
