@@ -38,89 +38,155 @@ __device__ __forceinline__ double reduce2(const double (&v)[2], int sl) {  // of
   return x + dpp<0xB1>(x);
 }
 
-// a.per blocks of one KV head for its G query heads, 16 at a time with the next ones on their way, four
-// heads at a time.  The larger of q lo and q hi is q (hi + lo) / 2 + |q| (hi - lo) / 2, whose
-// sums are exact as well: that needs half the registers of the positive and negative parts of
-// q (64 for four heads), so that four waves fit a SIMD.  A block is 512 bytes and 2 G 128 fused
-// operations in 64 bits, and about as many to make 64 bits of the bounds and to add up over the
-// lanes: bound by these from four heads on (65536 blocks of four heads each 8.9 us, 3.8 TB/s; with the
-// positive and negative parts 11 to 13).
+// What both forms of the scores have: a.per blocks of one KV head, 16 at a time, the next 16 on their
+// way (more on their way: 10 to 30% slower up to 4 x 2048 blocks of four heads).  The larger of q lo and
+// q hi is q (hi + lo) / 2 + |q| (hi - lo) / 2, whose sums are exact as well: half the registers of
+// the positive and negative parts of q.
+struct ScoreRange {
+  int64_t j0, j1;           // its blocks
+  const uint16_t* bounds;   // of the head's first block
+  bool none;
+};
+__device__ __forceinline__ ScoreRange score_range(const SelectArgs& a) {
+  const int g = blockIdx.y, b = blockIdx.z, lb = __builtin_ctz(a.block);
+  const int64_t kvb = a.kv_indptr[b], n = seq_tokens(a.kv_indptr, a.seq_len, b);
+  const int64_t nb = (n + a.block - 1) >> lb, j0 = (int64_t)blockIdx.x * a.per;
+  return {j0, min(nb, j0 + a.per), a.bounds + ((int64_t)g * ((a.total >> lb) + a.B) + first_block(kvb, lb, b)) * (2 * kHeadDim),
+          j0 >= nb || nb <= a.budget};  // (all of them are chosen)
+}
+__device__ __forceinline__ double wide(const uint4& w, int e) {  // the bf16 e of eight (a constant after unrolling)
+  const uint32_t u = e < 2 ? w.x : e < 4 ? w.y : e < 6 ? w.z : w.w;
+  return (double)(e & 1 ? bf16hi(u) : bf16lo(u));
+}
+
+// Up to four query heads, on the vector unit: 16 lanes have a block, 8 dimensions each.  A block is
+// 512 bytes and 2 G 128 fused operations in 64 bits, and about as many to make 64 bits of the
+// bounds and to add up over the lanes.  65536 blocks of four heads each 8.9 us (3.8 TB/s and
+// the start; with the positive and negative parts 11 to 13), 320000 blocks 37 (4.4 TB/s).
 template <int G>
 __global__ __launch_bounds__(256) void block_score_kernel(SelectArgs a) {
-  constexpr int H = G < 4 ? G : 4, kSpan = 16 / H;  // a head's score ends in kSpan lanes
-  constexpr int kAhead = 1;  // loads of 16 blocks on their way (2, 3 and 4 are slower: 10.4 against 11.8 us for 4 x 2048 blocks of 8 heads)
+  static_assert(G == 1 || G == 2 || G == 4, "eight heads: block_score8_kernel");
+  constexpr int kSpan = 16 / G;  // a head's score ends in kSpan lanes
   __shared__ double s_top[16][G];
   const int tid = threadIdx.x, sl = tid & 15, sub = tid >> 4;
-  const int g = blockIdx.y, b = blockIdx.z;
-  const int lb = __builtin_ctz(a.block);
-  const int64_t kvb = a.kv_indptr[b], n = seq_tokens(a.kv_indptr, a.seq_len, b);
-  const int64_t nb = (n + a.block - 1) >> lb;
-  const int64_t j0 = (int64_t)blockIdx.x * a.per, j1 = min(nb, j0 + a.per);
-  if (j0 >= nb || nb <= a.budget) return;  // (all of them are chosen)
-  const uint16_t* bounds = a.bounds + ((int64_t)g * ((a.total >> lb) + a.B) + first_block(kvb, lb, b)) * (2 * kHeadDim) + sl * 8;
-#pragma unroll 1
-  for (int h0 = 0; h0 < G; h0 += H) {
-    const int64_t head = (int64_t)b * a.Hq + g * G + h0;
-    auto load = [&](int64_t j, uint4& lo, uint4& hi) __attribute__((always_inline)) {
-      const uint16_t* p = bounds + min(j + sub, j1 - 1) * (2 * kHeadDim);
-      lo = *reinterpret_cast<const uint4*>(p);
-      hi = *reinterpret_cast<const uint4*>(p + kHeadDim);
-    };
-    uint4 lo[kAhead], hi[kAhead];
+  const ScoreRange r = score_range(a);
+  if (r.none) return;
+  const int64_t head = (int64_t)blockIdx.z * a.Hq + blockIdx.y * G;
+  auto load = [&](int64_t j, uint4& lo, uint4& hi) __attribute__((always_inline)) {
+    const uint16_t* p = r.bounds + min(j + sub, r.j1 - 1) * (2 * kHeadDim) + sl * 8;
+    lo = *reinterpret_cast<const uint4*>(p);
+    hi = *reinterpret_cast<const uint4*>(p + kHeadDim);
+  };
+  uint4 lo, hi, lo2, hi2;
+  load(r.j0, lo, hi);
+  double q[G][8], best = -INFINITY;
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) load(min(j0 + 16 * k, j1 - 1), lo[k], hi[k]);
-    double q[H][8], best = -INFINITY;
+  for (int h = 0; h < G; ++h) {
+    const uint4 w = *reinterpret_cast<const uint4*>(a.q + (head + h) * kHeadDim + sl * 8);
 #pragma unroll
-    for (int h = 0; h < H; ++h) {
-      const uint4 w = *reinterpret_cast<const uint4*>(a.q + (head + h) * kHeadDim + sl * 8);
-      const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        q[h][e] = 0.5 * (double)(e & 1 ? bf16hi(u[e >> 1]) : bf16lo(u[e >> 1]));
-      }
-    }
-    double* scores = a.scores + (head + sl / kSpan) * a.max_blocks;
-    auto score = [&](const uint4& lw, const uint4& tw, int64_t j) __attribute__((always_inline)) {
-      double u[H];
-#pragma unroll
-      for (int h = 0; h < H; ++h) u[h] = 0.0;
-      const uint32_t l[4] = {lw.x, lw.y, lw.z, lw.w}, t[4] = {tw.x, tw.y, tw.z, tw.w};
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const double x = (double)(e & 1 ? bf16hi(l[e >> 1]) : bf16lo(l[e >> 1]));
-        const double y = (double)(e & 1 ? bf16hi(t[e >> 1]) : bf16lo(t[e >> 1]));
-        const double sum = y + x, span = y - x;
-#pragma unroll
-        for (int h = 0; h < H; ++h) u[h] = fma(fabs(q[h][e]), span, fma(q[h][e], sum, u[h]));
-      }
-      double v;
-      if constexpr (H == 4) v = reduce4(u, sl);
-      else if constexpr (H == 2) v = reduce2(u, sl);
-      else v = sum16d(u[0]);
-      if (j + sub < j1) {
-        best = fmax(best, v);  // (NaN is passed over, and stored as what it counts as)
-        if (sl % kSpan == 0) scores[j + sub] = v != v ? INFINITY : v;
-      }
-    };
-#pragma unroll 1
-    for (int64_t j = j0; j < j1; j += 16 * kAhead) {
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        if (j + 16 * k >= j1) break;
-        const uint4 lw = lo[k], tw = hi[k];
-        load(min(j + 16 * (k + kAhead), j1 - 1), lo[k], hi[k]);
-        score(lw, tw, j + 16 * k);
-      }
-    }
-    if (sl % kSpan == 0) s_top[sub][h0 + sl / kSpan] = best;
+    for (int e = 0; e < 8; ++e) q[h][e] = 0.5 * wide(w, e);
   }
+  double* scores = a.scores + (head + sl / kSpan) * a.max_blocks;
+#pragma unroll 1
+  for (int64_t j = r.j0; j < r.j1; j += 16) {
+    load(min(j + 16, r.j1 - 1), lo2, hi2);
+    double u[G];
+#pragma unroll
+    for (int h = 0; h < G; ++h) u[h] = 0.0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const double x = wide(lo, e), y = wide(hi, e), sum = y + x, span = y - x;
+#pragma unroll
+      for (int h = 0; h < G; ++h) u[h] = fma(fabs(q[h][e]), span, fma(q[h][e], sum, u[h]));
+    }
+    double v;
+    if constexpr (G == 4) v = reduce4(u, sl);
+    else if constexpr (G == 2) v = reduce2(u, sl);
+    else v = sum16d(u[0]);
+    if (j + sub < r.j1) {
+      best = fmax(best, v);  // (NaN is passed over, and stored as what it counts as)
+      if (sl % kSpan == 0) scores[j + sub] = v != v ? INFINITY : v;
+    }
+    lo = lo2;
+    hi = hi2;
+  }
+  if (sl % kSpan == 0) s_top[sub][sl / kSpan] = best;
   __syncthreads();
   if (tid < G) {
     double v = s_top[0][tid];
 #pragma unroll
     for (int i = 1; i < 16; ++i) v = fmax(v, s_top[i][tid]);
-    a.top[((int64_t)b * a.Hq + g * G + tid) * a.tops + blockIdx.x] = v;
+    a.top[(head + tid) * a.tops + blockIdx.x] = v;
   }
+}
+
+// Eight query heads, on the matrix unit: v_mfma_f64_4x4x4_4b_f64 for four heads and four blocks at a time.
+// Lane l has block l % 4 and the dimensions 8 (l / 4) .. + 7 of its bounds, one to an instruction, and the
+// same dimensions of head l % 4's query; it receives the sums of head l / 16 and block l % 4 over a
+// quarter of the dimensions (l / 4 % 4).  16 instructions of 16 cycles for each four heads.  65536 blocks
+// 11.7 us, on the vector unit 15.4; with four heads or fewer the lanes' order, by which 16
+// of them read 64 bytes of four blocks, costs more than it saves (18.5 against 16.1 us with the
+// selection for one head, 21.1 against 19.9 for four).
+__global__ __launch_bounds__(256) void block_score8_kernel(SelectArgs a) {
+  __shared__ double s_top[4][8];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 3, row = lane >> 4;
+  const ScoreRange r = score_range(a);
+  if (r.none) return;
+  const int64_t head = (int64_t)blockIdx.z * a.Hq + blockIdx.y * 8;
+  auto load = [&](int64_t j, uint4& lo, uint4& hi) __attribute__((always_inline)) {
+    const uint16_t* p = r.bounds + min(j + wave * 4 + col, r.j1 - 1) * (2 * kHeadDim) + (lane >> 2) * 8;
+    lo = *reinterpret_cast<const uint4*>(p);
+    hi = *reinterpret_cast<const uint4*>(p + kHeadDim);
+  };
+  uint4 lo, hi, lo2, hi2;
+  load(r.j0, lo, hi);
+  double q[2][8], q_abs[2][8], best[2];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const uint4 w = *reinterpret_cast<const uint4*>(a.q + (head + 4 * s + col) * kHeadDim + (lane >> 2) * 8);
+    best[s] = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      q[s][e] = 0.5 * wide(w, e);
+      q_abs[s][e] = fabs(q[s][e]);
+    }
+  }
+  double* scores = a.scores + (head + row) * a.max_blocks;
+#pragma unroll 1
+  for (int64_t j = r.j0; j < r.j1; j += 16) {
+    load(min(j + 16, r.j1 - 1), lo2, hi2);
+    double sums[2] = {0.0, 0.0}, spans[2] = {0.0, 0.0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const double x = wide(lo, e), y = wide(hi, e), sum = y + x, span = y - x;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        sums[s] = __builtin_amdgcn_mfma_f64_4x4x4f64(q[s][e], sum, sums[s], 0, 0, 0);
+        spans[s] = __builtin_amdgcn_mfma_f64_4x4x4f64(q_abs[s][e], span, spans[s], 0, 0, 0);
+      }
+    }
+    const int64_t at = j + wave * 4 + col;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      double v = sums[s] + spans[s];
+      v += dpp<0x128>(v);  // row_ror:8 and :4, the quarters of the dimensions
+      v += dpp<0x124>(v);
+      if (at < r.j1) {
+        best[s] = fmax(best[s], v);
+        if ((lane & 12) == 0) scores[4 * s * a.max_blocks + at] = v != v ? INFINITY : v;
+      }
+    }
+    lo = lo2;
+    hi = hi2;
+  }
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    best[s] = fmax(best[s], dpp<0x4E>(best[s]));  // over the quad's four blocks
+    best[s] = fmax(best[s], dpp<0xB1>(best[s]));
+    if ((lane & 15) == 0) s_top[wave][4 * s + row] = best[s];
+  }
+  __syncthreads();
+  if (tid < 8) a.top[(head + tid) * a.tops + blockIdx.x] = fmax(fmax(s_top[0][tid], s_top[1][tid]), fmax(s_top[2][tid], s_top[3][tid]));
 }
 
 // Scores as integers that order as they do, NaN as +inf
@@ -433,7 +499,7 @@ hipError_t launch_block_scores(const SelectArgs& a, hipStream_t st) {
     case 1: hipLaunchKernelGGL((block_score_kernel<1>), grid, dim3(256), 0, st, a); break;
     case 2: hipLaunchKernelGGL((block_score_kernel<2>), grid, dim3(256), 0, st, a); break;
     case 4: hipLaunchKernelGGL((block_score_kernel<4>), grid, dim3(256), 0, st, a); break;
-    case 8: hipLaunchKernelGGL((block_score_kernel<8>), grid, dim3(256), 0, st, a); break;
+    case 8: hipLaunchKernelGGL(block_score8_kernel, grid, dim3(256), 0, st, a); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();
