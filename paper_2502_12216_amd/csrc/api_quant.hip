@@ -222,7 +222,7 @@ tactic_status tactic_block_select(const uint16_t* q, const tactic_quant_kv* kv, 
   a.tops = l.tops;
   a.scores = reinterpret_cast<double*>(ws + l.scores);
   a.top = reinterpret_cast<double*>(ws + l.top);
-  a.keys = reinterpret_cast<uint64_t*>(ws + l.keys);
+  a.keys = reinterpret_cast<double*>(ws + l.keys);
   a.blocks = blocks;
   a.counts = counts;
   hipError_t e = hipSuccess;

@@ -189,9 +189,8 @@ __global__ __launch_bounds__(256) void block_score8_kernel(SelectArgs a) {
   if (tid < 8) a.top[(head + tid) * a.tops + blockIdx.x] = fmax(fmax(s_top[0][tid], s_top[1][tid]), fmax(s_top[2][tid], s_top[3][tid]));
 }
 
-// Scores as integers that order as they do, NaN as +inf
+// Scores (none NaN) as integers that order as they do
 __device__ __forceinline__ uint64_t order_key(double x) {
-  if (x != x) x = INFINITY;
   const uint64_t u = __builtin_bit_cast(uint64_t, x);
   return u >> 63 ? ~u : u | 0x8000000000000000ull;
 }
@@ -207,25 +206,22 @@ __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
   return step(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x143, 0xC, 0xF, false));
 }
 
-// The score of a key, and where it lies in the range of the free blocks' scores [-width, 0], as a number
-// that rises with it: equal ones are told apart by their keys.
-__device__ __forceinline__ double score_of(uint64_t key) {
-  return __builtin_bit_cast(double, key >> 63 ? key & 0x7fffffffffffffffull : ~key);
-}
-__device__ __forceinline__ uint32_t place_in_range(uint64_t key, double per_width) {
-  return (uint32_t)fmin(fmax(fma(score_of(key), per_width, 4294966784.0), 0.0), 4294967295.0);
+// Where a score lies in the range of the free blocks' scores [-width, 0], as a number that rises with it:
+// equal ones are told apart by their keys.  (per_width need not be exact, only the same for all.)
+__device__ __forceinline__ uint32_t place_in_range(double score, double per_width) {
+  return (uint32_t)fmin(fmax(fma(score, per_width, 4294966784.0), 0.0), 4294967295.0);
 }
 
-// The `budget` blocks of the largest keys of one KV head, ascending.  A radix selection
+// The `budget` blocks of the largest scores of one KV head, ascending.  A radix selection
 // in digits of 11 bits, each with a histogram in LDS of the keys still level, that ends as
-// soon as all keys of the digit that holds the last one are wanted: first over a key's place
+// soon as all of the digit that holds the last one are wanted: first over a score's place
 // in the range of scores, 32 bits linear (the bits of the scores themselves fill few bins, whose
 // counts wait for one another: the first digit of 8192 blocks took 8 us), then, where that
-// does not tell, over the keys from the first bit in which they differ.  Block j is thread
+// does not tell, over the scores' bits from the first in which they differ.  Block j is thread
 // j mod 1024's; chosen ones find their places by one scan over the ballots of 64 blocks.
-// kPer = 0: the keys lie in the workspace and are gone through 16384 at a time.
-// Bound by its chain of loads, scans and barriers: 188 blocks 5.1 us, 2048 (32 groups) 7.8, 8192 (8
-// groups) 13.6, 16400 22, 40000 77.
+// kPer = 0: the scores lie in the workspace and are gone through 16384 at a time.
+// Bound by its chain of loads, scans and barriers: 188 blocks 4.6 us, 2048 (32 groups) 7.3, 8192 (8
+// groups) 12.1, 16384 21, 40000 75; with integer keys held in place of scores 5.5, 7.8, 13.7, 22.8, 79.
 template <int kPer>
 __global__ __launch_bounds__(1024) void block_select_kernel(SelectArgs a) {
   constexpr int kBins = 2048, kThreads = 1024, kHeld = kPer ? kPer : 16, kWords = kHeld * 16;
@@ -249,82 +245,77 @@ __global__ __launch_bounds__(1024) void block_select_kernel(SelectArgs a) {
     return;
   }
   const double* scores = a.scores + ((int64_t)b * a.Hq + g * G) * a.max_blocks;
-  uint64_t* stored = a.keys + ((int64_t)b * a.Hkv + g) * a.max_blocks;
-  // every head's best score: a wave for each
-  if (wave < G) {
-    const double* top = a.top + ((int64_t)b * a.Hq + g * G + wave) * a.tops;
-    double v = -INFINITY;
-    for (int i = lane; i < (nb + a.per - 1) / a.per; i += kWave) v = fmax(v, top[i]);
-    v = wave_allmax_d(v);
-    if (lane == 0) s_best[wave] = v;
-  }
-  for (int i = tid; i < kBins; i += kThreads) s_hist[i] = 0;
-  __syncthreads();
-  bool finite = true;  // else a difference may be NaN, which counts as +inf
-  for (int h = 0; h < G; ++h) finite &= fabs(s_best[h]) < INFINITY;
-  // the keys of K blocks from j on, kThreads apart, all loads first
-  auto keys_g = [&](auto count, auto heads, int j, uint64_t* keys) __attribute__((always_inline)) {
-    constexpr int K = decltype(count)::value, H = decltype(heads)::value;
-    double d[H][K];
-#pragma unroll
-    for (int h = 0; h < H; ++h)
-#pragma unroll
-      for (int i = 0; i < K; ++i) d[h][i] = scores[(int64_t)h * a.max_blocks + min(j + i * kThreads, nb - 1)];
-    double from[H];
-#pragma unroll
-    for (int h = 0; h < H; ++h) from[h] = s_best[h];
-#pragma unroll
-    for (int i = 0; i < K; ++i) {
-      double best = d[0][i] - from[0];
-      if (finite) {
-#pragma unroll
-        for (int h = 1; h < H; ++h) best = fmax(best, d[h][i] - from[h]);
-      } else {
-        bool odd = best != best;
-#pragma unroll
-        for (int h = 1; h < H; ++h) {
-          const double y = d[h][i] - from[h];
-          odd |= y != y;
-          best = fmax(best, y);
-        }
-        best = odd ? INFINITY : best;
-      }
-      keys[i] = order_key(best + 0.0);  // (-0 as 0)
-    }
-  };
-  auto keys_of = [&](auto count, int j, uint64_t* keys) __attribute__((always_inline)) {
-    switch (G) {
-      case 1: keys_g(count, std::integral_constant<int, 1>{}, j, keys); break;
-      case 2: keys_g(count, std::integral_constant<int, 2>{}, j, keys); break;
-      case 4: keys_g(count, std::integral_constant<int, 4>{}, j, keys); break;
-      default: keys_g(count, std::integral_constant<int, 8>{}, j, keys); break;
-    }
-  };
+  double* stored = a.keys + ((int64_t)b * a.Hkv + g) * a.max_blocks;
   // the first and the last blocks are chosen whatever their scores: they take no part in the selection
   const int begin = min(a.first, nb), end = max(begin, nb - a.last), forced = nb - (end - begin);
   auto free_block = [&](int j) { return j >= begin && j < end; };
-  uint64_t held[kHeld];
+  double held[kHeld];
   uint32_t place[kHeld];
   uint32_t width = 0;  // the least finite score, its size as the bits of a float
-  {
-    constexpr int K = kHeld < 4 ? kHeld : 4;
+  auto all_scores = [&](auto heads) __attribute__((always_inline)) {
+    constexpr int H = decltype(heads)::value, K = kHeld < 4 ? kHeld : 4;
+    double d[H][K], from[H];
+    auto load = [&](int j) __attribute__((always_inline)) {  // K blocks, all loads first
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int i = 0; i < K; ++i) d[h][i] = scores[(int64_t)h * a.max_blocks + min(j + i * kThreads, nb - 1)];
+    };
+    load(tid);  // (on their way while the best ones are looked up)
+    if (wave < H) {  // every head's best score: a wave for each
+      const double* top = a.top + ((int64_t)b * a.Hq + g * H + wave) * a.tops;
+      double v = -INFINITY;
+      for (int i = lane; i < (nb + a.per - 1) / a.per; i += kWave) v = fmax(v, top[i]);
+      v = wave_allmax_d(v);
+      if (lane == 0) s_best[wave] = v;
+    }
+    for (int i = tid; i < kBins; i += kThreads) s_hist[i] = 0;
+    __syncthreads();
+    bool finite = true;  // else a difference may be NaN, which counts as +inf
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      from[h] = s_best[h];
+      finite &= fabs(from[h]) < INFINITY;
+    }
     for (int c = 0; c < nb; c += kHeld * kThreads) {  // (once with kPer)
 #pragma unroll
       for (int i = 0; i < kHeld; i += K) {
         if (c + i * kThreads >= nb) break;
-        keys_of(std::integral_constant<int, K>{}, c + i * kThreads + tid, held + i);
+        if (c + i > 0) load(c + i * kThreads + tid);
 #pragma unroll
-        for (int k = i; k < i + K; ++k) {
-          const int j = c + k * kThreads + tid;
-          const float x = -(float)score_of(held[k]);
+        for (int k = 0; k < K; ++k) {
+          double best = d[0][k] - from[0];
+          if (finite) {
+#pragma unroll
+            for (int h = 1; h < H; ++h) best = fmax(best, d[h][k] - from[h]);
+          } else {
+            bool odd = best != best;
+#pragma unroll
+            for (int h = 1; h < H; ++h) {
+              const double y = d[h][k] - from[h];
+              odd |= y != y;
+              best = fmax(best, y);
+            }
+            best = odd ? INFINITY : best;
+          }
+          best += 0.0;  // (-0 as 0)
+          held[i + k] = best;
+          const int j = c + (i + k) * kThreads + tid;
+          const float x = -(float)best;
           if (free_block(j) && x < INFINITY) width = max(width, __float_as_uint(fmaxf(x, 0.f)));
           if constexpr (kPer == 0) {  // (read back by the thread that wrote it)
-            if (j < nb) stored[j] = held[k];
+            if (j < nb) stored[j] = best;
           }
         }
       }
       if constexpr (kPer > 0) break;
     }
+  };
+  switch (G) {
+    case 1: all_scores(std::integral_constant<int, 1>{}); break;
+    case 2: all_scores(std::integral_constant<int, 2>{}); break;
+    case 4: all_scores(std::integral_constant<int, 4>{}); break;
+    default: all_scores(std::integral_constant<int, 8>{}); break;
   }
   width = wave_max_u32(width);
   if (lane == kWave - 1) s_max[wave] = width;
@@ -332,8 +323,10 @@ __global__ __launch_bounds__(1024) void block_select_kernel(SelectArgs a) {
   width = s_max[0];
 #pragma unroll
   for (int w = 1; w < 16; ++w) width = max(width, s_max[w]);
-  const double per_width = width ? 4294966784.0 / (double)__uint_as_float(width) : 1.0;
-  // f(block, key, place) of this thread's free blocks
+  // (neither 0 nor infinite, for a score of +inf to lie above all and one of 0 above the others)
+  const float unit = fminf(fmaxf(__builtin_amdgcn_rcpf(__uint_as_float(width)), 0x1p-126f), 0x1p126f);
+  const double per_width = 4294966784.0 * (double)unit;
+  // f(score, place) of this thread's free blocks
   auto fetch = [&](int c) __attribute__((always_inline)) {
     if constexpr (kPer == 0) {
 #pragma unroll
@@ -361,8 +354,8 @@ __global__ __launch_bounds__(1024) void block_select_kernel(SelectArgs a) {
   bool all = need == 0;
   // a digit: counts of the level keys' digits, and the one that holds the last wanted key
   auto digit = [&](auto digit_of) __attribute__((always_inline)) -> uint32_t {
-    each([&](uint64_t k, uint32_t p) {
-      const int d = digit_of(k, p);
+    each([&](double x, uint32_t p) {
+      const int d = digit_of(x, p);
       if (d >= 0) atomicAdd(&s_hist[d], 1u);
     });
     __syncthreads();
@@ -394,7 +387,7 @@ __global__ __launch_bounds__(1024) void block_select_kernel(SelectArgs a) {
   uint32_t prefix = 0;
   while (!all && low > 0) {
     const int bits = min(low, 11), shift = low - bits;
-    const uint32_t d = digit([&](uint64_t, uint32_t p) {
+    const uint32_t d = digit([&](double, uint32_t p) {
       return low == 32 || p >> low == prefix ? (int)(p >> shift & ((1u << bits) - 1)) : -1;
     });
     prefix = prefix << bits | d;
@@ -406,10 +399,10 @@ __global__ __launch_bounds__(1024) void block_select_kernel(SelectArgs a) {
   uint64_t key_prefix = 0;
   if (!all) {
     uint64_t least = ~0ull, most = 0;
-    each([&](uint64_t k, uint32_t p) {
+    each([&](double x, uint32_t p) {
       if (level(p)) {
-        least = min(least, k);
-        most = max(most, k);
+        least = min(least, order_key(x));
+        most = max(most, order_key(x));
       }
     });
     for (int d = 32; d >= 1; d /= 2) {
@@ -429,7 +422,8 @@ __global__ __launch_bounds__(1024) void block_select_kernel(SelectArgs a) {
     key_prefix = key_low >= 64 ? 0 : most >> key_low;
     while (!all && key_low > 0) {
       const int bits = min(key_low, 11), shift = key_low - bits;
-      const uint32_t d = digit([&](uint64_t k, uint32_t p) {
+      const uint32_t d = digit([&](double x, uint32_t p) {
+        const uint64_t k = order_key(x);
         return level(p) && (key_low >= 64 || k >> key_low == key_prefix) ? (int)(k >> shift & ((1u << bits) - 1)) : -1;
       });
       key_prefix = key_low >= 64 ? (uint64_t)d : key_prefix << bits | d;
@@ -447,7 +441,7 @@ __global__ __launch_bounds__(1024) void block_select_kernel(SelectArgs a) {
       if (c + i * kThreads < nb) {
         const int j = c + i * kThreads + tid;
         const bool is_free = free_block(j), on = level(place[i]);
-        const uint64_t k = key_low >= 64 ? 0 : held[i] >> key_low;
+        const uint64_t k = key_low >= 64 ? 0 : order_key(held[i]) >> key_low;
         const bool over = (low < 32 && place[i] >> low > prefix) || (on && k > key_prefix);
         above[i] = __ballot(j < nb && (!is_free || (over && want > forced)));
         same[i] = __ballot(is_free && on && k == key_prefix);

@@ -280,7 +280,7 @@ struct SelectArgs {
   int64_t total, max_blocks, tops;  // tops: scoring workgroups of a sequence's head
   double* scores;               // [B][Hq][max_blocks]
   double* top;                  // [B][Hq][tops]: the largest score of each scoring workgroup
-  uint64_t* keys;               // [B][Hkv][max_blocks] where a workgroup's registers do not hold them
+  double* keys;                 // [B][Hkv][max_blocks] groups' scores, where a workgroup's registers do not hold them
   int32_t* blocks;              // [B][Hkv][budget]
   int32_t* counts;              // [B][Hkv]
 };

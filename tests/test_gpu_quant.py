@@ -311,6 +311,24 @@ def test_choice_among_equals(nb):
     assert np.array_equal(blocks[0, 0].cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("size", [1e-30, 1.0, 3e38])
+@pytest.mark.parametrize("nb", [300, 3000, 20000])
+def test_choice_of_any_size_beside_infinities(nb, size):
+    """Scores in the type's highest and lowest reaches, with one head's best infinite: its block above all."""
+    batch, cache = only_bounds(nb, 16, 2, 1)
+    cache.bounds.zero_()
+    cache.bounds[0, :nb, :, 0] = (-size * torch.rand(nb, 1, generator=gen(3), device="cuda")).to(torch.bfloat16)
+    cache.bounds[0, nb // 2, 1, 1] = float("inf")
+    q = torch.zeros(1, 2, D, dtype=torch.bfloat16, device="cuda")
+    q[0, 0, 0], q[0, 1, 1] = 1.0, 1.0
+    budget = nb // 4
+    with np.errstate(invalid="ignore"):
+        want = R.choose(q[0].double().cpu().numpy(), cache.bounds[0, :nb].double().cpu().numpy(), budget, 0, 0)
+    assert nb // 2 in want
+    blocks, _ = T.BlockSelector(batch, 16, budget, 0, 0)(q, cache)
+    assert np.array_equal(blocks[0, 0].cpu().numpy(), want)
+
+
 def test_decode_of_all_blocks_is_the_decode():
     lens = [700, 33]
     h = Held(lens, [n + 9 for n in lens], 8, 2, 8, block=32)
