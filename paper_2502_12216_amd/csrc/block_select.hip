@@ -218,10 +218,11 @@ __device__ __forceinline__ uint32_t place_in_range(double score, double per_widt
 // in the range of scores, 32 bits linear (the bits of the scores themselves fill few bins, whose
 // counts wait for one another: the first digit of 8192 blocks took 8 us), then, where that
 // does not tell, over the scores' bits from the first in which they differ.  Block j is thread
-// j mod 1024's; chosen ones find their places by one scan over the ballots of 64 blocks.
+// j mod 1024's; chosen ones find their places by a scan of every wave over the ballots of 64 blocks.
 // kPer = 0: the scores lie in the workspace and are gone through 16384 at a time.
-// Bound by its chain of loads, scans and barriers: 188 blocks 4.6 us, 2048 (32 groups) 7.3, 8192 (8
-// groups) 12.1, 16384 21, 40000 75; with integer keys held in place of scores 5.5, 7.8, 13.7, 22.8, 79.
+// Bound by its chain of loads, scans and barriers: 188 blocks 4.2 us, 2048 (32 groups) 6.8, 8192 (8
+// groups) 11.7, 16384 20.5, 40000 64; with integer keys held in place of scores and a block-wide scan
+// of the ballots (two barriers more) 5.5, 7.8, 13.7, 22.8, 79.
 template <int kPer>
 __global__ __launch_bounds__(1024) void block_select_kernel(SelectArgs a) {
   constexpr int kBins = 2048, kThreads = 1024, kHeld = kPer ? kPer : 16, kWords = kHeld * 16;
@@ -229,9 +230,9 @@ __global__ __launch_bounds__(1024) void block_select_kernel(SelectArgs a) {
   __shared__ double s_best[8];
   __shared__ uint32_t s_max[16];
   __shared__ uint64_t s_least[16], s_most[16];
-  __shared__ uint32_t s_wave[16][2];
+  __shared__ uint32_t s_wave[16];
   __shared__ uint32_t s_digit, s_above, s_in;
-  __shared__ uint32_t s_ahead[kWords][2];  // chosen and level blocks before each 64
+  __shared__ __align__(16) uint32_t s_words[kWords];  // chosen and level blocks of each 64
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int g = blockIdx.x, b = blockIdx.y;
   const int lb = __builtin_ctz(a.block), G = a.G;
@@ -362,12 +363,12 @@ __global__ __launch_bounds__(1024) void block_select_kernel(SelectArgs a) {
     // thread t: bins 2 t and 2 t + 1 counted from the top
     const uint32_t c0 = s_hist[kBins - 1 - 2 * tid], c1 = s_hist[kBins - 2 - 2 * tid];
     const uint32_t incl = wave_incl_scan(c0 + c1);
-    if (lane == 63) s_wave[wave][0] = incl;
+    if (lane == 63) s_wave[wave] = incl;
     s_hist[kBins - 1 - 2 * tid] = 0;  // for the next digit
     s_hist[kBins - 2 - 2 * tid] = 0;
     __syncthreads();
-    uint32_t ahead = incl - c0 - c1;
-    for (int w = 0; w < wave; ++w) ahead += s_wave[w][0];
+    const uint32_t of_wave = s_wave[lane & 15];  // (a row of 16 lanes scans the waves)
+    const uint32_t ahead = (uint32_t)__builtin_amdgcn_readlane((int)(row_incl_scan(of_wave) - of_wave), __builtin_amdgcn_readfirstlane(wave)) + incl - c0 - c1;
     if (ahead < need && ahead + c0 >= need) {
       s_digit = kBins - 1 - 2 * tid;
       s_above = ahead;
@@ -446,42 +447,34 @@ __global__ __launch_bounds__(1024) void block_select_kernel(SelectArgs a) {
         above[i] = __ballot(j < nb && (!is_free || (over && want > forced)));
         same[i] = __ballot(is_free && on && k == key_prefix);
       }
-      if (lane == 0) {
-        s_ahead[i * 16 + wave][0] = __popcll(above[i]);
-        s_ahead[i * 16 + wave][1] = __popcll(same[i]);
+      if (lane == 0) s_words[i * 16 + wave] = __popcll(above[i]) | __popcll(same[i]) << 16;
+    }
+    __syncthreads();
+    // counts before each 64 blocks, by every wave for itself: lane l has words W l .. W l + W - 1
+    constexpr int W = kWords > 64 ? kWords / 64 : 1;
+    uint32_t before_mine = 0, sum = 0;  // (before the word of this wave among a lane's)
+    if (W * lane < kWords) {
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        const uint32_t c = s_words[W * lane + i];
+        before_mine += i < wave % W ? c : 0;
+        sum += c;
       }
     }
-    __syncthreads();
-    const bool mine = tid < kWords;
-    const uint32_t ca = mine ? s_ahead[tid][0] : 0, cs = mine ? s_ahead[tid][1] : 0;
-    const uint32_t ia = wave_incl_scan(ca), is = wave_incl_scan(cs);
-    if (lane == 63) {
-      s_wave[wave][0] = ia;
-      s_wave[wave][1] = is;
-    }
-    __syncthreads();
-    uint32_t pa = done_above + ia - ca, ps = done_same + is - cs;
-#pragma unroll
-    for (int w = 0; w < 16; ++w) {
-      const uint32_t wa = s_wave[w][0], ws = s_wave[w][1];
-      done_above += wa;
-      done_same += ws;
-      pa += w < wave ? wa : 0;
-      ps += w < wave ? ws : 0;
-    }
-    if (mine) {
-      s_ahead[tid][0] = pa;
-      s_ahead[tid][1] = ps;
-    }
-    __syncthreads();
+    const uint32_t incl = wave_incl_scan(sum);
+    const int total = __builtin_amdgcn_readlane((int)incl, 63), word = __builtin_amdgcn_readfirstlane(wave / W);
+    before_mine += incl - sum;
     const uint64_t before = (1ull << lane) - 1;
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
       if ((above[i] | same[i]) == 0) continue;  // (the wave has none)
-      const uint32_t at = s_ahead[i * 16 + wave][0] + __popcll(above[i] & before);
-      const uint32_t level_at = s_ahead[i * 16 + wave][1] + __popcll(same[i] & before);
+      const uint32_t ahead = (uint32_t)__builtin_amdgcn_readlane((int)before_mine, i * (16 / W) + word);
+      const uint32_t at = done_above + (ahead & 0xffff) + __popcll(above[i] & before);
+      const uint32_t level_at = done_same + (ahead >> 16) + __popcll(same[i] & before);
       if ((above[i] >> lane & 1) || ((same[i] >> lane & 1) && level_at < need)) out[at + min(level_at, need)] = c + i * kThreads + tid;
     }
+    done_above += total & 0xffff;
+    done_same += (uint32_t)total >> 16;
     if constexpr (kPer > 0) break;
     __syncthreads();
   }
