@@ -15,6 +15,8 @@ using tactic::kHeadDim;
 namespace {
 
 constexpr int64_t kMaxInt = ((int64_t)1 << 31) - 1;
+// Scoring workgroups aimed at: 256, 512, 1024, 2048 of them for 65536 blocks 25.0, 22.1, 21.1, 22.6 us
+// (scores and selection, which reads a maximum of each).
 constexpr int64_t kScoreGroups = 1024;
 
 tactic_status check_aligned(std::initializer_list<const void*> arrays, int bytes) {
