@@ -505,7 +505,7 @@ tactic_status tactic_quant_read(const tactic_quant_kv* kv, const tactic_kv_shape
  *     u_hj  = sum over d of max(q_d lo_jd, q_d hi_jd)      (products and sums in 64 bits)
  *     score = max over the group's heads of u_hj - max_i u_hi
  * Ties go to the lower block; a score of NaN is above all others (of a query that is not
- * finite any scores may be). */
+ * finite, or of bounds of infinity, which no cache's values have, any scores may be). */
 typedef struct {
   int32_t budget;              /* blocks at most, >= 1 */
   int32_t first, last;         /* >= 0, together at most budget */

@@ -15,8 +15,9 @@ using tactic::kHeadDim;
 namespace {
 
 constexpr int64_t kMaxInt = ((int64_t)1 << 31) - 1;
-// Scoring workgroups aimed at: 256, 512, 1024, 2048 of them for 65536 blocks 25.0, 22.1, 21.1, 22.6 us
-// (scores and selection, which reads a maximum of each).
+// Scoring workgroups aimed at.  1024, 1536, 2048, 4096 of them, us for 65536 blocks: four heads, scores and
+// choice 18.6, 18.2, 18.6, 19.6; eight heads, with the decode 49.3, 50.6, 50.9, 53.6; 8192 blocks of 8 heads
+// 40.7, 40.7, 41.5, 43.6 (the choice reads a maximum of each); 256 and 512 were 4 and 1 slower than 1024.
 constexpr int64_t kScoreGroups = 1024;
 
 tactic_status check_aligned(std::initializer_list<const void*> arrays, int bytes) {

@@ -3,8 +3,10 @@
 // The score of block j for query head h is the largest product that a key inside the
 // block's bounds could have with the query, u_hj = sum_d (q_d >= 0 ? q_d hi_jd : q_d lo_jd).
 // A group's score of a block is the best of its heads', each counted from that head's
-// best block: max_h (u_hj - max_i u_hi).  The products of two bf16 are exact and their
-// sums are in 64 bits, so that the order of blocks does not depend on how they are summed.
+// best block: max_h (u_hj - max_i u_hi).  The products of two bf16 are exact and their sums
+// are in 64 bits: where the terms are less than 2^30 apart exact too, whatever their order.
+// The bound that does not count has no part in a sum (with q (hi + lo) / 2 + |q| (hi - lo) / 2
+// it swallows the other where they are more than 2^44 apart).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -17,20 +19,11 @@
 
 namespace tactic {
 
-// Sums over the 16 lanes of a DPP row of four values per lane, in every lane the total of value
-// sl / 4: each step pairs lanes over one lane bit, and while more than one value is left the lower
-// lane of a pair keeps the lower half of them and takes its partner's copy.  (Both partners
-// add the same two numbers, so lanes that end on the same value hold the same bits.)
-__device__ __forceinline__ double reduce4(const double (&v)[4], int sl) {
-  const bool up8 = sl & 8, up4 = sl & 4;
-  double c[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) c[i] = (up8 ? v[2 + i] : v[i]) + dpp<0x140>(up8 ? v[i] : v[2 + i]);  // row_mirror
-  double x = (up4 ? c[1] : c[0]) + dpp<0x141>(up4 ? c[0] : c[1]);  // row_half_mirror
-  x += dpp<0x4E>(x);
-  return x + dpp<0xB1>(x);
-}
-__device__ __forceinline__ double reduce2(const double (&v)[2], int sl) {  // of value sl / 8
+// Sums over the 16 lanes of a DPP row of two values per lane, in every lane the total of value
+// sl / 8: the first step pairs lanes over the upper lane bit, the lower lane of a pair keeps the first
+// value and takes its partner's copy.  (Both partners add the same two numbers, so lanes that end
+// on the same value hold the same bits.)
+__device__ __forceinline__ double reduce2(const double (&v)[2], int sl) {
   const bool up8 = sl & 8;
   double x = (up8 ? v[1] : v[0]) + dpp<0x140>(up8 ? v[0] : v[1]);
   x += dpp<0x141>(x);
@@ -39,9 +32,7 @@ __device__ __forceinline__ double reduce2(const double (&v)[2], int sl) {  // of
 }
 
 // What both forms of the scores have: a.per blocks of one KV head, 16 at a time, the next 16 on their
-// way (more on their way: 10 to 30% slower up to 4 x 2048 blocks of four heads).  The larger of q lo and
-// q hi is q (hi + lo) / 2 + |q| (hi - lo) / 2, whose sums are exact as well: half the registers of
-// the positive and negative parts of q.
+// way (two to four times as many: 0 to 16% slower for 4 x 2048 blocks of four heads).
 struct ScoreRange {
   int64_t j0, j1;           // its blocks
   const uint16_t* bounds;   // of the head's first block
@@ -59,13 +50,13 @@ __device__ __forceinline__ double wide(const uint4& w, int e) {  // the bf16 e o
   return (double)(e & 1 ? bf16hi(u) : bf16lo(u));
 }
 
-// Up to four query heads, on the vector unit: 16 lanes have a block, 8 dimensions each.  A block is
-// 512 bytes and 2 G 128 fused operations in 64 bits, and about as many to make 64 bits of the
-// bounds and to add up over the lanes.  65536 blocks of four heads each 8.9 us (3.8 TB/s and
-// the start; with the positive and negative parts 11 to 13), 320000 blocks 37 (4.4 TB/s).
+// One or two query heads, on the vector unit: 16 lanes have a block, 8 dimensions each, and take of
+// every two dimensions what the query's signs say before they make 64 bits of it.  A block is 512
+// bytes and 128 G conversions and fused operations.  65536 blocks of one head 7.7 us (4.4 TB/s and the
+// start), of two 8.4; by the matrix unit, as below, 9.5 both.
 template <int G>
 __global__ __launch_bounds__(256) void block_score_kernel(SelectArgs a) {
-  static_assert(G == 1 || G == 2 || G == 4, "eight heads: block_score8_kernel");
+  static_assert(G == 1 || G == 2, "four and eight heads: block_score_matrix_kernel");
   constexpr int kSpan = 16 / G;  // a head's score ends in kSpan lanes
   __shared__ double s_top[16][G];
   const int tid = threadIdx.x, sl = tid & 15, sub = tid >> 4;
@@ -80,11 +71,15 @@ __global__ __launch_bounds__(256) void block_score_kernel(SelectArgs a) {
   uint4 lo, hi, lo2, hi2;
   load(r.j0, lo, hi);
   double q[G][8], best = -INFINITY;
+  uint32_t neg[G][4];  // ones where a dimension of q is negative
 #pragma unroll
   for (int h = 0; h < G; ++h) {
     const uint4 w = *reinterpret_cast<const uint4*>(a.q + (head + h) * kHeadDim + sl * 8);
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) q[h][e] = 0.5 * wide(w, e);
+    for (int e = 0; e < 8; ++e) q[h][e] = wide(w, e);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) neg[h][i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(i16x2, u[i]) >> 15);
   }
   double* scores = a.scores + (head + sl / kSpan) * a.max_blocks;
 #pragma unroll 1
@@ -94,14 +89,14 @@ __global__ __launch_bounds__(256) void block_score_kernel(SelectArgs a) {
 #pragma unroll
     for (int h = 0; h < G; ++h) u[h] = 0.0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const double x = wide(lo, e), y = wide(hi, e), sum = y + x, span = y - x;
+    for (int h = 0; h < G; ++h) {
+      auto pick = [&](uint32_t m, uint32_t x, uint32_t y) { return (x & m) | (y & ~m); };
+      const uint4 w = make_uint4(pick(neg[h][0], lo.x, hi.x), pick(neg[h][1], lo.y, hi.y), pick(neg[h][2], lo.z, hi.z), pick(neg[h][3], lo.w, hi.w));
 #pragma unroll
-      for (int h = 0; h < G; ++h) u[h] = fma(fabs(q[h][e]), span, fma(q[h][e], sum, u[h]));
+      for (int e = 0; e < 8; ++e) u[h] = fma(q[h][e], wide(w, e), u[h]);
     }
     double v;
-    if constexpr (G == 4) v = reduce4(u, sl);
-    else if constexpr (G == 2) v = reduce2(u, sl);
+    if constexpr (G == 2) v = reduce2(u, sl);
     else v = sum16d(u[0]);
     if (j + sub < r.j1) {
       best = fmax(best, v);  // (NaN is passed over, and stored as what it counts as)
@@ -120,19 +115,21 @@ __global__ __launch_bounds__(256) void block_score_kernel(SelectArgs a) {
   }
 }
 
-// Eight query heads, on the matrix unit: v_mfma_f64_4x4x4_4b_f64 for four heads and four blocks at a time.
-// Lane l has block l % 4 and the dimensions 8 (l / 4) .. + 7 of its bounds, one to an instruction, and the
-// same dimensions of head l % 4's query; it receives the sums of head l / 16 and block l % 4 over a
-// quarter of the dimensions (l / 4 % 4).  16 instructions of 16 cycles for each four heads.  65536 blocks
-// 11.7 us, on the vector unit 15.4; with four heads or fewer the lanes' order, by which 16
-// of them read 64 bytes of four blocks, costs more than it saves (18.5 against 16.1 us with the
-// selection for one head, 21.1 against 19.9 for four).
-__global__ __launch_bounds__(256) void block_score8_kernel(SelectArgs a) {
-  __shared__ double s_top[4][8];
+// Four or eight query heads, on the matrix unit: v_mfma_f64_4x4x4_4b_f64 for four heads and four blocks at
+// a time.  Lane l has block l % 4 and the dimensions 8 (l / 4) .. + 7 of its bounds, one to an
+// instruction, and the same dimensions of head l % 4's query, its positive and its negative values
+// apart; it receives the sums of head l / 16 and block l % 4 over a quarter of the dimensions (l / 4 % 4).
+// 16 instructions of 16 cycles for each four heads.  65536 blocks of four heads 9.3 us (on the vector unit
+// 10.2), of eight 11.2 (15.4).
+template <int G>
+__global__ __launch_bounds__(256) void block_score_matrix_kernel(SelectArgs a) {
+  static_assert(G == 4 || G == 8, "sets of four heads");
+  constexpr int S = G / 4;
+  __shared__ double s_top[4][G];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 3, row = lane >> 4;
   const ScoreRange r = score_range(a);
   if (r.none) return;
-  const int64_t head = (int64_t)blockIdx.z * a.Hq + blockIdx.y * 8;
+  const int64_t head = (int64_t)blockIdx.z * a.Hq + blockIdx.y * G;
   auto load = [&](int64_t j, uint4& lo, uint4& hi) __attribute__((always_inline)) {
     const uint16_t* p = r.bounds + min(j + wave * 4 + col, r.j1 - 1) * (2 * kHeadDim) + (lane >> 2) * 8;
     lo = *reinterpret_cast<const uint4*>(p);
@@ -140,35 +137,36 @@ __global__ __launch_bounds__(256) void block_score8_kernel(SelectArgs a) {
   };
   uint4 lo, hi, lo2, hi2;
   load(r.j0, lo, hi);
-  double q[2][8], q_abs[2][8], best[2];
+  double above[S][8], below[S][8], best[S];  // q where it is positive, and where negative
 #pragma unroll
-  for (int s = 0; s < 2; ++s) {
+  for (int s = 0; s < S; ++s) {
     const uint4 w = *reinterpret_cast<const uint4*>(a.q + (head + 4 * s + col) * kHeadDim + (lane >> 2) * 8);
     best[s] = -INFINITY;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      q[s][e] = 0.5 * wide(w, e);
-      q_abs[s][e] = fabs(q[s][e]);
+      const double x = wide(w, e);
+      above[s][e] = x < 0 ? 0.0 : x;
+      below[s][e] = x < 0 ? x : 0.0;
     }
   }
   double* scores = a.scores + (head + row) * a.max_blocks;
 #pragma unroll 1
   for (int64_t j = r.j0; j < r.j1; j += 16) {
     load(min(j + 16, r.j1 - 1), lo2, hi2);
-    double sums[2] = {0.0, 0.0}, spans[2] = {0.0, 0.0};
+    double high[S] = {}, low[S] = {};
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const double x = wide(lo, e), y = wide(hi, e), sum = y + x, span = y - x;
+      const double x = wide(lo, e), y = wide(hi, e);
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        sums[s] = __builtin_amdgcn_mfma_f64_4x4x4f64(q[s][e], sum, sums[s], 0, 0, 0);
-        spans[s] = __builtin_amdgcn_mfma_f64_4x4x4f64(q_abs[s][e], span, spans[s], 0, 0, 0);
+      for (int s = 0; s < S; ++s) {
+        high[s] = __builtin_amdgcn_mfma_f64_4x4x4f64(above[s][e], y, high[s], 0, 0, 0);
+        low[s] = __builtin_amdgcn_mfma_f64_4x4x4f64(below[s][e], x, low[s], 0, 0, 0);
       }
     }
     const int64_t at = j + wave * 4 + col;
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      double v = sums[s] + spans[s];
+    for (int s = 0; s < S; ++s) {
+      double v = high[s] + low[s];
       v += dpp<0x128>(v);  // row_ror:8 and :4, the quarters of the dimensions
       v += dpp<0x124>(v);
       if (at < r.j1) {
@@ -180,13 +178,13 @@ __global__ __launch_bounds__(256) void block_score8_kernel(SelectArgs a) {
     hi = hi2;
   }
 #pragma unroll
-  for (int s = 0; s < 2; ++s) {
+  for (int s = 0; s < S; ++s) {
     best[s] = fmax(best[s], dpp<0x4E>(best[s]));  // over the quad's four blocks
     best[s] = fmax(best[s], dpp<0xB1>(best[s]));
     if ((lane & 15) == 0) s_top[wave][4 * s + row] = best[s];
   }
   __syncthreads();
-  if (tid < 8) a.top[(head + tid) * a.tops + blockIdx.x] = fmax(fmax(s_top[0][tid], s_top[1][tid]), fmax(s_top[2][tid], s_top[3][tid]));
+  if (tid < G) a.top[(head + tid) * a.tops + blockIdx.x] = fmax(fmax(s_top[0][tid], s_top[1][tid]), fmax(s_top[2][tid], s_top[3][tid]));
 }
 
 // Scores (none NaN) as integers that order as they do
@@ -485,8 +483,8 @@ hipError_t launch_block_scores(const SelectArgs& a, hipStream_t st) {
   switch (a.G) {
     case 1: hipLaunchKernelGGL((block_score_kernel<1>), grid, dim3(256), 0, st, a); break;
     case 2: hipLaunchKernelGGL((block_score_kernel<2>), grid, dim3(256), 0, st, a); break;
-    case 4: hipLaunchKernelGGL((block_score_kernel<4>), grid, dim3(256), 0, st, a); break;
-    case 8: hipLaunchKernelGGL(block_score8_kernel, grid, dim3(256), 0, st, a); break;
+    case 4: hipLaunchKernelGGL((block_score_matrix_kernel<4>), grid, dim3(256), 0, st, a); break;
+    case 8: hipLaunchKernelGGL((block_score_matrix_kernel<8>), grid, dim3(256), 0, st, a); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();

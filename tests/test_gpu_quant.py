@@ -329,6 +329,23 @@ def test_choice_of_any_size_beside_infinities(nb, size):
     assert np.array_equal(blocks[0, 0].cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("hq", [1, 2, 4, 8])
+def test_choice_with_bounds_far_apart(hq):
+    """The bound that a query's sign leaves out does not touch the score, however large it is."""
+    nb, budget = 700, 70
+    batch, cache = only_bounds(nb, 16, hq, 1)
+    x = torch.randn(nb, D, generator=gen(4), device="cuda")
+    far = 3e38 * torch.rand(nb, D, generator=gen(5), device="cuda") + 1e30
+    even = torch.arange(D, device="cuda") % 2 == 0
+    cache.bounds[0, :nb, 0] = torch.where(even, -far, x).to(torch.bfloat16)
+    cache.bounds[0, :nb, 1] = torch.where(even, x, far).to(torch.bfloat16)
+    q = torch.randn(1, hq, D, generator=gen(6), device="cuda").abs()
+    q = torch.where(even, q, -q).to(torch.bfloat16)
+    want = R.choose(q[0].double().cpu().numpy(), cache.bounds[0, :nb].double().cpu().numpy(), budget, 0, 0)
+    blocks, _ = T.BlockSelector(batch, 16, budget, 0, 0)(q, cache)
+    assert np.array_equal(blocks[0, 0].cpu().numpy(), want)
+
+
 def test_decode_of_all_blocks_is_the_decode():
     lens = [700, 33]
     h = Held(lens, [n + 9 for n in lens], 8, 2, 8, block=32)
