@@ -507,7 +507,7 @@ tactic_status tactic_quant_read(const tactic_quant_kv* kv, const tactic_kv_shape
  * Ties go to the lower block; a score of NaN is above all others (of a query that is not
  * finite, or of bounds of infinity, which no cache's values have, any scores may be). */
 typedef struct {
-  int32_t budget;              /* blocks at most, >= 1 */
+  int32_t budget;              /* blocks at most, 1 .. 2^27 */
   int32_t first, last;         /* >= 0, together at most budget */
 } tactic_block_params;
 /* kv: the bounds and the block are read, not the rows.

@@ -19,6 +19,7 @@ constexpr int64_t kMaxInt = ((int64_t)1 << 31) - 1;
 // choice 18.6, 18.2, 18.6, 19.6; eight heads, with the decode 49.3, 50.6, 50.9, 53.6; 8192 blocks of 8 heads
 // 40.7, 40.7, 41.5, 43.6 (the choice reads a maximum of each); 256 and 512 were 4 and 1 slower than 1024.
 constexpr int64_t kScoreGroups = 1024;
+constexpr int32_t kMaxBudget = 1 << 27;  // the blocks of 2^31 rows
 
 tactic_status check_aligned(std::initializer_list<const void*> arrays, int bytes) {
   for (const void* p : arrays)
@@ -58,9 +59,9 @@ tactic_status quant_args(const tactic_quant_kv* kv, const tactic_kv_shape* s, bo
 tactic_status check_new_rows(const tactic_query_shape* q, const tactic_kv_shape* s) {
   if (!q) return fail(TACTIC_ERR_INVALID_ARG, "rows is null");
   if (!q->q_indptr) return fail(TACTIC_ERR_INVALID_ARG, "q_indptr is null");
+  if (q->total_queries > kMaxInt / s->n_kv_heads) return fail(TACTIC_ERR_UNSUPPORTED, "total_queries * n_kv_heads >= 2^31");
   if (q->total_queries < 0 || q->max_queries < 0 || q->max_queries > q->total_queries || q->total_queries > q->max_queries * s->batch)
     return fail(TACTIC_ERR_INVALID_ARG, "inconsistent total_queries / max_queries");
-  if (q->total_queries * s->n_kv_heads > kMaxInt) return fail(TACTIC_ERR_UNSUPPORTED, "total_queries * n_kv_heads >= 2^31");
   return TACTIC_OK;
 }
 
@@ -200,6 +201,7 @@ tactic_status tactic_block_select(const uint16_t* q, const tactic_quant_kv* kv, 
   if (!params) return fail(TACTIC_ERR_INVALID_ARG, "params is null");
   if (params->budget < 1 || params->first < 0 || params->last < 0 || (int64_t)params->first + params->last > params->budget)
     return fail(TACTIC_ERR_INVALID_ARG, "budget must be >= 1 and at least first + last");
+  if (params->budget > kMaxBudget) return fail(TACTIC_ERR_UNSUPPORTED, "budget > 2^27 blocks");
   if (!q || !blocks || !counts || !c.bounds) return fail(TACTIC_ERR_INVALID_ARG, "null argument");
   if ((st = check_aligned({q, workspace}, 16)) != TACTIC_OK || (st = check_aligned({blocks, counts}, 4)) != TACTIC_OK) return st;
   const SelectLayout l = select_layout(shape, c.block);

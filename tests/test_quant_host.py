@@ -101,6 +101,12 @@ def test_unsupported_scores_and_small_workspaces():
     assert decode(n=need - 1) == 3 and decode(ws=None) == 3
 
 
+def test_counts_past_the_limits():
+    assert select(budget=(1 << 27) + 1) == 2 and select(budget=(1 << 31) - 1) == 2
+    for total in (1 << 62, (1 << 63) - 1):
+        assert write(rows=_rows(total=total, most=total)) == 2 and read(rows=_rows(total=total, most=total)) == 2
+
+
 def test_arrays_that_overlap():
     """k, v and the cache's arrays (of 2000 rows of 128 bytes), each a byte too near to the next."""
     at = {"k": 1 << 24, "v": 2 << 24, "K": 3 << 24, "Ks": 4 << 24, "V": 5 << 24, "Vs": 6 << 24, "bounds": 7 << 24}
