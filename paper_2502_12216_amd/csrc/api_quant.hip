@@ -118,23 +118,25 @@ SelectLayout select_layout(const tactic_kv_shape* s, int block) {
 }
 
 // Whether the decode gives every KV head one workgroup, which joins its own waves and writes the
-// outputs, or splits all rows evenly and joins the parts in a second launch.  One workgroup takes 4.7 us
-// and `step` us for 128 rows of its four waves, or what memory gives it; the split 11 to 14.5
-// us (a start that looks at every group, the second launch, and 4 us more on the host) and the
-// bytes at 6 TB/s.  Measured, one
-// against split, us a call, rows of 8 KV heads, 8 bits and 4 heads each: one sequence
-// of 256 rows 7.2, 11.3; 512 9.7, 11.7; 768 12.3, 11.9; 1024 15.1, 12.1; 32 sequences of 256 8.4,
-// 16.5; 1024 17.2, 25.9; 2048 28.6, 36.6; 8 sequences at 4 bits 512 8.0, 11.1; 1024 11.1,
-// 12.5; 1536 14.3, 12.9; with 8 heads at 8 bits 512 12.3, 14.4; 1024 18.4, 18.6.  One workgroup
-// is as slow as its longest sequence, so that it is not used from 2048 rows on.
+// outputs, or splits all rows evenly and joins the parts in a second launch.  One workgroup takes 4 us
+// (eight query heads: 5) and `step` us for 128 rows of its four waves, the longer the more of them
+// share the memory, or what memory gives it; the split 10 to 12 us (eight heads: 12 to 18; a start that
+// looks at every group, the second launch) and the bytes at 6 TB/s.  Measured, one against split, us
+// a call, rows of 8 KV heads, 8 bits and 4 heads each: one sequence of 512 rows 7.7, 10.5; 768 9.2,
+// 10.5; 1024 10.7, 10.5; 4 of 768 10.2, 10.8; 1024 12.0, 10.9; 16 of 1536 18.5, 19.6; 2048 24.2, 21.8; 32 of 2048 26.5,
+// 34.2; 4 bits: one of 1024 9.0, 10.0; 1536 12.1, 10.0; 16 of 2048 15.8, 17.1; eight heads at 8 bits: one of
+// 512 9.2, 12.0; 768 12.3, 12.1; 4 of 1024 13.4, 12.6; 16 of 2048 26.2, 26.8.  One workgroup is as slow
+// as its longest sequence, so that it is not used from 2048 rows on.
 bool one_workgroup(const tactic_kv_shape* s, int bits, int64_t most) {
   if (most > 2048) return false;
+  const bool eight = s->n_q_heads / s->n_kv_heads == 8;
   const double groups = (double)s->batch * s->n_kv_heads, row = 2 * (16.0 * bits + 4) / 6e6;
-  const double step = (bits == 8 ? 1.25 : 0.8) * (s->n_q_heads / s->n_kv_heads == 8 ? 1.2 : 1.0);
+  const double shared = std::min(groups, 256.0) / 256, doublings = std::max(0.0, log2(std::min(groups, 256.0) / 8));
+  const double step = (bits == 8 ? 0.81 + 0.118 * doublings : 0.66 + 0.03 * doublings) + (eight ? 0.2 : 0.0);
   const double rounds = std::max(1.0, ceil(groups / 512));
   const double all = std::min((double)s->total_tokens * s->n_kv_heads, groups * (double)most);
-  const double one = 4.7 + (double)most * rounds * std::max(step / 128, std::min(groups, 512.0) * row);
-  return one <= 12 + 3.5 * std::min(1.0, groups / 256) + all * row;
+  const double one = (eight ? 5.0 : 4.0) + (double)most * rounds * std::max(step / 128, std::min(groups, 512.0) * row);
+  return one <= (eight ? 11.7 + 6.5 * shared : 10.0 + 2.0 * shared) + all * row;
 }
 
 bool is_block(int block) { return block == 16 || block == 32 || block == 64 || block == 128; }

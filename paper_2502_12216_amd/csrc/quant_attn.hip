@@ -40,7 +40,9 @@ constexpr float kScaleLog2 = kLog2e * kInvSqrtDim;
 template <int kBits>
 constexpr int64_t kQuantShare = kBits == 8 ? 192 : 256;
 constexpr int kTableRows = 2048;      // rows looked up at once
-constexpr int kWaves = 4;             // waves of a workgroup (eight: 3 to 11% slower)
+// Waves of a workgroup.  Eight: 3 to 11% slower where they split all rows; with a group to itself 5 to 20% slower up to
+// 512 rows and 10 to 40% beyond 256 groups, at best 7% faster (128 groups of 2048 rows).
+constexpr int kWaves = 4;
 constexpr int kStep = 32 * kWaves;    // rows of a step of all of them
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -83,7 +85,9 @@ __device__ __forceinline__ Group group_of(const QuantAttnArgs& x, int bg) {
 
 // kRows: 0 rows lie at their positions; 1 every 16 positions from a multiple of 16 lie together
 // (chosen blocks, pages of a multiple of 16 rows); 2 rows lie anywhere
-template <int G, int kBits, int kRows, bool kMod>
+// kDirect: a workgroup for each group, which writes the outputs itself.  (A form of its own: with
+// the choice made inside the kernel 5 to 24% slower, and splits with eight heads by up to 14%.)
+template <int G, int kBits, int kRows, bool kMod, bool kDirect>
 __global__ __launch_bounds__(kWave * kWaves) __attribute__((amdgpu_waves_per_eu(2)))
 void quant_attn_kernel(QuantAttnArgs x) {
   constexpr int kPart = G * (kHeadDim + 2);
@@ -115,7 +119,7 @@ void quant_attn_kernel(QuantAttnArgs x) {
   // of which segments begin at multiples of 32 rows.
   int bg = blockIdx.x, bg_end = bg + 1;
   int64_t t0 = 0, t1 = INT64_MAX;
-  if (!x.direct) {
+  if constexpr (!kDirect) {
     const int per = (BG + kThreads - 1) / kThreads, g0 = min(BG, tid * per), g1 = min(BG, g0 + per);
     auto units = [&](int64_t n) { return n > 0 ? ((n + 31) & ~(int64_t)31) + kSegmentCost : 0; };
     Group* const groups = reinterpret_cast<Group*>(s_prefix + BG + 1);
@@ -157,7 +161,7 @@ void quant_attn_kernel(QuantAttnArgs x) {
   for (; bg < bg_end; ++bg) {
     int64_t seg_lo = 0, seg_hi, kvb;
     int nseq;
-    if (x.direct) {
+    if constexpr (kDirect) {
       const Group g = group_of(x, bg);
       seg_hi = uniform(g.rows);
       kvb = uniform(g.kvb);
@@ -468,39 +472,41 @@ void quant_attn_kernel(QuantAttnArgs x) {
       }
     }
     __syncthreads();
-    if (tid * 4 < G * kHeadDim) {
-      const int h = tid * 4 / kHeadDim, e = tid * 4 % kHeadDim;
+    constexpr int kEach = kDirect ? (G >= 2 ? G / 2 : 1) : 4;  // values of a thread
+    struct __attribute__((aligned(kEach * 4))) Values {
+      float v[kEach];
+    };
+    if (tid * kEach < G * kHeadDim) {
+      const int h = tid * kEach / kHeadDim, e = tid * kEach % kHeadDim;
       float mm = -INFINITY, ll = 0.f;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, s_ml[w][1][h] == 0.f ? -INFINITY : s_ml[w][0][h]);
-      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+      Values sum{};
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
         const float lw = s_ml[w][1][h], f = lw == 0.f ? 0.f : fast_exp2(s_ml[w][0][h] - mm);
         ll = fmaf(lw, f, ll);
-        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+        Values y{};
 #pragma unroll
         for (int q = 2; q >= 0; --q) {  // the small parts first
-          const float4 v = *reinterpret_cast<const float4*>(&sh.red[w * 3 + q][h][e]);
-          y.x += v.x;
-          y.y += v.y;
-          y.z += v.z;
-          y.w += v.w;
+          const Values part = *reinterpret_cast<const Values*>(&sh.red[w * 3 + q][h][e]);
+#pragma unroll
+          for (int i = 0; i < kEach; ++i) y.v[i] += part.v[i];
         }
-        sum.x = fmaf(y.x, f, sum.x);
-        sum.y = fmaf(y.y, f, sum.y);
-        sum.z = fmaf(y.z, f, sum.z);
-        sum.w = fmaf(y.w, f, sum.w);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) sum.v[i] = fmaf(y.v[i], f, sum.v[i]);
       }
-      if (x.direct) {
+      if constexpr (kDirect) {
         const int64_t row = (int64_t)b * a.Hq + kvh * G + h;
         const bool empty = mm == -INFINITY;
-        if (empty) sum = make_float4(0.f, 0.f, 0.f, 0.f), ll = 1.f;
-        *reinterpret_cast<float4*>(a.out + row * kHeadDim + e) = make_float4(sum.x / ll, sum.y / ll, sum.z / ll, sum.w / ll);
+        if (empty) sum = Values{}, ll = 1.f;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) sum.v[i] /= ll;
+        *reinterpret_cast<Values*>(a.out + row * kHeadDim + e) = sum;
         if (e == 0 && x.lse) x.lse[row] = empty ? -INFINITY : (mm + __builtin_amdgcn_logf(ll)) * kLn2;
       } else {
         float* part = a.partials + ((int64_t)bg + blockIdx.x) * kPart;
-        *reinterpret_cast<float4*>(part + tid * 4) = sum;
+        *reinterpret_cast<Values*>(part + tid * kEach) = sum;
         if (e == 0) {
           part[G * kHeadDim + h] = mm;
           part[G * kHeadDim + G + h] = ll;
@@ -512,21 +518,27 @@ void quant_attn_kernel(QuantAttnArgs x) {
 }
 
 // Calls f with the kernel of these arguments.
-template <int G, int kBits, typename F>
+template <int G, int kBits, bool kDirect, typename F>
 static hipError_t with_kernel_g(const QuantAttnArgs& x, F f) {
   const bool mod = x.cap > 0.f || x.slopes;
-  if (x.kv.paged && x.kv.pk.page_size % 16) return mod ? f(quant_attn_kernel<G, kBits, 2, true>) : f(quant_attn_kernel<G, kBits, 2, false>);
-  if (x.blocks || x.kv.paged) return mod ? f(quant_attn_kernel<G, kBits, 1, true>) : f(quant_attn_kernel<G, kBits, 1, false>);
-  return mod ? f(quant_attn_kernel<G, kBits, 0, true>) : f(quant_attn_kernel<G, kBits, 0, false>);
+  if (x.kv.paged && x.kv.pk.page_size % 16)
+    return mod ? f(quant_attn_kernel<G, kBits, 2, true, kDirect>) : f(quant_attn_kernel<G, kBits, 2, false, kDirect>);
+  if (x.blocks || x.kv.paged)
+    return mod ? f(quant_attn_kernel<G, kBits, 1, true, kDirect>) : f(quant_attn_kernel<G, kBits, 1, false, kDirect>);
+  return mod ? f(quant_attn_kernel<G, kBits, 0, true, kDirect>) : f(quant_attn_kernel<G, kBits, 0, false, kDirect>);
+}
+template <int G, typename F>
+static hipError_t with_kernel_of(const QuantAttnArgs& x, F f) {
+  if (x.direct) return x.kv.bits == 8 ? with_kernel_g<G, 8, true>(x, f) : with_kernel_g<G, 4, true>(x, f);
+  return x.kv.bits == 8 ? with_kernel_g<G, 8, false>(x, f) : with_kernel_g<G, 4, false>(x, f);
 }
 template <typename F>
 static hipError_t with_kernel(const QuantAttnArgs& x, int G, F f) {
-  const bool eight = x.kv.bits == 8;
   switch (G) {
-    case 1: return eight ? with_kernel_g<1, 8>(x, f) : with_kernel_g<1, 4>(x, f);
-    case 2: return eight ? with_kernel_g<2, 8>(x, f) : with_kernel_g<2, 4>(x, f);
-    case 4: return eight ? with_kernel_g<4, 8>(x, f) : with_kernel_g<4, 4>(x, f);
-    case 8: return eight ? with_kernel_g<8, 8>(x, f) : with_kernel_g<8, 4>(x, f);
+    case 1: return with_kernel_of<1>(x, f);
+    case 2: return with_kernel_of<2>(x, f);
+    case 4: return with_kernel_of<4>(x, f);
+    case 8: return with_kernel_of<8>(x, f);
     default: return hipErrorInvalidValue;
   }
 }
