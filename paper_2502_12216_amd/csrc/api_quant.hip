@@ -233,7 +233,7 @@ tactic_status tactic_block_select(const uint16_t* q, const tactic_quant_kv* kv, 
   a.blocks = blocks;
   a.counts = counts;
   hipError_t e = hipSuccess;
-  if (l.max_blocks > a.budget) e = tactic::launch_block_scores(a, stream);  // (else every block is chosen)
+  if (l.max_blocks > a.budget && !tactic::blocks_scored_by_select(a)) e = tactic::launch_block_scores(a, stream);  // (else every block is chosen)
   if (e == hipSuccess) e = tactic::launch_block_select(a, stream);
   return e == hipSuccess ? TACTIC_OK : hip_fail(e, "block selection launch");
 }

@@ -41,13 +41,32 @@ struct ScoreRange {
 __device__ __forceinline__ ScoreRange score_range(const SelectArgs& a) {
   const int g = blockIdx.y, b = blockIdx.z, lb = __builtin_ctz(a.block);
   const int64_t kvb = a.kv_indptr[b], n = seq_tokens(a.kv_indptr, a.seq_len, b);
-  const int64_t nb = (n + a.block - 1) >> lb, j0 = (int64_t)blockIdx.x * a.per;
+  const int64_t nb = min((n + a.block - 1) >> lb, a.max_blocks), j0 = (int64_t)blockIdx.x * a.per;
   return {j0, min(nb, j0 + a.per), a.bounds + ((int64_t)g * ((a.total >> lb) + a.B) + first_block(kvb, lb, b)) * (2 * kHeadDim),
           j0 >= nb || nb <= a.budget};  // (all of them are chosen)
 }
 __device__ __forceinline__ double wide(const uint4& w, int e) {  // the bf16 e of eight (a constant after unrolling)
   const uint32_t u = e < 2 ? w.x : e < 4 ? w.y : e < 6 ? w.z : w.w;
   return (double)(e & 1 ? bf16hi(u) : bf16lo(u));
+}
+
+// 8 dimensions of a query head in 64 bits, and ones where they are negative
+__device__ __forceinline__ void signed_query(const uint16_t* p, double (&q)[8], uint32_t (&neg)[4]) {
+  const uint4 w = *reinterpret_cast<const uint4*>(p);
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) q[e] = wide(w, e);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) neg[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(i16x2, u[i]) >> 15);
+}
+// A lane's part of u_hj from its 8 dimensions of the block's bounds
+__device__ __forceinline__ double score_of_lane(const double (&q)[8], const uint32_t (&neg)[4], const uint4& lo, const uint4& hi) {
+  auto pick = [](uint32_t m, uint32_t x, uint32_t y) { return (x & m) | (y & ~m); };
+  const uint4 w = make_uint4(pick(neg[0], lo.x, hi.x), pick(neg[1], lo.y, hi.y), pick(neg[2], lo.z, hi.z), pick(neg[3], lo.w, hi.w));
+  double u = 0.0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) u = fma(q[e], wide(w, e), u);
+  return u;
 }
 
 // One or two query heads, on the vector unit: 16 lanes have a block, 8 dimensions each, and take of
@@ -71,30 +90,16 @@ __global__ __launch_bounds__(256) void block_score_kernel(SelectArgs a) {
   uint4 lo, hi, lo2, hi2;
   load(r.j0, lo, hi);
   double q[G][8], best = -INFINITY;
-  uint32_t neg[G][4];  // ones where a dimension of q is negative
+  uint32_t neg[G][4];
 #pragma unroll
-  for (int h = 0; h < G; ++h) {
-    const uint4 w = *reinterpret_cast<const uint4*>(a.q + (head + h) * kHeadDim + sl * 8);
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) q[h][e] = wide(w, e);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) neg[h][i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(i16x2, u[i]) >> 15);
-  }
+  for (int h = 0; h < G; ++h) signed_query(a.q + (head + h) * kHeadDim + sl * 8, q[h], neg[h]);
   double* scores = a.scores + (head + sl / kSpan) * a.max_blocks;
 #pragma unroll 1
   for (int64_t j = r.j0; j < r.j1; j += 16) {
     load(min(j + 16, r.j1 - 1), lo2, hi2);
     double u[G];
 #pragma unroll
-    for (int h = 0; h < G; ++h) u[h] = 0.0;
-#pragma unroll
-    for (int h = 0; h < G; ++h) {
-      auto pick = [&](uint32_t m, uint32_t x, uint32_t y) { return (x & m) | (y & ~m); };
-      const uint4 w = make_uint4(pick(neg[h][0], lo.x, hi.x), pick(neg[h][1], lo.y, hi.y), pick(neg[h][2], lo.z, hi.z), pick(neg[h][3], lo.w, hi.w));
-#pragma unroll
-      for (int e = 0; e < 8; ++e) u[h] = fma(q[h][e], wide(w, e), u[h]);
-    }
+    for (int h = 0; h < G; ++h) u[h] = score_of_lane(q[h], neg[h], lo, hi);
     double v;
     if constexpr (G == 2) v = reduce2(u, sl);
     else v = sum16d(u[0]);
@@ -112,6 +117,17 @@ __global__ __launch_bounds__(256) void block_score_kernel(SelectArgs a) {
 #pragma unroll
     for (int i = 1; i < 16; ++i) v = fmax(v, s_top[i][tid]);
     a.top[(head + tid) * a.tops + blockIdx.x] = v;
+  }
+}
+
+// 8 dimensions of a query head in 64 bits, its positive and its negative values apart
+__device__ __forceinline__ void parts_of_query(const uint16_t* p, double (&above)[8], double (&below)[8]) {
+  const uint4 w = *reinterpret_cast<const uint4*>(p);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const double x = wide(w, e);
+    above[e] = x < 0 ? 0.0 : x;
+    below[e] = x < 0 ? x : 0.0;
   }
 }
 
@@ -140,14 +156,8 @@ __global__ __launch_bounds__(256) void block_score_matrix_kernel(SelectArgs a) {
   double above[S][8], below[S][8], best[S];  // q where it is positive, and where negative
 #pragma unroll
   for (int s = 0; s < S; ++s) {
-    const uint4 w = *reinterpret_cast<const uint4*>(a.q + (head + 4 * s + col) * kHeadDim + (lane >> 2) * 8);
+    parts_of_query(a.q + (head + 4 * s + col) * kHeadDim + (lane >> 2) * 8, above[s], below[s]);
     best[s] = -INFINITY;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const double x = wide(w, e);
-      above[s][e] = x < 0 ? 0.0 : x;
-      below[s][e] = x < 0 ? x : 0.0;
-    }
   }
   double* scores = a.scores + (head + row) * a.max_blocks;
 #pragma unroll 1
@@ -210,6 +220,76 @@ __device__ __forceinline__ uint32_t place_in_range(double score, double per_widt
   return (uint32_t)fmin(fmax(fma(score, per_width, 4294966784.0), 0.0), 4294967295.0);
 }
 
+constexpr int kFusedBlocks = 1024;  // of a workgroup that scores its blocks itself, at most
+
+// The scores of the nb blocks of one KV head into LDS by a workgroup of 1024 threads, 64 blocks side by side, as the
+// two kernels above; top: the best of every 16 lanes or of every wave.
+template <int H>
+__device__ __forceinline__ void score_blocks(const SelectArgs& a, int g, int b, int nb, double (*scores)[kFusedBlocks], double (*top)[8]) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lb = __builtin_ctz(a.block);
+  const uint16_t* bounds = a.bounds + ((int64_t)g * ((a.total >> lb) + a.B) + first_block(a.kv_indptr[b], lb, b)) * (2 * kHeadDim);
+  const uint16_t* query = a.q + ((int64_t)b * a.Hq + g * H) * kHeadDim;
+  auto load = [&](int j, int d, uint4& lo, uint4& hi) __attribute__((always_inline)) {
+    const uint16_t* p = bounds + (int64_t)min(j, nb - 1) * (2 * kHeadDim) + d;
+    lo = *reinterpret_cast<const uint4*>(p);
+    hi = *reinterpret_cast<const uint4*>(p + kHeadDim);
+  };
+  uint4 lo, hi, lo2, hi2;
+  if constexpr (H <= 2) {
+    constexpr int kSpan = 16 / H;
+    const int sl = tid & 15, sub = tid >> 4;
+    load(sub, sl * 8, lo, hi);
+    double q[H][8], best = -INFINITY;
+    uint32_t neg[H][4];
+#pragma unroll
+    for (int h = 0; h < H; ++h) signed_query(query + h * kHeadDim + sl * 8, q[h], neg[h]);
+#pragma unroll 1
+    for (int j = sub; j < nb; j += 64) {
+      load(j + 64, sl * 8, lo2, hi2);
+      double u[H], v;
+#pragma unroll
+      for (int h = 0; h < H; ++h) u[h] = score_of_lane(q[h], neg[h], lo, hi);
+      if constexpr (H == 2) v = reduce2(u, sl);
+      else v = sum16d(u[0]);
+      best = fmax(best, v);
+      if (sl % kSpan == 0) scores[sl / kSpan][j] = v != v ? INFINITY : v;
+      lo = lo2;
+      hi = hi2;
+    }
+    if (sl % kSpan == 0) top[sub][sl / kSpan] = best;
+  } else {
+    const int col = lane & 3, row = lane >> 4, d = (lane >> 2) * 8;
+#pragma unroll 1
+    for (int h0 = 0; h0 < H; h0 += 4) {
+      load(wave * 4 + col, d, lo, hi);
+      double above[8], below[8], best = -INFINITY;
+      parts_of_query(query + (h0 + col) * kHeadDim + d, above, below);
+#pragma unroll 1
+      for (int j = wave * 4; j < nb; j += 64) {
+        load(j + 64 + col, d, lo2, hi2);
+        double high = 0.0, low = 0.0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          high = __builtin_amdgcn_mfma_f64_4x4x4f64(above[e], wide(hi, e), high, 0, 0, 0);
+          low = __builtin_amdgcn_mfma_f64_4x4x4f64(below[e], wide(lo, e), low, 0, 0, 0);
+        }
+        double v = high + low;
+        v += dpp<0x128>(v);
+        v += dpp<0x124>(v);
+        if (j + col < nb) {
+          best = fmax(best, v);
+          if ((lane & 12) == 0) scores[h0 + row][j + col] = v != v ? INFINITY : v;
+        }
+        lo = lo2;
+        hi = hi2;
+      }
+      best = fmax(best, dpp<0x4E>(best));
+      best = fmax(best, dpp<0xB1>(best));
+      if ((lane & 15) == 0) top[wave][h0 + row] = best;
+    }
+  }
+}
+
 // The `budget` blocks of the largest scores of one KV head, ascending.  A radix selection
 // in digits of 11 bits, each with a histogram in LDS of the keys still level, that ends as
 // soon as all of the digit that holds the last one are wanted: first over a score's place
@@ -217,15 +297,17 @@ __device__ __forceinline__ uint32_t place_in_range(double score, double per_widt
 // counts wait for one another: the first digit of 8192 blocks took 8 us), then, where that
 // does not tell, over the scores' bits from the first in which they differ.  Block j is thread
 // j mod 1024's; chosen ones find their places by a scan of every wave over the ballots of 64 blocks.
-// kPer = 0: the scores lie in the workspace and are gone through 16384 at a time.
+// kPer = 0: the scores lie in the workspace and are gone through 16384 at a time.  kFused: they are made here.
 // Bound by its chain of loads, scans and barriers: 188 blocks 4.2 us, 2048 (32 groups) 6.8, 8192 (8
 // groups) 11.7, 16384 20.5, 40000 64; with integer keys held in place of scores and a block-wide scan
 // of the ballots (two barriers more) 5.5, 7.8, 13.7, 22.8, 79.
-template <int kPer>
+template <int kPer, bool kFused = false>
 __global__ __launch_bounds__(1024) void block_select_kernel(SelectArgs a) {
+  static_assert(!kFused || kPer == 1, "scores in LDS");
   constexpr int kBins = 2048, kThreads = 1024, kHeld = kPer ? kPer : 16, kWords = kHeld * 16;
   __shared__ uint32_t s_hist[kBins];
   __shared__ double s_best[8];
+  __shared__ double s_scores[kFused ? 8 : 1][kFusedBlocks], s_top[kFused ? 64 : 1][8];
   __shared__ uint32_t s_max[16];
   __shared__ uint64_t s_least[16], s_most[16];
   __shared__ uint32_t s_wave[16];
@@ -235,7 +317,7 @@ __global__ __launch_bounds__(1024) void block_select_kernel(SelectArgs a) {
   const int g = blockIdx.x, b = blockIdx.y;
   const int lb = __builtin_ctz(a.block), G = a.G;
   const int64_t n = seq_tokens(a.kv_indptr, a.seq_len, b);
-  const int nb = (int)((n + a.block - 1) >> lb), want = min(a.budget, nb);
+  const int nb = (int)min((n + a.block - 1) >> lb, a.max_blocks), want = min(a.budget, nb);
   int32_t* out = a.blocks + ((int64_t)b * a.Hkv + g) * a.budget;
   if (tid == 0) a.counts[(int64_t)b * a.Hkv + g] = want;
   for (int i = want + tid; i < a.budget; i += kThreads) out[i] = -1;
@@ -258,13 +340,25 @@ __global__ __launch_bounds__(1024) void block_select_kernel(SelectArgs a) {
 #pragma unroll
       for (int h = 0; h < H; ++h)
 #pragma unroll
-        for (int i = 0; i < K; ++i) d[h][i] = scores[(int64_t)h * a.max_blocks + min(j + i * kThreads, nb - 1)];
+        for (int i = 0; i < K; ++i) {
+          const int at = min(j + i * kThreads, nb - 1);
+          if constexpr (kFused) d[h][i] = s_scores[h][at];
+          else d[h][i] = scores[(int64_t)h * a.max_blocks + at];
+        }
     };
+    if constexpr (kFused) {
+      score_blocks<H>(a, g, b, nb, s_scores, s_top);
+      __syncthreads();
+    }
     load(tid);  // (on their way while the best ones are looked up)
     if (wave < H) {  // every head's best score: a wave for each
-      const double* top = a.top + ((int64_t)b * a.Hq + g * H + wave) * a.tops;
       double v = -INFINITY;
-      for (int i = lane; i < (nb + a.per - 1) / a.per; i += kWave) v = fmax(v, top[i]);
+      if constexpr (kFused) {
+        if (lane < (H <= 2 ? 64 : 16)) v = s_top[lane][wave];
+      } else {
+        const double* top = a.top + ((int64_t)b * a.Hq + g * H + wave) * a.tops;
+        for (int i = lane; i < (nb + a.per - 1) / a.per; i += kWave) v = fmax(v, top[i]);
+      }
       v = wave_allmax_d(v);
       if (lane == 0) s_best[wave] = v;
     }
@@ -490,9 +584,19 @@ hipError_t launch_block_scores(const SelectArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+// Whether the workgroup that selects scores its blocks itself.  us in one launch against two, which take 2.3 us
+// more on the host (8.6 against 6.3 to 7): 2 groups of one head 256 blocks 6.1, 6.4; 512 8.0, 6.6; of four heads
+// 64 5.8, 6.8; 188 7.9, 7.0; 384 10.9, 7.0; of eight 64 7.9, 7.8; 128 10.0, 8.0; 256 groups, a compute unit each,
+// of one head 1024 blocks 22.4, 26.2; of four 23.5, 29.2; of eight 512 24.1, 25.4; 768 33.1, 32.7.
+bool blocks_scored_by_select(const SelectArgs& a) {
+  if ((int64_t)a.B * a.Hkv >= 256) return a.max_blocks <= (a.G == 8 ? 512 : kFusedBlocks);
+  return a.max_blocks <= (a.G == 8 ? 64 : a.G == 4 ? 192 : 256);
+}
+
 hipError_t launch_block_select(const SelectArgs& a, hipStream_t st) {
   const dim3 grid(a.Hkv, a.B), threads(1024);
-  if (a.max_blocks <= 1024) hipLaunchKernelGGL((block_select_kernel<1>), grid, threads, 0, st, a);
+  if (blocks_scored_by_select(a)) hipLaunchKernelGGL((block_select_kernel<1, true>), grid, threads, 0, st, a);
+  else if (a.max_blocks <= 1024) hipLaunchKernelGGL((block_select_kernel<1>), grid, threads, 0, st, a);
   else if (a.max_blocks <= 2048) hipLaunchKernelGGL((block_select_kernel<2>), grid, threads, 0, st, a);
   else if (a.max_blocks <= 4096) hipLaunchKernelGGL((block_select_kernel<4>), grid, threads, 0, st, a);
   else if (a.max_blocks <= 8192) hipLaunchKernelGGL((block_select_kernel<8>), grid, threads, 0, st, a);

@@ -286,6 +286,7 @@ struct SelectArgs {
 };
 constexpr int kSelectHeld = 16384;  // blocks whose keys a workgroup holds in registers
 hipError_t launch_block_scores(const SelectArgs& a, hipStream_t st);
+bool blocks_scored_by_select(const SelectArgs& a);  // then launch_block_scores is not needed
 hipError_t launch_block_select(const SelectArgs& a, hipStream_t st);
 
 // One token per sequence over a quantised cache, all of it or the chosen blocks (quant_attn.hip).
