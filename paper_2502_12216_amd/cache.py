@@ -16,7 +16,7 @@ from typing import List, Optional, Sequence
 import numpy as np
 import torch
 
-from .attention import CacheEvictor, PromptAttention, ScoredDecoder, ScoreMod, TokenInserter
+from .attention import CacheEvictor, PromptAttention, ScoredDecoder, ScoreMod, TokenInserter, _Call
 from .quant import BlockSelector, CacheQuantizer, QuantizedCache, QuantizedDecoder
 from .tactic import (ClusterBuilder, ClusterSet, DenseDecoder, RaggedBatch, SparseDecoder, _check_tensor, decode_params,
                      sparse_decode_workspace_bytes)
@@ -255,9 +255,14 @@ class QuantizingCache:
             raise ValueError("a sequence outgrew its capacity")
         return lens
 
+    def _set_lens(self, lens: List[int]) -> None:
+        self.batch.seq_len.copy_(torch.as_tensor(np.asarray(lens, dtype=np.int64)))
+        self.batch.seq_lens = lens
+
     def extend(self, q: Sequence[torch.Tensor], K: Sequence[torch.Tensor], V: Sequence[torch.Tensor]) -> torch.Tensor:
         """q[b] bf16 [m_b][Hq][128], K[b], V[b] bf16 [m_b][Hkv][128], the next tokens of every prompt.  Returns their
-        attention, bf16 [sum m_b][Hq][128]."""
+        attention, bf16 [sum m_b][Hq][128].  All cached rows are held in bf16 while it runs.  A call that fails leaves
+        the lengths as they were."""
         new = [int(k.shape[0]) for k in K]
         if not len(new) == len(q) == len(V) == self.batch.batch:
             raise ValueError("extend needs tokens for every sequence")
@@ -270,11 +275,17 @@ class QuantizingCache:
             _check_tensor(x, name, torch.bfloat16, (rows.total, heads, 128))
             if x.device != self.device:
                 raise ValueError(f"{name} is on {x.device}, expected {self.device}")
-        self.batch.seq_len.copy_(torch.as_tensor(np.asarray(lens, dtype=np.int64)))
-        self.batch.seq_lens = lens
-        rows.write(Kc, Vc, self.cache)
-        full = RaggedBatch(lens, self.Hq, self.Hkv, device=self.device)
-        return PromptAttention(full, new)(qc, *held.read(self.cache), self.mod)[0]
+        self.mod.struct(_Call(self.device, None), self.batch)
+        prompt = PromptAttention(RaggedBatch(lens, self.Hq, self.Hkv, device=self.device), new)
+        out = [torch.empty(self.Hkv, held.total, 128, dtype=torch.bfloat16, device=self.device) for _ in range(2)]
+        before = self.batch.seq_lens
+        self._set_lens(lens)
+        try:
+            rows.write(Kc, Vc, self.cache)
+            return prompt(qc, *held.read(self.cache, K_out=out[0], V_out=out[1]), self.mod)[0]
+        except Exception:
+            self._set_lens(before)
+            raise
 
     def append(self, k: torch.Tensor, v: torch.Tensor) -> None:
         """k, v bf16 [B][Hkv][128], the new token of every sequence.  Only device work is enqueued."""

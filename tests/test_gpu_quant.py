@@ -537,3 +537,41 @@ def test_quantizing_cache(bits, budget):
     with pytest.raises((TypeError, ValueError)):
         c.append(k.float(), v)
     assert c.batch.seq_len.tolist() == lens
+
+
+@pytest.mark.parametrize("fails", ["slopes", "cache", "memory", "attention"])
+def test_extend_that_fails_counts_nothing(fails, monkeypatch):
+    """The lengths stay those of before, and the same chunk again gives what it gives a cache without a failure."""
+    import paper_2502_12216_amd.cache as module
+    sl, g = slopes(4), gen(31)
+
+    def some(heads):
+        return [torch.randn(m, heads, D, generator=g, device="cuda").to(torch.bfloat16) for m in (40, 7)]
+
+    first, chunk = ([some(4), some(2), some(2)] for _ in range(2))
+    c, e = (T.QuantizingCache(4, 2, [100, 100], bits=8, block=32, slopes=sl) for _ in range(2))
+    c.extend(*first)
+    e.extend(*first)
+    before = [getattr(c.cache, x).clone() for x in ("K", "K_scale", "V", "V_scale", "bounds")]
+
+    def no_memory(*args, **kw):
+        raise torch.OutOfMemoryError("no memory")
+
+    with monkeypatch.context() as mp:
+        if fails == "slopes":
+            mp.setattr(c, "mod", T.ScoreMod(slopes=sl.double()))
+        elif fails == "cache":
+            mp.setattr(c.cache, "V", c.cache.V[:, :-1].contiguous())
+        elif fails == "memory":
+            mp.setattr(module, "PromptAttention", no_memory)
+        else:
+            mp.setattr(module.PromptAttention, "__call__", no_memory)
+        with pytest.raises((TypeError, ValueError, torch.OutOfMemoryError)):
+            c.extend(*chunk)
+    assert c.batch.seq_lens == [40, 7] and c.batch.seq_len.tolist() == [40, 7]
+    if fails != "attention":  # (refused before anything was written)
+        assert all(torch.equal(getattr(c.cache, x), y) for x, y in zip(("K", "K_scale", "V", "V_scale", "bounds"), before))
+    assert torch.equal(c.extend(*chunk), e.extend(*chunk))
+    assert c.batch.seq_len.tolist() == [80, 14]
+    for x in ("K", "K_scale", "V", "V_scale", "bounds"):
+        assert torch.equal(getattr(c.cache, x), getattr(e.cache, x))
