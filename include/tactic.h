@@ -489,8 +489,9 @@ typedef struct {
  * left out): a prompt, a chunk, or a new token behind lengths that were advanced.
  * k, v: bf16 [rows->total_queries][Hkv][128].  With bounds, those of every block that has
  * a new row are set from the rows of the block up to the sequence's last.  A row whose
- * table entry is out of range is not written; no two sequences may write one page row.  k, v and
- * the cache's arrays must not overlap (else an invalid argument). */
+ * table entry is out of range is not written, and counts as zeros in the bounds, as it
+ * reads; no two sequences may write one page row.  k, v and the cache's arrays must not
+ * overlap (else an invalid argument). */
 tactic_status tactic_quant_write(const uint16_t* k, const uint16_t* v, const tactic_kv_shape* shape,
                                  const tactic_query_shape* rows, const tactic_quant_kv* kv, hipStream_t stream);
 /* The same rows in bf16 again, [Hkv][rows->total_queries][128] each (as the attention of a
@@ -522,7 +523,8 @@ tactic_status tactic_block_select(const uint16_t* q, const tactic_quant_kv* kv, 
  * as above (mod, or NULL, may hold a cap and slopes; the query is at position n_b - 1).
  * blocks, counts (both or neither): only the rows of these blocks of kv->block rows, as
  * tactic_block_select gives them with this budget (0 without); other lists have to be
- * ascending and without -1 up to the count.  Workspace: as tactic_dense_decode_workspace_size. */
+ * ascending and without -1 up to the count.  Rows of pages that are not there make the
+ * result meaningless, as in tactic_paged_kv.  Workspace: as tactic_dense_decode_workspace_size. */
 tactic_status tactic_quant_decode(const uint16_t* q, const tactic_quant_kv* kv, const tactic_kv_shape* shape,
                                   const tactic_score_mod* mod, const int32_t* blocks, const int32_t* counts,
                                   int32_t budget, float* out, float* lse, void* workspace,

@@ -163,6 +163,9 @@ __global__ __launch_bounds__(256) void quant_write_kernel(QuantRowsArgs a) {
         if constexpr (kBits == 8) *reinterpret_cast<uint2*>(to) = c;
         else *reinterpret_cast<uint32_t*>(to) = c.x;
         if ((sl & 3) == 0) scales[place[i] * 4 + (sl >> 2)] = (uint8_t)s;
+      } else {  // of a page that is not there: zeros, as they read
+        c = make_uint2(0u, 0u);
+        s = 127;
       }
     }
     if constexpr (kBounds) {

@@ -575,3 +575,42 @@ def test_extend_that_fails_counts_nothing(fails, monkeypatch):
     assert c.batch.seq_len.tolist() == [80, 14]
     for x in ("K", "K_scale", "V", "V_scale", "bounds"):
         assert torch.equal(getattr(c.cache, x), getattr(e.cache, x))
+
+
+@pytest.mark.parametrize("block", [16, 32, 64, 128])
+@pytest.mark.parametrize("bits", [8, 4])
+def test_rows_of_pages_that_are_not_there(bits, block):
+    """Table entries of -1, num_pages and beyond: their rows are not written, read as zeros and count as zeros in the
+    bounds, new rows as those from before; other pages are as they would be without them."""
+    n, page, hkv = 200, 16, 2
+    h, full = Held([n], [n], 4, hkv, bits, page, block), Held([n], [n], 4, hkv, bits, page, block)
+    num = h.cache.K.shape[0]
+    gone = {1: -1, 4: num, 9: num + 1000, 12: -2 ** 31}
+    for i, entry in gone.items():
+        h.cache.page_table[0, i] = entry
+    missing = np.isin(np.arange(n) // page, list(gone))
+    k, v = rows_like(gen(1), n, hkv), rows_like(gen(2), n, hkv)
+    k[:, :, 0] += 4.0   # a dimension whose least value is a missing row's zero
+    k[page, 0, 40] = float("nan")  # of a row that is not written
+    for x in (h, full):
+        for m in (75, 1, 124):  # a chunk, a token, the rest, from inside a missing page
+            x.batch.seq_len[0] = {75: 75, 1: 76, 124: n}[m]
+            at = slice(int(x.batch.seq_len[0]) - m, int(x.batch.seq_len[0]))
+            T.CacheQuantizer(x.batch, [m]).write(k[at].contiguous(), v[at].contiguous(), x.cache)
+    K, V = T.CacheQuantizer(h.batch, [n]).read(h.cache)
+    for name, got in (("K", K), ("V", V)):
+        for g in range(hkv):
+            held = full.values(name, 0, g, np.arange(n))
+            held[missing] = 0.0
+            assert np.array_equal(got[g].double().cpu().numpy(), held)
+            if name == "K":
+                ref = R.bounds_of(held, block)
+                assert np.array_equal(h.cache.bounds[g, :len(ref)].double().cpu().numpy(), ref), g
+    for name in ("K", "V", "K_scale", "V_scale"):  # only the pages that are there were written
+        x, y, fresh = (getattr(z.cache, name) for z in (h, full, Held([n], [n], 4, hkv, bits, page, block)))
+        ids = full.cache.page_table[0].long()
+        there = torch.tensor([i not in gone for i in range(len(ids))], device="cuda")
+        assert torch.equal(x[ids[there]], y[ids[there]])
+        other = torch.ones(num, dtype=torch.bool, device="cuda")
+        other[ids[there]] = False
+        assert torch.equal(x[other], fresh[other])
