@@ -47,6 +47,7 @@ constexpr int kStep = 32 * kWaves;    // rows of a step of all of them
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_words __attribute__((aligned(4)));  // (a row's powers begin at any word)
 
 __device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
@@ -264,7 +265,7 @@ void quant_attn_kernel(QuantAttnArgs x) {
             load_k(r, t, Kb + row * RB + (uint32_t)(sl * RB + grp * 16), Ks + row * 4 + (uint32_t)(sl * 4));
 #pragma unroll
             for (int i = 0; i < 4; ++i) load_v(r, 4 * t + i, Vb + row * RB + (uint32_t)(grp * (4 * RB) + sl * (RB / 16)) + i * RB);
-            const u32x4 w = *reinterpret_cast<const u32x4*>(Vs + row * 4 + (uint32_t)(grp * 16));
+            const u32x4 w = *reinterpret_cast<const u32x4_words*>(Vs + row * 4 + (uint32_t)(grp * 16));
 #pragma unroll
             for (int i = 0; i < 4; ++i) r.vs[4 * t + i] = w[i];
           }

@@ -614,3 +614,25 @@ def test_rows_of_pages_that_are_not_there(bits, block):
         other = torch.ones(num, dtype=torch.bool, device="cuda")
         other[ids[there]] = False
         assert torch.equal(x[other], fresh[other])
+
+
+@pytest.mark.parametrize("page", [0, 16, 50])
+@pytest.mark.parametrize("bits", [8, 4])
+def test_powers_at_any_word(bits, page):
+    """K_scale and V_scale need 4-byte alignment only, and sequences of spans begin at any row."""
+    lens = [2500, 33, 130, 7, 300]
+    a, c = (Held(lens, [n + 1 for n in lens], 8, 2, bits, page, 32) for _ in range(2))
+    for i, x in enumerate(("K_scale", "V_scale")):
+        old = getattr(c.cache, x)
+        room = torch.empty(old.numel() + 16, dtype=torch.uint8, device="cuda")
+        moved = room[4 + 4 * i:4 + 4 * i + old.numel()].view(old.shape)
+        assert moved.data_ptr() % 16 == 4 + 4 * i
+        setattr(c.cache, x, moved.copy_(old))
+    q = torch.randn(len(lens), 8, D, generator=gen(7), device="cuda").to(torch.bfloat16)
+    got = []
+    for h in (a, c):
+        h.fill()
+        got.append(T.CacheQuantizer(h.batch, lens).read(h.cache) + T.QuantizedDecoder(h.batch)(q, h.cache))
+        assert torch.equal(h.cache.V_scale, a.cache.V_scale) and torch.equal(h.cache.K_scale, a.cache.K_scale)
+    assert all(torch.equal(x, y) for x, y in zip(*got))
+    check_decode(c, q, got[1][2], got[1][3])
