@@ -468,7 +468,9 @@ tactic_status tactic_insert_token(const uint16_t* k, const uint16_t* v, const in
  *
  * Blocks: rows [j block, (j + 1) block) of a sequence.  bounds holds the least and the
  * largest value of every dimension of a block's keys, as they read; the blocks of
- * sequence b are at kv_indptr[b] / block + b and on. */
+ * sequence b are at kv_indptr[b] / block + b and on.  They belong to the sequence's span,
+ * with pages too, and only tactic_quant_write sets them: rows that come to a sequence in
+ * another way (a page shared or taken over, a sequence moved in its batch) have none. */
 typedef struct {
   uint8_t* K;                  /* device [Hkv][total_tokens][16 * bits], or pages
                                   [num_pages][Hkv][page_size][16 * bits] */

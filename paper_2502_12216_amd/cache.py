@@ -234,7 +234,8 @@ class QuantizingCache:
 
     extend() attends a chunk of every prompt in bf16 - its own tokens and the cached ones as the cache
     holds them - and keeps it; append() adds one token per sequence; decode() attends all rows, or with a
-    `budget` those of the blocks of `block` rows that the token's cheap score chooses."""
+    `budget` those of the blocks of `block` rows that the token's cheap score chooses.  The host's lengths
+    (batch.seq_lens), which extend() goes by, do not follow a captured append() that is replayed."""
 
     def __init__(self, n_q_heads: int, n_kv_heads: int, capacities: Sequence[int], bits: int = 8, block: int = 64,
                  budget: int = 0, first: int = 1, last: int = 2, cap: float = 0.0,

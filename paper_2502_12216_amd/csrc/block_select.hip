@@ -584,10 +584,14 @@ hipError_t launch_block_scores(const SelectArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-// Whether the workgroup that selects scores its blocks itself.  us in one launch against two, which take 2.3 us
-// more on the host (8.6 against 6.3 to 7): 2 groups of one head 256 blocks 6.1, 6.4; 512 8.0, 6.6; of four heads
-// 64 5.8, 6.8; 188 7.9, 7.0; 384 10.9, 7.0; of eight 64 7.9, 7.8; 128 10.0, 8.0; 256 groups, a compute unit each,
-// of one head 1024 blocks 22.4, 26.2; of four 23.5, 29.2; of eight 512 24.1, 25.4; 768 33.1, 32.7.
+// Whether the workgroup that selects scores its blocks itself.  A rule for eager calls, where a second launch takes 2
+// us more of the host; replayed from a graph the two meet at fewer blocks.  us a call in one launch and in two, eager |
+// replayed: 4 groups of one head 256 blocks 6.5, 8.7 | 6.2, 6.1; 512 8.0, 8.6 | 7.7, 6.3; of two heads 192 7.3, 8.5 | 7.0, 6.6;
+// 256 8.0, 8.6 | 7.7, 6.6; 320 8.5, 8.7 | 8.1, 6.6; of four 128 6.9, 8.7 | 6.6, 6.6; 160 7.8, 8.6 | 7.5, 6.6; 192 8.0, 9.4 | 7.6, 7.1;
+// of eight 48 7.3, 9.6 | 6.9, 7.6; 64 8.1, 9.5 | 7.8, 7.6; 128 10.1, 9.6 | 9.7, 7.9; 32 groups of four 160 7.9, 8.5 | 7.6, 7.6; 192
+// 8.6, 8.4 | 8.2, 7.5; 224 9.0, 8.3 | 8.7, 7.4; of eight 64 8.3, 8.6 | 8.0, 7.8; 80 9.1, 8.7 | 8.8, 8.1.  256 groups, a compute unit
+// each, where the GPU's time counts in both: of one head 1024 blocks 22.6, 26.5; of four 23.9, 29.2; of eight 512 23.9,
+// 25.2; 768 32.9, 32.5.
 bool blocks_scored_by_select(const SelectArgs& a) {
   if ((int64_t)a.B * a.Hkv >= 256) return a.max_blocks <= (a.G == 8 ? 512 : kFusedBlocks);
   return a.max_blocks <= (a.G == 8 ? 64 : a.G == 4 ? 192 : 256);
